@@ -17,7 +17,7 @@
  *                      deepest node whose whole root path the target's argmax
  *                      reproduces, and the free bonus token.
  *
- * Two more calls close the round around them:
+ * More calls close the round around them:
  *
  *   cape_expand        CaPE's confidence-aware proposal expansion (Section
  *                      3.2): from the draft's distributions, the proposal
@@ -25,6 +25,8 @@
  *                      tree_verify_attn and tree_accept take.
  *   glide_kv_compact   the cache update after acceptance (Section 3.1): the
  *                      accepted path's keys/values become contiguous rows.
+ *   glide_kv8_*        the same round on a cache held in 8 bits: append (quantise on
+ *                      write), read back, cross-attention and verification.
  *   spec_sample_accept speculative-sampling acceptance of a chain proposal
  *                      (Section 2's other acceptance strategy, used for GliDe
  *                      alone in Section 4.1), with caller-supplied uniforms.
@@ -347,6 +349,98 @@ glide_status glide_noalloc_read_device_status(glide_stream_t stream);
  * fails.  Allocates nothing.
  */
 glide_status glide_noalloc_scratch(void** device_ptr);
+
+/* ------------------------------------------------------------------ 8-bit cache
+ * The target's cache in 8 bits: half the bytes that the two attention calls
+ * read (the paper's caches are in 16 bits).  A layer's cache is
+ *     K, V          [B, H_kv, S_cap, D] codes: signed 8-bit floats with 4 exponent and 3
+ *                   mantissa bits (largest 448, smallest 2^-9, no infinities, 0x7f / 0xff NaN)
+ *     K_exp, V_exp  [B, H_kv, ceil(S_cap / 64)] int8: the exponent shared by a block of 64
+ *                   tokens (rows 64 j .. 64 j + 63 of a slab) of a cached head
+ *     value[b,h,t,d] = code[b,h,t,d] * 2^exp[b,h,t/64]
+ * Exponents are powers of two so that a code's value is exact in 16 bits, and so
+ * that a block whose exponent grows keeps its codes' mantissas: an 8-bit float
+ * has the same relative precision at any scale, and a finer one would buy nothing.
+ * Exponents lie in [-117, 119] (every value is a normal fp32 and bf16 number); the
+ * attention and read calls clamp others into that range.
+ * Unlike the 16-bit calls, the tree's own keys and values are NOT cache rows:
+ * tree_verify's form below takes them as they leave the target's projections, and
+ * glide_kv8_append writes the accepted ones.  A rejected token so never touches a
+ * block's exponent.
+ */
+#define GLIDE_KV8_BLOCK 64
+
+typedef struct {
+  void* K;       /* codes, 16-byte aligned */
+  void* V;
+  int8_t* K_exp;
+  int8_t* V_exp;
+} glide_kv8_cache;
+
+/*
+ * Quantises new rows as they join the cache, for n_layers layers at once:
+ *   m_b = len[b] + 1 (len clamped to [-1, n-1]; len NULL: m_b = n)
+ *   for k = 0 .. m_b - 1: row kv_len[b] + k of every cached head <-
+ *     k_new / v_new[b, path ? path[b,k] : k, h, :]
+ *   new_kv_len[b] = kv_len[b] + m_b.
+ * Each touched block's exponent is the least e with max |x| <= 448 * 2^e over the
+ * finite new elements x of the block (-117 if all are 0), and not less than the old
+ * one if the block holds rows from before (64 j < kv_len[b]); those rows' codes
+ * are then rounded to the grown exponent.  code = x * 2^-e rounded to nearest, ties to
+ * even; beyond 448 (an infinity) the largest code; NaN stays NaN.
+ * Rows before kv_len[b] in other blocks, and rows at and past new_kv_len[b], keep
+ * their codes.
+ * desc: B, H, H_kv, D, S_cap; dtype is that of k_new / v_new (scale, flags and
+ * max_ctas are ignored).  cache: layer 0 of dense stacks [n_layers][...]; k_new / v_new
+ * [n_layers][B, n, H_kv, D].  kv_len [B] (clamped to [0, S_cap - n]), path [B, n] or
+ * NULL (clamped to [0, n)), len [B] or NULL: int32 on the device.  path and len as
+ * tree_accept writes them append the accepted path; a prompt has path NULL.
+ * 1 <= n <= S_cap.  new_kv_len [B] int32 and not the kv_len buffer.  No workspace.
+ */
+glide_status glide_kv8_append(const glide_attn_desc* desc, int32_t n_layers, const glide_kv8_cache* cache,
+                              const void* k_new, const void* v_new, const int32_t* kv_len, int32_t n,
+                              const int32_t* path, const int32_t* len, int32_t* new_kv_len,
+                              glide_stream_t stream);
+
+/*
+ * Reads the cache back: K_out / V_out [n_layers][B, H_kv, S_out, D] of desc->dtype
+ * (fp32: exactly the codes' values; bf16: they are exact there too), rows at and past
+ * kv_len[b] zero, every element written.  1 <= S_out <= S_cap; kv_len [B] int32 on
+ * the device, clamped to [0, S_out].  desc and cache as above.  No workspace.
+ */
+glide_status glide_kv8_read(const glide_attn_desc* desc, int32_t n_layers, const glide_kv8_cache* cache,
+                            const int32_t* kv_len, int32_t S_out, void* K_out, void* V_out,
+                            glide_stream_t stream);
+
+/* Bytes of workspace that glide_kv8_cross_attn (n_queries = 1) and
+ * glide_kv8_verify_attn (n_queries = n) need; 0 if the descriptor is invalid.  A
+ * buffer sized for the largest n serves both. */
+size_t glide_kv8_workspace_bytes(const glide_attn_desc* desc, int32_t n_queries);
+
+/*
+ * glide_cross_attn over an 8-bit cache.  desc->dtype is that of q_draft [B,1,H,D] and
+ * of out [B,1,H,D]: bf16 queries give a bf16 result (one rounding of an fp32
+ * accumulation), fp32 queries an fp32 one.  0 <= max_kv_len <= S_cap; a sequence
+ * with kv_len 0 gets zeros.  H / H_kv <= 256.  desc->flags is ignored.  bf16 queries
+ * over a cache of 2^31 - 128 rows or more (B * H_kv * S_cap, 32-bit TMA coordinates), or
+ * over 2^30 tiles of 128 keys: GLIDE_ERR_UNSUPPORTED.
+ */
+glide_status glide_kv8_cross_attn(const glide_attn_desc* desc, const void* q_draft, const glide_kv8_cache* cache,
+                                  const int32_t* kv_len, int32_t max_kv_len, void* out, void* workspace,
+                                  size_t workspace_bytes, glide_stream_t stream);
+
+/*
+ * tree_verify_attn over an 8-bit cache and the tree's own keys and values:
+ *   out[b,i,h,:] = SoftMax over the cached rows t < kv_len[b] and the nodes j in A_i
+ *   (i itself and its ancestors) of the scores, times the values
+ * q_tree [B,n,H,D], k_tree / v_tree [B,n,H_kv,D] of desc->dtype, not quantised;
+ * out [B,n,H,D] of desc->dtype.  parent_idx [B,n] as in tree_verify_attn.
+ * 1 <= n <= 64, n * H / H_kv <= 256, 0 <= max_kv_len <= S_cap.  Limits as above.
+ */
+glide_status glide_kv8_verify_attn(const glide_attn_desc* desc, const void* q_tree, int32_t n,
+                                   const int32_t* parent_idx, const void* k_tree, const void* v_tree,
+                                   const glide_kv8_cache* cache, const int32_t* kv_len, int32_t max_kv_len,
+                                   void* out, void* workspace, size_t workspace_bytes, glide_stream_t stream);
 
 /*
  * Host-side check of a parent array (HOST memory, [B,n]): every entry is -1 or

@@ -37,6 +37,7 @@ GLIDE_BF16 = 0
 GLIDE_F32 = 1
 GLIDE_FLAG_FORCE_FMA = 1
 GLIDE_FLAG_TILE64 = 2
+GLIDE_KV8_BLOCK = 64
 
 
 class GlideError(RuntimeError):
@@ -49,6 +50,10 @@ class AttnDesc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("D", ctypes.c_int32),
                 ("S_cap", ctypes.c_int32), ("dtype", ctypes.c_int), ("scale", ctypes.c_float),
                 ("flags", ctypes.c_uint32), ("max_ctas", ctypes.c_int32), ("H_kv", ctypes.c_int32)]
+
+
+class Kv8Cache(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_exp", ctypes.c_void_p), ("V_exp", ctypes.c_void_p)]
 
 
 _P = ctypes.c_void_p
@@ -78,6 +83,16 @@ _SIG = {
     "glide_block_attn_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(AttnDesc), ctypes.c_int32]),
     "glide_block_cross_attn": (ctypes.c_int, [ctypes.POINTER(AttnDesc), _P, ctypes.c_int32, ctypes.c_int32, _P, _P,
                                               _P, _P, _P, ctypes.c_size_t, _P]),
+    "glide_kv8_append": (ctypes.c_int, [ctypes.POINTER(AttnDesc), ctypes.c_int32, ctypes.POINTER(Kv8Cache), _P, _P, _P,
+                                        ctypes.c_int32, _P, _P, _P, _P]),
+    "glide_kv8_read": (ctypes.c_int, [ctypes.POINTER(AttnDesc), ctypes.c_int32, ctypes.POINTER(Kv8Cache), _P,
+                                      ctypes.c_int32, _P, _P, _P]),
+    "glide_kv8_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(AttnDesc), ctypes.c_int32]),
+    "glide_kv8_cross_attn": (ctypes.c_int, [ctypes.POINTER(AttnDesc), _P, ctypes.POINTER(Kv8Cache), _P, ctypes.c_int32,
+                                            _P, _P, ctypes.c_size_t, _P]),
+    "glide_kv8_verify_attn": (ctypes.c_int, [ctypes.POINTER(AttnDesc), _P, ctypes.c_int32, _P, _P, _P,
+                                             ctypes.POINTER(Kv8Cache), _P, ctypes.c_int32, _P, _P, ctypes.c_size_t,
+                                             _P]),
     "spec_sample_accept": (ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P,
                                           _P, ctypes.c_size_t, _P]),
 }
@@ -402,6 +417,157 @@ def glide_block_cross_attn(q: torch.Tensor, K_cache: torch.Tensor, V_cache: torc
                                       V_cache.data_ptr(), seq_len.data_ptr(), out.data_ptr(), workspace.data_ptr(),
                                       workspace.numel() * workspace.element_size(), _stream(stream))
     _check(st, "glide_block_cross_attn")
+    return out
+
+
+# ------------------------------------------------------------------ 8-bit cache
+def _kv8_cache(K, V, K_exp, V_exp, dims: str):
+    """The C structure of an 8-bit cache, and its codes' shape as [layers, B, H_kv, S_cap, D]."""
+    if K.shape != V.shape or K.dim() not in ((4,) if dims == "4" else (4, 5)):
+        raise ValueError("codes must be [B, H_kv, S_cap, D]" + (" or [layers, B, H_kv, S_cap, D]" if dims != "4" else ""))
+    for t in (K, V):
+        if t.dtype not in (torch.float8_e4m3fn, torch.uint8):
+            raise TypeError("codes must be float8_e4m3fn (or their bytes, uint8)")
+    blocks = (K.shape[-2] + GLIDE_KV8_BLOCK - 1) // GLIDE_KV8_BLOCK
+    for t in (K_exp, V_exp):
+        if t.dtype != torch.int8 or tuple(t.shape) != tuple(K.shape[:-2]) + (blocks,):
+            raise TypeError("exponents must be int8 [..., H_kv, ceil(S_cap / 64)]")
+    _on_gpu(K, V, K_exp, V_exp)
+    shape = (1,) * (5 - K.dim()) + tuple(K.shape)
+    return Kv8Cache(K.data_ptr(), V.data_ptr(), K_exp.data_ptr(), V_exp.data_ptr()), shape
+
+
+def _on_gpu(*tensors):
+    for t in tensors:
+        if not t.is_cuda or t.device != tensors[0].device:
+            raise ValueError("tensors must be on one GPU")
+        if not t.is_contiguous():
+            raise ValueError("tensors must be contiguous")
+
+
+def _kv8_ints(t: torch.Tensor, shape, what: str):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape:
+        raise TypeError(f"{what} must be contiguous int32 {list(shape)}")
+
+
+def glide_kv8_workspace_bytes(desc: AttnDesc, n_queries: int) -> int:
+    return int(lib().glide_kv8_workspace_bytes(ctypes.byref(desc), int(n_queries)))
+
+
+def glide_kv8_append(k_new: torch.Tensor, v_new: torch.Tensor, K: torch.Tensor, V: torch.Tensor, K_exp: torch.Tensor,
+                     V_exp: torch.Tensor, kv_len: torch.Tensor, new_kv_len: torch.Tensor,
+                     path: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """Quantises rows of k_new / v_new [B, n, H_kv, D] into the 8-bit cache K / V [B, H_kv, S_cap, D] (float8_e4m3fn
+    codes), K_exp / V_exp [B, H_kv, ceil(S_cap / 64)] (int8) at rows kv_len[b] on; every tensor but the integer
+    ones may have a leading layer dimension.  Without `length` all n rows of a sequence join, with it
+    length[b] + 1; with `path` [B, n] row k is node path[b, k] (both as tree_accept writes them).
+    Returns new_kv_len [B]."""
+    st = (_CALL or _native()).kv8_append(k_new, v_new, K, V, K_exp, V_exp, kv_len, new_kv_len, path, length, stream)
+    if st == GLIDE_OK:
+        return new_kv_len
+    if st > 0:
+        raise GlideError(st, "glide_kv8_append")
+    cache, (layers, B, H_kv, S_cap, D) = _kv8_cache(K, V, K_exp, V_exp, "4 or 5")
+    if k_new.dim() != K.dim() or k_new.shape != v_new.shape or k_new.dtype != v_new.dtype:
+        raise ValueError("k_new and v_new must be [B, n, H_kv, D], with the cache's layers if it has them")
+    n = k_new.shape[-3]
+    if (1,) * (5 - K.dim()) + tuple(k_new.shape) != (layers, B, n, H_kv, D):
+        raise ValueError("k_new and v_new must be [B, n, H_kv, D] of the cache's sizes")
+    _on_gpu(K, k_new, v_new, kv_len, new_kv_len)
+    _kv8_ints(kv_len, (B,), "kv_len")
+    _kv8_ints(new_kv_len, (B,), "new_kv_len")
+    for t, shape, what in ((path, (B, n), "path"), (length, (B,), "length")):
+        if t is not None:
+            _on_gpu(K, t)
+            _kv8_ints(t, shape, what)
+    desc = make_desc(B, H_kv, D, S_cap, _dtype_code(k_new))
+    st = lib().glide_kv8_append(ctypes.byref(desc), layers, ctypes.byref(cache), k_new.data_ptr(), v_new.data_ptr(),
+                                kv_len.data_ptr(), n, path.data_ptr() if path is not None else None,
+                                length.data_ptr() if length is not None else None, new_kv_len.data_ptr(),
+                                _stream(stream))
+    _check(st, "glide_kv8_append")
+    return new_kv_len
+
+
+def glide_kv8_read(K: torch.Tensor, V: torch.Tensor, K_exp: torch.Tensor, V_exp: torch.Tensor, kv_len: torch.Tensor,
+                   K_out: torch.Tensor, V_out: torch.Tensor, stream=None):
+    """(K_out, V_out) [.., B, H_kv, S_out, D] bf16 or fp32 <- the values of the first S_out rows of an 8-bit cache,
+    zeros from row kv_len[b] on."""
+    st = (_CALL or _native()).kv8_read(K, V, K_exp, V_exp, kv_len, K_out, V_out, stream)
+    if st == GLIDE_OK:
+        return K_out, V_out
+    if st > 0:
+        raise GlideError(st, "glide_kv8_read")
+    cache, (layers, B, H_kv, S_cap, D) = _kv8_cache(K, V, K_exp, V_exp, "4 or 5")
+    if K_out.dim() != K.dim() or K_out.shape != V_out.shape or K_out.dtype != V_out.dtype or \
+            tuple(K_out.shape[:-2]) != tuple(K.shape[:-2]) or K_out.shape[-1] != D:
+        raise ValueError("K_out and V_out must be [..., B, H_kv, S_out, D] of the cache's sizes")
+    _on_gpu(K, kv_len, K_out, V_out)
+    _kv8_ints(kv_len, (B,), "kv_len")
+    desc = make_desc(B, H_kv, D, S_cap, _dtype_code(K_out))
+    st = lib().glide_kv8_read(ctypes.byref(desc), layers, ctypes.byref(cache), kv_len.data_ptr(), K_out.shape[-2],
+                              K_out.data_ptr(), V_out.data_ptr(), _stream(stream))
+    _check(st, "glide_kv8_read")
+    return K_out, V_out
+
+
+def _kv8_attn_desc(q, K, V, K_exp, V_exp, kv_len, out, workspace, scale, max_ctas, what: str):
+    cache, (_, B, H_kv, S_cap, D) = _kv8_cache(K, V, K_exp, V_exp, "4")
+    if q.dim() != 4 or q.shape[0] != B or q.shape[3] != D:
+        raise ValueError(f"{what} must be [B, n, H, D] of the cache's sizes")
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError(f"out must have the shape and type of {what}")
+    _on_gpu(K, q, kv_len, out, workspace)
+    _kv8_ints(kv_len, (B,), "kv_len")
+    H = q.shape[2]
+    return make_desc(B, H, D, S_cap, _dtype_code(q), scale, 0, max_ctas, H_kv=H_kv if H_kv != H else 0), cache
+
+
+def glide_kv8_cross_attn(q_draft: torch.Tensor, K: torch.Tensor, V: torch.Tensor, K_exp: torch.Tensor,
+                         V_exp: torch.Tensor, kv_len: torch.Tensor, max_kv_len: int, out: torch.Tensor,
+                         workspace: torch.Tensor, scale: float = 0.0, max_ctas: int = 0, stream=None) -> torch.Tensor:
+    """out[B,1,H,D] (q_draft's type) <- GliDe cross-attention of q_draft[B,1,H,D] over an 8-bit cache."""
+    st = (_CALL or _native()).kv8_cross(q_draft, K, V, K_exp, V_exp, kv_len, max_kv_len, out, workspace, scale,
+                                        max_ctas, stream)
+    if st == GLIDE_OK:
+        return out
+    if st > 0:
+        raise GlideError(st, "glide_kv8_cross_attn")
+    desc, cache = _kv8_attn_desc(q_draft, K, V, K_exp, V_exp, kv_len, out, workspace, scale, max_ctas, "q_draft")
+    if q_draft.shape[1] != 1:
+        raise ValueError("q_draft must be [B, 1, H, D]")
+    st = lib().glide_kv8_cross_attn(ctypes.byref(desc), q_draft.data_ptr(), ctypes.byref(cache), kv_len.data_ptr(),
+                                    int(max_kv_len), out.data_ptr(), workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "glide_kv8_cross_attn")
+    return out
+
+
+def glide_kv8_verify_attn(q_tree: torch.Tensor, parent_idx: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor,
+                          K: torch.Tensor, V: torch.Tensor, K_exp: torch.Tensor, V_exp: torch.Tensor,
+                          kv_len: torch.Tensor, max_kv_len: int, out: torch.Tensor, workspace: torch.Tensor,
+                          scale: float = 0.0, max_ctas: int = 0, stream=None) -> torch.Tensor:
+    """out[B,n,H,D] (q_tree's type) <- verification attention of q_tree[B,n,H,D] over an 8-bit cache and the tree's
+    own keys and values k_tree / v_tree[B,n,H_kv,D] (q_tree's type, not quantised) under the ancestor mask."""
+    st = (_CALL or _native()).kv8_verify(q_tree, parent_idx, k_tree, v_tree, K, V, K_exp, V_exp, kv_len, max_kv_len,
+                                         out, workspace, scale, max_ctas, stream)
+    if st == GLIDE_OK:
+        return out
+    if st > 0:
+        raise GlideError(st, "glide_kv8_verify_attn")
+    desc, cache = _kv8_attn_desc(q_tree, K, V, K_exp, V_exp, kv_len, out, workspace, scale, max_ctas, "q_tree")
+    B, n = q_tree.shape[:2]
+    for t in (k_tree, v_tree):
+        if tuple(t.shape) != (B, n, K.shape[1], K.shape[3]) or t.dtype != q_tree.dtype:
+            raise ValueError("k_tree and v_tree must be [B, n, H_kv, D] of q_tree's type")
+    _on_gpu(K, parent_idx, k_tree, v_tree)
+    _kv8_ints(parent_idx, (B, n), "parent_idx")
+    st = lib().glide_kv8_verify_attn(ctypes.byref(desc), q_tree.data_ptr(), n, parent_idx.data_ptr(),
+                                     k_tree.data_ptr(), v_tree.data_ptr(), ctypes.byref(cache), kv_len.data_ptr(),
+                                     int(max_kv_len), out.data_ptr(), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "glide_kv8_verify_attn")
     return out
 
 

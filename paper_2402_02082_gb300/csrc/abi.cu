@@ -8,6 +8,7 @@
 #include "../../include/glide.h"
 #include "common.cuh"
 #include "kernels.h"
+#include "kv8.h"
 
 namespace {
 
@@ -266,6 +267,99 @@ glide_status glide_block_cross_attn(const glide_attn_desc* desc, const void* q, 
   cudaError_t e = glide::launch_block_attn(a, reinterpret_cast<cudaStream_t>(stream));
   if (e == cudaErrorNotSupported) return GLIDE_ERR_UNSUPPORTED;
   return from_cuda(e);
+}
+
+// ---------------------------------------------------------------- 8-bit cache
+static bool kv8_cache_ok(const glide_kv8_cache* c) {
+  return c && c->K && c->V && c->K_exp && c->V_exp && aligned16(c->K) && aligned16(c->V);
+}
+// Stacks of layers: every offset of a layer's codes, rows and outputs stays in 63 bits.
+static bool kv8_layers_ok(const glide_attn_desc* d, int32_t n_layers) {
+  return n_layers >= 1 && (double)n_layers * d->B * hkv(d) * (double)d->S_cap * d->D <= 4.0e17;
+}
+
+glide_status glide_kv8_append(const glide_attn_desc* desc, int32_t n_layers, const glide_kv8_cache* cache,
+                              const void* k_new, const void* v_new, const int32_t* kv_len, int32_t n,
+                              const int32_t* path, const int32_t* len, int32_t* new_kv_len,
+                              glide_stream_t stream) {
+  if (!desc_ok(desc) || !kv8_layers_ok(desc, n_layers) || !kv8_cache_ok(cache)) return GLIDE_ERR_INVALID;
+  if (n < 1 || n > desc->S_cap) return GLIDE_ERR_INVALID;
+  if (!k_new || !v_new || !kv_len || !new_kv_len || new_kv_len == kv_len) return GLIDE_ERR_INVALID;
+  if (!aligned16(k_new) || !aligned16(v_new) || (reinterpret_cast<uintptr_t>(kv_len) & 3u) ||
+      (reinterpret_cast<uintptr_t>(path) & 3u) || (reinterpret_cast<uintptr_t>(len) & 3u) ||
+      (reinterpret_cast<uintptr_t>(new_kv_len) & 3u))
+    return GLIDE_ERR_INVALID;
+  glide::Kv8AppendArgs a;
+  a.K = static_cast<uint8_t*>(cache->K); a.V = static_cast<uint8_t*>(cache->V);
+  a.Ke = cache->K_exp; a.Ve = cache->V_exp; a.k_new = k_new; a.v_new = v_new;
+  a.kv_len = kv_len; a.path = path; a.len = len; a.new_kv_len = new_kv_len;
+  a.layers = n_layers; a.B = desc->B; a.H = hkv(desc); a.D = desc->D; a.S_cap = desc->S_cap; a.n = n;
+  a.dtype = desc->dtype == GLIDE_BF16 ? 0 : 1;
+  const cudaError_t e = glide::launch_kv8_append(a, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaErrorNotSupported ? GLIDE_ERR_UNSUPPORTED : from_cuda(e);
+}
+
+glide_status glide_kv8_read(const glide_attn_desc* desc, int32_t n_layers, const glide_kv8_cache* cache,
+                            const int32_t* kv_len, int32_t S_out, void* K_out, void* V_out,
+                            glide_stream_t stream) {
+  if (!desc_ok(desc) || !kv8_layers_ok(desc, n_layers) || !kv8_cache_ok(cache)) return GLIDE_ERR_INVALID;
+  if (S_out < 1 || S_out > desc->S_cap) return GLIDE_ERR_INVALID;
+  if (!kv_len || !K_out || !V_out || !aligned16(K_out) || !aligned16(V_out) ||
+      (reinterpret_cast<uintptr_t>(kv_len) & 3u))
+    return GLIDE_ERR_INVALID;
+  glide::Kv8ReadArgs a;
+  a.K = static_cast<const uint8_t*>(cache->K); a.V = static_cast<const uint8_t*>(cache->V);
+  a.Ke = cache->K_exp; a.Ve = cache->V_exp; a.kv_len = kv_len; a.K_out = K_out; a.V_out = V_out;
+  a.layers = n_layers; a.B = desc->B; a.H = hkv(desc); a.D = desc->D; a.S_cap = desc->S_cap; a.S_out = S_out;
+  a.dtype = desc->dtype == GLIDE_BF16 ? 0 : 1;
+  return from_cuda(glide::launch_kv8_read(a, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t glide_kv8_workspace_bytes(const glide_attn_desc* desc, int32_t n_queries) {
+  if (!desc_ok(desc) || n_queries < 1 || n_queries > glide::kMaxTree) return 0;
+  const int rows = n_queries * (desc->H / hkv(desc));
+  if (rows > glide::kKv8MaxRows) return 0;
+  return glide::kv8_workspace_bytes(desc->B, hkv(desc), desc->D, rows);
+}
+
+static glide_status kv8_attention(const glide_attn_desc* d, const void* q, int32_t n, const int32_t* parent,
+                                  const void* kt, const void* vt, const glide_kv8_cache* cache,
+                                  const int32_t* kv_len, int32_t max_kv_len, void* out, void* ws, size_t ws_bytes,
+                                  glide_stream_t stream) {
+  if (!q || !kv_len || !out || !ws || !kv8_cache_ok(cache)) return GLIDE_ERR_INVALID;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned16(kt) || !aligned16(vt) ||
+      (reinterpret_cast<uintptr_t>(kv_len) & 3u) || (reinterpret_cast<uintptr_t>(parent) & 3u))
+    return GLIDE_ERR_INVALID;
+  if (max_kv_len < 0 || max_kv_len > d->S_cap) return GLIDE_ERR_INVALID;
+  if ((long long)n * (d->H / hkv(d)) > glide::kKv8MaxRows) return GLIDE_ERR_UNSUPPORTED;
+  if (ws_bytes < glide_kv8_workspace_bytes(d, n)) return GLIDE_ERR_INVALID;
+  glide::Kv8AttnArgs a;
+  a.q = q; a.K = static_cast<const uint8_t*>(cache->K); a.V = static_cast<const uint8_t*>(cache->V);
+  a.Ke = cache->K_exp; a.Ve = cache->V_exp; a.kt = kt; a.vt = vt; a.parent = parent; a.kv_len = kv_len;
+  a.out = out; a.ws = ws; a.B = d->B; a.H = d->H; a.Hkv = hkv(d); a.D = d->D; a.S_cap = d->S_cap; a.nq = n;
+  a.max_kv_len = max_kv_len;
+  a.dtype = d->dtype == GLIDE_BF16 ? 0 : 1;
+  a.scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->D);
+  a.max_ctas = d->max_ctas;
+  return from_cuda(glide::launch_kv8_attn_fma(a, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+glide_status glide_kv8_cross_attn(const glide_attn_desc* desc, const void* q_draft, const glide_kv8_cache* cache,
+                                  const int32_t* kv_len, int32_t max_kv_len, void* out, void* workspace,
+                                  size_t workspace_bytes, glide_stream_t stream) {
+  if (!desc_ok(desc)) return GLIDE_ERR_INVALID;
+  return kv8_attention(desc, q_draft, 1, nullptr, nullptr, nullptr, cache, kv_len, max_kv_len, out, workspace,
+                       workspace_bytes, stream);
+}
+
+glide_status glide_kv8_verify_attn(const glide_attn_desc* desc, const void* q_tree, int32_t n,
+                                   const int32_t* parent_idx, const void* k_tree, const void* v_tree,
+                                   const glide_kv8_cache* cache, const int32_t* kv_len, int32_t max_kv_len,
+                                   void* out, void* workspace, size_t workspace_bytes, glide_stream_t stream) {
+  if (!desc_ok(desc)) return GLIDE_ERR_INVALID;
+  if (n < 1 || n > glide::kMaxTree || !parent_idx || !k_tree || !v_tree) return GLIDE_ERR_INVALID;
+  return kv8_attention(desc, q_tree, n, parent_idx, k_tree, v_tree, cache, kv_len, max_kv_len, out, workspace,
+                       workspace_bytes, stream);
 }
 
 glide_status glide_validate_tree(const int32_t* parent_idx_host, int32_t B, int32_t n, int32_t require_root0) {

@@ -1,0 +1,206 @@
+// Attention over the 8-bit cache on the CUDA cores, fp32 throughout:
+//
+//   s[r,t]  = q[r] . code_K[t] * 2^eK[t/64] * scale        (cached rows)
+//           = q[r] . k_tree[j] * scale                     (nodes j in A_r)
+//   out[r]  = sum_t softmax(s[r])_t value_V[t]
+//
+// A CTA takes kRT query rows of a slab (the rows that share a cached head) and all its keys; its
+// warps take tiles of 32 keys in turn.  Lane = key for the scores (the query comes from shared
+// memory, the same address in every lane), lane = slice of the head dimension for the values.
+// Running maximum, sum and output are kept per warp and joined at the end.
+#include <math_constants.h>
+
+#include "attn_common.cuh"
+#include "common.cuh"
+#include "device.h"
+#include "kv8.h"
+
+namespace glide {
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kRT = 4;  // query rows of a CTA
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void narrow(float x, float* to) { *to = x; }
+__device__ __forceinline__ void narrow(float x, __nv_bfloat16* to) { *to = __float2bfloat16_rn(x); }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArgs a) {
+  constexpr int kPer = D / 32;  // value elements per lane
+  __shared__ __align__(16) float q[kRT][D];
+  __shared__ float o_all[kWarps][kRT][D];
+  __shared__ float m_all[kWarps][kRT], l_all[kWarps][kRT];
+  __shared__ unsigned long long sees[kRT];
+  __shared__ int up[64];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = a.H / a.Hkv, rows = a.nq * group;
+  const int tiles = (rows + kRT - 1) / kRT;
+  const int slab = (int)(blockIdx.x / (unsigned)tiles), r0 = (int)(blockIdx.x - (unsigned)slab * tiles) * kRT;
+  const int b = slab / a.Hkv, h = slab - b * a.Hkv;
+  pdl_wait();
+  int L = a.kv_len[b];
+  L = L < 0 ? 0 : (L > a.max_kv_len ? a.max_kv_len : L);
+  const T* Q = static_cast<const T*>(a.q);
+  for (int i = threadIdx.x; i < kRT * D; i += kThreads) {
+    const int r = r0 + i / D;
+    q[i / D][i % D] = r < rows ? widen(Q[out_row(b, h, r, rows, group, a.H) * D + i % D]) : 0.f;
+  }
+  const int n = a.parent ? a.nq : 0;
+  if (threadIdx.x < n) up[threadIdx.x] = a.parent[(size_t)b * n + threadIdx.x];
+  __syncthreads();
+  if (threadIdx.x < kRT && n) {  // the row's node and its ancestors
+    unsigned long long set = 0;
+    const int r = r0 + threadIdx.x < rows ? r0 + threadIdx.x : rows - 1;
+    for (int j = r / group; j >= 0;) {
+      set |= 1ull << j;
+      j = up[j] < j ? up[j] : -1;
+    }
+    sees[threadIdx.x] = set;
+  }
+  __syncthreads();
+
+  const float c = a.scale * kLog2e;
+  float m[kRT], l[kRT], o[kRT][kPer];
+#pragma unroll
+  for (int r = 0; r < kRT; ++r) {
+    m[r] = -CUDART_INF_F;
+    l[r] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) o[r][k] = 0.f;
+  }
+  // Folds 32 keys in: s are this lane's scores (log2 domain), `seen` which rows see its key, v
+  // the exponent's factor of its value row, value(j, f) this lane's slice of key j's value row.
+  auto fold = [&](float (&s)[kRT], unsigned seen, float v, int keys, auto value) {
+    float w[kRT];
+#pragma unroll
+    for (int r = 0; r < kRT; ++r) {
+      const bool on = (seen >> r) & 1u;
+      const float top = fmaxf(m[r], warp_max(on ? s[r] : -CUDART_INF_F));
+      const float ref = top == -CUDART_INF_F ? 0.f : top;  // nothing seen yet, or NaN only
+      const float p = on ? fast_exp2(s[r] - ref) : 0.f;
+      const float keep = m[r] == -CUDART_INF_F ? (l[r] == 0.f ? 0.f : 1.f) : fast_exp2(m[r] - ref);
+      l[r] = l[r] * keep + warp_sum(p);
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) o[r][k] *= keep;
+      m[r] = top;
+      w[r] = p * v;
+    }
+    for (int j = 0; j < keys; ++j) {
+      float f[kPer];
+      value(j, f);
+#pragma unroll
+      for (int r = 0; r < kRT; ++r) {
+        const float pj = __shfl_sync(0xffffffffu, w[r], j);
+        if (pj != 0.f) {  // an unseen key's infinite value adds nothing
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) o[r][k] = fmaf(pj, f[k], o[r][k]);
+        }
+      }
+    }
+  };
+
+  const size_t base = (size_t)slab * a.S_cap;
+  const int8_t* Ke = a.Ke + (size_t)slab * kv8_blocks(a.S_cap);
+  const int8_t* Ve = a.Ve + (size_t)slab * kv8_blocks(a.S_cap);
+  const int cached = (L + 31) / 32, all = cached + (n + 31) / 32;
+  for (int tile = warp; tile < all; tile += kWarps) {
+    float s[kRT];
+#pragma unroll
+    for (int r = 0; r < kRT; ++r) s[r] = 0.f;
+    if (tile < cached) {
+      const int t = tile * 32 + lane, at = t < L ? t : L - 1, keys = L - tile * 32 < 32 ? L - tile * 32 : 32;
+      const uint8_t* row = a.K + (base + at) * D;
+#pragma unroll 2
+      for (int d = 0; d < D; d += 16) {
+        const uint4 w = *reinterpret_cast<const uint4*>(row + d);
+        float f[16];
+        kv8_decode4(w.x, f);
+        kv8_decode4(w.y, f + 4);
+        kv8_decode4(w.z, f + 8);
+        kv8_decode4(w.w, f + 12);
+#pragma unroll
+        for (int r = 0; r < kRT; ++r)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) s[r] = fmaf(q[r][d + k], f[k], s[r]);
+      }
+      const float ks = c * kv8_pow2(kv8_clamp_exp(Ke[at / kKv8Block]));
+#pragma unroll
+      for (int r = 0; r < kRT; ++r) s[r] *= ks;
+      const uint8_t* vrow = a.V + (base + tile * 32) * D + lane * kPer;
+      fold(s, t < L ? ~0u : 0u, kv8_pow2(kv8_clamp_exp(Ve[at / kKv8Block])), keys, [&](int j, float* f) {
+        if constexpr (kPer == 4) {
+          kv8_decode4(*reinterpret_cast<const uint32_t*>(vrow + (size_t)j * D), f);
+        } else {
+          const float2 v = kv8_f16pair(kv8_decode2_f16(*reinterpret_cast<const uint16_t*>(vrow + (size_t)j * D)));
+          f[0] = v.x;
+          f[1] = v.y;
+        }
+      });
+    } else {
+      const int j0 = (tile - cached) * 32, j = j0 + lane, at = j < n ? j : n - 1;
+      const T* row = static_cast<const T*>(a.kt) + (((size_t)b * n + at) * a.Hkv + h) * D;
+      for (int d = 0; d < D; ++d) {
+        const float k = widen(row[d]);
+#pragma unroll
+        for (int r = 0; r < kRT; ++r) s[r] = fmaf(q[r][d], k, s[r]);
+      }
+      unsigned seen = 0;
+#pragma unroll
+      for (int r = 0; r < kRT; ++r) {
+        s[r] *= c;
+        if (j < n && (sees[r] >> j) & 1ull) seen |= 1u << r;
+      }
+      const T* vt = static_cast<const T*>(a.vt) + (((size_t)b * n + j0) * a.Hkv + h) * D + lane * kPer;
+      fold(s, seen, 1.f, n - j0 < 32 ? n - j0 : 32, [&](int i, float* f) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) f[k] = widen(vt[(size_t)i * a.Hkv * D + k]);
+      });
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kRT; ++r) {
+    if (lane == 0) {
+      m_all[warp][r] = m[r];
+      l_all[warp][r] = l[r];
+    }
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) o_all[warp][r][lane * kPer + k] = o[r][k];
+  }
+  __syncthreads();
+  T* out = static_cast<T*>(a.out);
+  for (int i = threadIdx.x; i < kRT * D; i += kThreads) {
+    const int r = i / D, d = i % D;
+    if (r0 + r >= rows) break;
+    float M = -CUDART_INF_F, sum = 0.f, x = 0.f;
+    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, m_all[w][r]);
+    for (int w = 0; w < kWarps; ++w) {
+      const float f = m_all[w][r] == -CUDART_INF_F ? 1.f : fast_exp2(m_all[w][r] - M);  // -inf: nothing, or NaN
+      sum += f * l_all[w][r];
+      x += f * o_all[w][r][d];
+    }
+    narrow(sum == 0.f ? 0.f : x / sum, &out[out_row(b, h, r0 + r, rows, group, a.H) * D + d]);
+  }
+}
+
+template <typename T, int D>
+cudaError_t launch(const Kv8AttnArgs& a, cudaStream_t st) {
+  const int rows = a.nq * (a.H / a.Hkv);
+  const long long ctas = (long long)a.B * a.Hkv * ((rows + kRT - 1) / kRT);
+  return launch_pdl(kv8_attn_fma_kernel<T, D>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a);
+}
+
+}  // namespace
+
+size_t kv8_workspace_bytes(int B, int Hkv, int D, int rows) {
+  return WsLayout::kHeader;
+}
+
+cudaError_t launch_kv8_attn_fma(const Kv8AttnArgs& a, cudaStream_t st) {
+  if (a.dtype == 0) return a.D == 128 ? launch<__nv_bfloat16, 128>(a, st) : launch<__nv_bfloat16, 64>(a, st);
+  return a.D == 128 ? launch<float, 128>(a, st) : launch<float, 64>(a, st);
+}
+
+}  // namespace glide

@@ -52,6 +52,14 @@ class Args {
       if (s > INT_MAX) throw NotTaken{};
     return t;
   }
+  // an 8-bit cache's codes, contiguous, no size beyond 32 bits
+  const at::Tensor& codes() {
+    const at::Tensor& t = any_tensor();
+    if ((t.scalar_type() != at::kFloat8_e4m3fn && t.scalar_type() != at::kByte) || !t.is_contiguous()) throw NotTaken{};
+    for (int64_t s : t.sizes())
+      if (s > INT_MAX) throw NotTaken{};
+    return t;
+  }
   const at::Tensor& any_tensor() {
     PyObject* o = *v_++;
     if (!THPVariable_CheckExact(o)) throw NotTaken{};
@@ -334,6 +342,153 @@ PyObject* sample(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
+// An 8-bit cache: K, V codes (float8 or their bytes) and K_exp, V_exp, contiguous, of `rank` dimensions
+// ([B, H_kv, S_cap, D], and [layers, ...] before them where rank is 5).
+struct Cache8 {
+  glide_kv8_cache c;
+  at::IntArrayRef sizes;
+  int device;
+};
+Cache8 cache8(Args& a) {
+  const at::Tensor &K = a.codes(), &V = a.codes(), &Ke = a.tensor(at::kChar), &Ve = a.tensor(at::kChar);
+  const int64_t rank = K.dim();
+  if ((rank != 4 && rank != 5) || K.sizes() != V.sizes()) throw NotTaken{};
+  for (const at::Tensor* e : {&Ke, &Ve}) {
+    if (e->dim() != rank - 1 || !e->is_contiguous() || e->sizes().slice(0, rank - 2) != K.sizes().slice(0, rank - 2) ||
+        e->size(rank - 2) != (K.size(rank - 2) + GLIDE_KV8_BLOCK - 1) / GLIDE_KV8_BLOCK || e->device() != K.device())
+      throw NotTaken{};
+  }
+  if (V.device() != K.device()) throw NotTaken{};
+  return {{K.data_ptr(), V.data_ptr(), static_cast<int8_t*>(Ke.data_ptr()), static_cast<int8_t*>(Ve.data_ptr())},
+          K.sizes(), K.get_device()};
+}
+// Sizes of a cache's layer, and of the rows [.., B, rows, H_kv, D] or slabs [.., B, H_kv, rows, D] beside it.
+glide_attn_desc describe8(const Cache8& k, at::ScalarType type) {
+  const size_t o = k.sizes.size() - 4;
+  glide_attn_desc d{};
+  d.B = static_cast<int32_t>(k.sizes[o]);
+  d.H = static_cast<int32_t>(k.sizes[o + 1]);
+  d.S_cap = static_cast<int32_t>(k.sizes[o + 2]);
+  d.D = static_cast<int32_t>(k.sizes[o + 3]);
+  d.dtype = type == at::kBFloat16 ? GLIDE_BF16 : GLIDE_F32;
+  return d;
+}
+int32_t layers8(const Cache8& k) { return k.sizes.size() == 5 ? static_cast<int32_t>(k.sizes[0]) : 1; }
+void on(int device, std::initializer_list<const at::Tensor*> ts) {
+  for (const at::Tensor* t : ts)
+    if (t->get_device() != device) throw NotTaken{};
+}
+
+// k_new, v_new, K, V, K_exp, V_exp, kv_len, new_kv_len, path, length, stream
+PyObject* kv8_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return call([&] {
+    Args a(v, n, 11);
+    const at::Tensor &kn = a.data(), &vn = a.data();
+    const Cache8 k = cache8(a);
+    const glide_attn_desc d = describe8(k, kn.scalar_type());
+    const size_t o = k.sizes.size() - 4;
+    if (kn.sizes() != vn.sizes() || kn.scalar_type() != vn.scalar_type() || kn.dim() != int64_t(o) + 4 ||
+        (o && kn.size(0) != k.sizes[0]) || kn.size(o) != d.B || kn.size(o + 2) != d.H || kn.size(o + 3) != d.D)
+      throw NotTaken{};
+    const int32_t rows = dim(kn, static_cast<int>(o) + 1);
+    const at::Tensor &len = a.tensor(at::kInt, {d.B}), &fresh = a.tensor(at::kInt, {d.B});
+    on(k.device, {&kn, &vn, &len, &fresh});
+    const int32_t *path = nullptr, *m = nullptr;
+    if (!a.none()) {
+      const at::Tensor& t = a.tensor(at::kInt, {d.B, rows});
+      on(k.device, {&t});
+      path = ints(t);
+    }
+    if (!a.none()) {
+      const at::Tensor& t = a.tensor(at::kInt, {d.B});
+      on(k.device, {&t});
+      m = ints(t);
+    }
+    const glide_stream_t stream = a.stream();
+    const int32_t layers = layers8(k);
+    const void *pk = kn.data_ptr(), *pv = vn.data_ptr();
+    const int32_t* pl = ints(len);
+    int32_t* po = ints(fresh);
+    return without_gil(
+        [&] { return long(glide_kv8_append(&d, layers, &k.c, pk, pv, pl, rows, path, m, po, stream)); });
+  });
+}
+
+// K, V, K_exp, V_exp, kv_len, K_out, V_out, stream
+PyObject* kv8_read(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return call([&] {
+    Args a(v, n, 8);
+    const Cache8 k = cache8(a);
+    const at::Tensor& len = a.tensor(at::kInt);
+    const at::Tensor &K = a.data(), &V = a.data();
+    const glide_attn_desc d = describe8(k, K.scalar_type());
+    const size_t o = k.sizes.size() - 4;
+    if (len.dim() != 1 || len.size(0) != d.B || !len.is_contiguous() || K.sizes() != V.sizes() ||
+        K.scalar_type() != V.scalar_type() || K.dim() != int64_t(o) + 4 ||
+        K.sizes().slice(0, o + 2) != k.sizes.slice(0, o + 2) || K.size(o + 3) != d.D)
+      throw NotTaken{};
+    on(k.device, {&len, &K, &V});
+    const glide_stream_t stream = a.stream();
+    const int32_t layers = layers8(k), rows = dim(K, static_cast<int>(o) + 2);
+    const int32_t* pl = ints(len);
+    void *pk = K.data_ptr(), *pv = V.data_ptr();
+    return without_gil([&] { return long(glide_kv8_read(&d, layers, &k.c, pl, rows, pk, pv, stream)); });
+  });
+}
+
+// q, (parent, k_tree, v_tree where kTree,) K, V, K_exp, V_exp, kv_len, max_kv_len, out, workspace, scale, max_ctas, stream
+template <bool kTree>
+PyObject* kv8_attn(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return call([&] {
+    Args a(v, n, kTree ? 15 : 12);
+    const at::Tensor& q = a.data();
+    if (q.dim() != 4) throw NotTaken{};
+    const int32_t nodes = dim(q, 1);
+    const at::Tensor *parent = nullptr, *kt = nullptr, *vt = nullptr;
+    if constexpr (kTree) {
+      parent = &a.tensor(at::kInt, {q.size(0), nodes});
+      kt = &a.data();
+      vt = &a.data();
+    } else if (nodes != 1) {
+      throw NotTaken{};
+    }
+    const Cache8 k = cache8(a);
+    if (k.sizes.size() != 4) throw NotTaken{};
+    glide_attn_desc d = describe8(k, q.scalar_type());
+    if (q.size(0) != d.B || q.size(3) != d.D) throw NotTaken{};
+    if constexpr (kTree) {
+      for (const at::Tensor* t : {kt, vt})
+        if (t->scalar_type() != q.scalar_type() || t->sizes() != at::IntArrayRef({d.B, nodes, d.H, d.D})) throw NotTaken{};
+      on(k.device, {parent, kt, vt});
+    }
+    const int32_t heads = dim(q, 2);
+    if (heads != d.H) {
+      d.H_kv = d.H;
+      d.H = heads;
+    }
+    const at::Tensor& len = a.tensor(at::kInt, {d.B});
+    const int32_t most = a.i32();
+    const at::Tensor &out = a.data(), &w = a.any_tensor();
+    if (out.sizes() != q.sizes() || out.scalar_type() != q.scalar_type() || !w.is_contiguous()) throw NotTaken{};
+    on(k.device, {&q, &len, &out, &w});
+    d.scale = a.f32();
+    d.max_ctas = a.i32();
+    const glide_stream_t stream = a.stream();
+    const void* pq = q.data_ptr();
+    const int32_t* pl = ints(len);
+    void *po = out.data_ptr(), *ws = w.data_ptr();
+    const size_t bytes = w.nbytes();
+    if constexpr (kTree) {
+      const int32_t* pp = ints(*parent);
+      const void *pk = kt->data_ptr(), *pv = vt->data_ptr();
+      return without_gil(
+          [&] { return long(glide_kv8_verify_attn(&d, pq, nodes, pp, pk, pv, &k.c, pl, most, po, ws, bytes, stream)); });
+    } else {
+      return without_gil([&] { return long(glide_kv8_cross_attn(&d, pq, &k.c, pl, most, po, ws, bytes, stream)); });
+    }
+  });
+}
+
 #define FN(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FN("cross_attn", cross_attn<false>),
                           FN("cross_attn_noalloc", cross_attn<true>),
@@ -343,6 +498,10 @@ PyMethodDef kMethods[] = {FN("cross_attn", cross_attn<false>),
                           FN("expand", expand),
                           FN("compact", compact),
                           FN("sample", sample),
+                          FN("kv8_append", kv8_append),
+                          FN("kv8_read", kv8_read),
+                          FN("kv8_cross", kv8_attn<false>),
+                          FN("kv8_verify", kv8_attn<true>),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_glidecall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
