@@ -341,7 +341,10 @@ static glide_status kv8_attention(const glide_attn_desc* d, const void* q, int32
   a.dtype = d->dtype == GLIDE_BF16 ? 0 : 1;
   a.scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->D);
   a.max_ctas = d->max_ctas;
-  return from_cuda(glide::launch_kv8_attn_fma(a, reinterpret_cast<cudaStream_t>(stream)));
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (a.dtype != 0) return from_cuda(glide::launch_kv8_attn_fma(a, st));
+  const cudaError_t e = glide::launch_kv8_attn_tc(a, st);
+  return e == cudaErrorNotSupported ? GLIDE_ERR_UNSUPPORTED : from_cuda(e);
 }
 
 glide_status glide_kv8_cross_attn(const glide_attn_desc* desc, const void* q_draft, const glide_kv8_cache* cache,

@@ -194,12 +194,7 @@ cudaError_t launch(const Kv8AttnArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-size_t kv8_workspace_bytes(int B, int Hkv, int D, int rows) {
-  return WsLayout::kHeader;
-}
-
 cudaError_t launch_kv8_attn_fma(const Kv8AttnArgs& a, cudaStream_t st) {
-  if (a.dtype == 0) return a.D == 128 ? launch<__nv_bfloat16, 128>(a, st) : launch<__nv_bfloat16, 64>(a, st);
   return a.D == 128 ? launch<float, 128>(a, st) : launch<float, 64>(a, st);
 }
 

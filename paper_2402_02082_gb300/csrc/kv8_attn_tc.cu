@@ -1,0 +1,1060 @@
+// Attention over the 8-bit cache on the tcgen05 tensor cores: draft queries (cross-attention) and
+// tree queries (verification), bf16 in and out, fp32 sums.
+//
+// The mathematics.  With codes K8, V8 and block exponents eK, eV of key t,
+//   s[r,t] = q[r] . K8[t] * 2^eK * scale * log2(e),   u[r,t] = s[r,t] + eV[t]
+//   m[r]   = running maximum of u less 8,   p[r,t] = 2^(u - m)
+//   O[r]   = sum_t p[r,t] V8[t],     l[r]   = sum_t p[r,t] 2^-eV[t],    out[r] = O[r] / l[r]
+// Taking the value exponent into the weight's exponent leaves the codes as they are: no key or
+// value is widened or scaled, and the tensor cores multiply the cache's own bytes.
+//
+// 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with
+// the slab's largest query scaled to at most 448, q = hi + lo / 16 exactly (elements below 2^-14 of the
+// largest to 2^-23 of it).  A weight p <= 430 is hi + lo / 32 to 2^-9 of itself, or to 2^-23 of the
+// row's largest, which is at least 256.  hi and lo are columns of their own, so both products cost twice
+// the columns and nothing else.  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16 with
+// bf16 queries and weights into the columns of hi; its values are scaled to a block's range by a power
+// of two of their own, so that the weights of tree and cache lie in one range.
+//
+// Orientation.  Keys are the 128 rows of the MMA and the queries its columns:
+//   S^T = K8 Q^T  : M = 128 keys, N = 2 x NP (hi | lo), K = D, both operands K-major
+//   O^T += V8^T P^T : M = D, N = 2 x NP, K = keys, both operands M/N-major
+// so the tensor work goes with the query rows (NP = 8 .. 64), not with a padded 128, K and V tiles are
+// read from shared memory once, and thread = key in the softmax.  A row's maximum then lies across the
+// threads; it is looked for only when a weight would pass the largest code (one vote per tile), which after the
+// first tile of a slab is rare.
+//
+// Roles: SG groups of four softmax warps, one copy warp (TMA), one MMA warp; a persistent grid and the
+// cost-balanced split of the key sequence that the other kernels use.  A group takes 8 or 16 of the query
+// rows, thread = key: a thread's scores, weights and running sums then stay in ~100 registers and sixteen
+// softmax warps fill an SM (one group of 64 rows: 168 registers and spills, 660 us where this takes @64).
+// Up to 32 rows two CTAs share an SM and S and P have one buffer each (S is free again once it is in
+// registers); above, one CTA with two of each.  A tree is tile 0 of its slab: the softmax warps write its
+// operands while the first copies are on their way.
+//
+// A slab whose keys lie in several CTAs' shares leaves partials (m, l, O) in the workspace and
+// kv8_merge_kernel joins them.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "attn_common.cuh"
+#include "common.cuh"
+#include "device.h"
+#include "kernels.h"
+#include "kv8.h"
+#include "tc_attn.cuh"
+#include "tc_ptx.cuh"
+#include "tensor_map.h"
+
+namespace glide {
+namespace {
+
+constexpr int kTK = 128;          // keys per tile
+constexpr int kTreeKeys = 64;     // rows of the tree tile
+constexpr int kMaxStages8 = 6;
+constexpr float kLift = 8.f;      // log2 of the weight of a new maximum
+constexpr float kMost = 8.75f;    // log2 of the largest weight: 448 is the largest code
+constexpr float kQLo = 16.f, kPLo = 32.f;
+constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
+
+// What a switch of slabs costs a CTA, in tiles.
+__host__ __device__ constexpr int seg_weight8(int np) { return 2 + np / 16; }
+
+// barriers
+constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, SFREE8 = 27, PFULL8 = 29, PVDONE = 31,
+              MDONE8 = 33, kBars8 = 34;
+
+template <int D, int NP>
+struct Cfg {
+  static constexpr int kRT = NP <= 32 ? NP : NP / 2;                  // rows of a softmax group
+  static constexpr int kSG = NP / kRT;                                // softmax groups
+  static constexpr int kSoft = 128 * kSG;
+  static constexpr int kCopyWarp = 4 * kSG, kMmaWarp = kCopyWarp + 1, kThreads = kSoft + 64;
+  static constexpr int kCtas = NP <= 32 ? 2 : 1;                      // of an SM
+  static constexpr int kBuf = NP <= 32 ? 1 : 2;                       // S and P buffers
+  static constexpr int kN = 2 * NP;                                   // MMA columns
+  static constexpr int kNT = NP < 16 ? 16 : NP;                         // MMA columns of a tree tile
+  static constexpr int kPitch = NP <= 16 ? 32 : (NP <= 32 ? 64 : 128);  // bytes of a key's weights
+  static constexpr uint32_t kQBytes = kN * D;
+  static constexpr uint32_t kPBytes = kTK * kPitch;
+  static constexpr uint32_t kTile = kTK * D;
+  static constexpr uint32_t off_Q = 0;
+  static constexpr uint32_t off_P = (kQBytes + 1023) / 1024 * 1024;
+  static constexpr uint32_t off_K = off_P + kBuf * kPBytes;
+  static __host__ __device__ uint32_t off_V(int ns) { return off_K + ns * kTile; }
+  static __host__ __device__ uint32_t off_small(int ns) { return off_V(ns) + ns * kTile; }
+  static constexpr uint32_t kTmemS = kN == 96 ? 128 : kN;             // columns of an S buffer
+  static constexpr uint32_t kTmemO = kBuf * kTmemS;                   // S buffers from column 0, then O
+  static constexpr uint32_t kCols = kTmemO + kN <= 32 ? 32 : kTmemO + kN <= 64 ? 64 : kTmemO + kN <= 128 ? 128 : 512;
+};
+
+struct Small {  // per CTA, after the rings
+  uint64_t bars[kBars8];
+  ShareStart share;
+  unsigned long long sees[64];  // the rows' nodes and their ancestors
+  alignas(16) float m[64];      // running maximum of each row, less kLift
+  alignas(16) float up[64];     // by how much m rose last
+  alignas(16) float f[64];      // 2^-up; at the end 1 / l, or l
+  alignas(16) float part[4][64];  // per lane quarter: row maxima, row sums
+  alignas(4) uint8_t rise[2][2][4];  // tiles in turn, per group and lane quarter: the chunks whose m rises
+  int rel[64];                  // a row's place among a sequence's [node, head] rows from the slab's first head, -1: none
+  uint32_t top[8][2];           // per softmax warp: largest query, largest value of the tree
+  uint32_t tmem;
+  int abort_flag;
+  int odd_values;               // the tree has values that are not finite
+};
+
+struct Params8 {
+  const __nv_bfloat16 *q, *kt, *vt;
+  const int8_t *Ke, *Ve;
+  const int *kv_len, *parent;
+  __nv_bfloat16* out;
+  unsigned* status;
+  int2* ranges;
+  float* partials;
+  int B, H, Hkv, S_cap, max_kv_len, n, group, rows, R, per_tile, tree, ns, blocks;
+  float scale_log2;
+};
+
+// Named barriers: 1 among all softmax threads, 2 + g within group g.
+template <int kThreads>
+__device__ __forceinline__ void soft_sync(int id) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads) : "memory");
+}
+// The same, and whether any of the threads says so.
+template <int kThreads>
+__device__ __forceinline__ bool soft_any(int id, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)x), "r"(id), "n"(kThreads)
+      : "memory");
+  return r != 0;
+}
+
+// Shared-memory matrix descriptor; `pitch` (32, 64, 128 bytes) is the swizzle's width, 8 rows of it the
+// stride between groups of 8 rows.
+__device__ __forceinline__ uint64_t swizzled_desc(uint32_t saddr, int pitch) {
+  const uint64_t mode = pitch == 128 ? 2 : (pitch == 64 ? 4 : 6);
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)((8 * pitch) >> 4) << 32) | (1ull << 46) |
+         (mode << 61);
+}
+// Where byte `c` of row `r` lies in a tile of that pitch.
+template <int kPitch>
+__device__ __forceinline__ uint32_t swizzled(uint32_t r, uint32_t c) {
+  const uint32_t a = r * kPitch + c;
+  return a ^ ((a >> 3) & (kPitch == 128 ? 0x70u : (kPitch == 64 ? 0x30u : 0x10u)));
+}
+// Instruction descriptor of kind::f8f6f4, both operands 8-bit floats of 4 exponent bits, fp32 sums.
+__host__ __device__ constexpr uint32_t idesc_f8(int M, int N, bool a_mn, bool b_mn) {
+  return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) |
+         ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                       uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[N]) {
+  if constexpr (N == 16) {
+    tc::tmem_ld16(taddr, r);
+  } else {
+    static_assert(N == 8, "columns");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr));
+  }
+}
+template <int N>
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[N]) {
+  if constexpr (N == 16) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        GLIDE_TMEM_IN16(r)
+        : "memory");
+  } else {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+  }
+}
+
+// The largest of a value over the warp; NaN only if all are.
+__device__ __forceinline__ float warp_top(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// ---- sums of two codes
+__device__ __forceinline__ uint32_t cvt_e4m3x2_f16x2(uint32_t h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+  return r;
+}
+__device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Two weights in [0, 430] (or NaN) as codes hi and lo, p = hi + lo / 32: the fp16 in between has 11 bits.
+__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+  const uint32_t h = cvt_f16x2(p0, p1);
+  hi = cvt_e4m3x2_f16x2(h);
+  lo = cvt_e4m3x2_f16x2(hmul2(hsub2(h, kv8_decode2_f16(hi)), 0x50005000u));  // 32, 32
+}
+// Eight bf16 elements times s as codes hi and lo, x = hi + lo / 16; what is not finite becomes NaN.
+__device__ __forceinline__ void split8(const uint4& w, float s, uint2& hi, uint2& lo) {
+  const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = bf16lo(in[i]) * s, b = bf16hi(in[i]) * s;  // finite ones are at most 448
+    a = (in[i] & 0x7f80u) == 0x7f80u ? CUDART_NAN_F : a;
+    b = (in[i] & 0x7f800000u) == 0x7f800000u ? CUDART_NAN_F : b;
+    h[i] = kv8_encode2(a, b);
+    const float2 was = kv8_f16pair(kv8_decode2_f16(h[i]));
+    l[i] = kv8_encode2((a - was.x) * kQLo, (b - was.y) * kQLo);
+  }
+  hi = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+  lo = make_uint2(l[0] | (l[1] << 16), l[2] | (l[3] << 16));
+}
+// The largest finite magnitude among eight bf16 elements (as its bits).
+__device__ __forceinline__ uint32_t top8(const uint4& w) {
+  const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = in[i] & 0x7fffu, b = (in[i] >> 16) & 0x7fffu;
+    most = max(most, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
+  }
+  return most;
+}
+// Eight bf16 elements with zeros for those that are not finite; says whether there are any.
+__device__ __forceinline__ bool drop_odd(uint4& w) {
+  uint32_t in[4] = {w.x, w.y, w.z, w.w};
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((in[i] & 0x7f80u) == 0x7f80u) in[i] &= 0xffff0000u, odd = true;
+    if ((in[i] & 0x7f800000u) == 0x7f800000u) in[i] &= 0xffffu, odd = true;
+  }
+  w = make_uint4(in[0], in[1], in[2], in[3]);
+  return odd;
+}
+// The least e with x <= 448 * 2^e for the bf16 magnitude x with these bits.
+__device__ __forceinline__ int top_exponent(uint32_t bits) {
+  return kv8_clamp_exp((int)(bits >> 7) - 127 - 8 + ((bits & 0x7fu) > 0x60u ? 1 : 0));
+}
+
+// A block's value exponent as the weights take it.  A block of zero values has the least exponent there is; beside an
+// ordinary block its weights would leave fp32's range, and the sum l with them.  So an exponent counts as at least 64
+// below the largest seen: its values then show up 2^-64 of that block's at most.
+__device__ __forceinline__ int effective_exp(int e, int ref) { return max(max(e, ref - kVExpSpan), kVExpLeast); }
+
+template <int D, int NP>
+__global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
+    kv8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                       const Params8 p) {
+  using C = Cfg<D, NP>;
+  constexpr int RT = C::kRT, kSoft = C::kSoft, kCopyWarp = C::kCopyWarp, kMmaWarp = C::kMmaWarp;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const int ns = p.ns;
+  const uint32_t off_V = C::off_V(ns);
+  Small& sm = *reinterpret_cast<Small*>(base + C::off_small(ns));
+  uint64_t* bars = sm.bars;
+  volatile int* abort_flag = &sm.abort_flag;
+  BatchTiles bt;
+  bt.start = reinterpret_cast<long long*>(&sm + 1);
+  bt.len = reinterpret_cast<int*>(bt.start + p.B + 1);
+  bt.ntiles = bt.len + p.B;
+  bt.plen = bt.ntiles + p.B;
+  bt.sidx = bt.plen + p.B;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    tc::prefetch_tmap(&tmK);
+    tc::prefetch_tmap(&tmV);
+    for (int b = 0; b < kBars8; ++b) mbar_init(&bars[b], b == QFULL8 || (b >= SFREE8 && b < PVDONE) ? 4 * C::kSG : 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  const int G = gridDim.x / p.R, x = blockIdx.x / p.R, y = blockIdx.x - x * p.R;
+  const int row0 = y * p.per_tile, rows_here = min(p.per_tile, p.rows - row0);
+  const int weight = seg_weight8(NP);
+  if (threadIdx.x < 64) {
+    const int r = threadIdx.x, node = (row0 + r) / p.group;
+    sm.rel[r] = r < rows_here ? node * p.H + (row0 + r - node * p.group) : -1;
+  }
+  if (warp == 0) {
+    wait_and_build_share(bt, p.kv_len, p.B, p.Hkv, p.max_kv_len, p.tree ? kTK : 0, kTK, G, weight, x, &sm.share);
+    __syncwarp();
+  } else {
+    pdl_wait();
+  }
+  if (warp == kMmaWarp) {
+    tc::tmem_alloc(&sm.tmem, C::kCols);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = sm.tmem;
+  SegWalk s;
+  s.start(bt, sm.share);
+
+  if (warp == kCopyWarp) {
+    // -------------------------------------------------------------- copies
+    if (y == 0) write_ranges(bt, p.B, p.Hkv, G, weight, p.ranges, x * 32 + lane, G * 32);
+    __syncwarp();
+    if (lane == 0) {
+      const uint64_t policy = p.R == 1 ? policy_evict_first() : policy_evict_normal();
+      int at = 0, st = 0;
+      uint32_t phase = 1;
+      uint32_t k_out = 0, v_out = 0, par = 0;  // by stage: a copy issued, and the parity of its last one
+      bool ok = true;
+      for (; s.any() && ok; s.next(bt, p.Hkv)) {
+        for (int t = s.t0; t < s.t1 && ok; ++t, ++at) {
+          if (p.tree && t == 0) {
+            // the tree's operands: the softmax warps write them
+          } else {
+            const int row = (s.b * p.Hkv + s.h) * p.S_cap + (t - p.tree) * kTK;
+            ok = mbar_wait_small(&bars[E_K + st], phase, abort_flag);
+            if (!ok) break;
+            mbar_arrive_expect_tx(&bars[F_K + st], C::kTile);
+            tc::tma_load_2d(base + C::off_K + st * C::kTile, &tmK, 0, row, &bars[F_K + st], policy);
+            k_out |= 1u << st;
+            v_out &= ~(1u << st);
+            par = (par & ~(1u << st)) | ((phase ^ 1u) << st);
+            ok = mbar_wait_small(&bars[E_V + st], phase, abort_flag);
+            if (!ok) break;
+            mbar_arrive_expect_tx(&bars[F_V + st], C::kTile);
+            tc::tma_load_2d(base + off_V + st * C::kTile, &tmV, 0, row, &bars[F_V + st], policy);
+            v_out |= 1u << st;
+          }
+          if (++st == ns) {
+            st = 0;
+            phase ^= 1;
+          }
+        }
+      }
+      if (!ok) {  // aborted: issued copies land before the CTA exits
+        for (int k = 0; k < ns; ++k) {
+          if ((k_out >> k) & 1u) mbar_drain(&bars[F_K + k], (par >> k) & 1u);
+          if ((v_out >> k) & 1u) mbar_drain(&bars[F_V + k], (par >> k) & 1u);
+        }
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ----------------------------------------------------------------- MMA
+    if (lane == 0) {
+      constexpr uint32_t idS = idesc_f8(128, C::kN, false, false);
+      constexpr uint32_t idO = idesc_f8(D, C::kN, true, true);
+      constexpr int kPitchP = C::kPitch;
+      const uint64_t dQ = swizzled_desc(smem_u32(base + C::off_Q), D);
+      const uint64_t dP0 = swizzled_desc(smem_u32(base + C::off_P), kPitchP);
+      const uint64_t dK0 = swizzled_desc(smem_u32(base + C::off_K), D);
+      const uint64_t dV0 = swizzled_desc(smem_u32(base + off_V), D);
+      const uint32_t tO = tmem + C::kTmemO;
+      constexpr int kBuf = C::kBuf;
+      int kst = 0, vst = 0, seg = 0, si = 0, pi = 0;  // si, pi: tiles whose S, whose P.V were issued
+      uint32_t k_phase = 0, v_phase = 0;
+      bool ok = true;
+      auto issue_s = [&](bool tree) {
+        ok = mbar_wait_small(&bars[F_K + kst], k_phase, abort_flag) &&
+             mbar_wait_small(&bars[SFREE8 + si % kBuf], (si / kBuf & 1) ^ 1, abort_flag);
+        if (!ok) return;
+        tc::fence_after_sync();
+        const uint32_t tS = tmem + si % kBuf * C::kTmemS;
+        const uint64_t dK = dK0 + (uint64_t)kst * desc_step(C::kTile);
+        if (tree) {  // bf16 keys [D / 64][64 keys][64], bf16 queries [D / 64][kNT][64] in P's place
+          const uint64_t dA = tc::sw128_desc(smem_u32(base + C::off_K + kst * C::kTile), 16, 1024);
+          const uint64_t dB = tc::sw128_desc(smem_u32(base + C::off_P + si % kBuf * C::kPBytes), 16, 1024);
+          constexpr uint32_t id = tc::idesc_bf16_f32(128, C::kNT, false, false);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            tc::mma_bf16(tS, dA + desc_step((k / 4) * kTreeKeys * 128 + (k % 4) * 32),
+                         dB + desc_step((k / 4) * C::kNT * 128 + (k % 4) * 32), id, k > 0);
+        } else {
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) mma_f8(tS, dK + desc_step(32 * k), dQ + desc_step(32 * k), idS, k > 0);
+        }
+        tc::mma_commit(&bars[SFULL8 + si % kBuf]);
+        tc::mma_commit(&bars[E_K + kst]);
+        ++si;
+        if (++kst == ns) {
+          kst = 0;
+          k_phase ^= 1;
+        }
+      };
+      for (; s.any() && ok; s.next(bt, p.Hkv), ++seg) {
+        ok = mbar_wait_small(&bars[QFULL8], seg & 1, abort_flag);
+        if (!ok) break;
+        issue_s(p.tree && s.t0 == 0);
+        for (int t = s.t0; t < s.t1 && ok; ++t) {
+          if (t + 1 < s.t1) issue_s(false);
+          if (!ok) break;
+          ok = mbar_wait_small(&bars[F_V + vst], v_phase, abort_flag) &&
+               mbar_wait_small(&bars[PFULL8 + pi % kBuf], pi / kBuf & 1, abort_flag);
+          if (!ok) break;
+          tc::fence_after_sync();
+          const uint64_t dP = dP0 + (uint64_t)(pi % kBuf) * desc_step(C::kPBytes);
+          const uint64_t dV = dV0 + (uint64_t)vst * desc_step(C::kTile);
+          const uint32_t acc = t > s.t0 ? 1u : 0u;
+          if (p.tree && t == 0) {
+            const uint64_t dA = tc::sw128_desc(smem_u32(base + off_V + vst * C::kTile), kTreeKeys * 128, 1024);
+            constexpr uint32_t id = tc::idesc_bf16_f32(D, C::kNT, true, true);
+#pragma unroll
+            for (int k = 0; k < kTreeKeys / 16; ++k)
+              tc::mma_bf16(tO, dA + desc_step(k * 16 * 128), dP + desc_step(k * 16 * kPitchP), id, k > 0);
+          } else {
+#pragma unroll
+            for (int k = 0; k < kTK / 32; ++k)
+              mma_f8(tO, dV + desc_step(k * 32 * D), dP + desc_step(k * 32 * kPitchP), idO, k > 0 ? 1u : acc);
+          }
+          tc::mma_commit(&bars[E_V + vst]);
+          tc::mma_commit(&bars[PVDONE + pi % kBuf]);
+          ++pi;
+          if (++vst == ns) {
+            vst = 0;
+            v_phase ^= 1;
+          }
+        }
+      }
+      tc::mma_commit(&bars[MDONE8]);  // every MMA finished before TMEM is released
+      mbar_drain(&bars[MDONE8], 0);
+    }
+  } else {
+    // ------------------------------------------------------------- softmax
+    const int sid = threadIdx.x, tid = sid & 127, group = warp >> 2;
+    // tid: the key of a tile, and the value column of O^T; r_own: the group's first query row
+    const int r_own = group * RT, quarter = warp & 3, gbar = 2 + group;
+    const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t tO = lane_addr + C::kTmemO + r_own;
+    bool dead = false;
+    int st = 0, i = 0;  // stage, tiles so far
+    uint32_t ring = 0;
+    // P.V of tile j of this CTA is done
+    auto wait_pv = [&](int j) {
+      if (j >= 0 && !dead) dead = !warp_wait_small(&bars[PVDONE + j % C::kBuf], j / C::kBuf & 1, abort_flag);
+    };
+    if (!p.tree) {  // zeros for sequences without cached keys
+      const long long per = (long long)p.n * p.H * D;
+      for (int b = 0; b < p.B; ++b)
+        if (bt.ntiles[b] == 0)
+          for (long long e = (long long)blockIdx.x * kSoft + sid; e < per; e += (long long)gridDim.x * kSoft)
+            p.out[b * per + e] = __float2bfloat16_rn(0.f);
+    }
+    for (; s.any(); s.next(bt, p.Hkv)) {
+      const int plen = bt.plen[s.b], slab = s.b * p.Hkv + s.h;
+      const bool tree_here = p.tree && s.t0 == 0;
+      const int8_t *Ke = p.Ke + (size_t)slab * p.blocks, *Ve = p.Ve + (size_t)slab * p.blocks;
+      const int used = kv8_blocks(plen);
+      // The exponents of 32 blocks (16 tiles), a lane's own: the key's in the low half, the value's in the high one.
+      auto exponents = [&](int block) {
+        const int at = min(block + lane, used - 1);
+        return (uint32_t)(kv8_clamp_exp(Ke[at]) & 0xffff) | (uint32_t)kv8_clamp_exp(Ve[at]) << 16;
+      };
+      const int tile0 = tree_here ? 0 : s.t0 - p.tree;  // first tile of cached keys
+      uint32_t exps = used > 0 ? exponents(2 * tile0) : 0u;
+
+      // ---- the segment's queries, and the tree's own keys and values, as operands
+      const int first_tile = i;
+      int q_exp, vt_exp = 0;
+      {
+        constexpr int kPerRow = D / 8, kQ = (NP * kPerRow + kSoft - 1) / kSoft,
+                      kT = (kTreeKeys * kPerRow + kSoft - 1) / kSoft;
+        const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+        uint4 q[kQ], v[kT];
+        uint32_t most = 0, most_v = 0;
+        const size_t q0 = (size_t)s.b * p.n * p.H + (size_t)s.h * p.group;
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          const int c = sid + i * kSoft, r = c / kPerRow;
+          q[i] = none;
+          if (r < rows_here) q[i] = reinterpret_cast<const uint4*>(p.q + (q0 + sm.rel[r]) * D)[c % kPerRow];
+          most = max(most, top8(q[i]));
+        }
+        // Byte of element d of row r in a bf16 operand of `rows` rows: 64 elements (128 bytes) a row and part.
+        auto in_bf16 = [](int r, int d, int rows) { return (d / 64) * rows * 128 + swizzled<128>(r, (d % 64) * 2); };
+        bool odd = false;
+        if (tree_here) {
+          if (warp == 0) {  // the rows' nodes and their ancestors
+            const int2 up = parents_of(p.parent + (size_t)s.b * p.n, p.n, lane);
+#pragma unroll 1
+            for (int r = lane; r < 64; r += 32)
+              sm.sees[r] = ancestors(up, p.n, r < rows_here ? (row0 + r) / p.group : 0, true, lane);
+          }
+          if (!dead) dead = !warp_wait_small(&bars[E_K + st], ring ^ 1, abort_flag);
+          if (!dead) dead = !warp_wait_small(&bars[E_V + st], ring ^ 1, abort_flag);
+          unsigned char* kd = base + C::off_K + st * C::kTile;
+#pragma unroll
+          for (int i = 0; i < kT; ++i) {
+            const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
+            uint4 k = none;
+            v[i] = none;
+            if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;
+            if (r < p.n) {
+              const size_t at = (((size_t)s.b * p.n + r) * p.Hkv + s.h) * D + d;
+              k = *reinterpret_cast<const uint4*>(p.kt + at);
+              v[i] = *reinterpret_cast<const uint4*>(p.vt + at);
+            }
+            // An unseen value that is not finite must not meet a weight of zero: it is left out here, and put
+            // back at the end where it is seen.
+            odd |= drop_odd(v[i]);
+            most_v = max(most_v, top8(v[i]));
+            *reinterpret_cast<uint4*>(kd + in_bf16(r, d, kTreeKeys)) = k;
+          }
+          unsigned char* qd = base + C::off_P + first_tile % C::kBuf * C::kPBytes;  // P of this tile comes later
+#pragma unroll
+          for (int i = 0; i < kQ; ++i) {
+            const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
+            if (r < NP) *reinterpret_cast<uint4*>(qd + in_bf16(r, d, C::kNT)) = q[i];
+          }
+          if (NP < C::kNT && sid < (C::kNT - NP) * kPerRow)
+            *reinterpret_cast<uint4*>(qd + in_bf16(NP + sid / kPerRow, sid % kPerRow * 8, C::kNT)) = none;
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        most_v = __reduce_max_sync(0xffffffffu, most_v);
+        if (lane == 0) {
+          sm.top[warp][0] = most;
+          sm.top[warp][1] = most_v;
+        }
+        const bool odd_any = soft_any<kSoft>(1, odd);  // a barrier too
+        if (sid == 0) sm.odd_values = odd_any;
+#pragma unroll
+        for (int w = 0; w < 4 * C::kSG; ++w) {
+          most = max(most, sm.top[w][0]);
+          most_v = max(most_v, sm.top[w][1]);
+        }
+        if (tree_here) {
+          vt_exp = top_exponent(most_v);
+          const float vs = kv8_pow2(-vt_exp);
+          unsigned char* vd = base + off_V + st * C::kTile;
+#pragma unroll
+          for (int i = 0; i < kT; ++i) {
+            const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
+            if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;
+            const uint4 w = v[i];
+            *reinterpret_cast<uint4*>(vd + in_bf16(r, d, kTreeKeys)) =
+                make_uint4(pack_bf16x2(bf16lo(w.x) * vs, bf16hi(w.x) * vs), pack_bf16x2(bf16lo(w.y) * vs, bf16hi(w.y) * vs),
+                           pack_bf16x2(bf16lo(w.z) * vs, bf16hi(w.z) * vs), pack_bf16x2(bf16lo(w.w) * vs, bf16hi(w.w) * vs));
+          }
+        }
+        q_exp = top_exponent(most);
+        const float qs = kv8_pow2(-q_exp);
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
+          if (r < NP) {
+            uint2 hi, lo;
+            split8(q[i], qs, hi, lo);
+            *reinterpret_cast<uint2*>(base + C::off_Q + swizzled<D>(r, d)) = hi;
+            *reinterpret_cast<uint2*>(base + C::off_Q + swizzled<D>(NP + r, d)) = lo;
+          }
+        }
+        tc::fence_async_smem();
+        soft_sync<kSoft>(1);
+        if (lane == 0) mbar_arrive(&bars[QFULL8]);
+        if (tree_here && sid == 0) {
+          mbar_arrive(&bars[F_K + st]);
+          mbar_arrive(&bars[F_V + st]);
+        }
+      }
+
+      uint64_t l2[RT / 2];
+#pragma unroll
+      for (int k = 0; k < RT / 2; ++k) l2[k] = 0ull;
+      int ref = tree_here ? vt_exp : -128;
+      const float a_q = p.scale_log2 * kv8_pow2(q_exp);
+      for (int t = s.t0; t < s.t1; ++t, ++i) {
+        const bool is_tree = p.tree && t == 0, first = t == s.t0;
+        const int tile = t - p.tree, key0 = tile * kTK, buf = i % C::kBuf;
+        float a = p.scale_log2;
+        int e = vt_exp;
+        if (!is_tree) {
+          const int nth = (tile - tile0) & 15;
+          if (nth == 0) {
+            if (tile > tile0) exps = exponents(2 * tile);
+            ref = max(ref, __reduce_max_sync(0xffffffffu, (int)exps >> 16));
+          }
+          const uint32_t mine = __shfl_sync(0xffffffffu, exps, 2 * nth + (tid >> 6));
+          a = a_q * kv8_pow2((int)(int16_t)mine);
+          e = (int)mine >> 16;
+        }
+        e = effective_exp(e, ref);
+        const float inv_v = kv8_pow2(-e);
+
+        // ---- u = S_hi a + (S_lo a / 16 + e), less m (none yet in a segment's first tile)
+        uint64_t u[RT / 2];
+        const uint32_t tS = lane_addr + buf * C::kTmemS + r_own;
+        if (!dead) dead = !warp_wait_small(&bars[SFULL8 + buf], i / C::kBuf & 1, abort_flag);
+        tc::fence_after_sync();
+        if (opaque(is_tree) && NP >= 16) {  // no lower parts: of S, and of O, which this tile starts
+          const uint32_t none[8] = {};
+#pragma unroll
+          for (int c = 0; c < RT; c += 8) {
+            tmem_st<8>(tS + NP + c, none);
+            tmem_st<8>(tO + NP + c, none);
+          }
+          tc::tmem_wait_st();
+        }
+        {
+          constexpr int CH = RT % 16 == 0 ? 16 : 8;
+          const uint64_t a2 = f2(a, a), b2 = f2(a / kQLo, a / kQLo), e2 = f2((float)e, (float)e);
+#pragma unroll
+          for (int c = 0; c < RT; c += CH) {
+            uint32_t hi[CH], lo[CH];
+            tmem_ld<CH>(tS + c, hi);
+            tmem_ld<CH>(tS + NP + c, lo);
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < CH; k += 2) {
+              asm volatile("" : "+r"(hi[k]), "+r"(hi[k + 1]), "+r"(lo[k]), "+r"(lo[k + 1]));  // valid after the wait only
+              const uint64_t h2 = f2(__uint_as_float(hi[k]), __uint_as_float(hi[k + 1]));
+              const uint64_t o2 = f2(__uint_as_float(lo[k]), __uint_as_float(lo[k + 1]));
+              u[(c + k) / 2] = ffma2(h2, a2, ffma2(o2, b2, e2));
+            }
+          }
+        }
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[SFREE8 + buf]);
+        if (opaque(is_tree || key0 + kTK > plen)) {  // which rows see this thread's key
+          uint32_t vis = key0 + tid < plen ? ~0u : 0u;
+          if (is_tree) {
+            vis = 0;
+            if (tid < p.n)
+#pragma unroll 1
+              for (int r = 0; r < RT; ++r) vis |= (uint32_t)((sm.sees[r_own + r] >> tid) & 1ull) << r;
+          }
+#pragma unroll
+          for (int k = 0; k < RT; k += 2) {
+            float v0, v1;
+            unf2(u[k / 2], v0, v1);
+            v0 = (vis >> k) & 1u ? v0 : -CUDART_INF_F;
+            v1 = (vis >> (k + 1)) & 1u ? v1 : -CUDART_INF_F;
+            u[k / 2] = f2(v0, v1);
+          }
+        }
+        uint32_t rise = (1u << RT / 8) - 1u;  // by chunks of 8 rows
+        if (!first) {
+          rise = 0;
+#pragma unroll
+          for (int c = 0; c < RT; c += 8) {
+            float top = -CUDART_INF_F;
+#pragma unroll
+            for (int k = c; k < c + 8; k += 4) {
+              const float4 m = *reinterpret_cast<const float4*>(&sm.m[r_own + k]);
+              u[k / 2] = fadd2(u[k / 2], f2(-m.x, -m.y));
+              u[k / 2 + 1] = fadd2(u[k / 2 + 1], f2(-m.z, -m.w));
+              float v0, v1, v2, v3;
+              unf2(u[k / 2], v0, v1);
+              unf2(u[k / 2 + 1], v2, v3);
+              top = fmax3(fmax3(top, v0, v1), v2, v3);
+            }
+            if (top > kMost) rise |= 1u << c / 8;
+          }
+          rise = __reduce_or_sync(0xffffffffu, rise);
+          if (lane == 0) sm.rise[t & 1][group][quarter] = (uint8_t)rise;
+          soft_sync<128>(gbar);
+          rise = *reinterpret_cast<const uint32_t*>(sm.rise[t & 1][group]);
+          rise = (rise | rise >> 16);
+          rise = (rise | rise >> 8) & 0xffu;
+        }
+        if (opaque(rise != 0)) {  // a new m for the rows whose weights would pass the largest code
+#pragma unroll
+          for (int c = 0; c < RT; c += 8) {
+            if (!((rise >> c / 8) & 1u)) continue;
+            float mine = 0.f;  // lane k: the largest of row c + k
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+              float v0, v1;
+              unf2(u[(c + k) / 2], v0, v1);
+              v0 = warp_top(v0);
+              v1 = warp_top(v1);
+              mine = lane == k ? v0 : (lane == k + 1 ? v1 : mine);
+            }
+            if (lane < 8) sm.part[quarter][r_own + c + lane] = mine;
+          }
+          soft_sync<128>(gbar);
+          if (tid < RT && (rise >> tid / 8) & 1u) {
+            const int r = r_own + tid;
+            const float top = fmaxf(fmaxf(sm.part[0][r], sm.part[1][r]), fmaxf(sm.part[2][r], sm.part[3][r]));
+            // a row with nothing but NaN has no m, and keeps none
+            const float up = first || top > kMost || top != top ? top - kLift : 0.f;
+            sm.m[r] = first ? up : sm.m[r] + up;
+            sm.up[r] = up;
+            sm.f[r] = fast_exp2(-up);
+          }
+          soft_sync<128>(gbar);
+          if (!first) {
+            wait_pv(i - 1);
+            tc::fence_after_sync();
+          }
+#pragma unroll
+          for (int c = 0; c < RT; c += 8) {
+            if (!((rise >> c / 8) & 1u)) continue;
+            uint32_t hi[8], lo[8];
+            if (!first) {
+              tmem_ld<8>(tO + c, hi);
+              tmem_ld<8>(tO + NP + c, lo);
+              tc::tmem_wait_ld();
+            }
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+              const float2 up = *reinterpret_cast<const float2*>(&sm.up[r_own + c + k]);
+              const float2 f = *reinterpret_cast<const float2*>(&sm.f[r_own + c + k]);
+              u[(c + k) / 2] = fadd2(u[(c + k) / 2], f2(-up.x, -up.y));
+              if (!first) {
+                asm volatile("" : "+r"(hi[k]), "+r"(hi[k + 1]), "+r"(lo[k]), "+r"(lo[k + 1]));
+                l2[(c + k) / 2] = f2mul(l2[(c + k) / 2], f2(f.x, f.y));
+                hi[k] = __float_as_uint(__uint_as_float(hi[k]) * f.x);
+                lo[k] = __float_as_uint(__uint_as_float(lo[k]) * f.x);
+                hi[k + 1] = __float_as_uint(__uint_as_float(hi[k + 1]) * f.y);
+                lo[k + 1] = __float_as_uint(__uint_as_float(lo[k + 1]) * f.y);
+              }
+            }
+            if (!first) {
+              tmem_st<8>(tO + c, hi);
+              tmem_st<8>(tO + NP + c, lo);
+            }
+          }
+          if (!first) tc::tmem_wait_st();
+        }
+
+        // ---- weights: p = 2^(u - m), l += p 2^-e, hi and lo codes
+        const uint64_t w2 = f2(inv_v, inv_v);
+        wait_pv(i - C::kBuf);  // P's buffer is free when that P.V has read it
+        unsigned char* p_row = base + C::off_P + buf * C::kPBytes;
+        if (opaque(is_tree)) {  // bf16 weights
+#pragma unroll
+          for (int c = 0; c < RT; c += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float v0, v1;
+              unf2(u[c / 2 + k], v0, v1);
+              v0 = fast_exp2(v0);
+              v1 = fast_exp2(v1);
+              l2[c / 2 + k] = ffma2(f2(v0, v1), w2, l2[c / 2 + k]);
+              w[k] = pack_bf16x2(v0, v1);
+            }
+            *reinterpret_cast<uint4*>(p_row + swizzled<C::kPitch>(tid, 2 * (r_own + c))) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          if (NP < C::kNT)
+            *reinterpret_cast<uint4*>(p_row + swizzled<C::kPitch>(tid, 2 * NP)) = make_uint4(0u, 0u, 0u, 0u);
+        } else {
+#pragma unroll
+          for (int c = 0; c < RT; c += 8) {
+            uint32_t hw[2], lw[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              uint32_t h0, l0, h1, l1;
+              float v0, v1;
+              const int j = c / 2 + 2 * k;
+              unf2(u[j], v0, v1);
+              v0 = fast_exp2(v0);
+              v1 = fast_exp2(v1);
+              l2[j] = ffma2(f2(v0, v1), w2, l2[j]);
+              split_weights(v0, v1, h0, l0);
+              unf2(u[j + 1], v0, v1);
+              v0 = fast_exp2(v0);
+              v1 = fast_exp2(v1);
+              l2[j + 1] = ffma2(f2(v0, v1), w2, l2[j + 1]);
+              split_weights(v0, v1, h1, l1);
+              hw[k] = __byte_perm(h0, h1, 0x5410);
+              lw[k] = __byte_perm(l0, l1, 0x5410);
+            }
+            if constexpr (NP == 8) {
+              *reinterpret_cast<uint4*>(p_row + swizzled<C::kPitch>(tid, 0)) = make_uint4(hw[0], hw[1], lw[0], lw[1]);
+            } else {
+              *reinterpret_cast<uint2*>(p_row + swizzled<C::kPitch>(tid, r_own + c)) = make_uint2(hw[0], hw[1]);
+              *reinterpret_cast<uint2*>(p_row + swizzled<C::kPitch>(tid, NP + r_own + c)) = make_uint2(lw[0], lw[1]);
+            }
+          }
+        }
+        if (group == 0 && !is_tree && key0 + kTK > plen) {  // value rows past the end may hold NaN: zero times NaN is no zero
+          if (!dead) dead = !warp_wait_small(&bars[F_V + st], ring, abort_flag);
+          if (key0 + tid >= plen) {
+            uint4* row = reinterpret_cast<uint4*>(base + off_V + st * C::kTile + tid * D);
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) row[c] = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        tc::fence_async_smem();
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[PFULL8 + buf]);
+        if (++st == ns) {
+          st = 0;
+          ring ^= 1;
+        }
+      }
+
+      // ---- the segment's end: l over the threads, then O / l or a partial
+      {
+        float l[RT];
+#pragma unroll
+        for (int k = 0; k < RT / 2; ++k) unf2(l2[k], l[2 * k], l[2 * k + 1]);
+        // Halving exchanges, while the rows can be halved: each leaves a lane half as many rows, summed over
+        // twice as many lanes.
+        int r0 = 0;
+#pragma unroll
+        for (int off = 16, cnt = RT; off >= 1; off >>= 1) {
+          if (cnt % 2 == 0) {
+            const bool upper = (lane & off) != 0;
+            cnt /= 2;
+#pragma unroll
+            for (int j = 0; j < RT / 2; ++j) {
+              if (j < cnt) {
+                const float send = upper ? l[j] : l[j + cnt], keep = upper ? l[j + cnt] : l[j];
+                l[j] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+              }
+            }
+            r0 += upper ? cnt : 0;
+          } else {
+#pragma unroll
+            for (int j = 0; j < RT / 2; ++j)
+              if (j < cnt) l[j] += __shfl_xor_sync(0xffffffffu, l[j], off);
+          }
+          if (off == 1)
+#pragma unroll
+            for (int j = 0; j < RT / 2; ++j)
+              if (j < cnt) sm.part[quarter][r_own + r0 + j] = l[j];
+        }
+      }
+      soft_sync<128>(gbar);
+      const bool whole = s.whole(bt);
+      if (tid < RT) {
+        const int r = r_own + tid;
+        const float sum = (sm.part[0][r] + sm.part[1][r]) + (sm.part[2][r] + sm.part[3][r]);
+        sm.f[r] = whole ? 1.f / sum : sum;
+      }
+      soft_sync<128>(gbar);
+      wait_pv(i - 1);
+      tc::fence_after_sync();
+      // D = 64: an accumulator of 64 rows keeps rows 16 w .. 16 w + 15 in lanes 32 w .. 32 w + 15
+      const int d = D == 128 ? tid : quarter * 16 + lane;
+      const bool has = D == 128 || lane < 16;
+      const bool odd = tree_here && sm.odd_values;
+      float* part = partial_slot(p.partials, x + slab, p.rows, D) + (size_t)row0 * (D + 2);
+      const size_t o0 = (size_t)s.b * p.n * p.H + (size_t)s.h * p.group;
+#pragma unroll 1
+      for (int c = 0; c < RT; c += 8) {
+        uint32_t hi[8], lo[8];
+        tmem_ld<8>(tO + c, hi);
+        tmem_ld<8>(tO + NP + c, lo);
+        tc::tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          asm volatile("" : "+r"(hi[k]), "+r"(lo[k]));
+          const int r = r_own + c + k, rel = sm.rel[r];
+          if (rel < 0 || !has || dead) continue;
+          float o = fmaf(__uint_as_float(lo[k]), 1.f / kPLo, __uint_as_float(hi[k]));
+          if (odd) {  // a visible value that is not finite decides its column
+#pragma unroll 1
+            for (int j = 0; j < p.n; ++j) {
+              const float v = __bfloat162float(p.vt[(((size_t)s.b * p.n + j) * p.Hkv + s.h) * D + d]);
+              if ((sm.sees[r] >> j) & 1ull && !isfinite(v)) o += v;
+            }
+          }
+          if (whole) {
+            p.out[(o0 + rel) * D + d] = __float2bfloat16_rn(o * sm.f[r]);
+          } else {
+            float* row = part + (size_t)r * (D + 2);
+            row[2 + d] = o;
+            if (d == 0) {
+              row[0] = sm.m[r];
+              row[1] = sm.f[r];
+            }
+          }
+        }
+      }
+      tc::fence_before_sync();
+      soft_sync<kSoft>(1);  // m, f, sees and O are free for the next segment
+    }
+  }
+
+  __syncwarp();
+  tc::fence_before_sync();
+  __syncthreads();
+  if (threadIdx.x == 0) record_abort(abort_flag, p.status);
+  if (warp == kMmaWarp) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmem, C::kCols);
+  }
+}
+
+// Joins the partials of every split slab, one warp per query row: with M the largest m,
+//   out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.
+// l is a sum of 2^-eV, so its share's weight is taken in the logarithm: either may leave fp32's range.
+constexpr int kMergeW = 8;
+template <int D>
+__global__ void __launch_bounds__(kMergeW * 32) kv8_merge_kernel(const int2* ranges, const float* partials,
+                                                                 __nv_bfloat16* out, int BH, int rows, int group,
+                                                                 int Hq, int Hkv) {
+  constexpr int kPairs = D / 64;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int lane = threadIdx.x & 31;
+  const unsigned total = (unsigned)BH * (unsigned)rows, step = gridDim.x * kMergeW;
+  pdl_wait();
+  for (unsigned wr = blockIdx.x * kMergeW + (threadIdx.x >> 5); wr < total; wr += step) {
+    const int bh = (int)(wr / (unsigned)rows), r = (int)(wr - (unsigned)bh * (unsigned)rows);
+    const int b = bh / Hkv, h = bh - b * Hkv;
+    const int2 rg = __ldcg(&ranges[bh]);
+    if (rg.x < 0) continue;
+    const size_t stride = (size_t)rows * (D + 2);
+    const float* row0 = partials + (size_t)(rg.x + bh) * stride + (size_t)r * (D + 2);
+    const int shares = rg.y - rg.x + 1;
+    float M = -CUDART_INF_F, L = 0.f;
+    float2 acc[kPairs];
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) acc[k] = make_float2(0.f, 0.f);
+    for (int c0 = 0; c0 < shares; c0 += 8) {
+      float2 ml[8], o[8][kPairs];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float* pr = row0 + (size_t)(c0 + u < shares ? c0 + u : c0) * stride;
+        ml[u] = __ldcg(reinterpret_cast<const float2*>(pr));
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) o[u][k] = __ldcg(reinterpret_cast<const float2*>(pr + 2 + 64 * k + 2 * lane));
+      }
+      float now = M;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (c0 + u < shares) now = fmaxf(now, ml[u].x);
+      const float f = M == -CUDART_INF_F ? 0.f : fast_exp2(M - now);
+      if (M != -CUDART_INF_F) {
+        L = L > 0.f ? fast_exp2(M - now + __log2f(L)) : L;
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) acc[k] = make_float2(acc[k].x * f, acc[k].y * f);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (c0 + u >= shares) break;
+        const float w = fast_exp2(ml[u].x - now);
+        L += fast_exp2(ml[u].x - now + __log2f(ml[u].y));
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) {
+          acc[k].x += w * o[u][k].x;
+          acc[k].y += w * o[u][k].y;
+        }
+      }
+      M = now;
+    }
+    const float inv = 1.f / L;
+    __nv_bfloat16* dst = out + out_row(b, h, r, rows, group, Hq) * D;
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k)
+      *reinterpret_cast<uint32_t*>(dst + 64 * k + 2 * lane) = pack_bf16x2(acc[k].x * inv, acc[k].y * inv);
+  }
+}
+
+// ------------------------------------------------------------------- host
+// A [rows, D] matrix of codes in boxes of kTK whole rows, swizzled by the row's width.
+bool make_code_map(CUtensorMap* m, const void* base, long long rows, int D) {
+  PFN_cuTensorMapEncodeTiled_v12000 fn = tensor_map_encoder();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)D};
+  const cuuint32_t box[2] = {(cuuint32_t)D, kTK};
+  const cuuint32_t es[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kMaxShares = 1024;
+
+template <int D, int NP>
+cudaError_t launch_np(const Kv8AttnArgs& a, int R, int per_tile, cudaStream_t st) {
+  using C = Cfg<D, NP>;
+  static PerDevice<int> allowed;
+  const int limit = smem_optin_bytes();
+  cudaError_t e = allow_smem(allowed, kv8_attn_tc_kernel<D, NP>, limit);
+  if (e != cudaSuccess) return e;
+  auto bytes = [&](int ns) {
+    return (size_t)1024 + C::off_small(ns) + sizeof(Small) + (size_t)(a.B + 1) * 8 + (size_t)(4 * a.B + 1) * 4;
+  };
+  int ns = kMaxStages8;  // as many stages as let the SM's CTAs share it (228 KB, 1 KB of it each CTA's own)
+  while (ns > 2 && bytes(ns) > (size_t)(limit + 1024) / C::kCtas - 1024) --ns;
+  if (bytes(ns) > (size_t)limit) return cudaErrorNotSupported;
+  CUtensorMap mk, mv;
+  const long long rows = (long long)a.B * a.Hkv * a.S_cap;
+  if (!make_code_map(&mk, a.K, rows, D) || !make_code_map(&mv, a.V, rows, D)) return cudaErrorNotSupported;
+  const int tree = a.parent != nullptr;
+  const long long tiles = (long long)a.B * a.Hkv * ((a.max_kv_len + kTK - 1) / kTK + tree);
+  long long G = a.max_ctas > 0 ? a.max_ctas : C::kCtas * sm_count() / R;
+  if (G > kMaxShares) G = kMaxShares;
+  if (G > tiles) G = tiles;
+  if (G < 1) G = 1;
+  Params8 p;
+  p.q = static_cast<const __nv_bfloat16*>(a.q);
+  p.kt = static_cast<const __nv_bfloat16*>(a.kt);
+  p.vt = static_cast<const __nv_bfloat16*>(a.vt);
+  p.Ke = a.Ke; p.Ve = a.Ve; p.kv_len = a.kv_len; p.parent = a.parent;
+  p.out = static_cast<__nv_bfloat16*>(a.out);
+  unsigned char* ws = static_cast<unsigned char*>(a.ws);
+  p.status = reinterpret_cast<unsigned*>(ws);
+  p.ranges = reinterpret_cast<int2*>(ws + WsLayout::kHeader);
+  p.partials = reinterpret_cast<float*>(ws + WsLayout::align(WsLayout::kHeader + 8 * (size_t)a.B * a.Hkv));
+  p.B = a.B; p.H = a.H; p.Hkv = a.Hkv; p.S_cap = a.S_cap; p.max_kv_len = a.max_kv_len; p.n = a.nq;
+  p.group = a.H / a.Hkv; p.rows = a.nq * p.group; p.R = R; p.per_tile = per_tile; p.tree = tree; p.ns = ns;
+  p.blocks = kv8_blocks(a.S_cap);
+  p.scale_log2 = a.scale * kLog2e;
+  e = launch_pdl(kv8_attn_tc_kernel<D, NP>, dim3((unsigned)(G * R)), dim3(C::kThreads), bytes(ns), st, mk, mv, p);
+  if (e != cudaSuccess) return e;
+  long long grid = ((long long)a.B * a.Hkv * p.rows + kMergeW - 1) / kMergeW;
+  if (grid > 8LL * sm_count()) grid = 8LL * sm_count();
+  return launch_pdl(kv8_merge_kernel<D>, dim3((unsigned)grid), dim3(kMergeW * 32), 0, st, p.ranges, p.partials, p.out,
+                    a.B * a.Hkv, p.rows, p.group, a.H, a.Hkv);
+}
+
+template <int D>
+cudaError_t launch_d(const Kv8AttnArgs& a, cudaStream_t st) {
+  const int rows = a.nq * (a.H / a.Hkv);
+  const int R = (rows + 63) / 64, per = (rows + R - 1) / R;
+  if (per <= 8) return launch_np<D, 8>(a, R, per, st);
+  if (per <= 16) return launch_np<D, 16>(a, R, per, st);
+  if (per <= 32) return launch_np<D, 32>(a, R, per, st);
+  if (per <= 48) return launch_np<D, 48>(a, R, per, st);
+  return launch_np<D, 64>(a, R, per, st);
+}
+
+}  // namespace
+
+size_t kv8_workspace_bytes(int B, int Hkv, int D, int rows) {
+  return WsLayout::align(WsLayout::kHeader + 8 * (size_t)B * Hkv) +
+         ((size_t)kMaxShares + (size_t)B * Hkv) * rows * (D + 2) * sizeof(float);
+}
+
+cudaError_t launch_kv8_attn_tc(const Kv8AttnArgs& a, cudaStream_t st) {
+  if (a.dtype != 0) return cudaErrorNotSupported;
+  // 32-bit TMA coordinates and tile counts
+  if ((long long)a.B * a.Hkv * a.S_cap > 0x7fffffffLL - kTK) return cudaErrorNotSupported;
+  return a.D == 128 ? launch_d<128>(a, st) : launch_d<64>(a, st);
+}
+
+}  // namespace glide
