@@ -3,15 +3,15 @@
 //
 // The mathematics.  With codes K8, V8 and block exponents eK, eV of key t,
 //   s[r,t] = q[r] . K8[t] * 2^eK * scale * log2(e),   u[r,t] = s[r,t] + eV[t]
-//   m[r]   = running maximum of u less 8,   p[r,t] = 2^(u - m)
+//   m[r]   = running maximum of u less 6 .. 8,   p[r,t] = 2^(u - m)
 //   O[r]   = sum_t p[r,t] V8[t],     l[r]   = sum_t p[r,t] 2^-eV[t],    out[r] = O[r] / l[r]
 // Taking the value exponent into the weight's exponent leaves the codes as they are: no key or
 // value is widened or scaled, and the tensor cores multiply the cache's own bytes.
 //
 // 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with
 // the slab's largest query scaled to at most 448, q = hi + lo / 16 exactly (elements below 2^-14 of the
-// largest to 2^-23 of it).  A weight p <= 430 is hi + lo / 32 to 2^-9 of itself, or to 2^-23 of the
-// row's largest, which is at least 256.  hi and lo are columns of their own, so both products cost twice
+// largest to 2^-23 of it).  A weight p <= 430 is hi + lo / 32 to 2^-9 of itself, or to 2^-20 of the
+// row's largest, which is at least 64.  hi and lo are columns of their own, so both products cost twice
 // the columns and nothing else.  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16 with
 // bf16 queries and weights into the columns of hi; its values are scaled to a block's range by a power
 // of two of their own, so that the weights of tree and cache lie in one range.
@@ -24,7 +24,7 @@
 // threads; it is looked for only when a weight would pass the largest code (one vote per tile), which after the
 // first tile of a slab is rare.
 //
-// Roles: SG groups of four softmax warps, one copy warp (TMA), one MMA warp; a persistent grid and the
+// Roles: SG groups of four softmax warps, two copy warps (TMA), two MMA warps; a persistent grid and the
 // cost-balanced split of the key sequence that the other kernels use.  A group takes 8 or 16 of the query
 // rows, thread = key: a thread's scores, weights and running sums then stay in ~100 registers and sixteen
 // softmax warps fill an SM (one group of 64 rows: 168 registers and spills, 660 us where this takes @64).
@@ -53,9 +53,8 @@ namespace {
 constexpr int kTK = 128;          // keys per tile
 constexpr int kTreeKeys = 64;     // rows of the tree tile
 constexpr int kMaxStages8 = 6;
-constexpr float kLift = 8.f;      // log2 of the weight of a new maximum
 constexpr float kMost = 8.75f;    // log2 of the largest weight: 448 is the largest code
-constexpr float kQLo = 16.f, kPLo = 32.f;
+constexpr float kPLo = 32.f;
 constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
 
 // What a switch of slabs costs a CTA, in tiles.
@@ -63,18 +62,24 @@ __host__ __device__ constexpr int seg_weight8(int np) { return 2 + np / 16; }
 
 // barriers
 constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, SFREE8 = 27, PFULL8 = 29, PVDONE = 31,
-              MDONE8 = 33, kBars8 = 34;
+              MDONE8 = 33, kBars8 = 35;
 
 template <int D, int NP>
 struct Cfg {
-  static constexpr int kRT = NP <= 32 ? NP : NP / 2;                  // rows of a softmax group
+  static constexpr int kRT = NP < 16 ? NP : 16;                       // rows of a softmax group
   static constexpr int kSG = NP / kRT;                                // softmax groups
   static constexpr int kSoft = 128 * kSG;
-  static constexpr int kCopyWarp = 4 * kSG, kMmaWarp = kCopyWarp + 1, kThreads = kSoft + 64;
+  // Warps after the softmax: K's copies, V's copies, S products, P.V products.  One thread for both copies or both
+  // products sets a slower pace than the stream: a copy or a product keeps its issuer busy for over 100 cycles.
+  static constexpr int kCopyK = 4 * kSG, kCopyV = kCopyK + 1, kMmaS = kCopyK + 2, kMmaO = kCopyK + 3,
+                       kThreads = kSoft + 128;
   static constexpr int kCtas = NP <= 32 ? 2 : 1;                      // of an SM
   static constexpr int kBuf = NP <= 32 ? 1 : 2;                       // S and P buffers
-  static constexpr int kN = 2 * NP;                                   // MMA columns
-  static constexpr int kNT = NP < 16 ? 16 : NP;                         // MMA columns of a tree tile
+  static constexpr int kN = 2 * NP;                                   // columns of O: hi | lo
+  // S adds hi and lo up itself, as products along 2 D; 8 columns are less than an MMA has, so there they lie side by side.
+  static constexpr bool kSplitS = NP < 16;
+  static constexpr float kQLo = kSplitS ? 16.f : 1.f;                 // q = hi + lo / kQLo
+  static constexpr int kNS = NP < 16 ? 16 : NP;                         // MMA columns of S
   static constexpr int kPitch = NP <= 16 ? 32 : (NP <= 32 ? 64 : 128);  // bytes of a key's weights
   static constexpr uint32_t kQBytes = kN * D;
   static constexpr uint32_t kPBytes = kTK * kPitch;
@@ -84,22 +89,22 @@ struct Cfg {
   static constexpr uint32_t off_K = off_P + kBuf * kPBytes;
   static __host__ __device__ uint32_t off_V(int ns) { return off_K + ns * kTile; }
   static __host__ __device__ uint32_t off_small(int ns) { return off_V(ns) + ns * kTile; }
-  static constexpr uint32_t kTmemS = kN == 96 ? 128 : kN;             // columns of an S buffer
+  static constexpr uint32_t kTmemS = kNS == 48 ? 64 : kNS;            // columns of an S buffer
   static constexpr uint32_t kTmemO = kBuf * kTmemS;                   // S buffers from column 0, then O
-  static constexpr uint32_t kCols = kTmemO + kN <= 32 ? 32 : kTmemO + kN <= 64 ? 64 : kTmemO + kN <= 128 ? 128 : 512;
+  static constexpr uint32_t kCols = kTmemO + kN <= 32 ? 32 : kTmemO + kN <= 64 ? 64 : kTmemO + kN <= 128 ? 128 : 256;
 };
 
 struct Small {  // per CTA, after the rings
   uint64_t bars[kBars8];
   ShareStart share;
   unsigned long long sees[64];  // the rows' nodes and their ancestors
-  alignas(16) float m[64];      // running maximum of each row, less kLift
-  alignas(16) float up[64];     // by how much m rose last
+  alignas(16) float minus_m[64];  // what turns a row's u into its weight's logarithm
+  alignas(16) float minus_up[64];  // by how much m rose last, negative
   alignas(16) float f[64];      // 2^-up; at the end 1 / l, or l
   alignas(16) float part[4][64];  // per lane quarter: row maxima, row sums
-  alignas(4) uint8_t rise[2][2][4];  // tiles in turn, per group and lane quarter: the chunks whose m rises
+  alignas(4) uint8_t rise[2][4][4];  // tiles in turn, per group and lane quarter: the chunks whose m rises
   int rel[64];                  // a row's place among a sequence's [node, head] rows from the slab's first head, -1: none
-  uint32_t top[8][2];           // per softmax warp: largest query, largest value of the tree
+  uint32_t top[16][2];           // per softmax warp: largest query, largest value of the tree
   uint32_t tmem;
   int abort_flag;
   int odd_values;               // the tree has values that are not finite
@@ -117,6 +122,39 @@ struct Params8 {
   float scale_log2;
 };
 
+// Waits of at most a second, as mbar_wait_small, but asleep: the thread is woken when the phase completes, or after
+// 100 us to see whether another has given up.  A wait that spins takes its instructions from the warps that work (here
+// a quarter of all that were issued).  On giving up it sets *abort.
+__device__ __forceinline__ bool mbar_sleep(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(100000u)
+      : "memory");
+  return ok != 0;
+}
+__device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  const uint64_t t0 = global_timer_ns();
+  while (!mbar_sleep(bar, parity)) {
+    if (*abort) return false;
+    if (global_timer_ns() - t0 > kWaitLimitNs) {
+      *abort = 1;
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ bool wait8(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  return mbar_sleep(bar, parity) || wait_long(bar, parity, abort);
+}
+// For every lane of a converged warp, with one outcome.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  if (__all_sync(0xffffffffu, mbar_sleep(bar, parity))) return true;
+  return __all_sync(0xffffffffu, wait_long(bar, parity, abort));
+}
 // Named barriers: 1 among all softmax threads, 2 + g within group g.
 template <int kThreads>
 __device__ __forceinline__ void soft_sync(int id) {
@@ -163,15 +201,30 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t
       : "memory");
 }
 
+// N columns of this thread's TMEM lane from each of two places, complete on return.  Loads and wait are one block of
+// code: results that a later wait makes valid would have to be copied to keep their uses behind it.
 template <int N>
-__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[N]) {
+__device__ __forceinline__ void tmem_ld2(uint32_t at, uint32_t at2, uint32_t (&r)[N], uint32_t (&q)[N]) {
   if constexpr (N == 16) {
-    tc::tmem_ld16(taddr, r);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : GLIDE_TMEM_REGS16(r), GLIDE_TMEM_REGS16(q)
+        : "r"(at), "r"(at2)
+        : "memory");
   } else {
     static_assert(N == 8, "columns");
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(taddr));
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%16];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%17];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(q[0]),
+          "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7])
+        : "r"(at), "r"(at2)
+        : "memory");
   }
 }
 template <int N>
@@ -197,34 +250,29 @@ __device__ __forceinline__ float warp_top(float x) {
 }
 
 // ---- sums of two codes
-__device__ __forceinline__ uint32_t cvt_e4m3x2_f16x2(uint32_t h) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
-  return r;
+// Four weights in [0, 430] (or NaN) as codes hi and lo, p = hi + lo / 32: the fp16 in between has 11 bits.
+// One block of code: the halves of a register are then picked by the conversions themselves.
+__device__ __forceinline__ void split_weights(float p0, float p1, float p2, float p3, uint32_t& hi, uint32_t& lo) {
+  asm("{\n\t.reg .b32 h, g, d;\n\t.reg .b16 a, b, c, e;\n\t"
+      "cvt.rn.f16x2.f32 h, %3, %2;\n\t"
+      "cvt.rn.f16x2.f32 g, %5, %4;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 a, h;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 b, g;\n\t"
+      "mov.b32 %0, {a, b};\n\t"
+      "cvt.rn.f16x2.e4m3x2 d, a;\n\t"
+      "sub.rn.f16x2 h, h, d;\n\t"
+      "cvt.rn.f16x2.e4m3x2 d, b;\n\t"
+      "sub.rn.f16x2 g, g, d;\n\t"
+      "mul.rn.f16x2 h, h, %6;\n\t"
+      "mul.rn.f16x2 g, g, %6;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 c, h;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 e, g;\n\t"
+      "mov.b32 %1, {c, e};\n\t}"
+      : "=&r"(hi), "=r"(lo)
+      : "f"(p0), "f"(p1), "f"(p2), "f"(p3), "r"(0x50005000u));  // 32, 32
 }
-__device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// Two weights in [0, 430] (or NaN) as codes hi and lo, p = hi + lo / 32: the fp16 in between has 11 bits.
-__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t& hi, uint32_t& lo) {
-  const uint32_t h = cvt_f16x2(p0, p1);
-  hi = cvt_e4m3x2_f16x2(h);
-  lo = cvt_e4m3x2_f16x2(hmul2(hsub2(h, kv8_decode2_f16(hi)), 0x50005000u));  // 32, 32
-}
-// Eight bf16 elements times s as codes hi and lo, x = hi + lo / 16; what is not finite becomes NaN.
-__device__ __forceinline__ void split8(const uint4& w, float s, uint2& hi, uint2& lo) {
+// Eight bf16 elements times s as codes hi and lo, x = hi + lo / by; what is not finite becomes NaN.
+__device__ __forceinline__ void split8(const uint4& w, float s, float by, uint2& hi, uint2& lo) {
   const uint32_t in[4] = {w.x, w.y, w.z, w.w};
   uint32_t h[4], l[4];
 #pragma unroll
@@ -234,7 +282,7 @@ __device__ __forceinline__ void split8(const uint4& w, float s, uint2& hi, uint2
     b = (in[i] & 0x7f800000u) == 0x7f800000u ? CUDART_NAN_F : b;
     h[i] = kv8_encode2(a, b);
     const float2 was = kv8_f16pair(kv8_decode2_f16(h[i]));
-    l[i] = kv8_encode2((a - was.x) * kQLo, (b - was.y) * kQLo);
+    l[i] = kv8_encode2((a - was.x) * by, (b - was.y) * by);
   }
   hi = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
   lo = make_uint2(l[0] | (l[1] << 16), l[2] | (l[3] << 16));
@@ -277,7 +325,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
     kv8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                        const Params8 p) {
   using C = Cfg<D, NP>;
-  constexpr int RT = C::kRT, kSoft = C::kSoft, kCopyWarp = C::kCopyWarp, kMmaWarp = C::kMmaWarp;
+  constexpr int RT = C::kRT, kSoft = C::kSoft, kBuf = C::kBuf;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int ns = p.ns;
@@ -313,7 +361,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
   } else {
     pdl_wait();
   }
-  if (warp == kMmaWarp) {
+  if (warp == C::kMmaS) {
     tc::tmem_alloc(&sm.tmem, C::kCols);
     tc::tmem_relinquish();
   }
@@ -324,34 +372,28 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
   SegWalk s;
   s.start(bt, sm.share);
 
-  if (warp == kCopyWarp) {
+  if (warp == C::kCopyK || warp == C::kCopyV) {
     // -------------------------------------------------------------- copies
-    if (y == 0) write_ranges(bt, p.B, p.Hkv, G, weight, p.ranges, x * 32 + lane, G * 32);
-    __syncwarp();
     if (lane == 0) {
+      const bool is_k = warp == C::kCopyK;
+      const CUtensorMap* map = is_k ? &tmK : &tmV;
+      uint64_t *full = &bars[is_k ? F_K : F_V], *empty = &bars[is_k ? E_K : E_V];
+      unsigned char* dst = base + (is_k ? C::off_K : off_V);
+      // one reader per tile: evict it first; R row tiles read each tile R times
       const uint64_t policy = p.R == 1 ? policy_evict_first() : policy_evict_normal();
-      int at = 0, st = 0;
-      uint32_t phase = 1;
-      uint32_t k_out = 0, v_out = 0, par = 0;  // by stage: a copy issued, and the parity of its last one
+      int st = 0;
+      uint32_t phase = 1, out = 0, par = 0;  // out, par by stage: a copy issued, and the parity of its last one
       bool ok = true;
       for (; s.any() && ok; s.next(bt, p.Hkv)) {
-        for (int t = s.t0; t < s.t1 && ok; ++t, ++at) {
-          if (p.tree && t == 0) {
-            // the tree's operands: the softmax warps write them
-          } else {
-            const int row = (s.b * p.Hkv + s.h) * p.S_cap + (t - p.tree) * kTK;
-            ok = mbar_wait_small(&bars[E_K + st], phase, abort_flag);
+        int row = (s.b * p.Hkv + s.h) * p.S_cap + (s.t0 - p.tree) * kTK;
+        for (int t = s.t0; t < s.t1; ++t, row += kTK) {
+          if (!p.tree || t > 0) {  // tile 0 is the tree's: the softmax warps write it
+            ok = wait8(&empty[st], phase, abort_flag);
             if (!ok) break;
-            mbar_arrive_expect_tx(&bars[F_K + st], C::kTile);
-            tc::tma_load_2d(base + C::off_K + st * C::kTile, &tmK, 0, row, &bars[F_K + st], policy);
-            k_out |= 1u << st;
-            v_out &= ~(1u << st);
+            mbar_arrive_expect_tx(&full[st], C::kTile);
+            tc::tma_load_2d(dst + st * C::kTile, map, 0, row, &full[st], policy);
+            out |= 1u << st;
             par = (par & ~(1u << st)) | ((phase ^ 1u) << st);
-            ok = mbar_wait_small(&bars[E_V + st], phase, abort_flag);
-            if (!ok) break;
-            mbar_arrive_expect_tx(&bars[F_V + st], C::kTile);
-            tc::tma_load_2d(base + off_V + st * C::kTile, &tmV, 0, row, &bars[F_V + st], policy);
-            v_out |= 1u << st;
           }
           if (++st == ns) {
             st = 0;
@@ -359,91 +401,102 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           }
         }
       }
-      if (!ok) {  // aborted: issued copies land before the CTA exits
-        for (int k = 0; k < ns; ++k) {
-          if ((k_out >> k) & 1u) mbar_drain(&bars[F_K + k], (par >> k) & 1u);
-          if ((v_out >> k) & 1u) mbar_drain(&bars[F_V + k], (par >> k) & 1u);
-        }
-      }
+      if (!ok)  // aborted: issued copies land before the CTA exits
+        for (int k = 0; k < ns; ++k)
+          if ((out >> k) & 1u) mbar_drain(&full[k], (par >> k) & 1u);
     }
-  } else if (warp == kMmaWarp) {
-    // ----------------------------------------------------------------- MMA
+  } else if (warp == C::kMmaS) {
+    // ---------------------------------------------------------- S products
     if (lane == 0) {
-      constexpr uint32_t idS = idesc_f8(128, C::kN, false, false);
-      constexpr uint32_t idO = idesc_f8(D, C::kN, true, true);
-      constexpr int kPitchP = C::kPitch;
+      constexpr uint32_t idS = idesc_f8(128, C::kNS, false, false);
+      constexpr uint32_t idT = tc::idesc_bf16_f32(128, C::kNS, false, false);
       const uint64_t dQ = swizzled_desc(smem_u32(base + C::off_Q), D);
-      const uint64_t dP0 = swizzled_desc(smem_u32(base + C::off_P), kPitchP);
       const uint64_t dK0 = swizzled_desc(smem_u32(base + C::off_K), D);
-      const uint64_t dV0 = swizzled_desc(smem_u32(base + off_V), D);
-      const uint32_t tO = tmem + C::kTmemO;
-      constexpr int kBuf = C::kBuf;
-      int kst = 0, vst = 0, seg = 0, si = 0, pi = 0;  // si, pi: tiles whose S, whose P.V were issued
-      uint32_t k_phase = 0, v_phase = 0;
+      int st = 0, seg = 0, i = 0;
+      uint32_t phase = 0;
       bool ok = true;
-      auto issue_s = [&](bool tree) {
-        ok = mbar_wait_small(&bars[F_K + kst], k_phase, abort_flag) &&
-             mbar_wait_small(&bars[SFREE8 + si % kBuf], (si / kBuf & 1) ^ 1, abort_flag);
-        if (!ok) return;
-        tc::fence_after_sync();
-        const uint32_t tS = tmem + si % kBuf * C::kTmemS;
-        const uint64_t dK = dK0 + (uint64_t)kst * desc_step(C::kTile);
-        if (tree) {  // bf16 keys [D / 64][64 keys][64], bf16 queries [D / 64][kNT][64] in P's place
-          const uint64_t dA = tc::sw128_desc(smem_u32(base + C::off_K + kst * C::kTile), 16, 1024);
-          const uint64_t dB = tc::sw128_desc(smem_u32(base + C::off_P + si % kBuf * C::kPBytes), 16, 1024);
-          constexpr uint32_t id = tc::idesc_bf16_f32(128, C::kNT, false, false);
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-            tc::mma_bf16(tS, dA + desc_step((k / 4) * kTreeKeys * 128 + (k % 4) * 32),
-                         dB + desc_step((k / 4) * C::kNT * 128 + (k % 4) * 32), id, k > 0);
-        } else {
-#pragma unroll
-          for (int k = 0; k < D / 32; ++k) mma_f8(tS, dK + desc_step(32 * k), dQ + desc_step(32 * k), idS, k > 0);
-        }
-        tc::mma_commit(&bars[SFULL8 + si % kBuf]);
-        tc::mma_commit(&bars[E_K + kst]);
-        ++si;
-        if (++kst == ns) {
-          kst = 0;
-          k_phase ^= 1;
-        }
-      };
       for (; s.any() && ok; s.next(bt, p.Hkv), ++seg) {
-        ok = mbar_wait_small(&bars[QFULL8], seg & 1, abort_flag);
-        if (!ok) break;
-        issue_s(p.tree && s.t0 == 0);
-        for (int t = s.t0; t < s.t1 && ok; ++t) {
-          if (t + 1 < s.t1) issue_s(false);
-          if (!ok) break;
-          ok = mbar_wait_small(&bars[F_V + vst], v_phase, abort_flag) &&
-               mbar_wait_small(&bars[PFULL8 + pi % kBuf], pi / kBuf & 1, abort_flag);
+        ok = wait8(&bars[QFULL8], seg & 1, abort_flag);
+        for (int t = s.t0; t < s.t1 && ok; ++t, ++i) {
+          const int buf = i % kBuf;
+          ok = wait8(&bars[F_K + st], phase, abort_flag) &&
+               wait8(&bars[SFREE8 + buf], (i / kBuf & 1) ^ 1, abort_flag);
           if (!ok) break;
           tc::fence_after_sync();
-          const uint64_t dP = dP0 + (uint64_t)(pi % kBuf) * desc_step(C::kPBytes);
-          const uint64_t dV = dV0 + (uint64_t)vst * desc_step(C::kTile);
-          const uint32_t acc = t > s.t0 ? 1u : 0u;
-          if (p.tree && t == 0) {
-            const uint64_t dA = tc::sw128_desc(smem_u32(base + off_V + vst * C::kTile), kTreeKeys * 128, 1024);
-            constexpr uint32_t id = tc::idesc_bf16_f32(D, C::kNT, true, true);
-#pragma unroll
-            for (int k = 0; k < kTreeKeys / 16; ++k)
-              tc::mma_bf16(tO, dA + desc_step(k * 16 * 128), dP + desc_step(k * 16 * kPitchP), id, k > 0);
+          const uint32_t tS = tmem + buf * C::kTmemS;
+          if (p.tree && t == 0) {  // bf16 keys [D / 64][64 keys][64], bf16 queries [D / 64][kNT][64] in P's place
+            const uint64_t dA = tc::sw128_desc(smem_u32(base + C::off_K + st * C::kTile), 16, 1024);
+            const uint64_t dB = tc::sw128_desc(smem_u32(base + C::off_P + buf * C::kPBytes), 16, 1024);
+#pragma unroll 1
+            for (int k = 0; k < D / 16; ++k)
+              tc::mma_bf16(tS, dA + desc_step((k / 4) * kTreeKeys * 128 + (k % 4) * 32),
+                           dB + desc_step((k / 4) * C::kNS * 128 + (k % 4) * 32), idT, k > 0);
           } else {
+            const uint64_t dK = dK0 + (uint64_t)st * desc_step(C::kTile);
 #pragma unroll
-            for (int k = 0; k < kTK / 32; ++k)
-              mma_f8(tO, dV + desc_step(k * 32 * D), dP + desc_step(k * 32 * kPitchP), idO, k > 0 ? 1u : acc);
+            for (int k = 0; k < D / 32; ++k) mma_f8(tS, dK + desc_step(32 * k), dQ + desc_step(32 * k), idS, k > 0);
+            if (!C::kSplitS) {
+#pragma unroll
+              for (int k = 0; k < D / 32; ++k)
+                mma_f8(tS, dK + desc_step(32 * k), dQ + desc_step(NP * D + 32 * k), idS, 1);
+            }
           }
-          tc::mma_commit(&bars[E_V + vst]);
-          tc::mma_commit(&bars[PVDONE + pi % kBuf]);
-          ++pi;
-          if (++vst == ns) {
-            vst = 0;
-            v_phase ^= 1;
+          tc::mma_commit(&bars[SFULL8 + buf]);
+          tc::mma_commit(&bars[E_K + st]);
+          if (++st == ns) {
+            st = 0;
+            phase ^= 1;
           }
         }
       }
       tc::mma_commit(&bars[MDONE8]);  // every MMA finished before TMEM is released
       mbar_drain(&bars[MDONE8], 0);
+    }
+  } else if (warp == C::kMmaO) {
+    // -------------------------------------------------------- P.V products
+    if (y == 0) write_ranges(bt, p.B, p.Hkv, G, weight, p.ranges, x * 32 + lane, G * 32);
+    __syncwarp();
+    if (lane == 0) {
+      constexpr uint32_t idO = idesc_f8(D, C::kN, true, true);
+      constexpr uint32_t idT = tc::idesc_bf16_f32(D, C::kNS, true, true);
+      constexpr int kPitchP = C::kPitch;
+      const uint64_t dP0 = swizzled_desc(smem_u32(base + C::off_P), kPitchP);
+      const uint64_t dV0 = swizzled_desc(smem_u32(base + off_V), D);
+      const uint32_t tO = tmem + C::kTmemO;
+      int st = 0, i = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (; s.any() && ok; s.next(bt, p.Hkv)) {
+        for (int t = s.t0; t < s.t1; ++t, ++i) {
+          const int buf = i % kBuf;
+          // O of the segment before is read before the first weights of this one are written
+          ok = wait8(&bars[F_V + st], phase, abort_flag) &&
+               wait8(&bars[PFULL8 + buf], i / kBuf & 1, abort_flag);
+          if (!ok) break;
+          tc::fence_after_sync();
+          const uint64_t dP = dP0 + (uint64_t)buf * desc_step(C::kPBytes);
+          if (p.tree && t == 0) {
+            const uint64_t dA = tc::sw128_desc(smem_u32(base + off_V + st * C::kTile), kTreeKeys * 128, 1024);
+#pragma unroll 1
+            for (int k = 0; k < kTreeKeys / 16; ++k)
+              tc::mma_bf16(tO, dA + desc_step(k * 16 * 128), dP + desc_step(k * 16 * kPitchP), idT, k > 0);
+          } else {
+            const uint64_t dV = dV0 + (uint64_t)st * desc_step(C::kTile);
+            const uint32_t acc = t > s.t0 ? 1u : 0u;
+#pragma unroll
+            for (int k = 0; k < kTK / 32; ++k)
+              mma_f8(tO, dV + desc_step(k * 32 * D), dP + desc_step(k * 32 * kPitchP), idO, k > 0 ? 1u : acc);
+          }
+          tc::mma_commit(&bars[PVDONE + buf]);
+          tc::mma_commit(&bars[E_V + st]);
+          if (++st == ns) {
+            st = 0;
+            phase ^= 1;
+          }
+        }
+      }
+      tc::mma_commit(&bars[MDONE8 + 1]);
+      mbar_drain(&bars[MDONE8 + 1], 0);
     }
   } else {
     // ------------------------------------------------------------- softmax
@@ -452,12 +505,14 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
     const int r_own = group * RT, quarter = warp & 3, gbar = 2 + group;
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     const uint32_t tO = lane_addr + C::kTmemO + r_own;
+    unsigned char* const p_base = base + C::off_P;
+    const uint32_t p_hi = swizzled<C::kPitch>(tid, r_own);
     bool dead = false;
     int st = 0, i = 0;  // stage, tiles so far
     uint32_t ring = 0;
     // P.V of tile j of this CTA is done
     auto wait_pv = [&](int j) {
-      if (j >= 0 && !dead) dead = !warp_wait_small(&bars[PVDONE + j % C::kBuf], j / C::kBuf & 1, abort_flag);
+      if (j >= 0) dead |= !warp_wait(&bars[PVDONE + j % C::kBuf], j / C::kBuf & 1, abort_flag);
     };
     if (!p.tree) {  // zeros for sequences without cached keys
       const long long per = (long long)p.n * p.H * D;
@@ -506,8 +561,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             for (int r = lane; r < 64; r += 32)
               sm.sees[r] = ancestors(up, p.n, r < rows_here ? (row0 + r) / p.group : 0, true, lane);
           }
-          if (!dead) dead = !warp_wait_small(&bars[E_K + st], ring ^ 1, abort_flag);
-          if (!dead) dead = !warp_wait_small(&bars[E_V + st], ring ^ 1, abort_flag);
+          dead |= !warp_wait(&bars[E_K + st], ring ^ 1, abort_flag);
+          dead |= !warp_wait(&bars[E_V + st], ring ^ 1, abort_flag);
           unsigned char* kd = base + C::off_K + st * C::kTile;
 #pragma unroll
           for (int i = 0; i < kT; ++i) {
@@ -530,10 +585,10 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 #pragma unroll
           for (int i = 0; i < kQ; ++i) {
             const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
-            if (r < NP) *reinterpret_cast<uint4*>(qd + in_bf16(r, d, C::kNT)) = q[i];
+            if (r < NP) *reinterpret_cast<uint4*>(qd + in_bf16(r, d, C::kNS)) = q[i];
           }
-          if (NP < C::kNT && sid < (C::kNT - NP) * kPerRow)
-            *reinterpret_cast<uint4*>(qd + in_bf16(NP + sid / kPerRow, sid % kPerRow * 8, C::kNT)) = none;
+          if (NP < C::kNS && sid < (C::kNS - NP) * kPerRow)
+            *reinterpret_cast<uint4*>(qd + in_bf16(NP + sid / kPerRow, sid % kPerRow * 8, C::kNS)) = none;
         }
         most = __reduce_max_sync(0xffffffffu, most);
         most_v = __reduce_max_sync(0xffffffffu, most_v);
@@ -569,7 +624,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
           if (r < NP) {
             uint2 hi, lo;
-            split8(q[i], qs, hi, lo);
+            split8(q[i], qs, C::kQLo, hi, lo);
             *reinterpret_cast<uint2*>(base + C::off_Q + swizzled<D>(r, d)) = hi;
             *reinterpret_cast<uint2*>(base + C::off_Q + swizzled<D>(NP + r, d)) = lo;
           }
@@ -583,7 +638,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         }
       }
 
-      uint64_t l2[RT / 2];
+      uint64_t l2[RT / 2];  // pairs of rows
 #pragma unroll
       for (int k = 0; k < RT / 2; ++k) l2[k] = 0ull;
       int ref = tree_here ? vt_exp : -128;
@@ -607,34 +662,31 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         const float inv_v = kv8_pow2(-e);
 
         // ---- u = S_hi a + (S_lo a / 16 + e), less m (none yet in a segment's first tile)
-        uint64_t u[RT / 2];
+        float u[RT];
         const uint32_t tS = lane_addr + buf * C::kTmemS + r_own;
-        if (!dead) dead = !warp_wait_small(&bars[SFULL8 + buf], i / C::kBuf & 1, abort_flag);
+        dead |= !warp_wait(&bars[SFULL8 + buf], i / C::kBuf & 1, abort_flag);
         tc::fence_after_sync();
-        if (opaque(is_tree) && NP >= 16) {  // no lower parts: of S, and of O, which this tile starts
+        if (opaque(is_tree) && NP >= 16) {  // this tile starts O, and its product leaves the lower parts out
           const uint32_t none[8] = {};
-#pragma unroll
-          for (int c = 0; c < RT; c += 8) {
-            tmem_st<8>(tS + NP + c, none);
-            tmem_st<8>(tO + NP + c, none);
-          }
+#pragma unroll 1
+          for (int c = 0; c < RT; c += 8) tmem_st<8>(tO + NP + c, none);
           tc::tmem_wait_st();
         }
         {
-          constexpr int CH = RT % 16 == 0 ? 16 : 8;
-          const uint64_t a2 = f2(a, a), b2 = f2(a / kQLo, a / kQLo), e2 = f2((float)e, (float)e);
+          const float ef = (float)e;
 #pragma unroll
-          for (int c = 0; c < RT; c += CH) {
-            uint32_t hi[CH], lo[CH];
-            tmem_ld<CH>(tS + c, hi);
-            tmem_ld<CH>(tS + NP + c, lo);
-            tc::tmem_wait_ld();
+          for (int c = 0; c < RT; c += 16) {
+            constexpr int CH = RT < 16 ? RT : 8;
+            uint32_t x[CH], z[CH];  // split: hi, lo; else rows c .. c + 7, rows c + 8 .. c + 15
+            tmem_ld2<CH>(tS + c, tS + c + (C::kSplitS ? NP : 8), x, z);
 #pragma unroll
-            for (int k = 0; k < CH; k += 2) {
-              asm volatile("" : "+r"(hi[k]), "+r"(hi[k + 1]), "+r"(lo[k]), "+r"(lo[k + 1]));  // valid after the wait only
-              const uint64_t h2 = f2(__uint_as_float(hi[k]), __uint_as_float(hi[k + 1]));
-              const uint64_t o2 = f2(__uint_as_float(lo[k]), __uint_as_float(lo[k + 1]));
-              u[(c + k) / 2] = ffma2(h2, a2, ffma2(o2, b2, e2));
+            for (int k = 0; k < CH; ++k) {
+              if constexpr (C::kSplitS) {
+                u[c + k] = fmaf(__uint_as_float(x[k]), a, fmaf(__uint_as_float(z[k]), a / C::kQLo, ef));
+              } else {
+                u[c + k] = fmaf(__uint_as_float(x[k]), a, ef);
+                if (c + 8 + k < RT) u[c + 8 + k] = fmaf(__uint_as_float(z[k]), a, ef);
+              }
             }
           }
         }
@@ -650,13 +702,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
               for (int r = 0; r < RT; ++r) vis |= (uint32_t)((sm.sees[r_own + r] >> tid) & 1ull) << r;
           }
 #pragma unroll
-          for (int k = 0; k < RT; k += 2) {
-            float v0, v1;
-            unf2(u[k / 2], v0, v1);
-            v0 = (vis >> k) & 1u ? v0 : -CUDART_INF_F;
-            v1 = (vis >> (k + 1)) & 1u ? v1 : -CUDART_INF_F;
-            u[k / 2] = f2(v0, v1);
-          }
+          for (int k = 0; k < RT; ++k) u[k] = (vis >> k) & 1u ? u[k] : -CUDART_INF_F;
         }
         uint32_t rise = (1u << RT / 8) - 1u;  // by chunks of 8 rows
         if (!first) {
@@ -666,13 +712,12 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             float top = -CUDART_INF_F;
 #pragma unroll
             for (int k = c; k < c + 8; k += 4) {
-              const float4 m = *reinterpret_cast<const float4*>(&sm.m[r_own + k]);
-              u[k / 2] = fadd2(u[k / 2], f2(-m.x, -m.y));
-              u[k / 2 + 1] = fadd2(u[k / 2 + 1], f2(-m.z, -m.w));
-              float v0, v1, v2, v3;
-              unf2(u[k / 2], v0, v1);
-              unf2(u[k / 2 + 1], v2, v3);
-              top = fmax3(fmax3(top, v0, v1), v2, v3);
+              const float4 m = *reinterpret_cast<const float4*>(&sm.minus_m[r_own + k]);
+              u[k] += m.x;
+              u[k + 1] += m.y;
+              u[k + 2] += m.z;
+              u[k + 3] += m.w;
+              top = fmax3(fmax3(top, u[k], u[k + 1]), u[k + 2], u[k + 3]);
             }
             if (top > kMost) rise |= 1u << c / 8;
           }
@@ -689,114 +734,105 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             if (!((rise >> c / 8) & 1u)) continue;
             float mine = 0.f;  // lane k: the largest of row c + k
 #pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-              float v0, v1;
-              unf2(u[(c + k) / 2], v0, v1);
-              v0 = warp_top(v0);
-              v1 = warp_top(v1);
-              mine = lane == k ? v0 : (lane == k + 1 ? v1 : mine);
+            for (int k = 0; k < 8; ++k) {
+              const float v = warp_top(u[c + k]);
+              mine = lane == k ? v : mine;
             }
             if (lane < 8) sm.part[quarter][r_own + c + lane] = mine;
           }
           soft_sync<128>(gbar);
+          // A new maximum gets the weight 2^lift.  Of n scores that scatter alike the largest grows slowly with n, and
+          // a rise costs about a tile's time, so the more tiles are to come the more room is left.
+          const float lift = kMost - fminf(0.75f + 0.5f * __log2f((float)(s.t1 - t)), 2.75f);
           if (tid < RT && (rise >> tid / 8) & 1u) {
             const int r = r_own + tid;
             const float top = fmaxf(fmaxf(sm.part[0][r], sm.part[1][r]), fmaxf(sm.part[2][r], sm.part[3][r]));
             // a row with nothing but NaN has no m, and keeps none
-            const float up = first || top > kMost || top != top ? top - kLift : 0.f;
-            sm.m[r] = first ? up : sm.m[r] + up;
-            sm.up[r] = up;
-            sm.f[r] = fast_exp2(-up);
+            const float up = first || top > kMost || top != top ? top - lift : 0.f;
+            sm.minus_m[r] = first ? -up : sm.minus_m[r] - up;
+            sm.minus_up[r] = -up;
+            sm.f[r] = first ? 0.f : fast_exp2(-up);
           }
           soft_sync<128>(gbar);
-          if (!first) {
-            wait_pv(i - 1);
-            tc::fence_after_sync();
-          }
 #pragma unroll
           for (int c = 0; c < RT; c += 8) {
             if (!((rise >> c / 8) & 1u)) continue;
-            uint32_t hi[8], lo[8];
-            if (!first) {
-              tmem_ld<8>(tO + c, hi);
-              tmem_ld<8>(tO + NP + c, lo);
-              tc::tmem_wait_ld();
-            }
 #pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-              const float2 up = *reinterpret_cast<const float2*>(&sm.up[r_own + c + k]);
-              const float2 f = *reinterpret_cast<const float2*>(&sm.f[r_own + c + k]);
-              u[(c + k) / 2] = fadd2(u[(c + k) / 2], f2(-up.x, -up.y));
-              if (!first) {
-                asm volatile("" : "+r"(hi[k]), "+r"(hi[k + 1]), "+r"(lo[k]), "+r"(lo[k + 1]));
-                l2[(c + k) / 2] = f2mul(l2[(c + k) / 2], f2(f.x, f.y));
-                hi[k] = __float_as_uint(__uint_as_float(hi[k]) * f.x);
-                lo[k] = __float_as_uint(__uint_as_float(lo[k]) * f.x);
-                hi[k + 1] = __float_as_uint(__uint_as_float(hi[k + 1]) * f.y);
-                lo[k + 1] = __float_as_uint(__uint_as_float(lo[k + 1]) * f.y);
-              }
-            }
-            if (!first) {
-              tmem_st<8>(tO + c, hi);
-              tmem_st<8>(tO + NP + c, lo);
+            for (int k = c; k < c + 8; ++k) {
+              u[k] += sm.minus_up[r_own + k];
+              if (k % 2 == 0) l2[k / 2] = f2mul(l2[k / 2], *reinterpret_cast<const uint64_t*>(&sm.f[r_own + k]));
             }
           }
-          if (!first) tc::tmem_wait_st();
         }
 
         // ---- weights: p = 2^(u - m), l += p 2^-e, hi and lo codes
-        const uint64_t w2 = f2(inv_v, inv_v);
         wait_pv(i - C::kBuf);  // P's buffer is free when that P.V has read it
-        unsigned char* p_row = base + C::off_P + buf * C::kPBytes;
+        const uint32_t p_at = buf * C::kPBytes;
         if (opaque(is_tree)) {  // bf16 weights
 #pragma unroll
           for (int c = 0; c < RT; c += 8) {
             uint32_t w[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              float v0, v1;
-              unf2(u[c / 2 + k], v0, v1);
-              v0 = fast_exp2(v0);
-              v1 = fast_exp2(v1);
-              l2[c / 2 + k] = ffma2(f2(v0, v1), w2, l2[c / 2 + k]);
+              const float v0 = fast_exp2(u[c + 2 * k]), v1 = fast_exp2(u[c + 2 * k + 1]);
+              l2[c / 2 + k] = ffma2(f2(v0, v1), f2(inv_v, inv_v), l2[c / 2 + k]);
               w[k] = pack_bf16x2(v0, v1);
             }
-            *reinterpret_cast<uint4*>(p_row + swizzled<C::kPitch>(tid, 2 * (r_own + c))) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(p_base + p_at + swizzled<C::kPitch>(tid, 2 * (r_own + c))) =
+                make_uint4(w[0], w[1], w[2], w[3]);
           }
-          if (NP < C::kNT)
-            *reinterpret_cast<uint4*>(p_row + swizzled<C::kPitch>(tid, 2 * NP)) = make_uint4(0u, 0u, 0u, 0u);
+          if (NP < C::kNS)
+            *reinterpret_cast<uint4*>(p_base + p_at + swizzled<C::kPitch>(tid, 2 * NP)) = make_uint4(0u, 0u, 0u, 0u);
         } else {
+          uint32_t hw[RT / 4], lw[RT / 4];
 #pragma unroll
-          for (int c = 0; c < RT; c += 8) {
-            uint32_t hw[2], lw[2];
+          for (int k = 0; k < RT / 4; ++k) {
+            const float v0 = fast_exp2(u[4 * k]), v1 = fast_exp2(u[4 * k + 1]);
+            const float v2 = fast_exp2(u[4 * k + 2]), v3 = fast_exp2(u[4 * k + 3]);
+            l2[2 * k] = ffma2(f2(v0, v1), f2(inv_v, inv_v), l2[2 * k]);
+            l2[2 * k + 1] = ffma2(f2(v2, v3), f2(inv_v, inv_v), l2[2 * k + 1]);
+            split_weights(v0, v1, v2, v3, hw[k], lw[k]);
+          }
+          if constexpr (NP == 8) {
+            *reinterpret_cast<uint4*>(p_base + p_at + p_hi) = make_uint4(hw[0], hw[1], lw[0], lw[1]);
+          } else if constexpr (RT % 16 == 0) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              uint32_t h0, l0, h1, l1;
-              float v0, v1;
-              const int j = c / 2 + 2 * k;
-              unf2(u[j], v0, v1);
-              v0 = fast_exp2(v0);
-              v1 = fast_exp2(v1);
-              l2[j] = ffma2(f2(v0, v1), w2, l2[j]);
-              split_weights(v0, v1, h0, l0);
-              unf2(u[j + 1], v0, v1);
-              v0 = fast_exp2(v0);
-              v1 = fast_exp2(v1);
-              l2[j + 1] = ffma2(f2(v0, v1), w2, l2[j + 1]);
-              split_weights(v0, v1, h1, l1);
-              hw[k] = __byte_perm(h0, h1, 0x5410);
-              lw[k] = __byte_perm(l0, l1, 0x5410);
+            for (int k = 0; k < RT / 4; k += 4) {  // the swizzle moves 16-byte pieces
+              *reinterpret_cast<uint4*>(p_base + p_at + swizzled<C::kPitch>(tid, r_own + 4 * k)) =
+                  make_uint4(hw[k], hw[k + 1], hw[k + 2], hw[k + 3]);
+              *reinterpret_cast<uint4*>(p_base + p_at + swizzled<C::kPitch>(tid, NP + r_own + 4 * k)) =
+                  make_uint4(lw[k], lw[k + 1], lw[k + 2], lw[k + 3]);
             }
-            if constexpr (NP == 8) {
-              *reinterpret_cast<uint4*>(p_row + swizzled<C::kPitch>(tid, 0)) = make_uint4(hw[0], hw[1], lw[0], lw[1]);
-            } else {
-              *reinterpret_cast<uint2*>(p_row + swizzled<C::kPitch>(tid, r_own + c)) = make_uint2(hw[0], hw[1]);
-              *reinterpret_cast<uint2*>(p_row + swizzled<C::kPitch>(tid, NP + r_own + c)) = make_uint2(lw[0], lw[1]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < RT / 4; k += 2) {
+              *reinterpret_cast<uint2*>(p_base + p_at + swizzled<C::kPitch>(tid, r_own + 4 * k)) = make_uint2(hw[k], hw[k + 1]);
+              *reinterpret_cast<uint2*>(p_base + p_at + swizzled<C::kPitch>(tid, NP + r_own + 4 * k)) =
+                  make_uint2(lw[k], lw[k + 1]);
             }
           }
         }
+        if (opaque(rise != 0 && !first)) {  // what O holds so far, to the new m, before this tile's P.V adds to it
+          wait_pv(i - 1);
+          tc::fence_after_sync();
+#pragma unroll 1
+          for (int c = 0; c < RT; c += 8) {
+            if (!((rise >> c / 8) & 1u)) continue;
+            uint32_t hi[8], lo[8];
+            tmem_ld2<8>(tO + c, tO + NP + c, hi, lo);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float f = sm.f[r_own + c + k];
+              hi[k] = __float_as_uint(__uint_as_float(hi[k]) * f);
+              lo[k] = __float_as_uint(__uint_as_float(lo[k]) * f);
+            }
+            tmem_st<8>(tO + c, hi);
+            tmem_st<8>(tO + NP + c, lo);
+          }
+          tc::tmem_wait_st();
+        }
         if (group == 0 && !is_tree && key0 + kTK > plen) {  // value rows past the end may hold NaN: zero times NaN is no zero
-          if (!dead) dead = !warp_wait_small(&bars[F_V + st], ring, abort_flag);
+          dead |= !warp_wait(&bars[F_V + st], ring, abort_flag);
           if (key0 + tid >= plen) {
             uint4* row = reinterpret_cast<uint4*>(base + off_V + st * C::kTile + tid * D);
 #pragma unroll
@@ -864,12 +900,9 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 #pragma unroll 1
       for (int c = 0; c < RT; c += 8) {
         uint32_t hi[8], lo[8];
-        tmem_ld<8>(tO + c, hi);
-        tmem_ld<8>(tO + NP + c, lo);
-        tc::tmem_wait_ld();
+        tmem_ld2<8>(tO + c, tO + NP + c, hi, lo);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          asm volatile("" : "+r"(hi[k]), "+r"(lo[k]));
           const int r = r_own + c + k, rel = sm.rel[r];
           if (rel < 0 || !has || dead) continue;
           float o = fmaf(__uint_as_float(lo[k]), 1.f / kPLo, __uint_as_float(hi[k]));
@@ -886,7 +919,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             float* row = part + (size_t)r * (D + 2);
             row[2 + d] = o;
             if (d == 0) {
-              row[0] = sm.m[r];
+              row[0] = -sm.minus_m[r];
               row[1] = sm.f[r];
             }
           }
@@ -901,7 +934,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
   tc::fence_before_sync();
   __syncthreads();
   if (threadIdx.x == 0) record_abort(abort_flag, p.status);
-  if (warp == kMmaWarp) {
+  if (warp == C::kMmaS) {
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem, C::kCols);
   }
