@@ -53,8 +53,7 @@ namespace {
 constexpr int kTK = 128;          // keys per tile
 constexpr int kTreeKeys = 64;     // rows of the tree tile
 constexpr int kMaxStages8 = 6;
-constexpr float kMost = 8.75f;    // log2 of the largest weight: 448 is the largest code
-constexpr float kPLo = 32.f;
+constexpr float kPLo = 32.f;         // p = hi + lo / kPLo
 constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
 
 // What a switch of slabs costs a CTA, in tiles.
@@ -66,32 +65,39 @@ constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, SF
 
 template <int D, int NP>
 struct Cfg {
-  static constexpr int kRT = NP < 16 ? NP : 16;                       // rows of a softmax group
+  // Few rows: weights as two codes each.  Many: values widened to fp16, a part that the rows share.
+  static constexpr bool kWiden = NP > 16;
+  static constexpr float kMost = kWiden ? 15.5f : 8.75f;              // log2 of the largest weight: 2^16, 448 are too large
+  static constexpr float kLift = kWiden ? 6.f : 8.f;                  // log2 of the weight of a new maximum
+  static constexpr int kRT = NP == 64 ? 16 : kWiden ? NP / 2 : NP;                    // rows of a softmax group
   static constexpr int kSG = NP / kRT;                                // softmax groups
   static constexpr int kSoft = 128 * kSG;
   // Warps after the softmax: K's copies, V's copies, S products, P.V products.  One thread for both copies or both
   // products sets a slower pace than the stream: a copy or a product keeps its issuer busy for over 100 cycles.
   static constexpr int kCopyK = 4 * kSG, kCopyV = kCopyK + 1, kMmaS = kCopyK + 2, kMmaO = kCopyK + 3,
                        kThreads = kSoft + 128;
-  static constexpr int kCtas = NP <= 32 ? 2 : 1;                      // of an SM
-  static constexpr int kBuf = NP <= 32 ? 1 : 2;                       // S and P buffers
-  static constexpr int kN = 2 * NP;                                   // columns of O: hi | lo
+  static constexpr int kCtas = NP <= 16 ? 2 : 1;                      // of an SM
+  static constexpr int kBuf = NP <= 16 ? 1 : 2;                       // S and P buffers
+  static constexpr int kNO = kWiden ? NP : 2 * NP;                      // columns of O (few rows: hi | lo)
   // S adds hi and lo up itself, as products along 2 D; 8 columns are less than an MMA has, so there they lie side by side.
   static constexpr bool kSplitS = NP < 16;
   static constexpr float kQLo = kSplitS ? 16.f : 1.f;                 // q = hi + lo / kQLo
   static constexpr int kNS = NP < 16 ? 16 : NP;                         // MMA columns of S
   static constexpr int kPitch = NP <= 16 ? 32 : (NP <= 32 ? 64 : 128);  // bytes of a key's weights
-  static constexpr uint32_t kQBytes = kN * D;
+  static constexpr uint32_t kQBytes = 2 * NP * D;
+  static constexpr uint32_t kWide = kTK * D * 2;                      // a tile of widened values
   static constexpr uint32_t kPBytes = kTK * kPitch;
   static constexpr uint32_t kTile = kTK * D;
   static constexpr uint32_t off_Q = 0;
   static constexpr uint32_t off_P = (kQBytes + 1023) / 1024 * 1024;
-  static constexpr uint32_t off_K = off_P + kBuf * kPBytes;
+  static constexpr uint32_t off_W = off_P + kBuf * kPBytes;
+  static constexpr uint32_t off_K = off_W + (kWiden ? kBuf * kWide : 0);
   static __host__ __device__ uint32_t off_V(int ns) { return off_K + ns * kTile; }
   static __host__ __device__ uint32_t off_small(int ns) { return off_V(ns) + ns * kTile; }
   static constexpr uint32_t kTmemS = kNS == 48 ? 64 : kNS;            // columns of an S buffer
   static constexpr uint32_t kTmemO = kBuf * kTmemS;                   // S buffers from column 0, then O
-  static constexpr uint32_t kCols = kTmemO + kN <= 32 ? 32 : kTmemO + kN <= 64 ? 64 : kTmemO + kN <= 128 ? 128 : 256;
+  static constexpr uint32_t kUsed = kTmemO + kNO;
+  static constexpr uint32_t kCols = kUsed <= 32 ? 32 : kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : 256;
 };
 
 struct Small {  // per CTA, after the rings
@@ -122,37 +128,40 @@ struct Params8 {
   float scale_log2;
 };
 
-// Waits of at most a second, as mbar_wait_small, but asleep: the thread is woken when the phase completes, or after
-// 100 us to see whether another has given up.  A wait that spins takes its instructions from the warps that work (here
-// a quarter of all that were issued).  On giving up it sets *abort.
-__device__ __forceinline__ bool mbar_sleep(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity), "r"(100000u)
-      : "memory");
-  return ok != 0;
-}
+// Waits of at most a second, as mbar_wait_small, in few instructions: those that a wait spins through are taken from
+// the warps that work.  On giving up it sets *abort.
 __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile int* abort) {
   const uint64_t t0 = global_timer_ns();
-  while (!mbar_sleep(bar, parity)) {
+  while (true) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .u32 n;\n\t"
+        "mov.u32 %0, 1;\n\tmov.u32 n, 64;\n"
+        "AGAIN:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\t"
+        "setp.ne.u32 p, n, 0;\n\t"
+        "@p bra AGAIN;\n\t"
+        "mov.u32 %0, 0;\n"
+        "DONE:\n\t}"
+        : "=&r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(1000u)
+        : "memory");
+    if (ok) return true;
     if (*abort) return false;
     if (global_timer_ns() - t0 > kWaitLimitNs) {
       *abort = 1;
       return false;
     }
   }
-  return true;
 }
 __device__ __forceinline__ bool wait8(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  return mbar_sleep(bar, parity) || wait_long(bar, parity, abort);
+  return mbar_try_wait(bar, parity) || wait_long(bar, parity, abort);
 }
 // For every lane of a converged warp, with one outcome.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  if (__all_sync(0xffffffffu, mbar_sleep(bar, parity))) return true;
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   return __all_sync(0xffffffffu, wait_long(bar, parity, abort));
 }
 // Named barriers: 1 among all softmax threads, 2 + g within group g.
@@ -201,45 +210,30 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t
       : "memory");
 }
 
-// N columns of this thread's TMEM lane from each of two places, complete on return.  Loads and wait are one block of
+// 8 columns of this thread's TMEM lane (from each of two places), complete on return.  Loads and wait are one block of
 // code: results that a later wait makes valid would have to be copied to keep their uses behind it.
-template <int N>
-__device__ __forceinline__ void tmem_ld2(uint32_t at, uint32_t at2, uint32_t (&r)[N], uint32_t (&q)[N]) {
-  if constexpr (N == 16) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : GLIDE_TMEM_REGS16(r), GLIDE_TMEM_REGS16(q)
-        : "r"(at), "r"(at2)
-        : "memory");
-  } else {
-    static_assert(N == 8, "columns");
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%16];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%17];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(q[0]),
-          "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7])
-        : "r"(at), "r"(at2)
-        : "memory");
-  }
+__device__ __forceinline__ void tmem_ld8(uint32_t at, uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(at)
+      : "memory");
 }
-template <int N>
-__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[N]) {
-  if constexpr (N == 16) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-        GLIDE_TMEM_IN16(r)
-        : "memory");
-  } else {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
-                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
-  }
+__device__ __forceinline__ void tmem_ld8x2(uint32_t at, uint32_t at2, uint32_t (&r)[8], uint32_t (&q)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%16];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%17];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(q[0]),
+        "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7])
+      : "r"(at), "r"(at2)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 
 // The largest of a value over the warp; NaN only if all are.
@@ -249,7 +243,6 @@ __device__ __forceinline__ float warp_top(float x) {
   return r;
 }
 
-// ---- sums of two codes
 // Four weights in [0, 430] (or NaN) as codes hi and lo, p = hi + lo / 32: the fp16 in between has 11 bits.
 // One block of code: the halves of a register are then picked by the conversions themselves.
 __device__ __forceinline__ void split_weights(float p0, float p1, float p2, float p3, uint32_t& hi, uint32_t& lo) {
@@ -270,6 +263,17 @@ __device__ __forceinline__ void split_weights(float p0, float p1, float p2, floa
       "mov.b32 %1, {c, e};\n\t}"
       : "=&r"(hi), "=r"(lo)
       : "f"(p0), "f"(p1), "f"(p2), "f"(p3), "r"(0x50005000u));  // 32, 32
+}
+// Four codes as four fp16 values, exactly.
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& a, uint32_t& b) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(a), "=r"(b)
+      : "r"(w));
+}
+__device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
 }
 // Eight bf16 elements times s as codes hi and lo, x = hi + lo / by; what is not finite becomes NaN.
 __device__ __forceinline__ void split8(const uint4& w, float s, float by, uint2& hi, uint2& lo) {
@@ -344,7 +348,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
   if (threadIdx.x == 0) {
     tc::prefetch_tmap(&tmK);
     tc::prefetch_tmap(&tmV);
-    for (int b = 0; b < kBars8; ++b) mbar_init(&bars[b], b == QFULL8 || (b >= SFREE8 && b < PVDONE) ? 4 * C::kSG : 1);
+    for (int b = 0; b < kBars8; ++b) mbar_init(&bars[b], (C::kWiden && b >= E_V && b < QFULL8) || b == QFULL8 || (b >= SFREE8 && b < PVDONE) ? 4 * C::kSG : 1);
     *abort_flag = 0;
     fence_barrier_init();
   }
@@ -387,7 +391,9 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       for (; s.any() && ok; s.next(bt, p.Hkv)) {
         int row = (s.b * p.Hkv + s.h) * p.S_cap + (s.t0 - p.tree) * kTK;
         for (int t = s.t0; t < s.t1; ++t, row += kTK) {
-          if (!p.tree || t > 0) {  // tile 0 is the tree's: the softmax warps write it
+          if (p.tree && t == 0) {  // the tree's: the softmax warps write it, K's part into K's ring
+            if (C::kWiden && !is_k) continue;  // its values go into W
+          } else {
             ok = wait8(&empty[st], phase, abort_flag);
             if (!ok) break;
             mbar_arrive_expect_tx(&full[st], C::kTile);
@@ -457,41 +463,50 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
     if (y == 0) write_ranges(bt, p.B, p.Hkv, G, weight, p.ranges, x * 32 + lane, G * 32);
     __syncwarp();
     if (lane == 0) {
-      constexpr uint32_t idO = idesc_f8(D, C::kN, true, true);
+      constexpr uint32_t id8 = idesc_f8(D, C::kNO, true, true);
       constexpr uint32_t idT = tc::idesc_bf16_f32(D, C::kNS, true, true);
+      constexpr uint32_t id16 = idT & ~((1u << 7) | (1u << 10));  // fp16 for bf16
       constexpr int kPitchP = C::kPitch;
       const uint64_t dP0 = swizzled_desc(smem_u32(base + C::off_P), kPitchP);
-      const uint64_t dV0 = swizzled_desc(smem_u32(base + off_V), D);
+      const uint32_t values = smem_u32(base + (C::kWiden ? C::off_W : off_V));
+      const uint64_t dV0 = C::kWiden ? tc::sw128_desc(values, kTK * 128, 1024) : swizzled_desc(values, D);
+      const uint64_t dT0 = tc::sw128_desc(values, kTreeKeys * 128, 1024);
       const uint32_t tO = tmem + C::kTmemO;
-      int st = 0, i = 0;
+      int i = 0, st = 0;
       uint32_t phase = 0;
       bool ok = true;
       for (; s.any() && ok; s.next(bt, p.Hkv)) {
         for (int t = s.t0; t < s.t1; ++t, ++i) {
           const int buf = i % kBuf;
           // O of the segment before is read before the first weights of this one are written
-          ok = wait8(&bars[F_V + st], phase, abort_flag) &&
+          ok = (C::kWiden || wait8(&bars[F_V + st], phase, abort_flag)) &&
                wait8(&bars[PFULL8 + buf], i / kBuf & 1, abort_flag);
           if (!ok) break;
           tc::fence_after_sync();
           const uint64_t dP = dP0 + (uint64_t)buf * desc_step(C::kPBytes);
+          const uint64_t at = C::kWiden ? (uint64_t)buf * desc_step(C::kWide) : (uint64_t)st * desc_step(C::kTile);
+          const uint32_t acc = t > s.t0 ? 1u : 0u;
           if (p.tree && t == 0) {
-            const uint64_t dA = tc::sw128_desc(smem_u32(base + off_V + st * C::kTile), kTreeKeys * 128, 1024);
 #pragma unroll 1
             for (int k = 0; k < kTreeKeys / 16; ++k)
-              tc::mma_bf16(tO, dA + desc_step(k * 16 * 128), dP + desc_step(k * 16 * kPitchP), idT, k > 0);
+              tc::mma_bf16(tO, dT0 + at + desc_step(k * 16 * 128), dP + desc_step(k * 16 * kPitchP), idT, k > 0);
+          } else if (C::kWiden) {
+#pragma unroll
+            for (int k = 0; k < kTK / 16; ++k)
+              tc::mma_bf16(tO, dV0 + at + desc_step(k * 16 * 128), dP + desc_step(k * 16 * kPitchP), id16,
+                           k > 0 ? 1u : acc);
           } else {
-            const uint64_t dV = dV0 + (uint64_t)st * desc_step(C::kTile);
-            const uint32_t acc = t > s.t0 ? 1u : 0u;
 #pragma unroll
             for (int k = 0; k < kTK / 32; ++k)
-              mma_f8(tO, dV + desc_step(k * 32 * D), dP + desc_step(k * 32 * kPitchP), idO, k > 0 ? 1u : acc);
+              mma_f8(tO, dV0 + at + desc_step(k * 32 * D), dP + desc_step(k * 32 * kPitchP), id8, k > 0 ? 1u : acc);
           }
           tc::mma_commit(&bars[PVDONE + buf]);
-          tc::mma_commit(&bars[E_V + st]);
-          if (++st == ns) {
-            st = 0;
-            phase ^= 1;
+          if (!C::kWiden) {
+            tc::mma_commit(&bars[E_V + st]);
+            if (++st == ns) {
+              st = 0;
+              phase ^= 1;
+            }
           }
         }
       }
@@ -505,11 +520,15 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
     const int r_own = group * RT, quarter = warp & 3, gbar = 2 + group;
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     const uint32_t tO = lane_addr + C::kTmemO + r_own;
-    unsigned char* const p_base = base + C::off_P;
-    const uint32_t p_hi = swizzled<C::kPitch>(tid, r_own);
+    // Where this thread's pieces of its key's row lie: 16 codes at a time of V, widened to 32 bytes of W.
+    constexpr int kPieces = D / 16 / C::kSG;
+    const uint32_t x128 = (tid & 7) << 4, xD = D == 128 ? x128 : ((tid >> 1) & 3) << 4;
+    const uint32_t v_from = tid * D, v_mix = (group * 16) ^ xD, w_to = tid * 128, w_mix = (group * 32) ^ x128;
+    const uint32_t p_row = tid * C::kPitch,
+                   p_mix = C::kPitch == 128 ? x128 : (C::kPitch == 64 ? ((tid >> 1) & 3) << 4 : ((tid >> 2) & 1) << 4);
     bool dead = false;
-    int st = 0, i = 0;  // stage, tiles so far
-    uint32_t ring = 0;
+    int st = 0, vst = 0, i = 0;  // stages of K and V, tiles so far
+    uint32_t ring = 0, v_ring = 0;
     // P.V of tile j of this CTA is done
     auto wait_pv = [&](int j) {
       if (j >= 0) dead |= !warp_wait(&bars[PVDONE + j % C::kBuf], j / C::kBuf & 1, abort_flag);
@@ -526,13 +545,21 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       const bool tree_here = p.tree && s.t0 == 0;
       const int8_t *Ke = p.Ke + (size_t)slab * p.blocks, *Ve = p.Ve + (size_t)slab * p.blocks;
       const int used = kv8_blocks(plen);
-      // The exponents of 32 blocks (16 tiles), a lane's own: the key's in the low half, the value's in the high one.
-      auto exponents = [&](int block) {
+      // What 32 blocks (16 tiles) make of scores and weights, a lane's own: the upper halves of the fp32 numbers 2^eK
+      // (low half) and eV (high half), and 2^-eV.
+      uint32_t scales = 0;
+      float inv = 0.f;
+      int ref = -128;
+      auto load_scales = [&](int block) {
         const int at = min(block + lane, used - 1);
-        return (uint32_t)(kv8_clamp_exp(Ke[at]) & 0xffff) | (uint32_t)kv8_clamp_exp(Ve[at]) << 16;
+        const int ek = kv8_clamp_exp(Ke[at]), ev = kv8_clamp_exp(Ve[at]);
+        ref = max(ref, __reduce_max_sync(0xffffffffu, ev));
+        const int e = effective_exp(ev, ref);
+        scales = (uint32_t)(ek + 127) << 7 | (__float_as_uint((float)e) & 0xffff0000u);
+        inv = kv8_pow2(-e);
       };
       const int tile0 = tree_here ? 0 : s.t0 - p.tree;  // first tile of cached keys
-      uint32_t exps = used > 0 ? exponents(2 * tile0) : 0u;
+      if (used > 0 && !tree_here) load_scales(2 * tile0);
 
       // ---- the segment's queries, and the tree's own keys and values, as operands
       const int first_tile = i;
@@ -562,7 +589,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
               sm.sees[r] = ancestors(up, p.n, r < rows_here ? (row0 + r) / p.group : 0, true, lane);
           }
           dead |= !warp_wait(&bars[E_K + st], ring ^ 1, abort_flag);
-          dead |= !warp_wait(&bars[E_V + st], ring ^ 1, abort_flag);
+          if (!C::kWiden) dead |= !warp_wait(&bars[E_V + st], ring ^ 1, abort_flag);
           unsigned char* kd = base + C::off_K + st * C::kTile;
 #pragma unroll
           for (int i = 0; i < kT; ++i) {
@@ -606,7 +633,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         if (tree_here) {
           vt_exp = top_exponent(most_v);
           const float vs = kv8_pow2(-vt_exp);
-          unsigned char* vd = base + off_V + st * C::kTile;
+          unsigned char* vd =  // W's buffer is free, as P's is
+              base + (C::kWiden ? C::off_W + first_tile % kBuf * C::kWide : off_V + st * C::kTile);
 #pragma unroll
           for (int i = 0; i < kT; ++i) {
             const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
@@ -634,51 +662,80 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         if (lane == 0) mbar_arrive(&bars[QFULL8]);
         if (tree_here && sid == 0) {
           mbar_arrive(&bars[F_K + st]);
-          mbar_arrive(&bars[F_V + st]);
+          if (!C::kWiden) mbar_arrive(&bars[F_V + st]);
         }
       }
 
       uint64_t l2[RT / 2];  // pairs of rows
 #pragma unroll
       for (int k = 0; k < RT / 2; ++k) l2[k] = 0ull;
-      int ref = tree_here ? vt_exp : -128;
+      if (tree_here) {
+        ref = vt_exp;
+        if (used > 0) load_scales(0);
+      }
       const float a_q = p.scale_log2 * kv8_pow2(q_exp);
+      int nth = 0;  // of the tiles whose scales the lanes hold
       for (int t = s.t0; t < s.t1; ++t, ++i) {
         const bool is_tree = p.tree && t == 0, first = t == s.t0;
-        const int tile = t - p.tree, key0 = tile * kTK, buf = i % C::kBuf;
-        float a = p.scale_log2;
-        int e = vt_exp;
+        const int key0 = (t - p.tree) * kTK, buf = i % kBuf;
+        float a = p.scale_log2, ef = (float)effective_exp(vt_exp, vt_exp), inv_v = kv8_pow2(-effective_exp(vt_exp, vt_exp));
         if (!is_tree) {
-          const int nth = (tile - tile0) & 15;
-          if (nth == 0) {
-            if (tile > tile0) exps = exponents(2 * tile);
-            ref = max(ref, __reduce_max_sync(0xffffffffu, (int)exps >> 16));
+          if (nth == 32) {
+            load_scales(key0 / kKv8Block);
+            nth = 0;
           }
-          const uint32_t mine = __shfl_sync(0xffffffffu, exps, 2 * nth + (tid >> 6));
-          a = a_q * kv8_pow2((int)(int16_t)mine);
-          e = (int)mine >> 16;
+          const uint32_t mine = __shfl_sync(0xffffffffu, scales, nth + (tid >> 6));
+          inv_v = __shfl_sync(0xffffffffu, inv, nth + (tid >> 6));
+          a = a_q * __uint_as_float(mine << 16);
+          ef = __uint_as_float(mine & 0xffff0000u);
+          nth += 2;
         }
-        e = effective_exp(e, ref);
-        const float inv_v = kv8_pow2(-e);
 
-        // ---- u = S_hi a + (S_lo a / 16 + e), less m (none yet in a segment's first tile)
+        wait_pv(i - kBuf);  // the buffers of P and W are free when that P.V has read them
+        if (C::kWiden && !is_tree) {
+          // ---- the values as fp16, exactly: this thread's part of its key's row, zeros past the end (what lies there
+          // may be NaN, and zero times NaN is no zero)
+          dead |= !warp_wait(&bars[F_V + vst], v_ring, abort_flag);
+          const unsigned char* from = base + off_V + vst * C::kTile + v_from;
+          unsigned char* to = base + C::off_W + buf * C::kWide + w_to;
+#pragma unroll
+          for (int j = 0; j < kPieces; ++j) {
+            uint4 w = *reinterpret_cast<const uint4*>(from + (v_mix ^ (j * C::kSG * 16)));
+            if (opaque(key0 + kTK > plen) && key0 + tid >= plen) w = make_uint4(0u, 0u, 0u, 0u);
+            uint4 lo, hi;
+            widen4(w.x, lo.x, lo.y);
+            widen4(w.y, lo.z, lo.w);
+            widen4(w.z, hi.x, hi.y);
+            widen4(w.w, hi.z, hi.w);
+            const uint32_t at = (j * C::kSG / 4) * kTK * 128 + (w_mix ^ ((j * C::kSG % 4) * 32));
+            *reinterpret_cast<uint4*>(to + at) = lo;
+            *reinterpret_cast<uint4*>(to + (at ^ 16)) = hi;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[E_V + vst]);
+          if (++vst == ns) {
+            vst = 0;
+            v_ring ^= 1;
+          }
+        }
+
+        // ---- u = S a + e, less m (none yet in a segment's first tile)
         float u[RT];
         const uint32_t tS = lane_addr + buf * C::kTmemS + r_own;
         dead |= !warp_wait(&bars[SFULL8 + buf], i / C::kBuf & 1, abort_flag);
         tc::fence_after_sync();
-        if (opaque(is_tree) && NP >= 16) {  // this tile starts O, and its product leaves the lower parts out
+        if (!C::kWiden && NP >= 16 && opaque(is_tree)) {  // this tile starts O, and its product leaves the lower parts out
           const uint32_t none[8] = {};
 #pragma unroll 1
-          for (int c = 0; c < RT; c += 8) tmem_st<8>(tO + NP + c, none);
+          for (int c = 0; c < RT; c += 8) tmem_st8(tO + NP + c, none);
           tc::tmem_wait_st();
         }
         {
-          const float ef = (float)e;
 #pragma unroll
           for (int c = 0; c < RT; c += 16) {
-            constexpr int CH = RT < 16 ? RT : 8;
+            constexpr int CH = 8;
             uint32_t x[CH], z[CH];  // split: hi, lo; else rows c .. c + 7, rows c + 8 .. c + 15
-            tmem_ld2<CH>(tS + c, tS + c + (C::kSplitS ? NP : 8), x, z);
+            tmem_ld8x2(tS + c, tS + c + (C::kSplitS ? NP : 8), x, z);
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
               if constexpr (C::kSplitS) {
@@ -719,7 +776,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
               u[k + 3] += m.w;
               top = fmax3(fmax3(top, u[k], u[k + 1]), u[k + 2], u[k + 3]);
             }
-            if (top > kMost) rise |= 1u << c / 8;
+            if (top > C::kMost) rise |= 1u << c / 8;
           }
           rise = __reduce_or_sync(0xffffffffu, rise);
           if (lane == 0) sm.rise[t & 1][group][quarter] = (uint8_t)rise;
@@ -741,14 +798,11 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             if (lane < 8) sm.part[quarter][r_own + c + lane] = mine;
           }
           soft_sync<128>(gbar);
-          // A new maximum gets the weight 2^lift.  Of n scores that scatter alike the largest grows slowly with n, and
-          // a rise costs about a tile's time, so the more tiles are to come the more room is left.
-          const float lift = kMost - fminf(0.75f + 0.5f * __log2f((float)(s.t1 - t)), 2.75f);
           if (tid < RT && (rise >> tid / 8) & 1u) {
             const int r = r_own + tid;
             const float top = fmaxf(fmaxf(sm.part[0][r], sm.part[1][r]), fmaxf(sm.part[2][r], sm.part[3][r]));
             // a row with nothing but NaN has no m, and keeps none
-            const float up = first || top > kMost || top != top ? top - lift : 0.f;
+            const float up = first || top > C::kMost || top != top ? top - C::kLift : 0.f;
             sm.minus_m[r] = first ? -up : sm.minus_m[r] - up;
             sm.minus_up[r] = -up;
             sm.f[r] = first ? 0.f : fast_exp2(-up);
@@ -765,10 +819,10 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           }
         }
 
-        // ---- weights: p = 2^(u - m), l += p 2^-e, hi and lo codes
-        wait_pv(i - C::kBuf);  // P's buffer is free when that P.V has read it
-        const uint32_t p_at = buf * C::kPBytes;
-        if (opaque(is_tree)) {  // bf16 weights
+        // ---- weights: p = 2^(u - m), l += p 2^-e, in bf16 beside the tree's bf16 values, in fp16 beside widened
+        // ones, else as two codes
+        unsigned char* const p_to = base + C::off_P + buf * C::kPBytes + p_row;
+        if (opaque(is_tree)) {
 #pragma unroll
           for (int c = 0; c < RT; c += 8) {
             uint32_t w[4];
@@ -778,11 +832,21 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
               l2[c / 2 + k] = ffma2(f2(v0, v1), f2(inv_v, inv_v), l2[c / 2 + k]);
               w[k] = pack_bf16x2(v0, v1);
             }
-            *reinterpret_cast<uint4*>(p_base + p_at + swizzled<C::kPitch>(tid, 2 * (r_own + c))) =
-                make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(p_to + ((2 * (r_own + c)) ^ p_mix)) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          if (NP < C::kNS)
-            *reinterpret_cast<uint4*>(p_base + p_at + swizzled<C::kPitch>(tid, 2 * NP)) = make_uint4(0u, 0u, 0u, 0u);
+          if (NP < C::kNS) *reinterpret_cast<uint4*>(p_to + ((2 * NP) ^ p_mix)) = make_uint4(0u, 0u, 0u, 0u);
+        } else if constexpr (C::kWiden) {
+#pragma unroll
+          for (int c = 0; c < RT; c += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float v0 = fast_exp2(u[c + 2 * k]), v1 = fast_exp2(u[c + 2 * k + 1]);
+              l2[c / 2 + k] = ffma2(f2(v0, v1), f2(inv_v, inv_v), l2[c / 2 + k]);
+              w[k] = cvt_f16x2(v0, v1);
+            }
+            *reinterpret_cast<uint4*>(p_to + ((2 * (r_own + c)) ^ p_mix)) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
         } else {
           uint32_t hw[RT / 4], lw[RT / 4];
 #pragma unroll
@@ -794,21 +858,17 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             split_weights(v0, v1, v2, v3, hw[k], lw[k]);
           }
           if constexpr (NP == 8) {
-            *reinterpret_cast<uint4*>(p_base + p_at + p_hi) = make_uint4(hw[0], hw[1], lw[0], lw[1]);
-          } else if constexpr (RT % 16 == 0) {
-#pragma unroll
-            for (int k = 0; k < RT / 4; k += 4) {  // the swizzle moves 16-byte pieces
-              *reinterpret_cast<uint4*>(p_base + p_at + swizzled<C::kPitch>(tid, r_own + 4 * k)) =
-                  make_uint4(hw[k], hw[k + 1], hw[k + 2], hw[k + 3]);
-              *reinterpret_cast<uint4*>(p_base + p_at + swizzled<C::kPitch>(tid, NP + r_own + 4 * k)) =
-                  make_uint4(lw[k], lw[k + 1], lw[k + 2], lw[k + 3]);
-            }
+            *reinterpret_cast<uint4*>(p_to + p_mix) = make_uint4(hw[0], hw[1], lw[0], lw[1]);
           } else {
+            *reinterpret_cast<uint4*>(p_to + p_mix) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+            *reinterpret_cast<uint4*>(p_to + (16 ^ p_mix)) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+          }
+          if (opaque(key0 + kTK > plen)) {  // value rows past the end may hold NaN: zero times NaN is no zero
+            dead |= !warp_wait(&bars[F_V + st], ring, abort_flag);
+            if (key0 + tid >= plen) {
+              uint4* row = reinterpret_cast<uint4*>(base + off_V + st * C::kTile + tid * D);
 #pragma unroll
-            for (int k = 0; k < RT / 4; k += 2) {
-              *reinterpret_cast<uint2*>(p_base + p_at + swizzled<C::kPitch>(tid, r_own + 4 * k)) = make_uint2(hw[k], hw[k + 1]);
-              *reinterpret_cast<uint2*>(p_base + p_at + swizzled<C::kPitch>(tid, NP + r_own + 4 * k)) =
-                  make_uint2(lw[k], lw[k + 1]);
+              for (int c = 0; c < D / 16; ++c) row[c] = make_uint4(0u, 0u, 0u, 0u);
             }
           }
         }
@@ -818,26 +878,16 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 #pragma unroll 1
           for (int c = 0; c < RT; c += 8) {
             if (!((rise >> c / 8) & 1u)) continue;
-            uint32_t hi[8], lo[8];
-            tmem_ld2<8>(tO + c, tO + NP + c, hi, lo);
+            uint32_t o[8];
+#pragma unroll 1
+            for (int half = 0; half < (C::kWiden ? 1 : 2); ++half) {
+              tmem_ld8(tO + half * NP + c, o);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float f = sm.f[r_own + c + k];
-              hi[k] = __float_as_uint(__uint_as_float(hi[k]) * f);
-              lo[k] = __float_as_uint(__uint_as_float(lo[k]) * f);
+              for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * sm.f[r_own + c + k]);
+              tmem_st8(tO + half * NP + c, o);
             }
-            tmem_st<8>(tO + c, hi);
-            tmem_st<8>(tO + NP + c, lo);
           }
           tc::tmem_wait_st();
-        }
-        if (group == 0 && !is_tree && key0 + kTK > plen) {  // value rows past the end may hold NaN: zero times NaN is no zero
-          dead |= !warp_wait(&bars[F_V + st], ring, abort_flag);
-          if (key0 + tid >= plen) {
-            uint4* row = reinterpret_cast<uint4*>(base + off_V + st * C::kTile + tid * D);
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) row[c] = make_uint4(0u, 0u, 0u, 0u);
-          }
         }
         tc::fence_async_smem();
         tc::fence_before_sync();
@@ -899,13 +949,17 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       const size_t o0 = (size_t)s.b * p.n * p.H + (size_t)s.h * p.group;
 #pragma unroll 1
       for (int c = 0; c < RT; c += 8) {
-        uint32_t hi[8], lo[8];
-        tmem_ld2<8>(tO + c, tO + NP + c, hi, lo);
+        uint32_t acc[8], low[8];
+        if (C::kWiden)
+          tmem_ld8(tO + c, acc);
+        else
+          tmem_ld8x2(tO + c, tO + NP + c, acc, low);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const int r = r_own + c + k, rel = sm.rel[r];
           if (rel < 0 || !has || dead) continue;
-          float o = fmaf(__uint_as_float(lo[k]), 1.f / kPLo, __uint_as_float(hi[k]));
+          float o = __uint_as_float(acc[k]);
+          if (!C::kWiden) o = fmaf(__uint_as_float(low[k]), 1.f / kPLo, o);
           if (odd) {  // a visible value that is not finite decides its column
 #pragma unroll 1
             for (int j = 0; j < p.n; ++j) {
