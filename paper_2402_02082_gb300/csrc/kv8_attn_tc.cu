@@ -164,6 +164,15 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   return __all_sync(0xffffffffu, wait_long(bar, parity, abort));
 }
+// True in one lane of a converged warp.  The products and copies are issued behind it, by a warp whose loops all lanes
+// run: the compiler then knows that one thread issues, and that its operands are the warp's.  Behind `lane == 0` every
+// product took its issuer 120 - 210 cycles, behind this 60 - 70 (M = 128, N = 64: 8 fp16 products 978 -> 474 cycles).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
 // Named barriers: 1 among all softmax threads, 2 + g within group g.
 template <int kThreads>
 __device__ __forceinline__ void soft_sync(int id) {
@@ -343,7 +352,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
   bt.ntiles = bt.len + p.B;
   bt.plen = bt.ntiles + p.B;
   bt.sidx = bt.plen + p.B;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     tc::prefetch_tmap(&tmK);
@@ -378,67 +387,72 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 
   if (warp == C::kCopyK || warp == C::kCopyV) {
     // -------------------------------------------------------------- copies
-    if (lane == 0) {
-      const bool is_k = warp == C::kCopyK;
-      const CUtensorMap* map = is_k ? &tmK : &tmV;
-      uint64_t *full = &bars[is_k ? F_K : F_V], *empty = &bars[is_k ? E_K : E_V];
-      unsigned char* dst = base + (is_k ? C::off_K : off_V);
-      // one reader per tile: evict it first; R row tiles read each tile R times
-      const uint64_t policy = p.R == 1 ? policy_evict_first() : policy_evict_normal();
-      int st = 0;
-      uint32_t phase = 1, out = 0, par = 0;  // out, par by stage: a copy issued, and the parity of its last one
-      bool ok = true;
-      for (; s.any() && ok; s.next(bt, p.Hkv)) {
-        int row = (s.b * p.Hkv + s.h) * p.S_cap + (s.t0 - p.tree) * kTK;
-        for (int t = s.t0; t < s.t1; ++t, row += kTK) {
-          if (p.tree && t == 0) {  // the tree's: the softmax warps write it, K's part into K's ring
-            if (C::kWiden && !is_k) continue;  // its values go into W
-          } else {
-            ok = wait8(&empty[st], phase, abort_flag);
-            if (!ok) break;
+    const bool is_k = warp == C::kCopyK;
+    const CUtensorMap* map = is_k ? &tmK : &tmV;
+    uint64_t *full = &bars[is_k ? F_K : F_V], *empty = &bars[is_k ? E_K : E_V];
+    unsigned char* dst = base + (is_k ? C::off_K : off_V);
+    // one reader per tile: evict it first; R row tiles read each tile R times
+    const uint64_t policy = p.R == 1 ? policy_evict_first() : policy_evict_normal();
+    int st = 0;
+    uint32_t phase = 1, out = 0, par = 0;  // out, par by stage: a copy issued, and the parity of its last one
+    bool ok = true;
+    for (; s.any() && ok; s.next(bt, p.Hkv)) {
+      int row = (s.b * p.Hkv + s.h) * p.S_cap + (s.t0 - p.tree) * kTK;
+      for (int t = s.t0; t < s.t1; ++t, row += kTK) {
+        if (p.tree && t == 0) {  // the tree's: the softmax warps write it, K's part into K's ring
+          if (C::kWiden && !is_k) continue;  // its values go into W
+        } else {
+          ok = warp_wait(&empty[st], phase, abort_flag);
+          if (!ok) break;
+          if (elect_one()) {
             mbar_arrive_expect_tx(&full[st], C::kTile);
             tc::tma_load_2d(dst + st * C::kTile, map, 0, row, &full[st], policy);
-            out |= 1u << st;
-            par = (par & ~(1u << st)) | ((phase ^ 1u) << st);
           }
-          if (++st == ns) {
-            st = 0;
-            phase ^= 1;
-          }
+          __syncwarp();
+          out |= 1u << st;
+          par = (par & ~(1u << st)) | ((phase ^ 1u) << st);
+        }
+        if (++st == ns) {
+          st = 0;
+          phase ^= 1;
         }
       }
-      if (!ok)  // aborted: issued copies land before the CTA exits
-        for (int k = 0; k < ns; ++k)
-          if ((out >> k) & 1u) mbar_drain(&full[k], (par >> k) & 1u);
     }
+    if (!ok && lane == 0)  // aborted: issued copies land before the CTA exits
+      for (int k = 0; k < ns; ++k)
+        if ((out >> k) & 1u) mbar_drain(&full[k], (par >> k) & 1u);
   } else if (warp == C::kMmaS) {
     // ---------------------------------------------------------- S products
-    if (lane == 0) {
-      constexpr uint32_t idS = idesc_f8(128, C::kNS, false, false);
-      constexpr uint32_t idT = tc::idesc_bf16_f32(128, C::kNS, false, false);
-      const uint64_t dQ = swizzled_desc(smem_u32(base + C::off_Q), D);
-      const uint64_t dK0 = swizzled_desc(smem_u32(base + C::off_K), D);
-      int st = 0, seg = 0, i = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (; s.any() && ok; s.next(bt, p.Hkv), ++seg) {
-        ok = wait8(&bars[QFULL8], seg & 1, abort_flag);
-        for (int t = s.t0; t < s.t1 && ok; ++t, ++i) {
-          const int buf = i % kBuf;
-          ok = wait8(&bars[F_K + st], phase, abort_flag) &&
-               wait8(&bars[SFREE8 + buf], (i / kBuf & 1) ^ 1, abort_flag);
-          if (!ok) break;
-          tc::fence_after_sync();
-          const uint32_t tS = tmem + buf * C::kTmemS;
-          if (p.tree && t == 0) {  // bf16 keys [D / 64][64 keys][64], bf16 queries [D / 64][kNT][64] in P's place
-            const uint64_t dA = tc::sw128_desc(smem_u32(base + C::off_K + st * C::kTile), 16, 1024);
-            const uint64_t dB = tc::sw128_desc(smem_u32(base + C::off_P + buf * C::kPBytes), 16, 1024);
-#pragma unroll 1
+    constexpr uint32_t idS = idesc_f8(128, C::kNS, false, false);
+    constexpr uint32_t idT = tc::idesc_bf16_f32(128, C::kNS, false, false);
+    const uint64_t dQ = swizzled_desc(smem_u32(base + C::off_Q), D);
+    const uint64_t dK0 = swizzled_desc(smem_u32(base + C::off_K), D);
+    int st = 0, seg = 0, i = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (; s.any() && ok; s.next(bt, p.Hkv), ++seg) {
+      ok = warp_wait(&bars[QFULL8], seg & 1, abort_flag);
+      for (int t = s.t0; t < s.t1 && ok; ++t, ++i) {
+        const int buf = i % kBuf;
+        ok = warp_wait(&bars[F_K + st], phase, abort_flag) &&
+             warp_wait(&bars[SFREE8 + buf], (i / kBuf & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        tc::fence_after_sync();
+        const uint32_t tS = tmem + buf * C::kTmemS;
+        if (p.tree && t == 0) {  // bf16 keys [D / 64][64 keys][64], bf16 queries [D / 64][kNS][64] in P's place
+          const uint64_t dA = tc::sw128_desc(smem_u32(base + C::off_K + st * C::kTile), 16, 1024);
+          const uint64_t dB = tc::sw128_desc(smem_u32(base + C::off_P + buf * C::kPBytes), 16, 1024);
+          if (elect_one()) {
+#pragma unroll
             for (int k = 0; k < D / 16; ++k)
               tc::mma_bf16(tS, dA + desc_step((k / 4) * kTreeKeys * 128 + (k % 4) * 32),
                            dB + desc_step((k / 4) * C::kNS * 128 + (k % 4) * 32), idT, k > 0);
-          } else {
-            const uint64_t dK = dK0 + (uint64_t)st * desc_step(C::kTile);
+            tc::mma_commit(&bars[SFULL8 + buf]);
+            tc::mma_commit(&bars[E_K + st]);
+          }
+        } else {
+          const uint64_t dK = dK0 + (uint64_t)st * desc_step(C::kTile);
+          if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) mma_f8(tS, dK + desc_step(32 * k), dQ + desc_step(32 * k), idS, k > 0);
             if (!C::kSplitS) {
@@ -446,48 +460,50 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
               for (int k = 0; k < D / 32; ++k)
                 mma_f8(tS, dK + desc_step(32 * k), dQ + desc_step(NP * D + 32 * k), idS, 1);
             }
-          }
-          tc::mma_commit(&bars[SFULL8 + buf]);
-          tc::mma_commit(&bars[E_K + st]);
-          if (++st == ns) {
-            st = 0;
-            phase ^= 1;
+            tc::mma_commit(&bars[SFULL8 + buf]);
+            tc::mma_commit(&bars[E_K + st]);
           }
         }
+        __syncwarp();
+        if (++st == ns) {
+          st = 0;
+          phase ^= 1;
+        }
       }
-      tc::mma_commit(&bars[MDONE8]);  // every MMA finished before TMEM is released
-      mbar_drain(&bars[MDONE8], 0);
     }
+    if (elect_one()) tc::mma_commit(&bars[MDONE8]);  // every MMA finished before TMEM is released
+    __syncwarp();
+    mbar_drain(&bars[MDONE8], 0);
   } else if (warp == C::kMmaO) {
     // -------------------------------------------------------- P.V products
     if (y == 0) write_ranges(bt, p.B, p.Hkv, G, weight, p.ranges, x * 32 + lane, G * 32);
     __syncwarp();
-    if (lane == 0) {
-      constexpr uint32_t id8 = idesc_f8(D, C::kNO, true, true);
-      constexpr uint32_t idT = tc::idesc_bf16_f32(D, C::kNS, true, true);
-      constexpr uint32_t id16 = idT & ~((1u << 7) | (1u << 10));  // fp16 for bf16
-      constexpr int kPitchP = C::kPitch;
-      const uint64_t dP0 = swizzled_desc(smem_u32(base + C::off_P), kPitchP);
-      const uint32_t values = smem_u32(base + (C::kWiden ? C::off_W : off_V));
-      const uint64_t dV0 = C::kWiden ? tc::sw128_desc(values, kTK * 128, 1024) : swizzled_desc(values, D);
-      const uint64_t dT0 = tc::sw128_desc(values, kTreeKeys * 128, 1024);
-      const uint32_t tO = tmem + C::kTmemO;
-      int i = 0, st = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (; s.any() && ok; s.next(bt, p.Hkv)) {
-        for (int t = s.t0; t < s.t1; ++t, ++i) {
-          const int buf = i % kBuf;
-          // O of the segment before is read before the first weights of this one are written
-          ok = (C::kWiden || wait8(&bars[F_V + st], phase, abort_flag)) &&
-               wait8(&bars[PFULL8 + buf], i / kBuf & 1, abort_flag);
-          if (!ok) break;
-          tc::fence_after_sync();
-          const uint64_t dP = dP0 + (uint64_t)buf * desc_step(C::kPBytes);
-          const uint64_t at = C::kWiden ? (uint64_t)buf * desc_step(C::kWide) : (uint64_t)st * desc_step(C::kTile);
-          const uint32_t acc = t > s.t0 ? 1u : 0u;
+    constexpr uint32_t id8 = idesc_f8(D, C::kNO, true, true);
+    constexpr uint32_t idT = tc::idesc_bf16_f32(D, C::kNS, true, true);
+    constexpr uint32_t id16 = idT & ~((1u << 7) | (1u << 10));  // fp16 for bf16
+    constexpr int kPitchP = C::kPitch;
+    const uint64_t dP0 = swizzled_desc(smem_u32(base + C::off_P), kPitchP);
+    const uint32_t values = smem_u32(base + (C::kWiden ? C::off_W : off_V));
+    const uint64_t dV0 = C::kWiden ? tc::sw128_desc(values, kTK * 128, 1024) : swizzled_desc(values, D);
+    const uint64_t dT0 = tc::sw128_desc(values, kTreeKeys * 128, 1024);
+    int i = 0, st = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (; s.any() && ok; s.next(bt, p.Hkv)) {
+      for (int t = s.t0; t < s.t1; ++t, ++i) {
+        const int buf = i % kBuf;
+        // O of the segment before is read before the first weights of this one are written
+        ok = (C::kWiden || warp_wait(&bars[F_V + st], phase, abort_flag)) &&
+             warp_wait(&bars[PFULL8 + buf], i / kBuf & 1, abort_flag);
+        if (!ok) break;
+        tc::fence_after_sync();
+        const uint64_t dP = dP0 + (uint64_t)buf * desc_step(C::kPBytes);
+        const uint64_t at = C::kWiden ? (uint64_t)buf * desc_step(C::kWide) : (uint64_t)st * desc_step(C::kTile);
+        const uint32_t tO = tmem + C::kTmemO;
+        const uint32_t acc = t > s.t0 ? 1u : 0u;
+        if (elect_one()) {
           if (p.tree && t == 0) {
-#pragma unroll 1
+#pragma unroll
             for (int k = 0; k < kTreeKeys / 16; ++k)
               tc::mma_bf16(tO, dT0 + at + desc_step(k * 16 * 128), dP + desc_step(k * 16 * kPitchP), idT, k > 0);
           } else if (C::kWiden) {
@@ -501,18 +517,18 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
               mma_f8(tO, dV0 + at + desc_step(k * 32 * D), dP + desc_step(k * 32 * kPitchP), id8, k > 0 ? 1u : acc);
           }
           tc::mma_commit(&bars[PVDONE + buf]);
-          if (!C::kWiden) {
-            tc::mma_commit(&bars[E_V + st]);
-            if (++st == ns) {
-              st = 0;
-              phase ^= 1;
-            }
-          }
+          if (!C::kWiden) tc::mma_commit(&bars[E_V + st]);
+        }
+        __syncwarp();
+        if (!C::kWiden && ++st == ns) {
+          st = 0;
+          phase ^= 1;
         }
       }
-      tc::mma_commit(&bars[MDONE8 + 1]);
-      mbar_drain(&bars[MDONE8 + 1], 0);
     }
+    if (elect_one()) tc::mma_commit(&bars[MDONE8 + 1]);
+    __syncwarp();
+    mbar_drain(&bars[MDONE8 + 1], 0);
   } else {
     // ------------------------------------------------------------- softmax
     const int sid = threadIdx.x, tid = sid & 127, group = warp >> 2;
