@@ -65,19 +65,20 @@ constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, SF
 
 template <int D, int NP>
 struct Cfg {
-  // Few rows: weights as two codes each.  Many: values widened to fp16, a part that the rows share.
-  static constexpr bool kWiden = NP > 16;
+  // Up to 48 rows: weights as two codes each.  More: values widened to fp16, work that the rows share (64 nodes on 4 x
+  // 52 heads, 16384 keys: 226 us as two codes, 218 widened; 26 nodes on 8 x 40 heads, 512 - 4096 keys 69.9 and 74.2).
+  static constexpr bool kWiden = NP > 48;
   static constexpr float kMost = kWiden ? 15.5f : 8.75f;              // log2 of the largest weight: 2^16, 448 are too large
   static constexpr float kLift = kWiden ? 6.f : 8.f;                  // log2 of the weight of a new maximum
-  static constexpr int kRT = NP == 64 ? 16 : kWiden ? NP / 2 : NP;                    // rows of a softmax group
+  static constexpr int kRT = NP < 16 ? NP : 16;                    // rows of a softmax group
   static constexpr int kSG = NP / kRT;                                // softmax groups
   static constexpr int kSoft = 128 * kSG;
   // Warps after the softmax: K's copies, V's copies, S products, P.V products.  One thread for both copies or both
   // products sets a slower pace than the stream: a copy or a product keeps its issuer busy for over 100 cycles.
   static constexpr int kCopyK = 4 * kSG, kCopyV = kCopyK + 1, kMmaS = kCopyK + 2, kMmaO = kCopyK + 3,
                        kThreads = kSoft + 128;
-  static constexpr int kCtas = NP <= 16 ? 2 : 1;                      // of an SM
-  static constexpr int kBuf = NP <= 16 ? 1 : 2;                       // S and P buffers
+  static constexpr int kCtas = NP <= 32 ? 2 : 1;                      // of an SM
+  static constexpr int kBuf = NP <= 32 ? 1 : 2;                       // S and P buffers
   static constexpr int kNO = kWiden ? NP : 2 * NP;                      // columns of O (few rows: hi | lo)
   // S adds hi and lo up itself, as products along 2 D; 8 columns are less than an MMA has, so there they lie side by side.
   static constexpr bool kSplitS = NP < 16;
@@ -537,7 +538,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     const uint32_t tO = lane_addr + C::kTmemO + r_own;
     // Where this thread's pieces of its key's row lie: 16 codes at a time of V, widened to 32 bytes of W.
-    constexpr int kPieces = D / 16 / C::kSG;
+    constexpr int kPieces = C::kWiden ? D / 16 / C::kSG : 0;
     const uint32_t x128 = (tid & 7) << 4, xD = D == 128 ? x128 : ((tid >> 1) & 3) << 4;
     const uint32_t v_from = tid * D, v_mix = (group * 16) ^ xD, w_to = tid * 128, w_mix = (group * 32) ^ x128;
     const uint32_t p_row = tid * C::kPitch,
@@ -876,8 +877,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           if constexpr (NP == 8) {
             *reinterpret_cast<uint4*>(p_to + p_mix) = make_uint4(hw[0], hw[1], lw[0], lw[1]);
           } else {
-            *reinterpret_cast<uint4*>(p_to + p_mix) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-            *reinterpret_cast<uint4*>(p_to + (16 ^ p_mix)) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+            *reinterpret_cast<uint4*>(p_to + (r_own ^ p_mix)) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+            *reinterpret_cast<uint4*>(p_to + ((NP + r_own) ^ p_mix)) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
           }
           if (opaque(key0 + kTK > plen)) {  // value rows past the end may hold NaN: zero times NaN is no zero
             dead |= !warp_wait(&bars[F_V + st], ring, abort_flag);

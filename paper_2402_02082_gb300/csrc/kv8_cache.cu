@@ -4,8 +4,11 @@
 //          head, not below the exponent of rows that the block holds already
 //   code = x * 2^-e to the nearest 8-bit float
 //
-// One CTA takes one block of one slab: its new rows stay in registers between the maximum and the
-// rounding, so a new element is read once.  Rows from before are read only where their exponent grows.
+// What bounds it.  A prompt's rows are a stream (2 or 4 bytes in, 1 out): one CTA takes a block of K and
+// of V of one slab, all its loads in flight at once and kept as they came, so a new element is read once
+// between the maximum and the rounding.  A round's few rows are latency (the lengths, the path, the rows,
+// the exponent, one after another): a warp takes a block, so that all layers and heads fit the GPU at
+// once.  Rows from before are read only where their exponent grows.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -33,16 +36,43 @@ __device__ __forceinline__ int block_exponent(uint32_t bits) {
   return kv8_clamp_exp(e);  // zero and subnormal numbers too
 }
 
-// Eight consecutive elements as fp32.
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&f)[8]) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
-  f[0] = bf16lo(w.x); f[1] = bf16hi(w.x); f[2] = bf16lo(w.y); f[3] = bf16hi(w.y);
-  f[4] = bf16lo(w.z); f[5] = bf16hi(w.z); f[6] = bf16lo(w.w); f[7] = bf16hi(w.w);
-}
-__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+// Eight consecutive elements, as they lie in memory.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<__nv_bfloat16> {
+  uint4 w;
+  __device__ __forceinline__ void none() { w = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    f[0] = bf16lo(w.x); f[1] = bf16hi(w.x); f[2] = bf16lo(w.y); f[3] = bf16hi(w.y);
+    f[4] = bf16lo(w.z); f[5] = bf16hi(w.z); f[6] = bf16lo(w.w); f[7] = bf16hi(w.w);
+  }
+};
+template <>
+struct Eight<float> {
+  float4 a, b;
+  __device__ __forceinline__ void none() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldcs(reinterpret_cast<const float4*>(p));
+    b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+};
+// The bits of the largest finite magnitude, or of `most`.
+template <typename T>
+__device__ __forceinline__ uint32_t top8(const Eight<T>& x, uint32_t most) {
+  float f[8];
+  x.get(f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t a = __float_as_uint(f[j]) & 0x7fffffffu;
+    most = max(most, a < 0x7f800000u ? a : 0u);
+  }
+  return most;
 }
 
 __device__ __forceinline__ uint2 encode8(const float (&f)[8], float s) {
@@ -51,79 +81,163 @@ __device__ __forceinline__ uint2 encode8(const float (&f)[8], float s) {
   w.y = kv8_encode2(f[4] * s, f[5] * s) | (kv8_encode2(f[6] * s, f[7] * s) << 16);
   return w;
 }
+template <typename T>
+__device__ __forceinline__ uint2 encode8(const Eight<T>& x, float s) {
+  float f[8];
+  x.get(f);
+  return encode8(f, s);
+}
 
-// Grid: x = touched block of (layer, b, h), y = K or V.
+// A block's exponent from its new rows' largest magnitude and, if it holds rows, its old exponent.
+__device__ __forceinline__ int joined_exponent(uint32_t most, bool holds, int old) {
+  const int e = block_exponent(most);
+  return holds && old >= e ? kv8_clamp_exp(old) : e;
+}
+// What a grown exponent makes of the codes that a block holds.
+__device__ __forceinline__ float shrink_by(int old, int e) { return kv8_pow2(old - e < -126 ? -126 : old - e); }
+__device__ __forceinline__ uint2 shrink8(const uint2& w, float by) {
+  float f[8];
+  kv8_decode4(w.x, f);
+  kv8_decode4(w.y, f + 4);
+  return encode8(f, by);
+}
+
+struct Rows {  // of a sequence: its length so far, and how many join
+  int L, m;
+};
+__device__ __forceinline__ Rows rows_of(const AppendParams& p, int b) {
+  int L = p.kv_len[b], m = p.len ? p.len[b] : p.n - 1;
+  L = L < 0 ? 0 : (L > p.S_cap - p.n ? p.S_cap - p.n : L);
+  m = (m < -1 ? -1 : (m > p.n - 1 ? p.n - 1 : m)) + 1;
+  return {L, m};
+}
+// Where element 0 of new row k of (layer, b, h) lies in k_new / v_new.
+__device__ __forceinline__ size_t row_at(const AppendParams& p, int layer, int b, int h, int k, int D) {
+  int src = k;
+  if (p.path) {
+    src = p.path[(size_t)b * p.n + k];
+    src = src < 0 ? 0 : (src > p.n - 1 ? p.n - 1 : src);
+  }
+  return ((((size_t)layer * p.B + b) * p.n + src) * p.H + h) * D;
+}
+
+// A CTA takes a touched block of (layer, b, h), of K and of V.
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) kv8_append_kernel(const AppendParams p) {
-  constexpr int kPerRow = D / 8;                       // threads per row
-  constexpr int kRows = kThreads / kPerRow;            // rows per pass
+  constexpr int kPerRow = D / 8;             // threads per row
+  constexpr int kRows = kThreads / kPerRow;  // rows per pass
   constexpr int kPasses = kKv8Block / kRows;
-  __shared__ uint32_t top[kThreads / 32];
+  __shared__ uint32_t top[2][kThreads / 32];
   pdl_wait();
   const int slab = (int)(blockIdx.x / (unsigned)p.blocks), nth = (int)(blockIdx.x - (unsigned)slab * p.blocks);
   const int bh = slab % (p.B * p.H), layer = slab / (p.B * p.H);
   const int b = bh / p.H, h = bh - b * p.H;
-  int L = p.kv_len[b];
-  L = L < 0 ? 0 : (L > p.S_cap - p.n ? p.S_cap - p.n : L);
-  int m = p.n;
-  if (p.len) {
-    m = p.len[b];
-    m = (m < -1 ? -1 : (m > p.n - 1 ? p.n - 1 : m)) + 1;
-  }
-  if (nth == 0 && blockIdx.y == 0 && layer == 0 && h == 0 && threadIdx.x == 0) p.new_kv_len[b] = L + m;
-  const int block = L / kKv8Block + nth;
-  const int row0 = block * kKv8Block;
-  if (m == 0 || row0 >= L + m) return;
-  uint8_t* codes = (blockIdx.y ? p.V : p.K) + ((size_t)slab * p.S_cap + row0) * D;
-  int8_t* exps = (blockIdx.y ? p.Ve : p.Ke) + (size_t)slab * kv8_blocks(p.S_cap) + block;
-  const T* fresh = static_cast<const T*>(blockIdx.y ? p.v_new : p.k_new) + (size_t)layer * p.B * p.n * p.H * D;
-
-  const int r0 = threadIdx.x / kPerRow, d = (threadIdx.x % kPerRow) * 8;
-  float x[kPasses][8];
-  uint32_t most = 0;
+  const Rows r = rows_of(p, b);
+  if (nth == 0 && layer == 0 && h == 0 && threadIdx.x == 0) p.new_kv_len[b] = r.L + r.m;
+  const int block = r.L / kKv8Block + nth, row0 = block * kKv8Block;
+  if (r.m == 0 || row0 >= r.L + r.m) return;
+  const size_t codes_at = ((size_t)slab * p.S_cap + row0) * D, exp_at = (size_t)slab * kv8_blocks(p.S_cap) + block;
+  const int rt = threadIdx.x / kPerRow, d = (threadIdx.x % kPerRow) * 8;
+  const bool holds = row0 < r.L;
+  Eight<T> x[2][kPasses];
 #pragma unroll
   for (int i = 0; i < kPasses; ++i) {
-    const int k = row0 + r0 + i * kRows - L;  // new row
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
-    if (k >= 0 && k < m) {
-      int src = k;
-      if (p.path) {
-        src = p.path[(size_t)b * p.n + k];
-        src = src < 0 ? 0 : (src > p.n - 1 ? p.n - 1 : src);
-      }
-      load8(fresh + (((size_t)b * p.n + src) * p.H + h) * D + d, x[i]);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t a = __float_as_uint(x[i][j]) & 0x7fffffffu;
-      if (a < 0x7f800000u && a > most) most = a;
+    const int k = row0 + rt + i * kRows - r.L;  // new row
+    x[0][i].none();
+    x[1][i].none();
+    if (k >= 0 && k < r.m) {
+      const size_t at = row_at(p, layer, b, h, k, D) + d;
+      x[0][i].load(static_cast<const T*>(p.k_new) + at);
+      x[1][i].load(static_cast<const T*>(p.v_new) + at);
     }
   }
-  most = __reduce_max_sync(0xffffffffu, most);
-  if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = most;
-  const int old = row0 < L ? (int)*exps : kKv8ExpMin;
+  const int old_k = holds ? (int)p.Ke[exp_at] : 0, old_v = holds ? (int)p.Ve[exp_at] : 0;
+  uint32_t most[2] = {0, 0};
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) most[kv] = top8(x[kv][i], most[kv]);
+    most[kv] = __reduce_max_sync(0xffffffffu, most[kv]);
+    if ((threadIdx.x & 31) == 0) top[kv][threadIdx.x >> 5] = most[kv];
+  }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) most = top[w] > most ? top[w] : most;
-  int e = block_exponent(most);
-  if (row0 < L && old >= e) e = kv8_clamp_exp(old);
-  if (threadIdx.x == 0) *exps = (int8_t)e;  // every thread has read the old one before the barrier
-  const float s = kv8_pow2(-e);
-  const bool grown = row0 < L && e > old;
-  const float shrink = grown ? kv8_pow2(old - e < -126 ? -126 : old - e) : 1.f;
+  for (int kv = 0; kv < 2; ++kv) {
+    uint32_t t = 0;
 #pragma unroll
-  for (int i = 0; i < kPasses; ++i) {
-    const int r = r0 + i * kRows, k = row0 + r - L;
-    uint2* at = reinterpret_cast<uint2*>(codes + (size_t)r * D + d);
-    if (k >= 0 && k < m) {
-      *at = encode8(x[i], s);
-    } else if (k < 0 && grown) {
-      const uint2 w = *at;
-      float f[8];
-      kv8_decode4(w.x, f);
-      kv8_decode4(w.y, f + 4);
-      *at = encode8(f, shrink);
+    for (int w = 0; w < kThreads / 32; ++w) t = max(t, top[kv][w]);
+    const int old = kv ? old_v : old_k, e = joined_exponent(t, holds, old);
+    if (threadIdx.x == 0) (kv ? p.Ve : p.Ke)[exp_at] = (int8_t)e;  // every thread has read the old one
+    const float s = kv8_pow2(-e);
+    uint8_t* codes = (kv ? p.V : p.K) + codes_at + d;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const int row = rt + i * kRows, k = row0 + row - r.L;
+      uint2* at = reinterpret_cast<uint2*>(codes + (size_t)row * D);
+      if (k >= 0 && k < r.m)
+        *at = encode8(x[kv][i], s);
+      else if (k < 0 && holds && e > old)
+        *at = shrink8(*at, shrink_by(old, e));
+    }
+  }
+}
+
+// A warp takes a touched block of (layer, b, h), of K or of V: up to 64 new rows.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) kv8_append_few_kernel(const AppendParams p) {
+  constexpr int kPerRow = D / 8, kRows = 32 / kPerRow;  // lanes per row, rows per load
+  constexpr int kHeld = 8;                              // loads whose rows stay in registers
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const long long units = 2ll * p.blocks * p.layers * p.B * p.H;
+  const long long unit = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5;
+  if (unit >= units) return;
+  const int kv = (int)(unit & 1), nth = (int)((unit >> 1) % p.blocks);
+  const int slab = (int)((unit >> 1) / p.blocks);
+  const int bh = slab % (p.B * p.H), layer = slab / (p.B * p.H);
+  const int b = bh / p.H, h = bh - b * p.H;
+  const Rows r = rows_of(p, b);
+  if (kv == 0 && nth == 0 && layer == 0 && h == 0 && lane == 0) p.new_kv_len[b] = r.L + r.m;
+  const int block = r.L / kKv8Block + nth, row0 = block * kKv8Block;
+  if (r.m == 0 || row0 >= r.L + r.m) return;
+  uint8_t* codes = (kv ? p.V : p.K) + ((size_t)slab * p.S_cap + row0) * D;
+  int8_t* exp = (kv ? p.Ve : p.Ke) + (size_t)slab * kv8_blocks(p.S_cap) + block;
+  const T* fresh = static_cast<const T*>(kv ? p.v_new : p.k_new);
+  const bool holds = row0 < r.L;
+  const int old = holds ? (int)*exp : 0;
+  // rows first .. last - 1 of the block are new
+  const int first = holds ? r.L - row0 : 0, last = min(kKv8Block, r.L + r.m - row0);
+  const int rl = lane / kPerRow, d = (lane % kPerRow) * 8;
+  auto load = [&](int row) {
+    Eight<T> x;
+    x.none();
+    if (row < last) x.load(fresh + row_at(p, layer, b, h, row0 + row - r.L, D) + d);
+    return x;
+  };
+  Eight<T> x[kHeld];
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) x[i] = load(first + rl + i * kRows);
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) most = top8(x[i], most);
+  for (int row = first + rl + kHeld * kRows; row < last; row += kRows) most = top8(load(row), most);
+  most = __reduce_max_sync(0xffffffffu, most);
+  const int e = joined_exponent(most, holds, old);
+  __syncwarp();
+  if (lane == 0) *exp = (int8_t)e;  // every lane has read the old one
+  const float s = kv8_pow2(-e);
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int row = first + rl + i * kRows;
+    if (row < last) *reinterpret_cast<uint2*>(codes + (size_t)row * D + d) = encode8(x[i], s);
+  }
+  for (int row = first + rl + kHeld * kRows; row < last; row += kRows)
+    *reinterpret_cast<uint2*>(codes + (size_t)row * D + d) = encode8(load(row), s);
+  if (holds && e > old) {
+    const float by = shrink_by(old, e);
+    for (int row = rl; row < first; row += kRows) {
+      uint2* at = reinterpret_cast<uint2*>(codes + (size_t)row * D + d);
+      *at = shrink8(*at, by);
     }
   }
 }
@@ -135,9 +249,15 @@ cudaError_t append(const Kv8AppendArgs& a, cudaStream_t st) {
   p.kv_len = a.kv_len; p.path = a.path; p.len = a.len; p.new_kv_len = a.new_kv_len;
   p.layers = a.layers; p.B = a.B; p.H = a.H; p.S_cap = a.S_cap; p.n = a.n;
   p.blocks = (a.n + kKv8Block - 2) / kKv8Block + 1;
-  const long long ctas = (long long)p.blocks * a.layers * a.B * a.H;
-  if (ctas > 0x7fffffffll) return cudaErrorNotSupported;
-  return launch_pdl(kv8_append_kernel<T, D>, dim3((unsigned)ctas, 2), dim3(kThreads), 0, st, p);
+  const long long blocks = (long long)p.blocks * a.layers * a.B * a.H;
+  if (blocks > 0x7fffffffll) return cudaErrorNotSupported;
+  // A CTA a block streams; few rows leave most of it idle (5 rows of 33 nodes, 32 layers of 32 heads: 9.6 us, a warp a
+  // block 5.5).
+  if (a.n <= kKv8Block) {
+    const long long ctas = (2 * blocks * 32 + kThreads - 1) / kThreads;
+    return launch_pdl(kv8_append_few_kernel<T, D>, dim3((unsigned)ctas), dim3(kThreads), 0, st, p);
+  }
+  return launch_pdl(kv8_append_kernel<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, p);
 }
 
 struct ReadParams {
