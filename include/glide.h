@@ -395,7 +395,8 @@ typedef struct {
  * [n_layers][B, n, H_kv, D].  kv_len [B] (clamped to [0, S_cap - n]), path [B, n] or
  * NULL (clamped to [0, n)), len [B] or NULL: int32 on the device.  path and len as
  * tree_accept writes them append the accepted path; a prompt has path NULL.
- * 1 <= n <= S_cap.  new_kv_len [B] int32 and not the kv_len buffer.  No workspace.
+ * 1 <= n <= S_cap.  new_kv_len [B] int32 and not the kv_len buffer.  No workspace.  More
+ * than 2^31 - 1 blocks of 64 tokens over all slabs: GLIDE_ERR_UNSUPPORTED (read below too).
  */
 glide_status glide_kv8_append(const glide_attn_desc* desc, int32_t n_layers, const glide_kv8_cache* cache,
                               const void* k_new, const void* v_new, const int32_t* kv_len, int32_t n,

@@ -312,7 +312,8 @@ glide_status glide_kv8_read(const glide_attn_desc* desc, int32_t n_layers, const
   a.Ke = cache->K_exp; a.Ve = cache->V_exp; a.kv_len = kv_len; a.K_out = K_out; a.V_out = V_out;
   a.layers = n_layers; a.B = desc->B; a.H = hkv(desc); a.D = desc->D; a.S_cap = desc->S_cap; a.S_out = S_out;
   a.dtype = desc->dtype == GLIDE_BF16 ? 0 : 1;
-  return from_cuda(glide::launch_kv8_read(a, reinterpret_cast<cudaStream_t>(stream)));
+  const cudaError_t e = glide::launch_kv8_read(a, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaErrorNotSupported ? GLIDE_ERR_UNSUPPORTED : from_cuda(e);
 }
 
 size_t glide_kv8_workspace_bytes(const glide_attn_desc* desc, int32_t n_queries) {
