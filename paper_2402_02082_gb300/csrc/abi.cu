@@ -344,7 +344,9 @@ static glide_status kv8_attention(const glide_attn_desc* d, const void* q, int32
   a.max_ctas = d->max_ctas;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (a.dtype != 0) return from_cuda(glide::launch_kv8_attn_fma(a, st));
-  const cudaError_t e = glide::launch_kv8_attn_tc(a, st);
+  cudaError_t e = glide::launch_kv8_few(a, st);
+  if (e != cudaErrorNotSupported) return from_cuda(e);
+  e = glide::launch_kv8_attn_tc(a, st);
   return e == cudaErrorNotSupported ? GLIDE_ERR_UNSUPPORTED : from_cuda(e);
 }
 

@@ -58,6 +58,9 @@ cudaError_t launch_kv8_append(const Kv8AppendArgs& a, cudaStream_t st);
 cudaError_t launch_kv8_read(const Kv8ReadArgs& a, cudaStream_t st);
 // On the tensor cores, bf16 queries; cudaErrorNotSupported where launch_kv8_attn_fma is the one to take.
 cudaError_t launch_kv8_attn_tc(const Kv8AttnArgs& a, cudaStream_t st);
+// Few query rows, bf16, straight from global memory to registers; cudaErrorNotSupported where launch_kv8_attn_tc is
+// the one to take.
+cudaError_t launch_kv8_few(const Kv8AttnArgs& a, cudaStream_t st);
 // On the CUDA cores, fp32 throughout.
 cudaError_t launch_kv8_attn_fma(const Kv8AttnArgs& a, cudaStream_t st);
 size_t kv8_workspace_bytes(int B, int Hkv, int D, int rows);
