@@ -53,7 +53,7 @@ namespace {
 constexpr int kTK = 128;          // keys per tile
 constexpr int kTreeKeys = 64;     // rows of the tree tile
 constexpr int kMaxStages8 = 6;
-constexpr float kPLo = 32.f;         // p = hi + lo / kPLo
+constexpr float kPLo = 28.f;         // p = hi + lo / kPLo: of p <= 430 at most 16 are left to lo, 448 its largest code
 constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
 
 // What a switch of slabs costs a CTA, in tiles.
@@ -157,9 +157,6 @@ __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile 
     }
   }
 }
-__device__ __forceinline__ bool wait8(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  return mbar_try_wait(bar, parity) || wait_long(bar, parity, abort);
-}
 // For every lane of a converged warp, with one outcome.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
@@ -253,7 +250,7 @@ __device__ __forceinline__ float warp_top(float x) {
   return r;
 }
 
-// Four weights in [0, 430] (or NaN) as codes hi and lo, p = hi + lo / 32: the fp16 in between has 11 bits.
+// Four weights in [0, 430] (or NaN) as codes hi and lo, p = hi + lo / 28: the fp16 in between has 11 bits.
 // One block of code: the halves of a register are then picked by the conversions themselves.
 __device__ __forceinline__ void split_weights(float p0, float p1, float p2, float p3, uint32_t& hi, uint32_t& lo) {
   asm("{\n\t.reg .b32 h, g, d;\n\t.reg .b16 a, b, c, e;\n\t"
@@ -272,7 +269,7 @@ __device__ __forceinline__ void split_weights(float p0, float p1, float p2, floa
       "cvt.rn.satfinite.e4m3x2.f16x2 e, g;\n\t"
       "mov.b32 %1, {c, e};\n\t}"
       : "=&r"(hi), "=r"(lo)
-      : "f"(p0), "f"(p1), "f"(p2), "f"(p3), "r"(0x50005000u));  // 32, 32
+      : "f"(p0), "f"(p1), "f"(p2), "f"(p3), "r"(0x4f004f00u));  // 28, 28
 }
 // Four codes as four fp16 values, exactly.
 __device__ __forceinline__ void widen4(uint32_t w, uint32_t& a, uint32_t& b) {

@@ -75,6 +75,13 @@ __device__ __forceinline__ uint32_t top_pair(uint32_t w, uint32_t most) {
 // Two bf16 elements times a power of two as fp16; what is not finite stays so.
 __device__ __forceinline__ uint32_t scaled_pair(uint32_t w, float s) { return f16pair(bf16lo(w) * s, bf16hi(w) * s); }
 
+// A pair of floats to the same place in CTA `rank`'s shared memory.
+__device__ __forceinline__ void store_peer(float2* at, uint32_t rank, float2 v) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(at)), "r"(rank));
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(v.x), "f"(v.y) : "memory");
+}
+
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(const FewParams p) {
   constexpr int kR = 8 * NT;        // query rows
@@ -83,23 +90,26 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
   constexpr int kWV = D / 32;       // of a value row
   constexpr int kStride = D + 4;    // floats of a partial row: the lanes' stores then meet no bank twice
   extern __shared__ float smem[];
-  float* red = smem;                                              // [warps][kR][kStride]
-  float* part = red + kWarpsF * kR * kStride;                     // [kR][kStride]: this CTA's o for its peers
-  float2* stat = reinterpret_cast<float2*>(part + kR * kStride);  // [warps][kR] (m, l)
-  float2* mine = stat + kWarpsF * kR;                             // [kR]: this CTA's (m, l)
+  float* red = smem;                                                        // [warps][kR][kStride]
+  float2* stat = reinterpret_cast<float2*>(red + kWarpsF * kR * kStride);   // [warps][kR] (m, l)
+  float2* peer_ml = stat + kWarpsF * kR;                                    // [kMaxC][kR] (m, l), from the peers
+  float2* peer_o = peer_ml + kMaxC * kR;                                    // [kR D / 2 + kMaxC]: this CTA's pairs, from each
+  uint2* qf = reinterpret_cast<uint2*>(peer_o + kR * D / 2 + kMaxC);        // [NT][kSteps][32] the queries' fragments
+  float* q_unit = reinterpret_cast<float*>(qf + NT * kSteps * 32);          // [kR] what makes a product log2 units
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int rank = (int)cluster_rank();
   const int slab = blockIdx.x / p.C, b = slab / p.Hkv, h = slab - b * p.Hkv;
+  cluster_arrive();  // that every peer's shared memory is there is known when it is written to
   pdl_wait();
-  int L = p.kv_len[b];
-  L = L < 0 ? 0 : (L > p.max_kv_len ? p.max_kv_len : L);
+  const int L_told = p.kv_len[b];
+  const int Lmax = p.max_kv_len;
   const uint64_t pol = policy_evict_first();
   const uint8_t* Kg = p.K + (size_t)slab * p.S_cap * D;
   const uint8_t* Vg = p.V + (size_t)slab * p.S_cap * D;
   const int8_t *Ke = p.Ke + (size_t)slab * p.blocks, *Ve = p.Ve + (size_t)slab * p.blocks;
 
-  // this lane's pieces of a tile: keys g, g + 8, .. of K; of V keys 2t, 2t + 1, 2t + 8, 2t + 9 of each 16.  Rows past
-  // the end (the cache may hold anything there, or end) are zeros.
+  // this lane's pieces of a tile: keys g, g + 8, .. of K; of V keys 2t, 2t + 1, 2t + 8, 2t + 9 of each 16.  The first
+  // loads do not wait for the length but go by its bound; what lies past the length is masked, and V's made zeros.
   uint32_t kr[4][kWK], vr[8][kWV];
   auto load_k = [&](int key0) {
 #pragma unroll
@@ -109,7 +119,7 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
 #pragma unroll
       for (int w = 0; w < kWK; w += 4) {
         uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (key < L) x = load_once(at + 4 * w, pol);
+        if (key < Lmax) x = load_once(at + 4 * w, pol);
         kr[i][w] = x.x;
         kr[i][w + 1] = x.y;
         kr[i][w + 2] = x.z;
@@ -124,37 +134,74 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
       const uint8_t* at = Vg + (size_t)key * D + g * (D / 8);
       if constexpr (kWV == 4) {
         uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (key < L) x = load_once(at, pol);
+        if (key < Lmax) x = load_once(at, pol);
         vr[i][0] = x.x;
         vr[i][1] = x.y;
         vr[i][2] = x.z;
         vr[i][3] = x.w;
       } else {
         uint2 x = make_uint2(0u, 0u);
-        if (key < L) x = __ldcs(reinterpret_cast<const uint2*>(at));
+        if (key < Lmax) x = __ldcs(reinterpret_cast<const uint2*>(at));
         vr[i][0] = x.x;
         vr[i][1] = x.y;
       }
     }
   };
-  const int step = p.C * kWarpsF * kTKF;
-  int key0 = (rank * kWarpsF + warp) * kTKF;
+  // A tree is one more tile, of the cluster's last warp, which in clusters of four CTAs or more has no other: its keys,
+  // values and parents are loads of their own (32 heads, 2048 keys, 6 nodes: 12.7 us beside a tile, 11.1 alone).
+  const bool tree_warp = p.parent && rank == p.C - 1 && warp == kWarpsF - 1;
+  const int spare = p.parent && p.C >= 4 ? 1 : 0;
+  const int step = (p.C * kWarpsF - spare) * kTKF;
+  int key0 = tree_warp && spare ? p.max_kv_len : (rank * kWarpsF + warp) * kTKF;
   int ke = 0, ve = 0;
   auto load_exps = [&](int key) {
-    if (key < L) {
+    if (key < Lmax) {
       ke = kv8_clamp_exp(Ke[key / kKv8Block]);
       ve = kv8_clamp_exp(Ve[key / kKv8Block]);
     }
   };
-  load_k(key0);
-  load_exps(key0);
-
-  // the queries, each scaled by its own power of two; c: what turns a product into log2 units, of rows 2t, 2t + 1
-  uint32_t qf[NT][2 * kSteps];
-  float c[NT][2];
+  // The tree's own keys (g, g + 8; as K) and values (2t, 2t + 1, 2t + 8, 2t + 9; as V), bf16 as they lie, in the registers
+  // that a tile's take.
+  auto load_tree = [&] {
+    auto put = [](const __nv_bfloat16* at, bool there, uint32_t* w) {
+      const uint4 x = there ? *reinterpret_cast<const uint4*>(at) : make_uint4(0u, 0u, 0u, 0u);
+      w[0] = x.x;
+      w[1] = x.y;
+      w[2] = x.z;
+      w[3] = x.w;
+    };
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = 8 * nt + g, node = r / p.group;
+    for (int i = 0; i < 2; ++i) {
+      const int key = g + 8 * i;
+      const __nv_bfloat16* at = p.kt + (((size_t)b * p.n + key) * p.Hkv + h) * D + t * (D / 4);
+#pragma unroll
+      for (int w = 0; w < 2 * kSteps; w += 4) put(at + 2 * w, key < p.n, &kr[2 * i + w / kWK][w % kWK]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = 8 * (i / 2) + 2 * t + i % 2;
+      const __nv_bfloat16* at = p.vt + (((size_t)b * p.n + key) * p.Hkv + h) * D + g * (D / 8);
+      uint32_t w[2 * kWV];
+#pragma unroll
+      for (int k = 0; k < 2 * kWV; k += 4) put(at + 2 * k, key < p.n, w + k);
+#pragma unroll
+      for (int k = 0; k < 2 * kWV; ++k) vr[2 * i + k / kWV][k % kWV] = w[k];
+    }
+  };
+  int2 up = make_int2(-1, -1);
+  if (tree_warp) {
+    up = parents_of(p.parent + (size_t)b * p.n, p.n, lane);
+    load_tree();
+  } else {
+    load_k(key0);
+    load_v(key0);
+    load_exps(key0);
+  }
+
+
+  // the queries, each scaled by its own power of two, by one warp for 8 of them
+  if (warp < NT) {
+    const int r = 8 * warp + g, node = r / p.group;
     uint32_t w[2 * kSteps];
     uint32_t most = 0;
 #pragma unroll
@@ -175,10 +222,17 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
     const int e = exponent_of(most);
     const float s = kv8_pow2(-e);
 #pragma unroll
-    for (int i = 0; i < 2 * kSteps; ++i) qf[nt][i] = scaled_pair(w[i], s);
-    const float f = p.scale_log2 * kv8_pow2(e);
-    c[nt][0] = __shfl_sync(0xffffffffu, f, 8 * t);
-    c[nt][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+    for (int i = 0; i < kSteps; ++i)
+      qf[(warp * kSteps + i) * 32 + lane] = make_uint2(scaled_pair(w[2 * i], s), scaled_pair(w[2 * i + 1], s));
+    if (t == 0) q_unit[r] = p.scale_log2 * kv8_pow2(e);
+  }
+  const int L = L_told < 0 ? 0 : (L_told > Lmax ? Lmax : L_told);
+  __syncthreads();
+  float c[NT][2];  // of rows 2t, 2t + 1
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    c[nt][0] = q_unit[8 * nt + 2 * t];
+    c[nt][1] = q_unit[8 * nt + 2 * t + 1];
   }
 
   float m[NT][2], l[NT][2], o[D / 16][NT][4];
@@ -234,9 +288,120 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
   };
 
   int ref_v = -128;
+  // ---- the tree's own keys and values: at most 16
+  if (tree_warp) {
+    const int n = p.n;
+    // the nodes that node `lane` sees: itself and its ancestors, found by pointer jumping (at most 16 levels)
+    uint32_t sees = lane < n ? 1u << lane : 0u;
+    int next = lane < n && up.x >= 0 && up.x < lane ? up.x : -1;
+#pragma unroll
+    for (int round = 0; round < 4; ++round) {
+      const int from = next < 0 ? lane : next;
+      const uint32_t more = __shfl_sync(0xffffffffu, sees, from);
+      const int further = __shfl_sync(0xffffffffu, next, from);
+      sees |= more;
+      next = next < 0 ? -1 : further;
+    }
+    uint32_t vis[NT][2];  // the nodes that rows 2t, 2t + 1 see
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int r = 8 * nt + 2 * t + x;
+        vis[nt][x] = __shfl_sync(0xffffffffu, sees, r < p.rows ? r / p.group : 0);
+      }
+    auto kw = [&](int i, int w) { return kr[2 * i + w / kWK][w % kWK]; };
+    auto vw = [&](int i, int w) -> uint32_t& { return vr[2 * i + w / kWV][w % kWV]; };
+    uint32_t most = 0;  // keys and values are scaled to fp16 by a power of two each
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int w = 0; w < 2 * kSteps; ++w) most = top_pair(kw(i, w), most);
+    const int e_k = exponent_of(__reduce_max_sync(0xffffffffu, most));
+    float u[1][NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) u[0][nt][k] = 0.f;
+    const float sk = kv8_pow2(-e_k);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const uint32_t a[4] = {scaled_pair(kw(0, 2 * s), sk), scaled_pair(kw(1, 2 * s), sk), scaled_pair(kw(0, 2 * s + 1), sk),
+                             scaled_pair(kw(1, 2 * s + 1), sk)};
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const uint2 q = qf[(nt * kSteps + s) * 32 + lane];
+        mma_f16(u[0][nt], a, q.x, q.y);
+      }
+    }
+    most = 0;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int w = 0; w < 2 * kWV; ++w) {
+        uint32_t& x = vw(i, w);
+        // an unseen value that is not finite must not meet a weight of zero: left out here, put back below
+        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u, odd = true;
+        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu, odd = true;
+        most = top_pair(x, most);
+      }
+    const int e_v = exponent_of(__reduce_max_sync(0xffffffffu, most));
+    ref_v = e_v;
+    const int e = max(e_v, -90);
+    const float sv = kv8_pow2(-e_v), ks = kv8_pow2(e_k);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = fmaf(u[0][nt][k] * ks, c[nt][k & 1], (float)e);
+        u[0][nt][k] = (vis[nt][k & 1] >> (g + 4 * (k & 2))) & 1u ? x : -CUDART_INF_F;
+      }
+    uint32_t pt[1][NT][2];
+    weigh(u, pt, kv8_pow2(-e));
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      auto pair = [&](uint32_t x, uint32_t y, uint32_t& lo, uint32_t& hi) {  // dims 2j, 2j + 1 of two keys
+        lo = f16pair(bf16lo(x) * sv, bf16lo(y) * sv);
+        hi = f16pair(bf16hi(x) * sv, bf16hi(y) * sv);
+      };
+      uint32_t a[4];
+      pair(vw(0, j), vw(1, j), a[0], a[1]);
+      pair(vw(2, j), vw(3, j), a[2], a[3]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mma_f16(o[j][nt], a, pt[0][nt][0], pt[0][nt][1]);
+    }
+    if (__any_sync(0xffffffffu, odd)) {  // a visible value that is not finite decides its column
 #pragma unroll 1
-  for (; key0 < L; key0 += step) {
+      for (int key = 0; key < n; ++key)
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float v = __bfloat162float(p.vt[(((size_t)b * n + key) * p.Hkv + h) * D + g * (D / 8) + 2 * j + y]);
+            if (isfinite(v)) continue;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+                if ((vis[nt][x] >> key) & 1u) o[j][nt][2 * y + x] += v;
+          }
+    }
+    load_k(key0);
     load_v(key0);
+    load_exps(key0);
+  }
+#pragma unroll 1
+  for (bool first = true; key0 < L; key0 += step, first = false) {
+    if (!first) load_v(key0);
+    if (key0 + kTKF > L) {  // the last tile
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = key0 + 16 * (i / 4) + 8 * ((i / 2) % 2) + 2 * t + i % 2;
+#pragma unroll
+        for (int w = 0; w < kWV; ++w) vr[i][w] = key < L ? vr[i][w] : 0u;
+      }
+    }
     float u[2][NT][4];
     const float ks = kv8_pow2(ke);
     ref_v = max(ref_v, ve);
@@ -253,7 +418,10 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
         widen(kr[2 * kg][s], a[0], a[2]);
         widen(kr[2 * kg + 1][s], a[1], a[3]);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) mma_f16(u[kg][nt], a, qf[nt][2 * s], qf[nt][2 * s + 1]);
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint2 q = qf[(nt * kSteps + s) * 32 + lane];
+          mma_f16(u[kg][nt], a, q.x, q.y);
+        }
       }
     }
     load_k(key0 + step);  // the next tile's keys, under this one's softmax and values
@@ -283,103 +451,6 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
       }
   }
 
-  // ---- the tree's own keys and values: at most 16, one more tile for the cluster's last warp
-  if (p.parent && rank == p.C - 1 && warp == kWarpsF - 1) {
-    const int n = p.n;
-    const uint64_t sees = ancestors(parents_of(p.parent + (size_t)b * n, n, lane), n, lane, lane < n, lane);
-    uint32_t vis[NT][2];  // the nodes that rows 2t, 2t + 1 see
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int r = 8 * nt + 2 * t + x;
-        vis[nt][x] = __shfl_sync(0xffffffffu, (uint32_t)sees, r < p.rows ? r / p.group : 0);
-      }
-    // bf16 pairs as they lie, then scaled to fp16 by a power of two each for keys and values
-    uint32_t kw[2][2 * kSteps], most = 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int key = g + 8 * i;
-      const __nv_bfloat16* at = p.kt + (((size_t)b * n + key) * p.Hkv + h) * D + t * (D / 4);
-#pragma unroll
-      for (int w = 0; w < 2 * kSteps; ++w) {
-        kw[i][w] = key < n ? reinterpret_cast<const uint32_t*>(at)[w] : 0u;
-        most = top_pair(kw[i][w], most);
-      }
-    }
-    const int e_k = exponent_of(__reduce_max_sync(0xffffffffu, most));
-    float u[1][NT][4];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) u[0][nt][k] = 0.f;
-    const float sk = kv8_pow2(-e_k);
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const uint32_t a[4] = {scaled_pair(kw[0][2 * s], sk), scaled_pair(kw[1][2 * s], sk), scaled_pair(kw[0][2 * s + 1], sk),
-                             scaled_pair(kw[1][2 * s + 1], sk)};
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_f16(u[0][nt], a, qf[nt][2 * s], qf[nt][2 * s + 1]);
-    }
-    uint32_t vw[4][2 * kWV];
-    most = 0;
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = 8 * (i / 2) + 2 * t + i % 2;
-      const __nv_bfloat16* at = p.vt + (((size_t)b * n + key) * p.Hkv + h) * D + g * (D / 8);
-#pragma unroll
-      for (int w = 0; w < 2 * kWV; ++w) {
-        uint32_t x = key < n ? reinterpret_cast<const uint32_t*>(at)[w] : 0u;
-        // an unseen value that is not finite must not meet a weight of zero: left out here, put back below
-        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u, odd = true;
-        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu, odd = true;
-        vw[i][w] = x;
-        most = top_pair(x, most);
-      }
-    }
-    const int e_v = exponent_of(__reduce_max_sync(0xffffffffu, most));
-    const int e = max(max(e_v, ref_v - 110), -90);
-    const float sv = kv8_pow2(-e_v), ks = kv8_pow2(e_k);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float x = fmaf(u[0][nt][k] * ks, c[nt][k & 1], (float)e);
-        u[0][nt][k] = (vis[nt][k & 1] >> (g + 4 * (k & 2))) & 1u ? x : -CUDART_INF_F;
-      }
-    uint32_t pt[1][NT][2];
-    weigh(u, pt, kv8_pow2(-e));
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) {
-      auto pair = [&](uint32_t x, uint32_t y, uint32_t& lo, uint32_t& hi) {  // dims 2j, 2j + 1 of two keys
-        lo = f16pair(bf16lo(x) * sv, bf16lo(y) * sv);
-        hi = f16pair(bf16hi(x) * sv, bf16hi(y) * sv);
-      };
-      uint32_t a[4];
-      pair(vw[0][j], vw[1][j], a[0], a[1]);
-      pair(vw[2][j], vw[3][j], a[2], a[3]);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_f16(o[j][nt], a, pt[0][nt][0], pt[0][nt][1]);
-    }
-    if (__any_sync(0xffffffffu, odd)) {  // a visible value that is not finite decides its column
-#pragma unroll 1
-      for (int key = 0; key < n; ++key)
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const float v = __bfloat162float(p.vt[(((size_t)b * n + key) * p.Hkv + h) * D + g * (D / 8) + 2 * j + y]);
-            if (isfinite(v)) continue;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int x = 0; x < 2; ++x)
-                if ((vis[nt][x] >> key) & 1u) o[j][nt][2 * y + x] += v;
-          }
-    }
-  }
-
   // ---- the warps' results, then the cluster's.  Position 16 j + 2 g + y of a partial row is dim D/8 g + 2 j + y.
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
@@ -401,9 +472,10 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
     if (s.y != 0.f) L += s.x == -CUDART_INF_F ? s.y : fast_exp2(s.x - ref + __log2f(s.y));
     return s.x == -CUDART_INF_F ? 0.f : fast_exp2(s.x - ref);
   };
-  for (int i = threadIdx.x; i < kR * (D / 2); i += kThreadsF) {
+  const int pairs = p.rows * (D / 2), per = (pairs + p.C - 1) / p.C;
+  cluster_wait();
+  for (int i = threadIdx.x; i < pairs; i += kThreadsF) {
     const int r = i / (D / 2), d = 2 * (i % (D / 2));
-    if (r >= p.rows) break;
     float M = -CUDART_INF_F, Lr = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarpsF; ++w) M = fmaxf(M, stat[w * kR + r].x);
@@ -415,39 +487,31 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
       sum.x += f * v.x;
       sum.y += f * v.y;
     }
-    *reinterpret_cast<float2*>(&part[r * kStride + d]) = sum;
-    if (d == 0) mine[r] = make_float2(M, Lr);
+    // to the CTA that finishes this pair: pair i is CTA i / per's
+    const int to = i / per;
+    store_peer(&peer_o[rank * per + (i - to * per)], to, sum);
+    if (i % per == 0 || d == 0) store_peer(&peer_ml[rank * kR + r], to, make_float2(M, Lr));
   }
   cluster_arrive();
   cluster_wait();
-  for (int i = rank * kThreadsF + threadIdx.x; i < p.rows * (D / 2); i += p.C * kThreadsF) {
+  for (int k = threadIdx.x; k < per; k += kThreadsF) {
+    const int i = rank * per + k;
+    if (i >= pairs) break;
     const int r = i / (D / 2), d = 2 * (i % (D / 2));
-    float2 s[kMaxC], v[kMaxC];
     float M = -CUDART_INF_F, Lr = 0.f;
-#pragma unroll
-    for (int k = 0; k < kMaxC; ++k) {
-      s[k] = make_float2(-CUDART_INF_F, 0.f);  // no CTA k
-      v[k] = make_float2(0.f, 0.f);
-      if (k < p.C) {
-        s[k] = make_float2(load_peer(&mine[r].x, k), load_peer(&mine[r].y, k));
-        v[k] = make_float2(load_peer(&part[r * kStride + d], k), load_peer(&part[r * kStride + d + 1], k));
-      }
-      M = fmaxf(M, s[k].x);
-    }
+    for (int x = 0; x < p.C; ++x) M = fmaxf(M, peer_ml[x * kR + r].x);
     float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < kMaxC; ++k) {
-      const float f = weight(s[k], M, Lr);
-      sum.x += f * v[k].x;
-      sum.y += f * v[k].y;
+    for (int x = 0; x < p.C; ++x) {
+      const float f = weight(peer_ml[x * kR + r], M, Lr);
+      const float2 v = peer_o[x * per + k];
+      sum.x += f * v.x;
+      sum.y += f * v.y;
     }
     const float inv = Lr == 0.f ? 0.f : 1.f / Lr;  // no keys at all: zeros
     const int node = r / p.group, dim = (D / 8) * (d % 16 / 2) + 2 * (d / 16);
     *reinterpret_cast<uint32_t*>(p.out + (((size_t)b * p.n + node) * p.H + h * p.group + (r - node * p.group)) * D + dim) =
         pack_bf16x2(sum.x * inv, sum.y * inv);
   }
-  cluster_arrive();  // a CTA's shared memory stays until its peers have read it
-  cluster_wait();
 }
 
 cudaLaunchConfig_t config(long long slabs, int C, size_t smem, cudaStream_t st, cudaLaunchAttribute* attr) {
@@ -469,13 +533,20 @@ cudaLaunchConfig_t config(long long slabs, int C, size_t smem, cudaStream_t st, 
 
 template <int D, int NT>
 cudaError_t launch_typed(const Kv8AttnArgs& a, cudaStream_t st) {
-  constexpr size_t kSmem = sizeof(float) * ((kWarpsF + 1) * 8 * NT * (D + 4) + 2 * (kWarpsF + 1) * 8 * NT);
+  constexpr size_t kSmem = sizeof(float) * (kWarpsF * 8 * NT * (D + 4) + 2 * (kWarpsF + kMaxC) * 8 * NT +
+                                            8 * NT * D + 2 * kMaxC + NT * (D / 16) * 64 + 8 * NT);
   static PerDevice<int> allowed;
   cudaError_t e = allow_smem(allowed, kv8_few_kernel<D, NT>, (int)kSmem);
   if (e != cudaSuccess) return e;
   const long long slabs = (long long)a.B * a.Hkv, slots = (NT == 1 ? 2LL : 1LL) * sm_count();
   int C = kMaxC;
   while (C > 1 && (slabs * C > slots || (long long)C * kWarpsF * kTKF >= 2LL * a.max_kv_len)) C >>= 1;
+  // One wave, and short: with 32 keys a warp at a time and nothing but registers to hold what is on its way, the tcgen05
+  // kernel's ring streams faster once the warps have many tiles, or where clusters leave SMs out (here / there, us: 32
+  // heads of 2048 keys 8.4 / 10.4, 8192 17.0 / 18.3, 16384 28.0 / 27.3; 4 x 8 heads under 32 queries, 16384 keys 28.3 /
+  // 29.9; 8 heads 20.8 / 18.9; 4 x 52, 4096 45 / 39; 12 nodes, 32 heads, 2048 13.4 / 16.1, 4 x 32, 4096 40 / 34).
+  const long long rounds = (a.max_kv_len + C * kWarpsF * kTKF - 1LL) / (C * kWarpsF * kTKF);
+  if (rounds > 8 || (rounds > 4 && 4 * slabs * C < 3 * slots)) return cudaErrorNotSupported;
   if (a.max_ctas > 0 && slabs * C > a.max_ctas) return cudaErrorNotSupported;
   if (slabs * C > 0x7fffffffLL) return cudaErrorNotSupported;
   FewParams p;
