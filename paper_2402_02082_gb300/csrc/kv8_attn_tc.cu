@@ -78,7 +78,7 @@ struct Cfg {
   static constexpr int kCopyK = 4 * kSG, kCopyV = kCopyK + 1, kMmaS = kCopyK + 2, kMmaO = kCopyK + 3,
                        kThreads = kSoft + 128;
   static constexpr int kCtas = NP <= 32 ? 2 : 1;                      // of an SM
-  static constexpr int kBuf = NP <= 32 ? 1 : 2;                       // S and P buffers
+  static constexpr int kBuf = 2;                                      // S and P buffers
   static constexpr int kNO = kWiden ? NP : 2 * NP;                      // columns of O (few rows: hi | lo)
   // S adds hi and lo up itself, as products along 2 D; 8 columns are less than an MMA has, so there they lie side by side.
   static constexpr bool kSplitS = NP < 16;
