@@ -1,4 +1,4 @@
-// Attention over the 8-bit cache on the CUDA cores, fp32 throughout:
+// Attention over the 8-bit cache on the CUDA cores, for fp32 queries:
 //
 //   s[r,t]  = q[r] . code_K[t] * 2^eK[t/64] * scale        (cached rows)
 //           = q[r] . k_tree[j] * scale                     (nodes j in A_r)
@@ -8,6 +8,10 @@
 // warps take tiles of 32 keys in turn.  Lane = key for the scores (the query comes from shared
 // memory, the same address in every lane), lane = slice of the head dimension for the values.
 // Running maximum, sum and output are kept per warp and joined at the end.
+//
+// What bounds it: fp32 queries are for checks and comparisons at small sizes, where a call is a chain of latencies.
+// 5 nodes on 4 heads of 64 dims, 128 keys: 6.4 us.  Tiles of 32 keys over the CTA's warps make that chain one tile long
+// there; nothing splits a slab's keys over CTAs, so a long cache in fp32 leaves most of the GPU idle.
 #include <math_constants.h>
 
 #include "attn_common.cuh"
@@ -22,12 +26,7 @@ constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kRT = 4;  // query rows of a CTA
 
-__device__ __forceinline__ float widen(float x) { return x; }
-__device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void narrow(float x, float* to) { *to = x; }
-__device__ __forceinline__ void narrow(float x, __nv_bfloat16* to) { *to = __float2bfloat16_rn(x); }
-
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArgs a) {
   constexpr int kPer = D / 32;  // value elements per lane
   __shared__ __align__(16) float q[kRT][D];
@@ -43,10 +42,10 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
   pdl_wait();
   int L = a.kv_len[b];
   L = L < 0 ? 0 : (L > a.max_kv_len ? a.max_kv_len : L);
-  const T* Q = static_cast<const T*>(a.q);
+  const float* Q = static_cast<const float*>(a.q);
   for (int i = threadIdx.x; i < kRT * D; i += kThreads) {
     const int r = r0 + i / D;
-    q[i / D][i % D] = r < rows ? widen(Q[out_row(b, h, r, rows, group, a.H) * D + i % D]) : 0.f;
+    q[i / D][i % D] = r < rows ? Q[out_row(b, h, r, rows, group, a.H) * D + i % D] : 0.f;
   }
   const int n = a.parent ? a.nq : 0;
   if (threadIdx.x < n) up[threadIdx.x] = a.parent[(size_t)b * n + threadIdx.x];
@@ -141,9 +140,9 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
       });
     } else {
       const int j0 = (tile - cached) * 32, j = j0 + lane, at = j < n ? j : n - 1;
-      const T* row = static_cast<const T*>(a.kt) + (((size_t)b * n + at) * a.Hkv + h) * D;
+      const float* row = static_cast<const float*>(a.kt) + (((size_t)b * n + at) * a.Hkv + h) * D;
       for (int d = 0; d < D; ++d) {
-        const float k = widen(row[d]);
+        const float k = row[d];
 #pragma unroll
         for (int r = 0; r < kRT; ++r) s[r] = fmaf(q[r][d], k, s[r]);
       }
@@ -153,10 +152,10 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
         s[r] *= c;
         if (j < n && (sees[r] >> j) & 1ull) seen |= 1u << r;
       }
-      const T* vt = static_cast<const T*>(a.vt) + (((size_t)b * n + j0) * a.Hkv + h) * D + lane * kPer;
+      const float* vt = static_cast<const float*>(a.vt) + (((size_t)b * n + j0) * a.Hkv + h) * D + lane * kPer;
       fold(s, seen, 1.f, n - j0 < 32 ? n - j0 : 32, [&](int i, float* f) {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) f[k] = widen(vt[(size_t)i * a.Hkv * D + k]);
+        for (int k = 0; k < kPer; ++k) f[k] = vt[(size_t)i * a.Hkv * D + k];
       });
     }
   }
@@ -170,7 +169,7 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
     for (int k = 0; k < kPer; ++k) o_all[warp][r][lane * kPer + k] = o[r][k];
   }
   __syncthreads();
-  T* out = static_cast<T*>(a.out);
+  float* out = static_cast<float*>(a.out);
   for (int i = threadIdx.x; i < kRT * D; i += kThreads) {
     const int r = i / D, d = i % D;
     if (r0 + r >= rows) break;
@@ -181,21 +180,21 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
       sum += f * l_all[w][r];
       x += f * o_all[w][r][d];
     }
-    narrow(sum == 0.f ? 0.f : x / sum, &out[out_row(b, h, r0 + r, rows, group, a.H) * D + d]);
+    out[out_row(b, h, r0 + r, rows, group, a.H) * D + d] = sum == 0.f ? 0.f : x / sum;
   }
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t launch(const Kv8AttnArgs& a, cudaStream_t st) {
   const int rows = a.nq * (a.H / a.Hkv);
   const long long ctas = (long long)a.B * a.Hkv * ((rows + kRT - 1) / kRT);
-  return launch_pdl(kv8_attn_fma_kernel<T, D>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a);
+  return launch_pdl(kv8_attn_fma_kernel<D>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a);
 }
 
 }  // namespace
 
 cudaError_t launch_kv8_attn_fma(const Kv8AttnArgs& a, cudaStream_t st) {
-  return a.D == 128 ? launch<float, 128>(a, st) : launch<float, 64>(a, st);
+  return a.D == 128 ? launch<128>(a, st) : launch<64>(a, st);
 }
 
 }  // namespace glide

@@ -3,34 +3,39 @@
 //
 // The mathematics.  With codes K8, V8 and block exponents eK, eV of key t,
 //   s[r,t] = q[r] . K8[t] * 2^eK * scale * log2(e),   u[r,t] = s[r,t] + eV[t]
-//   m[r]   = running maximum of u less 6 .. 8,   p[r,t] = 2^(u - m)
+//   m[r]   = running maximum of u less kLift,    p[r,t] = 2^(u - m)
 //   O[r]   = sum_t p[r,t] V8[t],     l[r]   = sum_t p[r,t] 2^-eV[t],    out[r] = O[r] / l[r]
 // Taking the value exponent into the weight's exponent leaves the codes as they are: no key or
 // value is widened or scaled, and the tensor cores multiply the cache's own bytes.
 //
-// 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with
-// the slab's largest query scaled to at most 448, q = hi + lo / 16 exactly (elements below 2^-14 of the
-// largest to 2^-23 of it).  A weight p <= 430 is hi + lo / 32 to 2^-9 of itself, or to 2^-20 of the
-// row's largest, which is at least 64.  hi and lo are columns of their own, so both products cost twice
-// the columns and nothing else.  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16 with
-// bf16 queries and weights into the columns of hi; its values are scaled to a block's range by a power
-// of two of their own, so that the weights of tree and cache lie in one range.
+// 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with the slab's
+// largest query scaled to at most 448, q = hi + lo exactly down to the codes' least step (2^-9, or 2^-13 at 8 rows,
+// where lo is held 16 times itself).  Weights, up to 48 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
+// of the row's largest, which is at least 2^8.  64 rows: values are widened to fp16 in shared memory, weights rounded
+// to fp16 (2^-12 of themselves).  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16
+// with bf16 queries and weights; its values are scaled to a block's range by a power of two of their own, so that the
+// weights of tree and cache lie in one range.
 //
 // Orientation.  Keys are the 128 rows of the MMA and the queries its columns:
-//   S^T = K8 Q^T  : M = 128 keys, N = 2 x NP (hi | lo), K = D, both operands K-major
-//   O^T += V8^T P^T : M = D, N = 2 x NP, K = keys, both operands M/N-major
-// so the tensor work goes with the query rows (NP = 8 .. 64), not with a padded 128, K and V tiles are
-// read from shared memory once, and thread = key in the softmax.  A row's maximum then lies across the
-// threads; it is looked for only when a weight would pass the largest code (one vote per tile), which after the
-// first tile of a slab is rare.
+//   S^T = K8 Q^T    : M = 128 keys, N = NP, K = D twice (hi, then lo, into the same columns; at 8 rows, less than an MMA's
+//                     columns, they lie side by side), both operands K-major
+//   O^T += V8^T P^T : M = D, N = 2 x NP (hi | lo; NP where values are widened), K = keys, both operands M/N-major
+// so the tensor work goes with the query rows (NP = 8 .. 64), not with a padded 128, K and V tiles are read from shared
+// memory once, and thread = key in the softmax.  A row's maximum then lies across the threads; it is looked for only
+// when a weight would pass the largest there is (one vote per tile), which after a slab's first tile is rare.
 //
-// Roles: SG groups of four softmax warps, two copy warps (TMA), two MMA warps; a persistent grid and the
-// cost-balanced split of the key sequence that the other kernels use.  A group takes 8 or 16 of the query
-// rows, thread = key: a thread's scores, weights and running sums then stay in ~100 registers and sixteen
-// softmax warps fill an SM (one group of 64 rows: 168 registers and spills, 660 us where this takes @64).
-// Up to 32 rows two CTAs share an SM and S and P have one buffer each (S is free again once it is in
-// registers); above, one CTA with two of each.  A tree is tile 0 of its slab: the softmax warps write its
-// operands while the first copies are on their way.
+// Roles: groups of four softmax warps, two copy warps (TMA: K, V), two MMA warps (S, P.V); a persistent grid and the
+// cost-balanced split of the key sequence that the other kernels use.  A group takes 8 or 16 of the query rows,
+// thread = key: sixteen softmax warps fill an SM at 64 rows (one group of 64 rows spilled: 660 us for the 218 below).
+// Up to 32 rows two CTAs share an SM, above one has it.  S and P have two buffers each (26 nodes on 8 x 40 heads, 512 -
+// 4096 keys: 69.5 us with one, 66 with two).  A tree is tile 0 of its slab: the softmax warps write its operands while
+// the first copies are on their way.
+//
+// What bounds it, and what it takes: 64 nodes on 4 x 52 heads of 16384 keys 218 us, 4.0 TB/s of the cache, where the
+// bytes alone take 130: a tile of 128 keys costs ~2060 cycles (HBM's rate: 1394), the softmax warps' instructions and the
+// chain S -> weights -> P.V.  26 nodes on 8 x 40 heads of 512 - 4096 keys: 66 us (bytes: 32), where the ~10 k cycles in
+// which a slab's queries become operands and its sums results weigh in.  33 nodes of 4 query heads to a cached one: three row tiles
+// of 44 that read the cache three times, from L2 twice: 103 us on 4 x 8 cached heads of 16384 keys (bytes: 20).
 //
 // A slab whose keys lie in several CTAs' shares leaves partials (m, l, O) in the workspace and
 // kv8_merge_kernel joins them.
@@ -327,8 +332,8 @@ __device__ __forceinline__ int top_exponent(uint32_t bits) {
 }
 
 // A block's value exponent as the weights take it.  A block of zero values has the least exponent there is; beside an
-// ordinary block its weights would leave fp32's range, and the sum l with them.  So an exponent counts as at least 64
-// below the largest seen: its values then show up 2^-64 of that block's at most.
+// ordinary block its weights would leave fp32's range, and the sum l with them.  So an exponent counts as at least
+// 110 below the largest seen, and as -90: its values then show up 2^-102 of that block's largest at most.
 __device__ __forceinline__ int effective_exp(int e, int ref) { return max(max(e, ref - kVExpSpan), kVExpLeast); }
 
 template <int D, int NP>
