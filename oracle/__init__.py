@@ -26,8 +26,12 @@ It is a plain, slow, fp64 restatement of what the path computes:
 * ``sampling.spec_sample_accept`` -- speculative-sampling acceptance of a
   chain proposal (the strategy Section 2 names and Section 4.1 uses for GliDe
   alone), with the random numbers as inputs.
+* ``kv8.kv8_append``, ``kv8.kv8_read``, ``kv8.kv8_attn`` -- the cache in 8 bits with
+  a power-of-two scale per block of 64 tokens and head (not in the paper): rows
+  quantised as they join it, read back, and both attentions over it.
 
-Every function here is pinned by tests in ``tests/test_oracle.py`` against
+Every function here is pinned by tests in ``tests/test_oracle.py`` (the 8-bit
+cache's in ``tests/test_kv8_oracle.py``) against
 closed forms, library routines, brute force and invariants; none is marked
 "parity unpinned".
 """
@@ -35,9 +39,10 @@ from .attention import (ancestors_or_self, block_cross_attn, block_mask, cape_ma
                         tree_allowed_mask, tree_verify_attn, widen)
 from .accept import row_argmax, tree_accept
 from .cape import cape_expand, expansion_size
+from .kv8 import kv8_append, kv8_attn, kv8_read
 from .kvcache import kv_compact
 from .sampling import spec_sample_accept
 
 __all__ = ["ancestors_or_self", "block_cross_attn", "block_mask", "cape_mask", "cross_attn", "tree_allowed_mask",
            "tree_verify_attn", "widen", "row_argmax", "tree_accept", "cape_expand", "expansion_size", "kv_compact",
-           "spec_sample_accept"]
+           "kv8_append", "kv8_attn", "kv8_read", "spec_sample_accept"]
