@@ -129,9 +129,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) kv8_append_k
   constexpr int kPasses = kKv8Block / kRows;
   __shared__ uint32_t top[2][kThreads / 32];
   pdl_wait();
-  const int slab = (int)(blockIdx.x / (unsigned)p.blocks), nth = (int)(blockIdx.x - (unsigned)slab * p.blocks);
-  const int bh = slab % (p.B * p.H), layer = slab / (p.B * p.H);
-  const int b = bh / p.H, h = bh - b * p.H;
+  // heads first: CTAs that run together then read whole tokens' rows
+  const int bn = (int)(blockIdx.x / (unsigned)p.H), h = (int)(blockIdx.x - (unsigned)bn * p.H);
+  const int lb = bn / p.blocks, nth = bn - lb * p.blocks;
+  const int layer = lb / p.B, b = lb - layer * p.B, slab = lb * p.H + h;
   const Rows r = rows_of(p, b);
   if (nth == 0 && layer == 0 && h == 0 && threadIdx.x == 0) p.new_kv_len[b] = r.L + r.m;
   const int block = r.L / kKv8Block + nth, row0 = block * kKv8Block;
