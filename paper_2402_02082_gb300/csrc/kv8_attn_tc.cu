@@ -115,7 +115,7 @@ struct Small {  // per CTA, after the rings
   alignas(16) float f[64];      // 2^-up; at the end 1 / l, or l
   alignas(16) float part[4][64];  // per lane quarter: row maxima, row sums
   alignas(4) uint8_t rise[2][4][4];  // tiles in turn, per group and lane quarter: the chunks whose m rises
-  int rel[64];                  // a row's place among a sequence's [node, head] rows from the slab's first head, -1: none
+  alignas(16) int rel[64];                  // a row's place among a sequence's [node, head] rows from the slab's first head, -1: none
   uint32_t top[16][2];           // per softmax warp: largest query, largest value of the tree
   uint32_t tmem;
   int abort_flag;
@@ -547,6 +547,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
                    p_mix = C::kPitch == 128 ? x128 : (C::kPitch == 64 ? ((tid >> 1) & 3) << 4 : ((tid >> 2) & 1) << 4);
     bool dead = false;
     int st = 0, vst = 0, i = 0;  // stages of K and V, tiles so far
+    int sees_b = -1;             // the sequence that sm.sees is of
     uint32_t ring = 0, v_ring = 0;
     // P.V of tile j of this CTA is done
     auto wait_pv = [&](int j) {
@@ -569,16 +570,22 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       uint32_t scales = 0;
       float inv = 0.f;
       int ref = -128;
-      auto load_scales = [&](int block) {
+      auto fetch = [&](int block) {
         const int at = min(block + lane, used - 1);
-        const int ek = kv8_clamp_exp(Ke[at]), ev = kv8_clamp_exp(Ve[at]);
+        return make_int2(Ke[at], Ve[at]);
+      };
+      auto set_scales = [&](int2 raw) {
+        const int ek = kv8_clamp_exp(raw.x), ev = kv8_clamp_exp(raw.y);
         ref = max(ref, __reduce_max_sync(0xffffffffu, ev));
         const int e = effective_exp(ev, ref);
         scales = (uint32_t)(ek + 127) << 7 | (__float_as_uint((float)e) & 0xffff0000u);
         inv = kv8_pow2(-e);
       };
-      const int tile0 = tree_here ? 0 : s.t0 - p.tree;  // first tile of cached keys
-      if (used > 0 && !tree_here) load_scales(2 * tile0);
+      // Everything that the segment's start reads from global memory is on its way before any of it is used.
+      int2 raw = make_int2(0, 0), up = make_int2(-1, -1);
+      if (used > 0) raw = fetch(tree_here ? 0 : 2 * (s.t0 - p.tree));
+      const bool walk = tree_here && s.b != sees_b;  // the rows' ancestors, the same for a sequence's heads
+      if (walk && quarter == 0) up = parents_of(p.parent + (size_t)s.b * p.n, p.n, lane);
 
       // ---- the segment's queries, and the tree's own keys and values, as operands
       const int first_tile = i;
@@ -587,7 +594,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         constexpr int kPerRow = D / 8, kQ = (NP * kPerRow + kSoft - 1) / kSoft,
                       kT = (kTreeKeys * kPerRow + kSoft - 1) / kSoft;
         const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-        uint4 q[kQ], v[kT];
+        uint4 q[kQ], kt[kT], v[kT];
         uint32_t most = 0, most_v = 0;
         const size_t q0 = (size_t)s.b * p.n * p.H + (size_t)s.h * p.group;
 #pragma unroll
@@ -595,37 +602,37 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           const int c = sid + i * kSoft, r = c / kPerRow;
           q[i] = none;
           if (r < rows_here) q[i] = reinterpret_cast<const uint4*>(p.q + (q0 + sm.rel[r]) * D)[c % kPerRow];
-          most = max(most, top8(q[i]));
         }
+        if (tree_here) {
+#pragma unroll
+          for (int i = 0; i < kT; ++i) {
+            const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
+            kt[i] = v[i] = none;
+            if (r < p.n) {  // p.n <= kTreeKeys
+              const size_t at = (((size_t)s.b * p.n + r) * p.Hkv + s.h) * D + d;
+              kt[i] = *reinterpret_cast<const uint4*>(p.kt + at);
+              v[i] = *reinterpret_cast<const uint4*>(p.vt + at);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) most = max(most, top8(q[i]));
         // Byte of element d of row r in a bf16 operand of `rows` rows: 64 elements (128 bytes) a row and part.
         auto in_bf16 = [](int r, int d, int rows) { return (d / 64) * rows * 128 + swizzled<128>(r, (d % 64) * 2); };
         bool odd = false;
         if (tree_here) {
-          if (warp == 0) {  // the rows' nodes and their ancestors
-            const int2 up = parents_of(p.parent + (size_t)s.b * p.n, p.n, lane);
-#pragma unroll 1
-            for (int r = lane; r < 64; r += 32)
-              sm.sees[r] = ancestors(up, p.n, r < rows_here ? (row0 + r) / p.group : 0, true, lane);
-          }
           dead |= !warp_wait(&bars[E_K + st], ring ^ 1, abort_flag);
           if (!C::kWiden) dead |= !warp_wait(&bars[E_V + st], ring ^ 1, abort_flag);
           unsigned char* kd = base + C::off_K + st * C::kTile;
 #pragma unroll
           for (int i = 0; i < kT; ++i) {
             const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
-            uint4 k = none;
-            v[i] = none;
             if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;
-            if (r < p.n) {
-              const size_t at = (((size_t)s.b * p.n + r) * p.Hkv + s.h) * D + d;
-              k = *reinterpret_cast<const uint4*>(p.kt + at);
-              v[i] = *reinterpret_cast<const uint4*>(p.vt + at);
-            }
             // An unseen value that is not finite must not meet a weight of zero: it is left out here, and put
             // back at the end where it is seen.
             odd |= drop_odd(v[i]);
             most_v = max(most_v, top8(v[i]));
-            *reinterpret_cast<uint4*>(kd + in_bf16(r, d, kTreeKeys)) = k;
+            *reinterpret_cast<uint4*>(kd + in_bf16(r, d, kTreeKeys)) = kt[i];
           }
           unsigned char* qd = base + C::off_P + first_tile % C::kBuf * C::kPBytes;  // P of this tile comes later
 #pragma unroll
@@ -688,9 +695,16 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       uint64_t l2[RT / 2];  // pairs of rows
 #pragma unroll
       for (int k = 0; k < RT / 2; ++k) l2[k] = 0ull;
-      if (tree_here) {
-        ref = vt_exp;
-        if (used > 0) load_scales(0);
+      if (tree_here) ref = vt_exp;
+      if (used > 0) set_scales(raw);
+      if (walk) {  // while the first product runs
+        if (quarter == 0) {
+          const int r = r_own + lane;
+          const unsigned long long set = ancestors(up, p.n, r < rows_here ? (row0 + r) / p.group : 0, true, lane);
+          if (lane < RT) sm.sees[r] = set;
+        }
+        sees_b = s.b;
+        soft_sync<128>(gbar);
       }
       const float a_q = p.scale_log2 * kv8_pow2(q_exp);
       int nth = 0;  // of the tiles whose scales the lanes hold
@@ -700,7 +714,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         float a = p.scale_log2, ef = (float)effective_exp(vt_exp, vt_exp), inv_v = kv8_pow2(-effective_exp(vt_exp, vt_exp));
         if (!is_tree) {
           if (nth == 32) {
-            load_scales(key0 / kKv8Block);
+            set_scales(fetch(key0 / kKv8Block));
             nth = 0;
           }
           const uint32_t mine = __shfl_sync(0xffffffffu, scales, nth + (tid >> 6));
@@ -774,7 +788,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           if (is_tree) {
             vis = 0;
             if (tid < p.n)
-#pragma unroll 1
+#pragma unroll 4
               for (int r = 0; r < RT; ++r) vis |= (uint32_t)((sm.sees[r_own + r] >> tid) & 1ull) << r;
           }
 #pragma unroll
@@ -966,36 +980,49 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       const bool odd = tree_here && sm.odd_values;
       float* part = partial_slot(p.partials, x + slab, p.rows, D) + (size_t)row0 * (D + 2);
       const size_t o0 = (size_t)s.b * p.n * p.H + (size_t)s.h * p.group;
+      if (!whole && tid < RT && !dead && sm.rel[r_own + tid] >= 0)
+        *reinterpret_cast<float2*>(part + (size_t)(r_own + tid) * (D + 2)) =
+            make_float2(-sm.minus_m[r_own + tid], sm.f[r_own + tid]);
+      const bool live = has && !dead;
 #pragma unroll 1
       for (int c = 0; c < RT; c += 8) {
         uint32_t acc[8], low[8];
+        float o[8];
         if (C::kWiden)
           tmem_ld8(tO + c, acc);
         else
           tmem_ld8x2(tO + c, tO + NP + c, acc, low);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int r = r_own + c + k, rel = sm.rel[r];
-          if (rel < 0 || !has || dead) continue;
-          float o = __uint_as_float(acc[k]);
-          if (!C::kWiden) o = fmaf(__uint_as_float(low[k]), 1.f / kPLo, o);
-          if (odd) {  // a visible value that is not finite decides its column
+          o[k] = __uint_as_float(acc[k]);
+          if (!C::kWiden) o[k] = fmaf(__uint_as_float(low[k]), 1.f / kPLo, o[k]);
+        }
+        if (opaque(odd) && live) {  // a visible value that is not finite decides its column
 #pragma unroll 1
-            for (int j = 0; j < p.n; ++j) {
-              const float v = __bfloat162float(p.vt[(((size_t)s.b * p.n + j) * p.Hkv + s.h) * D + d]);
-              if ((sm.sees[r] >> j) & 1ull && !isfinite(v)) o += v;
-            }
+          for (int j = 0; j < p.n; ++j) {
+            const float v = __bfloat162float(p.vt[(((size_t)s.b * p.n + j) * p.Hkv + s.h) * D + d]);
+            if (isfinite(v)) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if ((sm.sees[r_own + c + k] >> j) & 1ull) o[k] += v;
           }
-          if (whole) {
-            p.out[(o0 + rel) * D + d] = __float2bfloat16_rn(o * sm.f[r]);
-          } else {
-            float* row = part + (size_t)r * (D + 2);
-            row[2 + d] = o;
-            if (d == 0) {
-              row[0] = -sm.minus_m[r];
-              row[1] = sm.f[r];
-            }
-          }
+        }
+        const int4 ra = *reinterpret_cast<const int4*>(&sm.rel[r_own + c]),
+                   rb = *reinterpret_cast<const int4*>(&sm.rel[r_own + c + 4]);
+        const int rel[8] = {ra.x, ra.y, ra.z, ra.w, rb.x, rb.y, rb.z, rb.w};
+        if (whole) {
+          const float4 fa = *reinterpret_cast<const float4*>(&sm.f[r_own + c]),
+                       fb = *reinterpret_cast<const float4*>(&sm.f[r_own + c + 4]);
+          const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
+          __nv_bfloat16* to = p.out + o0 * D + d;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (live && rel[k] >= 0) to[(size_t)rel[k] * D] = __float2bfloat16_rn(o[k] * f[k]);
+        } else {
+          float* to = part + (size_t)(r_own + c) * (D + 2) + 2 + d;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (live && rel[k] >= 0) to[k * (D + 2)] = o[k];
         }
       }
       tc::fence_before_sync();
