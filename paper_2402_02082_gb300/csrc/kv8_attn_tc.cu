@@ -65,8 +65,8 @@ constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
 __host__ __device__ constexpr int seg_weight8(int np) { return 2 + np / 16; }
 
 // barriers
-constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, SFREE8 = 27, PFULL8 = 29, PVDONE = 31,
-              MDONE8 = 33, kBars8 = 35;
+constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, PFULL8 = 27, PVDONE = 29, MDONE8 = 31,
+              kBars8 = 33;
 
 template <int D, int NP>
 struct Cfg {
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
   if (threadIdx.x == 0) {
     tc::prefetch_tmap(&tmK);
     tc::prefetch_tmap(&tmV);
-    for (int b = 0; b < kBars8; ++b) mbar_init(&bars[b], (C::kWiden && b >= E_V && b < QFULL8) || b == QFULL8 || (b >= SFREE8 && b < PVDONE) ? 4 * C::kSG : 1);
+    for (int b = 0; b < kBars8; ++b) mbar_init(&bars[b], (C::kWiden && b >= E_V && b < QFULL8) || b == QFULL8 || (b >= PFULL8 && b < PVDONE) ? 4 * C::kSG : 1);
     *abort_flag = 0;
     fence_barrier_init();
   }
@@ -437,8 +437,10 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       ok = warp_wait(&bars[QFULL8], seg & 1, abort_flag);
       for (int t = s.t0; t < s.t1 && ok; ++t, ++i) {
         const int buf = i % kBuf;
+        // P.V of the tile that had the buffers is done: its scores were read before its weights were written, so S is free;
+        // and these scores will tell the softmax that P and W are (one warp waits here for all of its warps).
         ok = warp_wait(&bars[F_K + st], phase, abort_flag) &&
-             warp_wait(&bars[SFREE8 + buf], (i / kBuf & 1) ^ 1, abort_flag);
+             (i < kBuf || warp_wait(&bars[PVDONE + buf], (i - kBuf) / kBuf & 1, abort_flag));
         if (!ok) break;
         tc::fence_after_sync();
         const uint32_t tS = tmem + buf * C::kTmemS;
@@ -724,7 +726,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           nth += 2;
         }
 
-        wait_pv(i - kBuf);  // the buffers of P and W are free when that P.V has read them
+        dead |= !warp_wait(&bars[SFULL8 + buf], i / C::kBuf & 1, abort_flag);
+        tc::fence_after_sync();
         if (C::kWiden && !is_tree) {
           // ---- the values as fp16, exactly: this thread's part of its key's row, zeros past the end (what lies there
           // may be NaN, and zero times NaN is no zero)
@@ -755,8 +758,6 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         // ---- u = S a + e, less m (none yet in a segment's first tile)
         float u[RT];
         const uint32_t tS = lane_addr + buf * C::kTmemS + r_own;
-        dead |= !warp_wait(&bars[SFULL8 + buf], i / C::kBuf & 1, abort_flag);
-        tc::fence_after_sync();
         if (!C::kWiden && NP >= 16 && opaque(is_tree)) {  // this tile starts O, and its product leaves the lower parts out
           const uint32_t none[8] = {};
 #pragma unroll 1
@@ -769,20 +770,20 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             constexpr int CH = 8;
             uint32_t x[CH], z[CH];  // split: hi, lo; else rows c .. c + 7, rows c + 8 .. c + 15
             tmem_ld8x2(tS + c, tS + c + (C::kSplitS ? NP : 8), x, z);
+            const uint64_t a2 = f2(a, a), ef2 = f2(ef, ef);
+            auto pair = [](const uint32_t* x) { return f2(__uint_as_float(x[0]), __uint_as_float(x[1])); };
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
+            for (int k = 0; k < CH; k += 2) {
               if constexpr (C::kSplitS) {
-                u[c + k] = fmaf(__uint_as_float(x[k]), a, fmaf(__uint_as_float(z[k]), a / C::kQLo, ef));
+                const uint64_t lo2 = f2(a / C::kQLo, a / C::kQLo);
+                unf2(ffma2(pair(x + k), a2, ffma2(pair(z + k), lo2, ef2)), u[c + k], u[c + k + 1]);
               } else {
-                u[c + k] = fmaf(__uint_as_float(x[k]), a, ef);
-                if (c + 8 + k < RT) u[c + 8 + k] = fmaf(__uint_as_float(z[k]), a, ef);
+                unf2(ffma2(pair(x + k), a2, ef2), u[c + k], u[c + k + 1]);
+                if (c + 8 + k < RT) unf2(ffma2(pair(z + k), a2, ef2), u[c + 8 + k], u[c + 9 + k]);
               }
             }
           }
         }
-        tc::fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars[SFREE8 + buf]);
         if (opaque(is_tree || key0 + kTK > plen)) {  // which rows see this thread's key
           uint32_t vis = key0 + tid < plen ? ~0u : 0u;
           if (is_tree) {
@@ -802,11 +803,9 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             float top = -CUDART_INF_F;
 #pragma unroll
             for (int k = c; k < c + 8; k += 4) {
-              const float4 m = *reinterpret_cast<const float4*>(&sm.minus_m[r_own + k]);
-              u[k] += m.x;
-              u[k + 1] += m.y;
-              u[k + 2] += m.z;
-              u[k + 3] += m.w;
+              const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(&sm.minus_m[r_own + k]);
+              unf2(fadd2(f2(u[k], u[k + 1]), m.x), u[k], u[k + 1]);
+              unf2(fadd2(f2(u[k + 2], u[k + 3]), m.y), u[k + 2], u[k + 3]);
               top = fmax3(fmax3(top, u[k], u[k + 1]), u[k + 2], u[k + 3]);
             }
             if (top > C::kMost) rise |= 1u << c / 8;
