@@ -10,8 +10,8 @@
 //
 // 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with the slab's
 // largest query scaled to at most 448, q = hi + lo exactly down to the codes' least step (2^-9, or 2^-13 at 8 rows,
-// where lo is held 16 times itself).  Weights, up to 48 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
-// of the row's largest, which is at least 2^8.  64 rows: values are widened to fp16 in shared memory, weights rounded
+// where lo is held 16 times itself).  Weights, up to 32 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
+// of the row's largest, which is at least 2^8.  More rows: values are widened to fp16 in shared memory, weights rounded
 // to fp16 (2^-12 of themselves).  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16
 // with bf16 queries and weights; its values are scaled to a block's range by a power of two of their own, so that the
 // weights of tree and cache lie in one range.
@@ -70,9 +70,10 @@ constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, PF
 
 template <int D, int NP>
 struct Cfg {
-  // Up to 48 rows: weights as two codes each.  More: values widened to fp16, work that the rows share (64 nodes on 4 x
-  // 52 heads, 16384 keys: 226 us as two codes, 218 widened; 26 nodes on 8 x 40 heads, 512 - 4096 keys 69.9 and 74.2).
-  static constexpr bool kWiden = NP > 48;
+  // Up to 32 rows: weights as two codes each, and two CTAs an SM, for which widened values leave no shared memory.  More:
+  // values widened to fp16, work that the rows share (16384 keys, two codes / widened, us: 44 nodes on 4 x 52 heads 182 /
+  // 177, 33 nodes of 4 query heads to each of 4 x 8 cached 96.5 / 90.5; 40 nodes on 8 x 40 heads of 512 - 4096 76 / 65).
+  static constexpr bool kWiden = NP > 32;
   static constexpr float kMost = kWiden ? 15.5f : 8.75f;              // log2 of the largest weight: 2^16, 448 are too large
   static constexpr float kLift = kWiden ? 6.f : 8.f;                  // log2 of the weight of a new maximum
   static constexpr int kRT = NP < 16 ? NP : 16;                    // rows of a softmax group
@@ -542,7 +543,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     const uint32_t tO = lane_addr + C::kTmemO + r_own;
     // Where this thread's pieces of its key's row lie: 16 codes at a time of V, widened to 32 bytes of W.
-    constexpr int kPieces = C::kWiden ? D / 16 / C::kSG : 0;
+    constexpr int kAll = D / 16, kPieces = C::kWiden ? (kAll + C::kSG - 1) / C::kSG : 0;
     const uint32_t x128 = (tid & 7) << 4, xD = D == 128 ? x128 : ((tid >> 1) & 3) << 4;
     const uint32_t v_from = tid * D, v_mix = (group * 16) ^ xD, w_to = tid * 128, w_mix = (group * 32) ^ x128;
     const uint32_t p_row = tid * C::kPitch,
@@ -736,14 +737,17 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           unsigned char* to = base + C::off_W + buf * C::kWide + w_to;
 #pragma unroll
           for (int j = 0; j < kPieces; ++j) {
-            uint4 w = *reinterpret_cast<const uint4*>(from + (v_mix ^ (j * C::kSG * 16)));
+            const int piece = j * C::kSG + group;
+            if (kAll % C::kSG != 0 && piece >= kAll) break;
+            // four groups: a group's place among four pieces is its own, and the rest is known here
+            uint4 w = *reinterpret_cast<const uint4*>(from + (C::kSG == 4 ? v_mix ^ (j * 64) : (piece * 16) ^ xD));
             if (opaque(key0 + kTK > plen) && key0 + tid >= plen) w = make_uint4(0u, 0u, 0u, 0u);
             uint4 lo, hi;
             widen4(w.x, lo.x, lo.y);
             widen4(w.y, lo.z, lo.w);
             widen4(w.z, hi.x, hi.y);
             widen4(w.w, hi.z, hi.w);
-            const uint32_t at = (j * C::kSG / 4) * kTK * 128 + (w_mix ^ ((j * C::kSG % 4) * 32));
+            const uint32_t at = C::kSG == 4 ? j * kTK * 128 + w_mix : (piece / 4) * kTK * 128 + ((piece % 4 * 32) ^ x128);
             *reinterpret_cast<uint4*>(to + at) = lo;
             *reinterpret_cast<uint4*>(to + (at ^ 16)) = hi;
           }
