@@ -542,11 +542,14 @@ cudaError_t launch_typed(const Kv8AttnArgs& a, cudaStream_t st) {
   int C = kMaxC;
   while (C > 1 && (slabs * C > slots || (long long)C * kWarpsF * kTKF >= 2LL * a.max_kv_len)) C >>= 1;
   // One wave, and short: with 32 keys a warp at a time and nothing but registers to hold what is on its way, the tcgen05
-  // kernel's ring streams faster once the warps have many tiles, or where clusters leave SMs out (here / there, us: 32
-  // heads of 2048 keys 8.4 / 10.4, 8192 17.0 / 18.3, 16384 28.0 / 27.3; 4 x 8 heads under 32 queries, 16384 keys 28.3 /
-  // 29.9; 8 heads 20.8 / 18.9; 4 x 52, 4096 45 / 39; 12 nodes, 32 heads, 2048 13.4 / 16.1, 4 x 32, 4096 40 / 34).
+  // kernel's ring streams faster once the warps have several tiles.  Here / there, us, with the tiles a warp has.  Up to 8
+  // rows: 32 heads of 2048 keys (1) 8.5 / 10.1, 4096 (2) 11.9 / 12.8, 6144 (3) 15.0 / 14.2, 16384 (8) 29.0 / 26.1; the
+  // GPU half empty, 8 heads of 8192 (4) 14.1 / 17.8, 16384 (8) 22.1 / 17.9; two waves, 8 x 40 heads of 512 18.0 / 13.6.
+  // Up to 16 rows: 12 nodes on 32 heads of 4096 (4) 16.4 / 17.4, 6144 (6) 20.7 / 19.5.  Rows of 64 dims are half a tile:
+  // 32 heads of 8192 (4) 11.8 / 13.1.
   const long long rounds = (a.max_kv_len + C * kWarpsF * kTKF - 1LL) / (C * kWarpsF * kTKF);
-  if (rounds > 8 || (rounds > 4 && 4 * slabs * C < 3 * slots)) return cudaErrorNotSupported;
+  const int most = NT == 1 && 2 * slabs * C > slots ? 2 : 4;
+  if (slabs * C > slots || rounds * D > most * 128LL) return cudaErrorNotSupported;
   if (a.max_ctas > 0 && slabs * C > a.max_ctas) return cudaErrorNotSupported;
   if (slabs * C > 0x7fffffffLL) return cudaErrorNotSupported;
   FewParams p;
