@@ -66,7 +66,7 @@ __host__ __device__ constexpr int seg_weight8(int np) { return 2 + np / 16; }
 
 // barriers
 constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, PFULL8 = 27, PVDONE = 29, MDONE8 = 31,
-              kBars8 = 33;
+              WFULL = 33, kBars8 = 35;
 
 template <int D, int NP>
 struct Cfg {
@@ -82,7 +82,13 @@ struct Cfg {
   // Warps after the softmax: K's copies, V's copies, S products, P.V products.  One thread for both copies or both
   // products sets a slower pace than the stream: a copy or a product keeps its issuer busy for over 100 cycles.
   static constexpr int kCopyK = 4 * kSG, kCopyV = kCopyK + 1, kMmaS = kCopyK + 2, kMmaO = kCopyK + 3,
-                       kThreads = kSoft + 128;
+                       kWideW = kCopyK + 4;                           // the first that widens values
+  // Four warps after those widen, beside the softmax (16384 keys, softmax warps / these, us: 44 nodes on 4 x 52 heads 177 /
+  // 164, 33 nodes of 4 query heads to each of 4 x 8 cached 90 / 84.5, 64 nodes on 4 x 52 heads of 64 dims 182 / 167).
+  // With 64 rows of 128 dims they and the softmax take longer than the softmax alone: 216 / 200, half each 240.
+  static constexpr bool kWideWarps = kWiden && (NP < 64 || D == 64);
+  static constexpr int kOwn = kWiden && !kWideWarps ? D / 16 / kSG : 0;  // else: pieces of 16 codes of a softmax group
+  static constexpr int kThreads = kSoft + 128 + (kWideWarps ? 128 : 0);
   static constexpr int kCtas = NP <= 32 ? 2 : 1;                      // of an SM
   static constexpr int kBuf = 2;                                      // S and P buffers
   static constexpr int kNO = kWiden ? NP : 2 * NP;                      // columns of O (few rows: hi | lo)
@@ -283,6 +289,18 @@ __device__ __forceinline__ void widen4(uint32_t w, uint32_t& a, uint32_t& b) {
       : "=r"(a), "=r"(b)
       : "r"(w));
 }
+// 16 codes as fp16 values to two places of a swizzled row (zeros if they are not there).
+__device__ __forceinline__ void widen_piece(const unsigned char* from, unsigned char* row, uint32_t at, bool there) {
+  uint4 w = *reinterpret_cast<const uint4*>(from);
+  if (!there) w = make_uint4(0u, 0u, 0u, 0u);
+  uint4 lo, hi;
+  widen4(w.x, lo.x, lo.y);
+  widen4(w.y, lo.z, lo.w);
+  widen4(w.z, hi.x, hi.y);
+  widen4(w.w, hi.z, hi.w);
+  *reinterpret_cast<uint4*>(row + at) = lo;
+  *reinterpret_cast<uint4*>(row + (at ^ 16)) = hi;
+}
 __device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -361,7 +379,10 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
   if (threadIdx.x == 0) {
     tc::prefetch_tmap(&tmK);
     tc::prefetch_tmap(&tmV);
-    for (int b = 0; b < kBars8; ++b) mbar_init(&bars[b], (C::kWiden && b >= E_V && b < QFULL8) || b == QFULL8 || (b >= PFULL8 && b < PVDONE) ? 4 * C::kSG : 1);
+    for (int b = 0; b < kBars8; ++b) {
+      const bool soft = b == QFULL8 || (b >= PFULL8 && b < PVDONE), v_read = b >= E_V && b < QFULL8;
+      mbar_init(&bars[b], soft || (v_read && C::kOwn) ? 4 * C::kSG : b >= WFULL || (v_read && C::kWideWarps) ? 4 : 1);
+    }
     *abort_flag = 0;
     fence_barrier_init();
   }
@@ -499,7 +520,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       for (int t = s.t0; t < s.t1; ++t, ++i) {
         const int buf = i % kBuf;
         // O of the segment before is read before the first weights of this one are written
-        ok = (C::kWiden || warp_wait(&bars[F_V + st], phase, abort_flag)) &&
+        ok = (C::kOwn || warp_wait(C::kWiden ? &bars[WFULL + buf] : &bars[F_V + st], C::kWiden ? i / kBuf & 1 : phase,
+                                   abort_flag)) &&
              warp_wait(&bars[PFULL8 + buf], i / kBuf & 1, abort_flag);
         if (!ok) break;
         tc::fence_after_sync();
@@ -535,6 +557,41 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
     if (elect_one()) tc::mma_commit(&bars[MDONE8 + 1]);
     __syncwarp();
     mbar_drain(&bars[MDONE8 + 1], 0);
+  } else if (C::kWideWarps && warp >= C::kWideW) {
+    // ------------------------------------------------- values as fp16, exactly
+    // Thread = key; zeros past the end (what lies there may be NaN, and zero times NaN is no zero).
+    const int key = (warp - C::kWideW) * 32 + lane;
+    const uint32_t x128 = (key & 7) << 4, xD = D == 128 ? x128 : ((key >> 1) & 3) << 4;
+    int st = 0, i = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (; s.any() && ok; s.next(bt, p.Hkv)) {
+      const int plen = bt.plen[s.b];
+      for (int t = s.t0; t < s.t1; ++t, ++i) {
+        const int buf = i % kBuf;
+        if (i >= kBuf) ok = warp_wait(&bars[PVDONE + buf], (i - kBuf) / kBuf & 1, abort_flag);
+        if (!ok) break;
+        if (!(p.tree && t == 0)) {  // the tree's are the softmax warps' to write
+          ok = warp_wait(&bars[F_V + st], phase, abort_flag);
+          if (!ok) break;
+          const unsigned char* from = base + off_V + st * C::kTile + key * D;
+          unsigned char* to = base + C::off_W + buf * C::kWide + key * 128;
+          const bool there = (t - p.tree) * kTK + key < plen;
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+            widen_piece(from + ((j * 16) ^ xD), to + (j / 4) * kTK * 128, (j % 4 * 32) ^ x128, there);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[E_V + st]);
+          if (++st == ns) {
+            st = 0;
+            phase ^= 1;
+          }
+        }
+        tc::fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[WFULL + buf]);
+      }
+    }
   } else {
     // ------------------------------------------------------------- softmax
     const int sid = threadIdx.x, tid = sid & 127, group = warp >> 2;
@@ -542,14 +599,11 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
     const int r_own = group * RT, quarter = warp & 3, gbar = 2 + group;
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     const uint32_t tO = lane_addr + C::kTmemO + r_own;
-    // Where this thread's pieces of its key's row lie: 16 codes at a time of V, widened to 32 bytes of W.
-    constexpr int kAll = D / 16, kPieces = C::kWiden ? (kAll + C::kSG - 1) / C::kSG : 0;
-    const uint32_t x128 = (tid & 7) << 4, xD = D == 128 ? x128 : ((tid >> 1) & 3) << 4;
-    const uint32_t v_from = tid * D, v_mix = (group * 16) ^ xD, w_to = tid * 128, w_mix = (group * 32) ^ x128;
+    const uint32_t v_mix = (group * 16) ^ ((tid & 7) << 4), w_mix = (group * 32) ^ ((tid & 7) << 4);
     const uint32_t p_row = tid * C::kPitch,
-                   p_mix = C::kPitch == 128 ? x128 : (C::kPitch == 64 ? ((tid >> 1) & 3) << 4 : ((tid >> 2) & 1) << 4);
+                   p_mix = C::kPitch == 128 ? (tid & 7) << 4 : (C::kPitch == 64 ? ((tid >> 1) & 3) << 4 : ((tid >> 2) & 1) << 4);
     bool dead = false;
-    int st = 0, vst = 0, i = 0;  // stages of K and V, tiles so far
+    int st = 0, vst = 0, i = 0;  // stages of K (and V, where values are not widened) and V, tiles so far
     int sees_b = -1;             // the sequence that sm.sees is of
     uint32_t ring = 0, v_ring = 0;
     // P.V of tile j of this CTA is done
@@ -729,28 +783,13 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 
         dead |= !warp_wait(&bars[SFULL8 + buf], i / C::kBuf & 1, abort_flag);
         tc::fence_after_sync();
-        if (C::kWiden && !is_tree) {
-          // ---- the values as fp16, exactly: this thread's part of its key's row, zeros past the end (what lies there
-          // may be NaN, and zero times NaN is no zero)
+        if (C::kOwn && !is_tree) {  // this group's pieces of the key's values
           dead |= !warp_wait(&bars[F_V + vst], v_ring, abort_flag);
-          const unsigned char* from = base + off_V + vst * C::kTile + v_from;
-          unsigned char* to = base + C::off_W + buf * C::kWide + w_to;
+          const unsigned char* from = base + off_V + vst * C::kTile + tid * D;
+          unsigned char* to = base + C::off_W + buf * C::kWide + tid * 128;
 #pragma unroll
-          for (int j = 0; j < kPieces; ++j) {
-            const int piece = j * C::kSG + group;
-            if (kAll % C::kSG != 0 && piece >= kAll) break;
-            // four groups: a group's place among four pieces is its own, and the rest is known here
-            uint4 w = *reinterpret_cast<const uint4*>(from + (C::kSG == 4 ? v_mix ^ (j * 64) : (piece * 16) ^ xD));
-            if (opaque(key0 + kTK > plen) && key0 + tid >= plen) w = make_uint4(0u, 0u, 0u, 0u);
-            uint4 lo, hi;
-            widen4(w.x, lo.x, lo.y);
-            widen4(w.y, lo.z, lo.w);
-            widen4(w.z, hi.x, hi.y);
-            widen4(w.w, hi.z, hi.w);
-            const uint32_t at = C::kSG == 4 ? j * kTK * 128 + w_mix : (piece / 4) * kTK * 128 + ((piece % 4 * 32) ^ x128);
-            *reinterpret_cast<uint4*>(to + at) = lo;
-            *reinterpret_cast<uint4*>(to + (at ^ 16)) = hi;
-          }
+          for (int j = 0; j < C::kOwn; ++j)  // four groups, 128 dims: of 4 pieces in a half row, group's is its own
+            widen_piece(from + (v_mix ^ (j * 64)), to + j * kTK * 128, w_mix, key0 + tid < plen);
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars[E_V + vst]);
           if (++vst == ns) {
@@ -758,7 +797,6 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             v_ring ^= 1;
           }
         }
-
         // ---- u = S a + e, less m (none yet in a segment's first tile)
         float u[RT];
         const uint32_t tS = lane_addr + buf * C::kTmemS + r_own;
