@@ -10,7 +10,7 @@
 //
 // 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with the slab's
 // largest query scaled to at most 448, q = hi + lo exactly down to the codes' least step (2^-9, or 2^-13 at 8 rows,
-// where lo is held 16 times itself).  Weights, up to 32 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
+// where lo is held 16 times itself).  Weights, up to 16 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
 // of the row's largest, which is at least 2^8.  More rows: values are widened to fp16 in shared memory, weights rounded
 // to fp16 (2^-12 of themselves).  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16
 // with bf16 queries and weights; its values are scaled to a block's range by a power of two of their own, so that the
@@ -27,7 +27,7 @@
 // Roles: groups of four softmax warps, two copy warps (TMA: K, V), two MMA warps (S, P.V); a persistent grid and the
 // cost-balanced split of the key sequence that the other kernels use.  A group takes 8 or 16 of the query rows,
 // thread = key: sixteen softmax warps fill an SM at 64 rows (one group of 64 rows spilled: 660 us for the 218 below).
-// Up to 32 rows two CTAs share an SM, above one has it.  S and P have two buffers each (26 nodes on 8 x 40 heads, 512 -
+// Up to 16 rows two CTAs share an SM, above one has it.  S and P have two buffers each (26 nodes on 8 x 40 heads, 512 -
 // 4096 keys: 69.5 us with one, 66 with two).  A tree is tile 0 of its slab: the softmax warps write its operands while
 // the first copies are on their way.
 //
@@ -70,10 +70,11 @@ constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, PF
 
 template <int D, int NP>
 struct Cfg {
-  // Up to 32 rows: weights as two codes each, and two CTAs an SM, for which widened values leave no shared memory.  More:
-  // values widened to fp16, work that the rows share (16384 keys, two codes / widened, us: 44 nodes on 4 x 52 heads 182 /
-  // 177, 33 nodes of 4 query heads to each of 4 x 8 cached 96.5 / 90.5; 40 nodes on 8 x 40 heads of 512 - 4096 76 / 65).
-  static constexpr bool kWiden = NP > 32;
+  // Up to 16 rows: weights as two codes each, and two CTAs an SM, for which widened values leave no shared memory.  More:
+  // values widened to fp16, work that the rows share, by warps that work beside the softmax (two codes / widened, us: 26
+  // nodes on 4 x 52 heads of 16384 keys 145 / 137, on 8 x 40 heads of 512 - 4096 59 / 53, of 1024 35.4 / 34.3, of 128 18.3 /
+  // 20.6; 32 nodes on 32 heads of 8192 25.9 / 21.8; 44 nodes on 4 x 52 heads of 16384 182 / 164).
+  static constexpr bool kWiden = NP > 16;
   static constexpr float kMost = kWiden ? 15.5f : 8.75f;              // log2 of the largest weight: 2^16, 448 are too large
   static constexpr float kLift = kWiden ? 6.f : 8.f;                  // log2 of the weight of a new maximum
   static constexpr int kRT = NP < 16 ? NP : 16;                    // rows of a softmax group
@@ -89,7 +90,7 @@ struct Cfg {
   static constexpr bool kWideWarps = kWiden && (NP < 64 || D == 64);
   static constexpr int kOwn = kWiden && !kWideWarps ? D / 16 / kSG : 0;  // else: pieces of 16 codes of a softmax group
   static constexpr int kThreads = kSoft + 128 + (kWideWarps ? 128 : 0);
-  static constexpr int kCtas = NP <= 32 ? 2 : 1;                      // of an SM
+  static constexpr int kCtas = kWiden ? 1 : 2;                        // of an SM
   static constexpr int kBuf = 2;                                      // S and P buffers
   static constexpr int kNO = kWiden ? NP : 2 * NP;                      // columns of O (few rows: hi | lo)
   // S adds hi and lo up itself, as products along 2 D; 8 columns are less than an MMA has, so there they lie side by side.
