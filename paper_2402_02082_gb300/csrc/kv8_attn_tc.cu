@@ -765,23 +765,42 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         soft_sync<128>(gbar);
       }
       const float a_q = p.scale_log2 * kv8_pow2(q_exp);
-      int nth = 0;  // of the tiles whose scales the lanes hold
+      int nth = 0;  // of the blocks whose scales the lanes hold
+      auto scales_of = [&](float& a, float& ef, float& inv_v) {  // the next cached tile's
+        const uint32_t mine = __shfl_sync(0xffffffffu, scales, nth + (tid >> 6));
+        inv_v = __shfl_sync(0xffffffffu, inv, nth + (tid >> 6));
+        a = a_q * __uint_as_float(mine << 16);
+        ef = __uint_as_float(mine & 0xffff0000u);
+        nth += 2;
+      };
+      auto first_scales = [&](float& a, float& ef, float& inv_v) {  // the segment's first tile's
+        if (tree_here) {
+          const int e = effective_exp(vt_exp, vt_exp);
+          a = p.scale_log2;
+          ef = (float)e;
+          inv_v = kv8_pow2(-e);
+        } else {
+          scales_of(a, ef, inv_v);
+        }
+      };
+      // Where one CTA has an SM, a tile's scales are made ready during the tile before it (44 nodes on 4 x 52 heads of 16384 keys: 164 -> 161 us);
+      // two have no registers for that (12 nodes on 8 x 40 heads of 1024 keys: 28.2 -> 30.5).
+      float a_next, ef_next, inv_next;
+      if (C::kWiden) first_scales(a_next, ef_next, inv_next);
       for (int t = s.t0; t < s.t1; ++t, ++i) {
         const bool is_tree = p.tree && t == 0, first = t == s.t0;
         const int key0 = (t - p.tree) * kTK, buf = i % kBuf;
-        float a = p.scale_log2, ef = (float)effective_exp(vt_exp, vt_exp), inv_v = kv8_pow2(-effective_exp(vt_exp, vt_exp));
-        if (!is_tree) {
-          if (nth == 32) {
-            set_scales(fetch(key0 / kKv8Block));
-            nth = 0;
-          }
-          const uint32_t mine = __shfl_sync(0xffffffffu, scales, nth + (tid >> 6));
-          inv_v = __shfl_sync(0xffffffffu, inv, nth + (tid >> 6));
-          a = a_q * __uint_as_float(mine << 16);
-          ef = __uint_as_float(mine & 0xffff0000u);
-          nth += 2;
+        if (opaque(nth == 32)) {  // the next 16 tiles' (past a slab's last block: that one's, for nothing)
+          set_scales(fetch((t + (C::kWiden ? 1 : 0) - p.tree) * (kTK / kKv8Block)));
+          nth = 0;
         }
-
+        float a, ef, inv_v;
+        if (C::kWiden)
+          a = a_next, ef = ef_next, inv_v = inv_next;
+        else if (first)
+          first_scales(a, ef, inv_v);
+        else
+          scales_of(a, ef, inv_v);
         dead |= !warp_wait(&bars[SFULL8 + buf], i / C::kBuf & 1, abort_flag);
         tc::fence_after_sync();
         if (C::kOwn && !is_tree) {  // this group's pieces of the key's values
@@ -838,6 +857,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 #pragma unroll
           for (int k = 0; k < RT; ++k) u[k] = (vis >> k) & 1u ? u[k] : -CUDART_INF_F;
         }
+        if (C::kWiden) scales_of(a_next, ef_next, inv_next);
         uint32_t rise = (1u << RT / 8) - 1u;  // by chunks of 8 rows
         if (!first) {
           rise = 0;
