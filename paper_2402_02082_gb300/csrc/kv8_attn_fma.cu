@@ -9,9 +9,11 @@
 // memory, the same address in every lane), lane = slice of the head dimension for the values.
 // Running maximum, sum and output are kept per warp and joined at the end.
 //
-// What bounds it: fp32 queries are for checks and comparisons at small sizes, where a call is a chain of latencies.
-// 5 nodes on 4 heads of 64 dims, 128 keys: 6.4 us.  Tiles of 32 keys over the CTA's warps make that chain one tile long
-// there; nothing splits a slab's keys over CTAs, so a long cache in fp32 leaves most of the GPU idle.
+// What bounds it: fp32 queries are for checks and comparisons at small sizes, where a call is a chain of latencies:
+// a tile after the other in each warp.  Sixteen warps with two rows keep it short and still share a tile's keys and values
+// (8 warps x 4 rows / 16 x 2 / 16 x 1, us: 5 nodes on 4 heads of 64 dims, 128 keys 6.4 / 6.5 / 6.1; 16 nodes on 2 x 2
+// cached heads of 1024 42 / 22 / 23; 32 nodes on 2 x 32 heads of 2048 307 / 251 / 816).  Nothing splits a slab's keys over
+// CTAs, so few heads leave most of the GPU idle.
 #include <math_constants.h>
 
 #include "attn_common.cuh"
@@ -22,9 +24,9 @@
 namespace glide {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
-constexpr int kRT = 4;  // query rows of a CTA
+constexpr int kRT = 2;  // query rows of a CTA
 
 template <int D>
 __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArgs a) {
