@@ -19,23 +19,26 @@
 // Orientation.  Keys are the 128 rows of the MMA and the queries its columns:
 //   S^T = K8 Q^T    : M = 128 keys, N = NP, K = D twice (hi, then lo, into the same columns; at 8 rows, less than an MMA's
 //                     columns, they lie side by side), both operands K-major
-//   O^T += V8^T P^T : M = D, N = 2 x NP (hi | lo; NP where values are widened), K = keys, both operands M/N-major
+//   O^T += V^T P^T  : M = D, N = NP (2 x NP, hi | lo, where weights are codes), K = keys, both operands M/N-major
 // so the tensor work goes with the query rows (NP = 8 .. 64), not with a padded 128, K and V tiles are read from shared
 // memory once, and thread = key in the softmax.  A row's maximum then lies across the threads; it is looked for only
-// when a weight would pass the largest there is (one vote per tile), which after a slab's first tile is rare.
+// when a weight would pass the largest there is (one vote per tile), which after a slab's first tiles is rare.
 //
-// Roles: groups of four softmax warps, two copy warps (TMA: K, V), two MMA warps (S, P.V); a persistent grid and the
-// cost-balanced split of the key sequence that the other kernels use.  A group takes 8 or 16 of the query rows,
-// thread = key: sixteen softmax warps fill an SM at 64 rows (one group of 64 rows spilled: 660 us for the 218 below).
-// Up to 16 rows two CTAs share an SM, above one has it.  S and P have two buffers each (26 nodes on 8 x 40 heads, 512 -
-// 4096 keys: 69.5 us with one, 66 with two).  A tree is tile 0 of its slab: the softmax warps write its operands while
-// the first copies are on their way.
+// Roles: groups of four softmax warps, two copy warps (TMA: K, V), two MMA warps (S, P.V), four warps that widen values
+// (17 - 48 rows, and 64 of 64 dims); a persistent grid and the cost-balanced split of the key sequence that the other
+// kernels use.  A group takes 8 or 16 of the query rows, thread = key: sixteen softmax warps fill an SM at 64 rows (one
+// group of 64 rows spilled: 660 us for the 198 below).  Up to 16 rows two CTAs share an SM, above one has it.  S and P
+// have two buffers each.  A buffer's P.V is waited for by the S products' warp alone, whose scores then say to all softmax
+// warps that S, P and W are free (each warp waiting for itself: 208 us for 201).  A tree is tile 0 of its slab: the softmax
+// warps write its operands while the first copies are on their way.
 //
-// What bounds it, and what it takes: 64 nodes on 4 x 52 heads of 16384 keys 218 us, 4.0 TB/s of the cache, where the
-// bytes alone take 130: a tile of 128 keys costs ~2060 cycles (HBM's rate: 1394), the softmax warps' instructions and the
-// chain S -> weights -> P.V.  26 nodes on 8 x 40 heads of 512 - 4096 keys: 66 us (bytes: 32), where the ~10 k cycles in
-// which a slab's queries become operands and its sums results weigh in.  33 nodes of 4 query heads to a cached one: three row tiles
-// of 44 that read the cache three times, from L2 twice: 103 us on 4 x 8 cached heads of 16384 keys (bytes: 20).
+// What bounds it, and what it takes: 64 nodes on 4 x 52 heads of 16384 keys 198 us, 4.5 TB/s of the cache, where the
+// bytes alone take 130: a tile of 128 keys costs ~1800 cycles (HBM's rate: 1394), spread over a softmax warp's chain of
+// waits, loads, vote, weights and stores; issue slots are a little over half used.  26 nodes there 135 us, 12 nodes 137,
+// one query 128.  26 nodes on 8 x 40 heads of 512 - 4096 keys: 55 us (bytes: 32), where the ~4 k cycles in which a slab's
+// queries become operands and the two tiles in which its maxima settle weigh in (all of a slab's loads in flight at once,
+// ancestors found beside the first product: 23.4 -> 18.2 us for 128 keys).  33 nodes of 4 query heads to a cached one:
+// three row tiles of 44 that read the cache three times, from L2 twice: 84 us on 4 x 8 cached heads of 16384 keys.
 //
 // A slab whose keys lie in several CTAs' shares leaves partials (m, l, O) in the workspace and
 // kv8_merge_kernel joins them.
@@ -61,7 +64,7 @@ constexpr int kMaxStages8 = 6;
 constexpr float kPLo = 28.f;         // p = hi + lo / kPLo: of p <= 430 at most 16 are left to lo, 448 its largest code
 constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
 
-// What a switch of slabs costs a CTA, in tiles.
+// What a switch of slabs costs a CTA, in tiles (from 1 + np / 32 to 3 + np / 16: within 5% of each other, either way).
 __host__ __device__ constexpr int seg_weight8(int np) { return 2 + np / 16; }
 
 // barriers

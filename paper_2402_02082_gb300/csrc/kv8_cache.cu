@@ -7,7 +7,7 @@
 // What bounds it.  A prompt's rows are a stream (2 or 4 bytes in, 1 out): one CTA takes a block of K or
 // of V of one slab, all its loads in flight at once and kept as they came, so a new element is read once
 // between the maximum and the rounding.  Instructions weigh beside the bytes (29.6 us): a maximum over packed
-// magnitudes instead of over each element's finite value 37.4 -> 32.9 us for 4 x 32 heads of 2048 bf16 rows, 6.1 TB/s.  A round's few rows are latency (the lengths, the path, the rows,
+// magnitudes instead of over each element's finite value 37.4 -> 32.7 us for 4 x 32 heads of 2048 bf16 rows, 6.2 TB/s.  A round's few rows are latency (the lengths, the path, the rows,
 // the exponent, one after another): a warp takes a block, so that all layers and heads fit the GPU at
 // once.  Rows from before are read only where their exponent grows.
 #include <cuda_runtime.h>
