@@ -5,8 +5,8 @@
 //   s[r,t] = q[r] . K8[t] * 2^eK * scale * log2(e),   u[r,t] = s[r,t] + eV[t]
 //   m[r]   = running maximum of u less kLift,    p[r,t] = 2^(u - m)
 //   O[r]   = sum_t p[r,t] V8[t],     l[r]   = sum_t p[r,t] 2^-eV[t],    out[r] = O[r] / l[r]
-// Taking the value exponent into the weight's exponent leaves the codes as they are: no key or
-// value is widened or scaled, and the tensor cores multiply the cache's own bytes.
+// Taking the value exponent into the weight's exponent leaves the codes as they are: no key or value is scaled, no key is
+// widened, and values only where many rows share that work (below).
 //
 // 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with the slab's
 // largest query scaled to at most 448, q = hi + lo exactly down to the codes' least step (2^-9, or 2^-13 at 8 rows,
