@@ -123,7 +123,7 @@ struct Small {  // per CTA, after the rings
   unsigned long long sees[64];  // the rows' nodes and their ancestors
   alignas(16) float minus_m[64];  // what turns a row's u into its weight's logarithm
   alignas(16) float minus_up[64];  // by how much m rose last, negative
-  alignas(16) float f[64];      // 2^-up; at the end 1 / l, or l
+  alignas(16) float f[64];      // 2^(-up / 2); at the end 1 / l, or l
   alignas(16) float part[4][64];  // per lane quarter: row maxima, row sums
   alignas(4) uint8_t rise[2][4][4];  // tiles in turn, per group and lane quarter: the chunks whose m rises
   alignas(16) int rel[64];                  // a row's place among a sequence's [node, head] rows from the slab's first head, -1: none
@@ -883,7 +883,9 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           rise = (rise | rise >> 16);
           rise = (rise | rise >> 8) & 0xffu;
         }
-        if (opaque(rise != 0)) {  // a new m for the rows whose weights would pass the largest code
+        // A new m for the rows whose weights would pass the largest code.  l holds 2^-eV and so may be far larger than the
+        // weights that it sums: it takes 2^-up in two steps, neither of which leaves fp32's range before the result does.
+        if (opaque(rise != 0)) {
 #pragma unroll
           for (int c = 0; c < RT; c += 8) {
             if (!((rise >> c / 8) & 1u)) continue;
@@ -903,7 +905,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             const float up = first || top > C::kMost || top != top ? top - C::kLift : 0.f;
             sm.minus_m[r] = first ? -up : sm.minus_m[r] - up;
             sm.minus_up[r] = -up;
-            sm.f[r] = first ? 0.f : fast_exp2(-up);
+            sm.f[r] = first ? 0.f : fast_exp2(-0.5f * up);
           }
           soft_sync<128>(gbar);
 #pragma unroll
@@ -912,7 +914,10 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 #pragma unroll
             for (int k = c; k < c + 8; ++k) {
               u[k] += sm.minus_up[r_own + k];
-              if (k % 2 == 0) l2[k / 2] = f2mul(l2[k / 2], *reinterpret_cast<const uint64_t*>(&sm.f[r_own + k]));
+              if (k % 2 == 0) {
+                const uint64_t f = *reinterpret_cast<const uint64_t*>(&sm.f[r_own + k]);
+                l2[k / 2] = f2mul(f2mul(l2[k / 2], f), f);
+              }
             }
           }
         }
@@ -981,7 +986,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             for (int half = 0; half < (C::kWiden ? 1 : 2); ++half) {
               tmem_ld8(tO + half * NP + c, o);
 #pragma unroll
-              for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * sm.f[r_own + c + k]);
+              for (int k = 0; k < 8; ++k)
+                o[k] = __float_as_uint(__uint_as_float(o[k]) * sm.f[r_own + c + k] * sm.f[r_own + c + k]);
               tmem_st8(tO + half * NP + c, o);
             }
           }

@@ -261,7 +261,11 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
         for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
         top = fmaxf(m[nt][x], top);
         const float ref = (top == -CUDART_INF_F ? 0.f : top) - kLiftF;  // nothing seen yet, or NaN only
-        corr[x] = fast_exp2(m[nt][x] - (ref + kLiftF));
+        // l holds 2^-eV and so may be far larger than the weights that it sums: it takes 2^(m - top) in two steps, neither
+        // of which leaves fp32's range before the result does
+        const float half = fast_exp2(0.5f * (m[nt][x] - (ref + kLiftF)));
+        corr[x] = half * half;
+        l[nt][x] = l[nt][x] == 0.f ? 0.f : l[nt][x] * half * half;
         float sum = 0.f;
 #pragma unroll
         for (int kg = 0; kg < KG; ++kg) {
@@ -269,7 +273,7 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
           u[kg][nt][x + 2] = fast_exp2(u[kg][nt][x + 2] - ref);
           sum += u[kg][nt][x] + u[kg][nt][x + 2];
         }
-        l[nt][x] = (l[nt][x] == 0.f ? 0.f : l[nt][x] * corr[x]) + sum * inv_v;
+        l[nt][x] += sum * inv_v;
         m[nt][x] = top;
       }
 #pragma unroll
