@@ -379,7 +379,9 @@ typedef struct {
 
 /*
  * Quantises new rows as they join the cache, for n_layers layers at once:
- *   m_b = len[b] + 1 (len clamped to [-1, n-1]; len NULL: m_b = n)
+ *   m_b = len[b] + 1 (len clamped to [-1, n-1]; len NULL: m_b = n), but at most
+ *         S_cap - kv_len[b]: rows that the cache has no room for do not join, which
+ *         new_kv_len shows
  *   for k = 0 .. m_b - 1: row kv_len[b] + k of every cached head <-
  *     k_new / v_new[b, path ? path[b,k] : k, h, :]
  *   new_kv_len[b] = kv_len[b] + m_b.
@@ -392,7 +394,7 @@ typedef struct {
  * their codes.
  * desc: B, H, H_kv, D, S_cap; dtype is that of k_new / v_new (scale, flags and
  * max_ctas are ignored).  cache: layer 0 of dense stacks [n_layers][...]; k_new / v_new
- * [n_layers][B, n, H_kv, D].  kv_len [B] (clamped to [0, S_cap - n]), path [B, n] or
+ * [n_layers][B, n, H_kv, D].  kv_len [B] (clamped to [0, S_cap]), path [B, n] or
  * NULL (clamped to [0, n)), len [B] or NULL: int32 on the device.  path and len as
  * tree_accept writes them append the accepted path; a prompt has path NULL.
  * 1 <= n <= S_cap.  new_kv_len [B] int32 and not the kv_len buffer.  No workspace.  More

@@ -79,8 +79,9 @@ def kv8_append(codes: np.ndarray, exps: np.ndarray, new: np.ndarray, kv_len: Seq
     n = new.shape[2]
     out_len = np.zeros(B, dtype=np.int32)
     for b in range(B):
-        start = min(max(int(kv_len[b]), 0), cap - n)
+        start = min(max(int(kv_len[b]), 0), cap)
         m = n if length is None else min(max(int(length[b]), -1), n - 1) + 1
+        m = min(m, cap - start)
         out_len[b] = start + m
         nodes = [min(max(int(path[b][k]), 0), n - 1) if path is not None else k for k in range(m)]
         for layer in range(layers):

@@ -461,8 +461,8 @@ def glide_kv8_append(k_new: torch.Tensor, v_new: torch.Tensor, K: torch.Tensor, 
     """Quantises rows of k_new / v_new [B, n, H_kv, D] into the 8-bit cache K / V [B, H_kv, S_cap, D] (float8_e4m3fn
     codes), K_exp / V_exp [B, H_kv, ceil(S_cap / 64)] (int8) at rows kv_len[b] on; every tensor but the integer
     ones may have a leading layer dimension.  Without `length` all n rows of a sequence join, with it
-    length[b] + 1; with `path` [B, n] row k is node path[b, k] (both as tree_accept writes them).
-    Returns new_kv_len [B]."""
+    length[b] + 1, and in either case as many as the cache has room for; with `path` [B, n] row k is node path[b, k]
+    (both as tree_accept writes them).  Returns new_kv_len [B]."""
     st = (_CALL or _native()).kv8_append(k_new, v_new, K, V, K_exp, V_exp, kv_len, new_kv_len, path, length, stream)
     if st == GLIDE_OK:
         return new_kv_len

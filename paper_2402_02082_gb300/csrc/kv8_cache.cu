@@ -127,13 +127,14 @@ __device__ __forceinline__ uint2 shrink8(const uint2& w, float by) {
   return encode8(f, by);
 }
 
-struct Rows {  // of a sequence: its length so far, and how many join
+struct Rows {  // of a sequence: its length so far, and how many join (as many as the slab has room for)
   int L, m;
 };
 __device__ __forceinline__ Rows rows_of(const AppendParams& p, int b) {
   int L = p.kv_len[b], m = p.len ? p.len[b] : p.n - 1;
-  L = L < 0 ? 0 : (L > p.S_cap - p.n ? p.S_cap - p.n : L);
+  L = L < 0 ? 0 : (L > p.S_cap ? p.S_cap : L);
   m = (m < -1 ? -1 : (m > p.n - 1 ? p.n - 1 : m)) + 1;
+  m = m > p.S_cap - L ? p.S_cap - L : m;
   return {L, m};
 }
 // Where element 0 of new row k of (layer, b, h) lies in k_new / v_new.
