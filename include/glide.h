@@ -361,8 +361,8 @@ glide_status glide_noalloc_scratch(void** device_ptr);
  * Exponents are powers of two so that a code's value is exact in 16 bits, and so
  * that a block whose exponent grows keeps its codes' mantissas: an 8-bit float
  * has the same relative precision at any scale, and a finer one would buy nothing.
- * Exponents lie in [-117, 119] (every value is a normal fp32 and bf16 number); the
- * attention and read calls clamp others into that range.
+ * Exponents lie in [-117, 119] (every value is a normal fp32 and bf16 number); every
+ * call takes others as the nearest in that range.
  * Unlike the 16-bit calls, the tree's own keys and values are NOT cache rows:
  * tree_verify's form below takes them as they leave the target's projections, and
  * glide_kv8_append writes the accepted ones.  A rejected token so never touches a

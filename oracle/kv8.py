@@ -93,7 +93,7 @@ def kv8_append(codes: np.ndarray, exps: np.ndarray, new: np.ndarray, kv_len: Seq
                     x = new[layer, b, [nodes[t - start] for t in range(lo, hi)], h]
                     e = exponent(x)
                     if blk * BLOCK < start:
-                        old = int(exps[layer, b, h, blk])
+                        old = min(max(int(exps[layer, b, h, blk]), EXP_MIN), EXP_MAX)
                         if old > e:
                             e = old
                         elif e > old:

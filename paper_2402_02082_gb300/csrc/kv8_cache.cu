@@ -113,10 +113,10 @@ __device__ __forceinline__ uint2 encode8(const Eight<T>& x, float s) {
   return encode8(f, s);
 }
 
-// A block's exponent from its new rows' largest magnitude and, if it holds rows, its old exponent.
+// A block's exponent from its new rows' largest magnitude and, if it holds rows, its old exponent (within the range).
 __device__ __forceinline__ int joined_exponent(uint32_t most, bool holds, int old) {
   const int e = block_exponent(most);
-  return holds && old >= e ? kv8_clamp_exp(old) : e;
+  return holds && old >= e ? old : e;
 }
 // What a grown exponent makes of the codes that a block holds.
 __device__ __forceinline__ float shrink_by(int old, int e) { return kv8_pow2(old - e < -126 ? -126 : old - e); }
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kAppendThreads, sizeof(T) == 2 ? 8 : 5) kv8_ap
     x[i].none();
     if (k >= 0 && k < r.m) x[i].load(fresh + row_at(p, layer, b, h, k, D) + d);
   }
-  const int old = holds ? (int)*exp : 0;
+  const int old = holds ? kv8_clamp_exp(*exp) : 0;
   auto joined = [&](uint32_t mine, int nth) {  // over the CTA
     mine = __reduce_max_sync(0xffffffffu, mine);
     if ((threadIdx.x & 31) == 0) top[nth][threadIdx.x >> 5] = mine;
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) kv8_append_few_kernel(const AppendPa
   int8_t* exp = (kv ? p.Ve : p.Ke) + (size_t)slab * kv8_blocks(p.S_cap) + block;
   const T* fresh = static_cast<const T*>(kv ? p.v_new : p.k_new);
   const bool holds = row0 < r.L;
-  const int old = holds ? (int)*exp : 0;
+  const int old = holds ? kv8_clamp_exp(*exp) : 0;
   // rows first .. last - 1 of the block are new
   const int first = holds ? r.L - row0 : 0, last = min(kKv8Block, r.L + r.m - row0);
   const int rl = lane / kPerRow, d = (lane % kPerRow) * 8;
