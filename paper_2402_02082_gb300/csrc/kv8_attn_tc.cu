@@ -13,8 +13,8 @@
 // where lo is held 16 times itself).  Weights, up to 16 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
 // of the row's largest, which is at least 2^8.  More rows: values are widened to fp16 in shared memory, weights rounded
 // to fp16 (2^-12 of themselves).  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16
-// with bf16 queries and weights; its values are scaled to a block's range by a power of two of their own, so that the
-// weights of tree and cache lie in one range.
+// with bf16 queries and weights; a node's values are scaled by a power of two of its own, which its weight's exponent takes
+// as a block's, so that what a row does not see has no say in how finely the rest is held.
 //
 // Orientation.  Keys are the 128 rows of the MMA and the queries its columns:
 //   S^T = K8 Q^T    : M = 128 keys, N = NP, K = D twice (hi, then lo, into the same columns; at 8 rows, less than an MMA's
@@ -63,6 +63,7 @@ constexpr int kTreeKeys = 64;     // rows of the tree tile
 constexpr int kMaxStages8 = 6;
 constexpr float kPLo = 28.f;         // p = hi + lo / kPLo: of p <= 430 at most 16 are left to lo, 448 its largest code
 constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
+constexpr int kTreeExpMost = 20;                  // see tree_exp
 
 // What a switch of slabs costs a CTA, in tiles (from 1 + np / 32 to 3 + np / 16: within 5% of each other, either way).
 __host__ __device__ constexpr int seg_weight8(int np) { return 2 + np / 16; }
@@ -127,7 +128,8 @@ struct Small {  // per CTA, after the rings
   alignas(16) float part[4][64];  // per lane quarter: row maxima, row sums
   alignas(4) uint8_t rise[2][4][4];  // tiles in turn, per group and lane quarter: the chunks whose m rises
   alignas(16) int rel[64];                  // a row's place among a sequence's [node, head] rows from the slab's first head, -1: none
-  uint32_t top[16][2];           // per softmax warp: largest query, largest value of the tree
+  uint32_t top[16];              // per softmax warp: the largest query
+  alignas(16) float v_exp[kTreeKeys];  // the tree's nodes' value exponents
   uint32_t tmem;
   int abort_flag;
   int odd_values;               // the tree has values that are not finite
@@ -358,6 +360,9 @@ __device__ __forceinline__ int top_exponent(uint32_t bits) {
 // ordinary block its weights would leave fp32's range, and the sum l with them.  So an exponent counts as at least
 // 110 below the largest seen, and as -90: its values then show up 2^-102 of that block's largest at most.
 __device__ __forceinline__ int effective_exp(int e, int ref) { return max(max(e, ref - kVExpSpan), kVExpLeast); }
+// A tree node's value exponent, from the bits of its largest value: its own, as most rows do not see the node.  Its values
+// are multiplied as bf16, whose range lets the exponent stay within 110 of any other's.
+__device__ __forceinline__ int tree_exp(uint32_t bits) { return min(max(top_exponent(bits), kVExpLeast), kTreeExpMost); }
 
 template <int D, int NP>
 __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
@@ -650,13 +655,13 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 
       // ---- the segment's queries, and the tree's own keys and values, as operands
       const int first_tile = i;
-      int q_exp, vt_exp = 0;
+      int q_exp;
       {
         constexpr int kPerRow = D / 8, kQ = (NP * kPerRow + kSoft - 1) / kSoft,
                       kT = (kTreeKeys * kPerRow + kSoft - 1) / kSoft;
         const uint4 none = make_uint4(0u, 0u, 0u, 0u);
         uint4 q[kQ], kt[kT], v[kT];
-        uint32_t most = 0, most_v = 0;
+        uint32_t most = 0;
         const size_t q0 = (size_t)s.b * p.n * p.H + (size_t)s.h * p.group;
 #pragma unroll
         for (int i = 0; i < kQ; ++i) {
@@ -685,15 +690,31 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           dead |= !warp_wait(&bars[E_K + st], ring ^ 1, abort_flag);
           if (!C::kWiden) dead |= !warp_wait(&bars[E_V + st], ring ^ 1, abort_flag);
           unsigned char* kd = base + C::off_K + st * C::kTile;
+          unsigned char* vd =  // W's buffer is free, as P's is
+              base + (C::kWiden ? C::off_W + first_tile % kBuf * C::kWide : off_V + st * C::kTile);
 #pragma unroll
           for (int i = 0; i < kT; ++i) {
             const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
             if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;
+            *reinterpret_cast<uint4*>(kd + in_bf16(r, d, kTreeKeys)) = kt[i];
+          }
+#pragma unroll
+          for (int i = 0; i < kT; ++i) {
+            const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
+            if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;  // whole warps
             // An unseen value that is not finite must not meet a weight of zero: it is left out here, and put
             // back at the end where it is seen.
             odd |= drop_odd(v[i]);
-            most_v = max(most_v, top8(v[i]));
-            *reinterpret_cast<uint4*>(kd + in_bf16(r, d, kTreeKeys)) = kt[i];
+            uint32_t most_v = top8(v[i]);  // of the row: kPerRow neighbouring lanes have it
+#pragma unroll
+            for (int off = 1; off < kPerRow; off <<= 1) most_v = max(most_v, __shfl_xor_sync(0xffffffffu, most_v, off));
+            const int e = tree_exp(most_v);
+            const float vs = kv8_pow2(-e);
+            const uint4 w = v[i];
+            *reinterpret_cast<uint4*>(vd + in_bf16(r, d, kTreeKeys)) =
+                make_uint4(pack_bf16x2(bf16lo(w.x) * vs, bf16hi(w.x) * vs), pack_bf16x2(bf16lo(w.y) * vs, bf16hi(w.y) * vs),
+                           pack_bf16x2(bf16lo(w.z) * vs, bf16hi(w.z) * vs), pack_bf16x2(bf16lo(w.w) * vs, bf16hi(w.w) * vs));
+            if (d == 0) sm.v_exp[r] = (float)e;
           }
           unsigned char* qd = base + C::off_P + first_tile % C::kBuf * C::kPBytes;  // P of this tile comes later
 #pragma unroll
@@ -705,33 +726,11 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             *reinterpret_cast<uint4*>(qd + in_bf16(NP + sid / kPerRow, sid % kPerRow * 8, C::kNS)) = none;
         }
         most = __reduce_max_sync(0xffffffffu, most);
-        most_v = __reduce_max_sync(0xffffffffu, most_v);
-        if (lane == 0) {
-          sm.top[warp][0] = most;
-          sm.top[warp][1] = most_v;
-        }
+        if (lane == 0) sm.top[warp] = most;
         const bool odd_any = soft_any<kSoft>(1, odd);  // a barrier too
         if (sid == 0) sm.odd_values = odd_any;
 #pragma unroll
-        for (int w = 0; w < 4 * C::kSG; ++w) {
-          most = max(most, sm.top[w][0]);
-          most_v = max(most_v, sm.top[w][1]);
-        }
-        if (tree_here) {
-          vt_exp = top_exponent(most_v);
-          const float vs = kv8_pow2(-vt_exp);
-          unsigned char* vd =  // W's buffer is free, as P's is
-              base + (C::kWiden ? C::off_W + first_tile % kBuf * C::kWide : off_V + st * C::kTile);
-#pragma unroll
-          for (int i = 0; i < kT; ++i) {
-            const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
-            if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;
-            const uint4 w = v[i];
-            *reinterpret_cast<uint4*>(vd + in_bf16(r, d, kTreeKeys)) =
-                make_uint4(pack_bf16x2(bf16lo(w.x) * vs, bf16hi(w.x) * vs), pack_bf16x2(bf16lo(w.y) * vs, bf16hi(w.y) * vs),
-                           pack_bf16x2(bf16lo(w.z) * vs, bf16hi(w.z) * vs), pack_bf16x2(bf16lo(w.w) * vs, bf16hi(w.w) * vs));
-          }
-        }
+        for (int w = 0; w < 4 * C::kSG; ++w) most = max(most, sm.top[w]);
         q_exp = top_exponent(most);
         const float qs = kv8_pow2(-q_exp);
 #pragma unroll
@@ -756,7 +755,6 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       uint64_t l2[RT / 2];  // pairs of rows
 #pragma unroll
       for (int k = 0; k < RT / 2; ++k) l2[k] = 0ull;
-      if (tree_here) ref = vt_exp;
       if (used > 0) set_scales(raw);
       if (walk) {  // while the first product runs
         if (quarter == 0) {
@@ -778,10 +776,9 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       };
       auto first_scales = [&](float& a, float& ef, float& inv_v) {  // the segment's first tile's
         if (tree_here) {
-          const int e = effective_exp(vt_exp, vt_exp);
           a = p.scale_log2;
-          ef = (float)e;
-          inv_v = kv8_pow2(-e);
+          ef = sm.v_exp[tid % kTreeKeys];  // what lies past the nodes is masked
+          inv_v = kv8_pow2(-(int)ef);
         } else {
           scales_of(a, ef, inv_v);
         }

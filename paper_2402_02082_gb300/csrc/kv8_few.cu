@@ -246,9 +246,12 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
       for (int k = 0; k < 4; ++k) o[j][nt][k] = 0.f;
   }
   // A new maximum over `u` (16 KG keys: [group][row tile][key g: rows 2t, 2t + 1; key g + 8: the same]), then the
-  // weights, transposed for the second product.
-  auto weigh = [&](auto& u, auto& pt, float inv_v) {
+  // weights, transposed for the second product.  The keys of a cached tile share the exponent e[0]; those of the tree's one
+  // group have their own, e[0] of key g and e[1] of key g + 8, so far apart that 2^-e must not meet a weight that has
+  // become zero: their terms of l are exponentials of their own.
+  auto weigh = [&](auto& u, auto& pt, const int (&e)[2]) {
     constexpr int KG = sizeof(u) / sizeof(u[0]);
+    const float inv_v = kv8_pow2(-e[0]);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float corr[2];
@@ -266,6 +269,8 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
         const float half = fast_exp2(0.5f * (m[nt][x] - (ref + kLiftF)));
         corr[x] = half * half;
         l[nt][x] = l[nt][x] == 0.f ? 0.f : l[nt][x] * half * half;
+        if constexpr (KG == 1)
+          l[nt][x] += fast_exp2(u[0][nt][x] - ref - (float)e[0]) + fast_exp2(u[0][nt][x + 2] - ref - (float)e[1]);
         float sum = 0.f;
 #pragma unroll
         for (int kg = 0; kg < KG; ++kg) {
@@ -273,7 +278,7 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
           u[kg][nt][x + 2] = fast_exp2(u[kg][nt][x + 2] - ref);
           sum += u[kg][nt][x] + u[kg][nt][x + 2];
         }
-        l[nt][x] += sum * inv_v;
+        if constexpr (KG > 1) l[nt][x] += sum * inv_v;
         m[nt][x] = top;
       }
 #pragma unroll
@@ -291,7 +296,7 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
     }
   };
 
-  int ref_v = -128;
+  int ref_v = -128;  // the largest value exponent of the cached blocks so far, which every row sees
   // ---- the tree's own keys and values: at most 16
   if (tree_warp) {
     const int n = p.n;
@@ -316,32 +321,40 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
       }
     auto kw = [&](int i, int w) { return kr[2 * i + w / kWK][w % kWK]; };
     auto vw = [&](int i, int w) -> uint32_t& { return vr[2 * i + w / kWV][w % kWV]; };
-    uint32_t most = 0;  // keys and values are scaled to fp16 by a power of two each
+    // keys and values are scaled to fp16, each node's by powers of two of its own: a row that does not see a node must not
+    // lose anything to that node's size
+    float sk[2], ks[2];  // keys g, g + 8
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
+      uint32_t most = 0;
 #pragma unroll
       for (int w = 0; w < 2 * kSteps; ++w) most = top_pair(kw(i, w), most);
-    const int e_k = exponent_of(__reduce_max_sync(0xffffffffu, most));
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      const int e = exponent_of(most);
+      sk[i] = kv8_pow2(-e);
+      ks[i] = kv8_pow2(e);
+    }
     float u[1][NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int k = 0; k < 4; ++k) u[0][nt][k] = 0.f;
-    const float sk = kv8_pow2(-e_k);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      const uint32_t a[4] = {scaled_pair(kw(0, 2 * s), sk), scaled_pair(kw(1, 2 * s), sk), scaled_pair(kw(0, 2 * s + 1), sk),
-                             scaled_pair(kw(1, 2 * s + 1), sk)};
+      const uint32_t a[4] = {scaled_pair(kw(0, 2 * s), sk[0]), scaled_pair(kw(1, 2 * s), sk[1]),
+                             scaled_pair(kw(0, 2 * s + 1), sk[0]), scaled_pair(kw(1, 2 * s + 1), sk[1])};
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const uint2 q = qf[(nt * kSteps + s) * 32 + lane];
         mma_f16(u[0][nt], a, q.x, q.y);
       }
     }
-    most = 0;
     bool odd = false;
+    int e_v[4];  // of keys 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      uint32_t most = 0;
 #pragma unroll
       for (int w = 0; w < 2 * kWV; ++w) {
         uint32_t& x = vw(i, w);
@@ -350,28 +363,35 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
         if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu, odd = true;
         most = top_pair(x, most);
       }
-    const int e_v = exponent_of(__reduce_max_sync(0xffffffffu, most));
-    ref_v = e_v;
-    const int e = max(e_v, -90);
-    const float sv = kv8_pow2(-e_v), ks = kv8_pow2(e_k);
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, off));
+      e_v[i] = max(exponent_of(most), -90);
+    }
+    int e[2];  // of keys g, g + 8
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int even = __shfl_sync(0xffffffffu, e_v[2 * i], g >> 1), other = __shfl_sync(0xffffffffu, e_v[2 * i + 1], g >> 1);
+      e[i] = g & 1 ? other : even;
+    }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float x = fmaf(u[0][nt][k] * ks, c[nt][k & 1], (float)e);
+        const float x = fmaf(u[0][nt][k] * ks[k >> 1], c[nt][k & 1], (float)e[k >> 1]);
         u[0][nt][k] = (vis[nt][k & 1] >> (g + 4 * (k & 2))) & 1u ? x : -CUDART_INF_F;
       }
     uint32_t pt[1][NT][2];
-    weigh(u, pt, kv8_pow2(-e));
+    weigh(u, pt, e);
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
-      auto pair = [&](uint32_t x, uint32_t y, uint32_t& lo, uint32_t& hi) {  // dims 2j, 2j + 1 of two keys
-        lo = f16pair(bf16lo(x) * sv, bf16lo(y) * sv);
-        hi = f16pair(bf16hi(x) * sv, bf16hi(y) * sv);
+      auto pair = [&](int i, uint32_t& lo, uint32_t& hi) {  // dims 2j, 2j + 1 of two keys
+        const float sx = kv8_pow2(-e_v[i]), sy = kv8_pow2(-e_v[i + 1]);
+        lo = f16pair(bf16lo(vw(i, j)) * sx, bf16lo(vw(i + 1, j)) * sy);
+        hi = f16pair(bf16hi(vw(i, j)) * sx, bf16hi(vw(i + 1, j)) * sy);
       };
       uint32_t a[4];
-      pair(vw(0, j), vw(1, j), a[0], a[1]);
-      pair(vw(2, j), vw(3, j), a[2], a[3]);
+      pair(0, a[0], a[1]);
+      pair(2, a[2], a[3]);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) mma_f16(o[j][nt], a, pt[0][nt][0], pt[0][nt][1]);
     }
@@ -440,7 +460,7 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
           u[kg][nt][k] = key0 + 16 * kg + g + 4 * (k & 2) < L ? x : -CUDART_INF_F;
         }
     uint32_t pt[2][NT][2];
-    weigh(u, pt, kv8_pow2(-e));
+    weigh(u, pt, {e, e});
 #pragma unroll
     for (int kg = 0; kg < 2; ++kg)
 #pragma unroll
