@@ -8,9 +8,9 @@
 // Taking the value exponent into the weight's exponent leaves the codes as they are: no key or value is scaled, no key is
 // widened, and values only where many rows share that work (below).
 //
-// 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with the slab's
-// largest query scaled to at most 448, q = hi + lo exactly down to the codes' least step (2^-9, or 2^-13 at 8 rows,
-// where lo is held 16 times itself).  Weights, up to 16 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
+// 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with a row's largest
+// element scaled to at most 448, and at least 28, q = hi + lo exactly down to the codes' least step (2^-9, or 2^-13 at 8
+// rows, where lo is held 16 times itself).  Weights, up to 16 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
 // of the row's largest, which is at least 2^8.  More rows: values are widened to fp16 in shared memory, weights rounded
 // to fp16 (2^-12 of themselves).  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16
 // with bf16 queries and weights; a node's values are scaled by a power of two of its own, which its weight's exponent takes
@@ -64,6 +64,7 @@ constexpr int kMaxStages8 = 6;
 constexpr float kPLo = 28.f;         // p = hi + lo / kPLo: of p <= 430 at most 16 are left to lo, 448 its largest code
 constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
 constexpr int kTreeExpMost = 20;                  // see tree_exp
+constexpr int kQExpSpan = 3;                      // rows of queries share a power of two if it is within 2^3 of their own
 
 // What a switch of slabs costs a CTA, in tiles (from 1 + np / 32 to 3 + np / 16: within 5% of each other, either way).
 __host__ __device__ constexpr int seg_weight8(int np) { return 2 + np / 16; }
@@ -95,6 +96,12 @@ struct Cfg {
   static constexpr int kOwn = kWiden && !kWideWarps ? D / 16 / kSG : 0;  // else: pieces of 16 codes of a softmax group
   static constexpr int kThreads = kSoft + 128 + (kWideWarps ? 128 : 0);
   static constexpr int kCtas = kWiden ? 1 : 2;                        // of an SM
+  // Each row's queries are scaled by a power of two of their own: always, or only where one is far smaller than another,
+  // which takes the rows' largest and least element at a slab's start and leaves out a product per score (always / so, us:
+  // 7 nodes on 4 x 40 heads of 322 - 2583 keys 18.0 / 18.9, 12 rows on 6 x 8 heads of 2005 - 16045 30.5 / 32.5, 33 nodes
+  // of 4 query heads on 4 x 8 cached of 16384 83 / 87; 26 nodes on 8 x 40 ragged heads 60 / 57, 64 nodes on 4 x 52 heads
+  // of 16384 207 / 199).
+  static constexpr bool kRowScales = NP <= 16 || NP == 48;
   static constexpr int kBuf = 2;                                      // S and P buffers
   static constexpr int kNO = kWiden ? NP : 2 * NP;                      // columns of O (few rows: hi | lo)
   // S adds hi and lo up itself, as products along 2 D; 8 columns are less than an MMA has, so there they lie side by side.
@@ -125,11 +132,12 @@ struct Small {  // per CTA, after the rings
   alignas(16) float minus_m[64];  // what turns a row's u into its weight's logarithm
   alignas(16) float minus_up[64];  // by how much m rose last, negative
   alignas(16) float f[64];      // 2^(-up / 2); at the end 1 / l, or l
+  alignas(16) float q_unit[64];    // what makes a row's scores log2 units where its queries have a scale of their own
   alignas(16) float part[4][64];  // per lane quarter: row maxima, row sums
   alignas(4) uint8_t rise[2][4][4];  // tiles in turn, per group and lane quarter: the chunks whose m rises
   alignas(16) int rel[64];                  // a row's place among a sequence's [node, head] rows from the slab's first head, -1: none
-  uint32_t top[16];              // per softmax warp: the largest query
-  alignas(16) float v_exp[kTreeKeys];  // the tree's nodes' value exponents
+  uint2 top[16];                 // per softmax warp: the largest query element, the least of its rows' largest
+  int8_t v_exp[kTreeKeys];       // the tree's nodes' value exponents
   uint32_t tmem;
   int abort_flag;
   int odd_values;               // the tree has values that are not finite
@@ -261,6 +269,15 @@ __device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
                : "memory");
 }
 
+// Four floats times four in shared memory.
+__device__ __forceinline__ void scale4(uint32_t* x, const float* f) {
+  const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(f);
+  float y[4];
+  unf2(f2mul(f2(__uint_as_float(x[0]), __uint_as_float(x[1])), w.x), y[0], y[1]);
+  unf2(f2mul(f2(__uint_as_float(x[2]), __uint_as_float(x[3])), w.y), y[2], y[3]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = __float_as_uint(y[k]);
+}
 // The largest of a value over the warp; NaN only if all are.
 __device__ __forceinline__ float warp_top(float x) {
   float r;
@@ -360,9 +377,12 @@ __device__ __forceinline__ int top_exponent(uint32_t bits) {
 // ordinary block its weights would leave fp32's range, and the sum l with them.  So an exponent counts as at least
 // 110 below the largest seen, and as -90: its values then show up 2^-102 of that block's largest at most.
 __device__ __forceinline__ int effective_exp(int e, int ref) { return max(max(e, ref - kVExpSpan), kVExpLeast); }
-// A tree node's value exponent, from the bits of its largest value: its own, as most rows do not see the node.  Its values
-// are multiplied as bf16, whose range lets the exponent stay within 110 of any other's.
-__device__ __forceinline__ int tree_exp(uint32_t bits) { return min(max(top_exponent(bits), kVExpLeast), kTreeExpMost); }
+// A tree node's value exponent, from the bits of its largest value: its own, as most rows do not see the node, but at least
+// the cached blocks' (so that the first of these do not raise m).  Its values are multiplied as bf16, whose range lets the
+// exponent stay within 110 of any other's.
+__device__ __forceinline__ int tree_exp(uint32_t bits, int ref) {
+  return min(max(max(top_exponent(bits), ref), kVExpLeast), kTreeExpMost);
+}
 
 template <int D, int NP>
 __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
@@ -655,13 +675,19 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 
       // ---- the segment's queries, and the tree's own keys and values, as operands
       const int first_tile = i;
-      int q_exp;
+      float a_q = 1.f;    // what makes a score of S and of 2^eK
+      bool apart = true;  // each row's queries are scaled by a power of two of its own
       {
         constexpr int kPerRow = D / 8, kQ = (NP * kPerRow + kSoft - 1) / kSoft,
                       kT = (kTreeKeys * kPerRow + kSoft - 1) / kSoft;
         const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+        auto over_row = [](uint32_t x) {  // the largest of a row's pieces, which kPerRow neighbouring lanes have
+#pragma unroll
+          for (int off = 1; off < kPerRow; off <<= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, off));
+          return x;
+        };
         uint4 q[kQ], kt[kT], v[kT];
-        uint32_t most = 0;
+        uint32_t most = 0, least = ~0u, row_top[kQ];
         const size_t q0 = (size_t)s.b * p.n * p.H + (size_t)s.h * p.group;
 #pragma unroll
         for (int i = 0; i < kQ; ++i) {
@@ -681,8 +707,14 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             }
           }
         }
+        if constexpr (!C::kRowScales) {
 #pragma unroll
-        for (int i = 0; i < kQ; ++i) most = max(most, top8(q[i]));
+          for (int i = 0; i < kQ; ++i) {
+            row_top[i] = over_row(top8(q[i]));
+            most = max(most, row_top[i]);
+            if (row_top[i] != 0) least = min(least, row_top[i]);
+          }
+        }
         // Byte of element d of row r in a bf16 operand of `rows` rows: 64 elements (128 bytes) a row and part.
         auto in_bf16 = [](int r, int d, int rows) { return (d / 64) * rows * 128 + swizzled<128>(r, (d % 64) * 2); };
         bool odd = false;
@@ -690,8 +722,6 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           dead |= !warp_wait(&bars[E_K + st], ring ^ 1, abort_flag);
           if (!C::kWiden) dead |= !warp_wait(&bars[E_V + st], ring ^ 1, abort_flag);
           unsigned char* kd = base + C::off_K + st * C::kTile;
-          unsigned char* vd =  // W's buffer is free, as P's is
-              base + (C::kWiden ? C::off_W + first_tile % kBuf * C::kWide : off_V + st * C::kTile);
 #pragma unroll
           for (int i = 0; i < kT; ++i) {
             const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
@@ -699,23 +729,10 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             *reinterpret_cast<uint4*>(kd + in_bf16(r, d, kTreeKeys)) = kt[i];
           }
 #pragma unroll
-          for (int i = 0; i < kT; ++i) {
-            const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
-            if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;  // whole warps
+          for (int i = 0; i < kT; ++i)
             // An unseen value that is not finite must not meet a weight of zero: it is left out here, and put
             // back at the end where it is seen.
             odd |= drop_odd(v[i]);
-            uint32_t most_v = top8(v[i]);  // of the row: kPerRow neighbouring lanes have it
-#pragma unroll
-            for (int off = 1; off < kPerRow; off <<= 1) most_v = max(most_v, __shfl_xor_sync(0xffffffffu, most_v, off));
-            const int e = tree_exp(most_v);
-            const float vs = kv8_pow2(-e);
-            const uint4 w = v[i];
-            *reinterpret_cast<uint4*>(vd + in_bf16(r, d, kTreeKeys)) =
-                make_uint4(pack_bf16x2(bf16lo(w.x) * vs, bf16hi(w.x) * vs), pack_bf16x2(bf16lo(w.y) * vs, bf16hi(w.y) * vs),
-                           pack_bf16x2(bf16lo(w.z) * vs, bf16hi(w.z) * vs), pack_bf16x2(bf16lo(w.w) * vs, bf16hi(w.w) * vs));
-            if (d == 0) sm.v_exp[r] = (float)e;
-          }
           unsigned char* qd = base + C::off_P + first_tile % C::kBuf * C::kPBytes;  // P of this tile comes later
 #pragma unroll
           for (int i = 0; i < kQ; ++i) {
@@ -725,20 +742,52 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           if (NP < C::kNS && sid < (C::kNS - NP) * kPerRow)
             *reinterpret_cast<uint4*>(qd + in_bf16(NP + sid / kPerRow, sid % kPerRow * 8, C::kNS)) = none;
         }
-        most = __reduce_max_sync(0xffffffffu, most);
-        if (lane == 0) sm.top[warp] = most;
+        if (!C::kRowScales) {
+          most = __reduce_max_sync(0xffffffffu, most);
+          least = __reduce_min_sync(0xffffffffu, least);
+          if (lane == 0) sm.top[warp] = make_uint2(most, least);
+        }
         const bool odd_any = soft_any<kSoft>(1, odd);  // a barrier too
         if (sid == 0) sm.odd_values = odd_any;
 #pragma unroll
-        for (int w = 0; w < 4 * C::kSG; ++w) most = max(most, sm.top[w]);
-        q_exp = top_exponent(most);
-        const float qs = kv8_pow2(-q_exp);
+        for (int w = 0; w < (C::kRowScales ? 0 : 4 * C::kSG); ++w) {
+          most = max(most, sm.top[w].x);
+          least = min(least, sm.top[w].y);
+        }
+        if (used > 0) set_scales(raw);
+        if (tree_here) {
+          unsigned char* vd =  // W's buffer is free, as P's is
+              base + (C::kWiden ? C::off_W + first_tile % kBuf * C::kWide : off_V + st * C::kTile);
+#pragma unroll
+          for (int i = 0; i < kT; ++i) {
+            const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
+            if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;  // whole warps
+            int e = kVExpLeast;
+            if (opaque(i * kSoft / kPerRow < p.n)) e = tree_exp(over_row(top8(v[i])), ref);
+            const float vs = kv8_pow2(-e);
+            const uint4 w = v[i];
+            *reinterpret_cast<uint4*>(vd + in_bf16(r, d, kTreeKeys)) =
+                make_uint4(pack_bf16x2(bf16lo(w.x) * vs, bf16hi(w.x) * vs), pack_bf16x2(bf16lo(w.y) * vs, bf16hi(w.y) * vs),
+                           pack_bf16x2(bf16lo(w.z) * vs, bf16hi(w.z) * vs), pack_bf16x2(bf16lo(w.w) * vs, bf16hi(w.w) * vs));
+            if (d == 0) sm.v_exp[r] = (int8_t)e;
+          }
+        }
+        // The rows' largest elements decide one power of two, unless a row is so small that its codes would be coarse.
+        int q_exp = 0;
+        if constexpr (!C::kRowScales) {
+          q_exp = top_exponent(most);
+          apart = most != 0 && top_exponent(least) < q_exp - kQExpSpan;
+          if (!apart) a_q = p.scale_log2 * kv8_pow2(q_exp);
+        }
 #pragma unroll
         for (int i = 0; i < kQ; ++i) {
           const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
+          const uint32_t top = C::kRowScales ? over_row(top8(q[i])) : row_top[i];
           if (r < NP) {
+            const int e = apart ? top_exponent(top) : q_exp;
             uint2 hi, lo;
-            split8(q[i], qs, C::kQLo, hi, lo);
+            split8(q[i], kv8_pow2(-e), C::kQLo, hi, lo);
+            if (d == 0) sm.q_unit[r] = p.scale_log2 * kv8_pow2(e);
             *reinterpret_cast<uint2*>(base + C::off_Q + swizzled<D>(r, d)) = hi;
             *reinterpret_cast<uint2*>(base + C::off_Q + swizzled<D>(NP + r, d)) = lo;
           }
@@ -755,7 +804,6 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       uint64_t l2[RT / 2];  // pairs of rows
 #pragma unroll
       for (int k = 0; k < RT / 2; ++k) l2[k] = 0ull;
-      if (used > 0) set_scales(raw);
       if (walk) {  // while the first product runs
         if (quarter == 0) {
           const int r = r_own + lane;
@@ -765,7 +813,6 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         sees_b = s.b;
         soft_sync<128>(gbar);
       }
-      const float a_q = p.scale_log2 * kv8_pow2(q_exp);
       int nth = 0;  // of the blocks whose scales the lanes hold
       auto scales_of = [&](float& a, float& ef, float& inv_v) {  // the next cached tile's
         const uint32_t mine = __shfl_sync(0xffffffffu, scales, nth + (tid >> 6));
@@ -777,8 +824,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       auto first_scales = [&](float& a, float& ef, float& inv_v) {  // the segment's first tile's
         if (tree_here) {
           a = p.scale_log2;
-          ef = sm.v_exp[tid % kTreeKeys];  // what lies past the nodes is masked
-          inv_v = kv8_pow2(-(int)ef);
+          ef = 0.f;  // each key has its own: below
+          inv_v = 1.f;
         } else {
           scales_of(a, ef, inv_v);
         }
@@ -832,6 +879,13 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             constexpr int CH = 8;
             uint32_t x[CH], z[CH];  // split: hi, lo; else rows c .. c + 7, rows c + 8 .. c + 15
             tmem_ld8x2(tS + c, tS + c + (C::kSplitS ? NP : 8), x, z);
+            if (opaque(apart && !is_tree)) {  // the rows' own scales; the tree's queries are not scaled
+#pragma unroll
+              for (int k = 0; k < CH; k += 4) {
+                scale4(x + k, &sm.q_unit[r_own + c + k]);
+                scale4(z + k, &sm.q_unit[r_own + c + (C::kSplitS ? 0 : 8) + k]);
+              }
+            }
             const uint64_t a2 = f2(a, a), ef2 = f2(ef, ef);
             auto pair = [](const uint32_t* x) { return f2(__uint_as_float(x[0]), __uint_as_float(x[1])); };
 #pragma unroll
@@ -849,6 +903,9 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         if (opaque(is_tree || key0 + kTK > plen)) {  // which rows see this thread's key
           uint32_t vis = key0 + tid < plen ? ~0u : 0u;
           if (is_tree) {
+            const float e = (float)sm.v_exp[tid % kTreeKeys];
+#pragma unroll
+            for (int k = 0; k < RT; ++k) u[k] += e;
             vis = 0;
             if (tid < p.n)
 #pragma unroll 4
@@ -923,6 +980,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         // ones, else as two codes
         unsigned char* const p_to = base + C::off_P + buf * C::kPBytes + p_row;
         if (opaque(is_tree)) {
+          const float inv_v = kv8_pow2(-sm.v_exp[tid % kTreeKeys]);
 #pragma unroll
           for (int c = 0; c < RT; c += 8) {
             uint32_t w[4];
