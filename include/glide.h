@@ -427,9 +427,12 @@ size_t glide_kv8_workspace_bytes(const glide_attn_desc* desc, int32_t n_queries)
  * with kv_len 0 gets zeros.  H / H_kv <= 256.  desc->flags is ignored.  bf16 queries
  * over a cache of 2^31 - 128 rows or more (B * H_kv * S_cap, 32-bit TMA coordinates), or
  * over 2^30 tiles of 128 keys: GLIDE_ERR_UNSUPPORTED.
- * A query or a seen key that is not finite makes the rows that meet it NaN.  bf16
- * queries: elements below 2^-6 of the largest of their row are held to 2^-14 of that one, and a block's value exponent counts as at least -90 and
- * at least the largest before it in its head less 110.
+ * What is not finite has the definition's result: a query row with an infinity or a NaN
+ * is NaN if it sees anything, a key with a NaN or of score +inf makes the rows that see it
+ * NaN, and one of score -inf has no weight (a row that sees no other key is NaN).
+ * bf16 queries: elements below 2^-6 of the largest of their row are held to 2^-14 of that
+ * one, and a block's value exponent counts as at least -90 and at least the largest before
+ * it in its head less 110.
  */
 glide_status glide_kv8_cross_attn(const glide_attn_desc* desc, const void* q_draft, const glide_kv8_cache* cache,
                                   const int32_t* kv_len, int32_t max_kv_len, void* out, void* workspace,

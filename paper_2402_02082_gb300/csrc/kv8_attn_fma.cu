@@ -182,7 +182,8 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
       sum += f * l_all[w][r];
       x += f * o_all[w][r][d];
     }
-    out[out_row(b, h, r0 + r, rows, group, a.H) * D + d] = sum == 0.f ? 0.f : x / sum;
+    // no keys at all: zeros; scores of -inf alone: NaN
+    out[out_row(b, h, r0 + r, rows, group, a.H) * D + d] = all == 0 ? 0.f : x / sum;
   }
 }
 

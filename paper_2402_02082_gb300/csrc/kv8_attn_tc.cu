@@ -64,6 +64,7 @@ constexpr int kMaxStages8 = 6;
 constexpr float kPLo = 28.f;         // p = hi + lo / kPLo: of p <= 430 at most 16 are left to lo, 448 its largest code
 constexpr int kVExpSpan = 110, kVExpLeast = -90;  // see effective_exp
 constexpr int kTreeExpMost = 20;                  // see tree_exp
+constexpr float kNoM = -1.f;                      // of a row whose scores in the tree tile are all -inf: it has no m yet
 constexpr int kQExpSpan = 3;                      // rows of queries share a power of two if it is within 2^3 of their own
 
 // What a switch of slabs costs a CTA, in tiles (from 1 + np / 32 to 3 + np / 16: within 5% of each other, either way).
@@ -130,8 +131,8 @@ struct Small {  // per CTA, after the rings
   ShareStart share;
   unsigned long long sees[64];  // the rows' nodes and their ancestors
   alignas(16) float minus_m[64];  // what turns a row's u into its weight's logarithm
-  alignas(16) float minus_up[64];  // by how much m rose last, negative
-  alignas(16) float f[64];      // 2^(-up / 2); at the end 1 / l, or l
+  alignas(16) float minus_up[64];  // by how much m rose last, negative; what turns a raw u into the logarithm
+  alignas(16) float f[64];      // 2^(-up / 2), or kNoM; at the end 1 / l, or l
   alignas(16) float q_unit[64];    // what makes a row's scores log2 units where its queries have a scale of their own
   alignas(16) float part[4][64];  // per lane quarter: row maxima, row sums
   alignas(4) uint8_t rise[2][4][4];  // tiles in turn, per group and lane quarter: the chunks whose m rises
@@ -834,8 +835,9 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       // two have no registers for that (12 nodes on 8 x 40 heads of 1024 keys: 28.2 -> 30.5).
       float a_next, ef_next, inv_next;
       if (C::kWiden) first_scales(a_next, ef_next, inv_next);
+      int late = -1;  // the tile that gives an m to rows that the tree's, with infinite keys, left without
       for (int t = s.t0; t < s.t1; ++t, ++i) {
-        const bool is_tree = p.tree && t == 0, first = t == s.t0;
+        const bool is_tree = p.tree && t == 0, first = t == s.t0, raw = first || t == late;
         const int key0 = (t - p.tree) * kTK, buf = i % kBuf;
         if (opaque(nth == 32)) {  // the next 16 tiles' (past a slab's last block: that one's, for nothing)
           set_scales(fetch((t + (C::kWiden ? 1 : 0) - p.tree) * (kTK / kKv8Block)));
@@ -885,6 +887,9 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
                 scale4(x + k, &sm.q_unit[r_own + c + k]);
                 scale4(z + k, &sm.q_unit[r_own + c + (C::kSplitS ? 0 : 8) + k]);
               }
+            } else if (C::kSplitS) {  // columns without a query, NaN for an infinite key
+#pragma unroll
+              for (int k = 0; k < CH; ++k) z[k] = 0u;
             }
             const uint64_t a2 = f2(a, a), ef2 = f2(ef, ef);
             auto pair = [](const uint32_t* x) { return f2(__uint_as_float(x[0]), __uint_as_float(x[1])); };
@@ -916,7 +921,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         }
         if (C::kWiden) scales_of(a_next, ef_next, inv_next);
         uint32_t rise = (1u << RT / 8) - 1u;  // by chunks of 8 rows
-        if (!first) {
+        if (!raw) {
           rise = 0;
 #pragma unroll
           for (int c = 0; c < RT; c += 8) {
@@ -955,11 +960,13 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           if (tid < RT && (rise >> tid / 8) & 1u) {
             const int r = r_own + tid;
             const float top = fmaxf(fmaxf(sm.part[0][r], sm.part[1][r]), fmaxf(sm.part[2][r], sm.part[3][r]));
-            // a row with nothing but NaN has no m, and keeps none
-            const float up = first || top > C::kMost || top != top ? top - C::kLift : 0.f;
-            sm.minus_m[r] = first ? -up : sm.minus_m[r] - up;
-            sm.minus_up[r] = -up;
-            sm.f[r] = first ? 0.f : fast_exp2(-0.5f * up);
+            // `raw`: u holds no m yet.  A row with nothing but NaN has no m, and keeps none.
+            const bool none = first && top == -CUDART_INF_F, fresh = first || (raw && sm.f[r] == kNoM);
+            const float was = fresh ? 0.f : sm.minus_m[r], now = raw ? top + was : top;
+            const float up = !none && (fresh || now > C::kMost || now != now) ? now - C::kLift : 0.f;
+            sm.minus_m[r] = was - up;
+            sm.minus_up[r] = raw ? was - up : -up;
+            sm.f[r] = none ? kNoM : fresh ? 0.f : fast_exp2(-0.5f * up);
           }
           soft_sync<128>(gbar);
 #pragma unroll
@@ -974,6 +981,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
               }
             }
           }
+          if (opaque(is_tree) && __any_sync(0xffffffffu, sm.f[r_own + lane % RT] == kNoM)) late = 1;
         }
 
         // ---- weights: p = 2^(u - m), l += p 2^-e, in bf16 beside the tree's bf16 values, in fp16 beside widened
@@ -1108,7 +1116,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
       const size_t o0 = (size_t)s.b * p.n * p.H + (size_t)s.h * p.group;
       if (!whole && tid < RT && !dead && sm.rel[r_own + tid] >= 0)
         *reinterpret_cast<float2*>(part + (size_t)(r_own + tid) * (D + 2)) =
-            make_float2(-sm.minus_m[r_own + tid], sm.f[r_own + tid]);
+            make_float2(sm.f[r_own + tid] == 0.f ? -CUDART_INF_F : -sm.minus_m[r_own + tid], sm.f[r_own + tid]);
       const bool live = has && !dead;
 #pragma unroll 1
       for (int c = 0; c < RT; c += 8) {

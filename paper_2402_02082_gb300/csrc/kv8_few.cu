@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
       sum.x += f * v.x;
       sum.y += f * v.y;
     }
-    const float inv = Lr == 0.f ? 0.f : 1.f / Lr;  // no keys at all: zeros
+    const float inv = L == 0 && !p.parent ? 0.f : 1.f / Lr;  // no keys at all: zeros; scores of -inf alone: NaN
     const int node = r / p.group, dim = (D / 8) * (d % 16 / 2) + 2 * (d / 16);
     *reinterpret_cast<uint32_t*>(p.out + (((size_t)b * p.n + node) * p.H + h * p.group + (r - node * p.group)) * D + dim) =
         pack_bf16x2(sum.x * inv, sum.y * inv);
