@@ -429,7 +429,8 @@ size_t glide_kv8_workspace_bytes(const glide_attn_desc* desc, int32_t n_queries)
  * over 2^30 tiles of 128 keys: GLIDE_ERR_UNSUPPORTED.
  * What is not finite has the definition's result: a query row with an infinity or a NaN
  * is NaN if it sees anything, a key with a NaN or of score +inf makes the rows that see it
- * NaN, and one of score -inf has no weight (a row that sees no other key is NaN).
+ * NaN, and one of score -inf has no weight (a row that sees no other key is NaN); a value
+ * that is not finite decides its column in the rows that see it.
  * bf16 queries: elements below 2^-6 of the largest of their row are held to 2^-14 of that
  * one, and a block's value exponent counts as at least -90 and at least the largest before
  * it in its head less 110.

@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
   __shared__ float m_all[kWarps][kRT], l_all[kWarps][kRT];
   __shared__ unsigned long long sees[kRT];
   __shared__ int up[64];
+  __shared__ int odd_values;  // the tree has values that are not finite
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int group = a.H / a.Hkv, rows = a.nq * group;
   const int tiles = (rows + kRT - 1) / kRT;
@@ -50,6 +51,7 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
     q[i / D][i % D] = r < rows ? Q[out_row(b, h, r, rows, group, a.H) * D + i % D] : 0.f;
   }
   const int n = a.parent ? a.nq : 0;
+  if (threadIdx.x == 0) odd_values = 0;
   if (threadIdx.x < n) up[threadIdx.x] = a.parent[(size_t)b * n + threadIdx.x];
   __syncthreads();
   if (threadIdx.x < kRT && n) {  // the row's node and its ancestors
@@ -95,10 +97,8 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
 #pragma unroll
       for (int r = 0; r < kRT; ++r) {
         const float pj = __shfl_sync(0xffffffffu, w[r], j);
-        if (pj != 0.f) {  // an unseen key's infinite value adds nothing
 #pragma unroll
-          for (int k = 0; k < kPer; ++k) o[r][k] = fmaf(pj, f[k], o[r][k]);
-        }
+        for (int k = 0; k < kPer; ++k) o[r][k] = fmaf(pj, f[k], o[r][k]);
       }
     }
   };
@@ -157,7 +157,11 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
       const float* vt = static_cast<const float*>(a.vt) + (((size_t)b * n + j0) * a.Hkv + h) * D + lane * kPer;
       fold(s, seen, 1.f, n - j0 < 32 ? n - j0 : 32, [&](int i, float* f) {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) f[k] = vt[(size_t)i * a.Hkv * D + k];
+        for (int k = 0; k < kPer; ++k) {
+          f[k] = vt[(size_t)i * a.Hkv * D + k];
+          // what is not finite must not meet a weight of zero: it is left out here, and put back at the end where it is seen
+          if (!isfinite(f[k])) f[k] = 0.f, odd_values = 1;
+        }
       });
     }
   }
@@ -182,6 +186,11 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
       sum += f * l_all[w][r];
       x += f * o_all[w][r][d];
     }
+    if (odd_values)
+      for (int j = 0; j < n; ++j) {
+        const float v = static_cast<const float*>(a.vt)[(((size_t)b * n + j) * a.Hkv + h) * D + d];
+        if (!isfinite(v) && (sees[r] >> j) & 1ull) x += v;
+      }
     // no keys at all: zeros; scores of -inf alone: NaN
     out[out_row(b, h, r0 + r, rows, group, a.H) * D + d] = all == 0 ? 0.f : x / sum;
   }

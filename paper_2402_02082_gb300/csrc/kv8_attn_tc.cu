@@ -1176,7 +1176,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 
 // Joins the partials of every split slab, one warp per query row: with M the largest m,
 //   out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.
-// l is a sum of 2^-eV, so its share's weight is taken in the logarithm: either may leave fp32's range.
+// l is a sum of 2^-eV, so its share's weight is taken in the logarithm: either may leave fp32's range.  An o's weight
+// is at least the least number there is: zero times an infinite o, of an infinite value, were NaN.
 constexpr int kMergeW = 8;
 template <int D>
 __global__ void __launch_bounds__(kMergeW * 32) kv8_merge_kernel(const int2* ranges, const float* partials,
@@ -1184,6 +1185,7 @@ __global__ void __launch_bounds__(kMergeW * 32) kv8_merge_kernel(const int2* ran
                                                                  int Hq, int Hkv) {
   constexpr int kPairs = D / 64;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const float least = __int_as_float(1);
   const int lane = threadIdx.x & 31;
   const unsigned total = (unsigned)BH * (unsigned)rows, step = gridDim.x * kMergeW;
   pdl_wait();
@@ -1212,7 +1214,7 @@ __global__ void __launch_bounds__(kMergeW * 32) kv8_merge_kernel(const int2* ran
 #pragma unroll
       for (int u = 0; u < 8; ++u)
         if (c0 + u < shares) now = fmaxf(now, ml[u].x);
-      const float f = M == -CUDART_INF_F ? 0.f : fast_exp2(M - now);
+      const float f = M == -CUDART_INF_F ? 0.f : fmaxf(fast_exp2(M - now), least);
       if (M != -CUDART_INF_F) {
         L = L > 0.f ? fast_exp2(M - now + __log2f(L)) : L;
 #pragma unroll
@@ -1221,7 +1223,7 @@ __global__ void __launch_bounds__(kMergeW * 32) kv8_merge_kernel(const int2* ran
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         if (c0 + u >= shares) break;
-        const float w = fast_exp2(ml[u].x - now);
+        const float w = fmaxf(fast_exp2(ml[u].x - now), least);
         L += fast_exp2(ml[u].x - now + __log2f(ml[u].y));
 #pragma unroll
         for (int k = 0; k < kPairs; ++k) {

@@ -15,6 +15,7 @@
 //   O^T (16 dims x 8 queries): lane (g, t) reads dims D/8 g .. of keys 2t, 2t + 1, 2t + 8, 2t + 9
 // The weights of S^T become the second product's operand by a transpose of 8 x 8 within the warp; rows of both results lie
 // in the same lanes, so the running maximum and sum need no exchange but the maximum's over the keys.
+#include <cfloat>
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -298,6 +299,8 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
 
   int ref_v = -128;  // the largest value exponent of the cached blocks so far, which every row sees
   // ---- the tree's own keys and values: at most 16
+  bool odd_values = false;  // the tree has values that are not finite
+  uint32_t* const own_vis = reinterpret_cast<uint32_t*>(red + warp * kR * kStride);  // then: the nodes that each row sees
   if (tree_warp) {
     const int n = p.n;
     // the nodes that node `lane` sees: itself and its ancestors, found by pointer jumping (at most 16 levels)
@@ -395,21 +398,10 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) mma_f16(o[j][nt], a, pt[0][nt][0], pt[0][nt][1]);
     }
-    if (__any_sync(0xffffffffu, odd)) {  // a visible value that is not finite decides its column
-#pragma unroll 1
-      for (int key = 0; key < n; ++key)
+    odd_values = __any_sync(0xffffffffu, odd);
+    if (odd_values && g == 0) {
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const float v = __bfloat162float(p.vt[(((size_t)b * n + key) * p.Hkv + h) * D + g * (D / 8) + 2 * j + y]);
-            if (isfinite(v)) continue;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int x = 0; x < 2; ++x)
-                if ((vis[nt][x] >> key) & 1u) o[j][nt][2 * y + x] += v;
-          }
+      for (int nt = 0; nt < NT; ++nt) own_vis[8 * nt + 2 * t] = vis[nt][0], own_vis[8 * nt + 2 * t + 1] = vis[nt][1];
     }
     load_k(key0);
     load_v(key0);
@@ -475,6 +467,28 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
       }
   }
 
+  if (odd_values) {  // a visible one decides its column, however small its weight
+    __syncwarp();
+    uint32_t vis[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) vis[nt][0] = own_vis[8 * nt + 2 * t], vis[nt][1] = own_vis[8 * nt + 2 * t + 1];
+    __syncwarp();
+#pragma unroll 1
+    for (int key = 0; key < p.n; ++key)
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const float v = __bfloat162float(p.vt[(((size_t)b * p.n + key) * p.Hkv + h) * D + g * (D / 8) + 2 * j + y]);
+          if (isfinite(v)) continue;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              if ((vis[nt][x] >> key) & 1u) o[j][nt][2 * y + x] += v;
+        }
+  }
+
   // ---- the warps' results, then the cluster's.  Position 16 j + 2 g + y of a partial row is dim D/8 g + 2 j + y.
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
@@ -490,11 +504,11 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
     }
   __syncthreads();
   // The weight of a partial (m, l, o) against the largest M, and its l: in the logarithm, as 2^-eV may take either
-  // factor out of fp32's range.
+  // factor out of fp32's range.  The weight is at least the least normal number: zero times an infinite o were NaN.
   auto weight = [](float2 s, float M, float& L) {
     const float ref = M == -CUDART_INF_F ? 0.f : M;
     if (s.y != 0.f) L += s.x == -CUDART_INF_F ? s.y : fast_exp2(s.x - ref + __log2f(s.y));
-    return s.x == -CUDART_INF_F ? 0.f : fast_exp2(s.x - ref);
+    return s.x == -CUDART_INF_F ? 0.f : fmaxf(fast_exp2(s.x - ref), FLT_MIN);
   };
   const int pairs = p.rows * (D / 2), per = (pairs + p.C - 1) / p.C;
   cluster_wait();
