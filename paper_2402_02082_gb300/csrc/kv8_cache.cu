@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kAppendThreads, sizeof(T) == 2 ? 8 : 5) kv8_ap
     x[i].none();
     if (k >= 0 && k < r.m) x[i].load(fresh + row_at(p, layer, b, h, k, D) + d);
   }
-  const int old = holds ? kv8_clamp_exp(*exp) : 0;
+  const int old_raw = holds ? (int)*exp : 0;
   auto joined = [&](uint32_t mine, int nth) {  // over the CTA
     mine = __reduce_max_sync(0xffffffffu, mine);
     if ((threadIdx.x & 31) == 0) top[nth][threadIdx.x >> 5] = mine;
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kAppendThreads, sizeof(T) == 2 ? 8 : 5) kv8_ap
     for (int i = 0; i < kPasses; ++i) most = top8(x[i], most);
     most = joined(most, 1);
   }
-  const int e = joined_exponent(most, holds, old);
+  const int old = kv8_clamp_exp(old_raw), e = joined_exponent(most, holds, old);
   if (threadIdx.x == 0) *exp = (int8_t)e;  // every thread has read the old one
   const float s = kv8_pow2(-e);
   uint8_t* const codes = (is_v ? p.V : p.K) + ((size_t)slab * p.S_cap + row0) * D + d;
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) kv8_append_few_kernel(const AppendPa
   int8_t* exp = (kv ? p.Ve : p.Ke) + (size_t)slab * kv8_blocks(p.S_cap) + block;
   const T* fresh = static_cast<const T*>(kv ? p.v_new : p.k_new);
   const bool holds = row0 < r.L;
-  const int old = holds ? kv8_clamp_exp(*exp) : 0;
+  const int old_raw = holds ? (int)*exp : 0;
   // rows first .. last - 1 of the block are new
   const int first = holds ? r.L - row0 : 0, last = min(kKv8Block, r.L + r.m - row0);
   const int rl = lane / kPerRow, d = (lane % kPerRow) * 8;
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kThreads) kv8_append_few_kernel(const AppendPa
   for (int i = 0; i < kHeld; ++i) most = top8(x[i], most);
   for (int row = first + rl + kHeld * kRows; row < last; row += kRows) most = top8(load(row), most);
   most = __reduce_max_sync(0xffffffffu, most);
-  const int e = joined_exponent(most, holds, old);
+  const int old = kv8_clamp_exp(old_raw), e = joined_exponent(most, holds, old);
   __syncwarp();
   if (lane == 0) *exp = (int8_t)e;  // every lane has read the old one
   const float s = kv8_pow2(-e);
