@@ -424,7 +424,9 @@ size_t glide_kv8_workspace_bytes(const glide_attn_desc* desc, int32_t n_queries)
  * glide_cross_attn over an 8-bit cache.  desc->dtype is that of q_draft [B,1,H,D] and
  * of out [B,1,H,D]: bf16 queries give a bf16 result (one rounding of an fp32
  * accumulation), fp32 queries an fp32 one.  0 <= max_kv_len <= S_cap; a sequence
- * with kv_len 0 gets zeros.  H / H_kv <= 256.  desc->flags is ignored.  bf16 queries
+ * with kv_len 0 gets zeros.  H / H_kv <= 256.  desc->flags is ignored.  desc->max_ctas
+ * bounds the attention kernel's CTAs (more than 64 query rows of bf16 for a cached head are
+ * ceil(rows / 64) CTAs at least), not those that merge its partial results.  bf16 queries
  * over a cache of 2^31 - 128 rows or more (B * H_kv * S_cap, 32-bit TMA coordinates), or
  * over 2^30 tiles of 128 keys: GLIDE_ERR_UNSUPPORTED.
  * What is not finite has the definition's result: a query row with an infinity or a NaN

@@ -28,8 +28,9 @@ constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
 constexpr int kRT = 2;  // query rows of a CTA
 
+// Row tile `unit` of all slabs' tiles.
 template <int D>
-__global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArgs a) {
+__device__ __forceinline__ void attend(const Kv8AttnArgs& a, unsigned unit, int tiles) {
   constexpr int kPer = D / 32;  // value elements per lane
   __shared__ __align__(16) float q[kRT][D];
   __shared__ float o_all[kWarps][kRT][D];
@@ -39,10 +40,8 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
   __shared__ int odd_values;  // the tree has values that are not finite
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int group = a.H / a.Hkv, rows = a.nq * group;
-  const int tiles = (rows + kRT - 1) / kRT;
-  const int slab = (int)(blockIdx.x / (unsigned)tiles), r0 = (int)(blockIdx.x - (unsigned)slab * tiles) * kRT;
+  const int slab = (int)(unit / (unsigned)tiles), r0 = (int)(unit - (unsigned)slab * tiles) * kRT;
   const int b = slab / a.Hkv, h = slab - b * a.Hkv;
-  pdl_wait();
   int L = a.kv_len[b];
   L = L < 0 ? 0 : (L > a.max_kv_len ? a.max_kv_len : L);
   const float* Q = static_cast<const float*>(a.q);
@@ -197,9 +196,21 @@ __global__ void __launch_bounds__(kThreads) kv8_attn_fma_kernel(const Kv8AttnArg
 }
 
 template <int D>
+__global__ void __launch_bounds__(kThreads, 2) kv8_attn_fma_kernel(const Kv8AttnArgs a) {
+  const int tiles = (a.nq * (a.H / a.Hkv) + kRT - 1) / kRT;
+  const unsigned units = (unsigned)(a.B * a.Hkv) * (unsigned)tiles;
+  pdl_wait();
+  for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {  // once, unless the caller bounds the CTAs
+    attend<D>(a, unit, tiles);
+    if (unit + gridDim.x < units) __syncthreads();  // before its shared memory is written again
+  }
+}
+
+template <int D>
 cudaError_t launch(const Kv8AttnArgs& a, cudaStream_t st) {
   const int rows = a.nq * (a.H / a.Hkv);
-  const long long ctas = (long long)a.B * a.Hkv * ((rows + kRT - 1) / kRT);
+  long long ctas = (long long)a.B * a.Hkv * ((rows + kRT - 1) / kRT);
+  if (a.max_ctas > 0 && ctas > a.max_ctas) ctas = a.max_ctas;
   return launch_pdl(kv8_attn_fma_kernel<D>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a);
 }
 

@@ -1275,7 +1275,7 @@ cudaError_t launch_np(const Kv8AttnArgs& a, int R, int per_tile, cudaStream_t st
   if (!make_code_map(&mk, a.K, rows, D) || !make_code_map(&mv, a.V, rows, D)) return cudaErrorNotSupported;
   const int tree = a.parent != nullptr;
   const long long tiles = (long long)a.B * a.Hkv * ((a.max_kv_len + kTK - 1) / kTK + tree);
-  long long G = a.max_ctas > 0 ? a.max_ctas : C::kCtas * sm_count() / R;
+  long long G = (a.max_ctas > 0 ? a.max_ctas : C::kCtas * sm_count()) / R;
   if (G > kMaxShares) G = kMaxShares;
   if (G > tiles) G = tiles;
   if (G < 1) G = 1;
