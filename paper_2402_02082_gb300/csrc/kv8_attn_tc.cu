@@ -51,6 +51,7 @@
 #include "device.h"
 #include "kernels.h"
 #include "kv8.h"
+#include "kv8_wait.cuh"
 #include "tc_attn.cuh"
 #include "tc_ptx.cuh"
 #include "tensor_map.h"
@@ -156,39 +157,6 @@ struct Params8 {
   float scale_log2;
 };
 
-// Waits of at most a second, as mbar_wait_small, in few instructions: those that a wait spins through are taken from
-// the warps that work.  On giving up it sets *abort.
-__device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  const uint64_t t0 = global_timer_ns();
-  while (true) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .u32 n;\n\t"
-        "mov.u32 %0, 1;\n\tmov.u32 n, 64;\n"
-        "AGAIN:\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "@p bra DONE;\n\t"
-        "sub.u32 n, n, 1;\n\t"
-        "setp.ne.u32 p, n, 0;\n\t"
-        "@p bra AGAIN;\n\t"
-        "mov.u32 %0, 0;\n"
-        "DONE:\n\t}"
-        : "=&r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity), "r"(1000u)
-        : "memory");
-    if (ok) return true;
-    if (*abort) return false;
-    if (global_timer_ns() - t0 > kWaitLimitNs) {
-      *abort = 1;
-      return false;
-    }
-  }
-}
-// For every lane of a converged warp, with one outcome.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return __all_sync(0xffffffffu, wait_long(bar, parity, abort));
-}
 // True in one lane of a converged warp.  The products and copies are issued behind it, by a warp whose loops all lanes
 // run: the compiler then knows that one thread issues, and that its operands are the warp's.  Behind `lane == 0` every
 // product took its issuer 120 - 210 cycles, behind this 60 - 70 (M = 128, N = 64: 8 fp16 products 978 -> 474 cycles).
