@@ -325,6 +325,16 @@ __device__ __forceinline__ uint32_t top8(const uint4& w) {
   }
   return most;
 }
+// The largest magnitude among eight bf16 elements, infinities and NaN among them (as its bits).
+__device__ __forceinline__ uint32_t top8_of_all(const uint4& w) {
+  const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+  return max(m & 0xffffu, m >> 16);
+}
+// The largest finite one (which all are but seldom).
+__device__ __forceinline__ uint32_t finite_top8(const uint4& w) {
+  const uint32_t m = top8_of_all(w);
+  return opaque(m >= 0x7f80u) ? top8(w) : m;
+}
 // Eight bf16 elements with zeros for those that are not finite; says whether there are any.
 __device__ __forceinline__ bool drop_odd(uint4& w) {
   uint32_t in[4] = {w.x, w.y, w.z, w.w};
@@ -651,9 +661,14 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
                       kT = (kTreeKeys * kPerRow + kSoft - 1) / kSoft;
         const uint4 none = make_uint4(0u, 0u, 0u, 0u);
         auto over_row = [](uint32_t x) {  // the largest of a row's pieces, which kPerRow neighbouring lanes have
+          uint32_t r = 0;
 #pragma unroll
-          for (int off = 1; off < kPerRow; off <<= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, off));
-          return x;
+          for (int g = 0; g < 32 / kPerRow; ++g) {
+            const bool mine = (threadIdx.x & 31) / kPerRow == g;
+            const uint32_t y = __reduce_max_sync(0xffffffffu, mine ? x : 0u);
+            r = mine ? y : r;
+          }
+          return r;
         };
         uint4 q[kQ], kt[kT], v[kT];
         uint32_t most = 0, least = ~0u, row_top[kQ];
@@ -679,7 +694,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
         if constexpr (!C::kRowScales) {
 #pragma unroll
           for (int i = 0; i < kQ; ++i) {
-            row_top[i] = over_row(top8(q[i]));
+            row_top[i] = over_row(finite_top8(q[i]));
             most = max(most, row_top[i]);
             if (row_top[i] != 0) least = min(least, row_top[i]);
           }
@@ -701,7 +716,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           for (int i = 0; i < kT; ++i)
             // An unseen value that is not finite must not meet a weight of zero: it is left out here, and put
             // back at the end where it is seen.
-            odd |= drop_odd(v[i]);
+            if (opaque(top8_of_all(v[i]) >= 0x7f80u)) odd |= drop_odd(v[i]);
           unsigned char* qd = base + C::off_P + first_tile % C::kBuf * C::kPBytes;  // P of this tile comes later
 #pragma unroll
           for (int i = 0; i < kQ; ++i) {
@@ -732,7 +747,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
             const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
             if (kTreeKeys * kPerRow % kSoft != 0 && r >= kTreeKeys) continue;  // whole warps
             int e = kVExpLeast;
-            if (opaque(i * kSoft / kPerRow < p.n)) e = tree_exp(over_row(top8(v[i])), ref);
+            e = tree_exp(over_row(top8_of_all(v[i])), ref);
             const float vs = kv8_pow2(-e);
             const uint4 w = v[i];
             *reinterpret_cast<uint4*>(vd + in_bf16(r, d, kTreeKeys)) =
@@ -751,7 +766,7 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
 #pragma unroll
         for (int i = 0; i < kQ; ++i) {
           const int c = sid + i * kSoft, r = c / kPerRow, d = c % kPerRow * 8;
-          const uint32_t top = C::kRowScales ? over_row(top8(q[i])) : row_top[i];
+          const uint32_t top = C::kRowScales ? over_row(finite_top8(q[i])) : row_top[i];
           if (r < NP) {
             const int e = apart ? top_exponent(top) : q_exp;
             uint2 hi, lo;
@@ -928,13 +943,21 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           if (tid < RT && (rise >> tid / 8) & 1u) {
             const int r = r_own + tid;
             const float top = fmaxf(fmaxf(sm.part[0][r], sm.part[1][r]), fmaxf(sm.part[2][r], sm.part[3][r]));
-            // `raw`: u holds no m yet.  A row with nothing but NaN has no m, and keeps none.
-            const bool none = first && top == -CUDART_INF_F, fresh = first || (raw && sm.f[r] == kNoM);
-            const float was = fresh ? 0.f : sm.minus_m[r], now = raw ? top + was : top;
-            const float up = !none && (fresh || now > C::kMost || now != now) ? now - C::kLift : 0.f;
+            // a row with nothing but NaN has no m, and keeps none
+            float up = first || top > C::kMost || top != top ? top - C::kLift : 0.f, f = first ? 0.f : fast_exp2(-0.5f * up);
+            const float was = first ? 0.f : sm.minus_m[r];
+            float add = -up;
+            if (opaque(t == late)) {  // u holds no m yet
+              const bool fresh = sm.f[r] == kNoM;
+              const float now = top + was;
+              up = fresh || now > C::kMost || now != now ? now - C::kLift : 0.f;
+              f = fresh ? 0.f : fast_exp2(-0.5f * up);
+              add = was - up;
+            }
+            if (opaque(first && top == -CUDART_INF_F)) up = add = 0.f, f = kNoM;
             sm.minus_m[r] = was - up;
-            sm.minus_up[r] = raw ? was - up : -up;
-            sm.f[r] = none ? kNoM : fresh ? 0.f : fast_exp2(-0.5f * up);
+            sm.minus_up[r] = add;
+            sm.f[r] = f;
           }
           soft_sync<128>(gbar);
 #pragma unroll
