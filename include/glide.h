@@ -398,7 +398,8 @@ typedef struct {
  * NULL (clamped to [0, n)), len [B] or NULL: int32 on the device.  path and len as
  * tree_accept writes them append the accepted path; a prompt has path NULL.
  * 1 <= n <= S_cap.  new_kv_len [B] int32 and not the kv_len buffer.  No workspace.  More
- * than 2^31 - 1 blocks of 64 tokens over all slabs: GLIDE_ERR_UNSUPPORTED (read below too).
+ * than 2^31 - 1 blocks that the rows can touch ((n + 62) / 64 + 1 of each layer, sequence and
+ * cached head): GLIDE_ERR_UNSUPPORTED.
  */
 glide_status glide_kv8_append(const glide_attn_desc* desc, int32_t n_layers, const glide_kv8_cache* cache,
                               const void* k_new, const void* v_new, const int32_t* kv_len, int32_t n,
@@ -409,7 +410,8 @@ glide_status glide_kv8_append(const glide_attn_desc* desc, int32_t n_layers, con
  * Reads the cache back: K_out / V_out [n_layers][B, H_kv, S_out, D] of desc->dtype
  * (fp32: exactly the codes' values; bf16: they are exact there too), rows at and past
  * kv_len[b] zero, every element written.  1 <= S_out <= S_cap; kv_len [B] int32 on
- * the device, clamped to [0, S_out].  desc and cache as above.  No workspace.
+ * the device, clamped to [0, S_out].  desc and cache as above.  No workspace.  More than
+ * 2^31 - 1 parts (of 8192 / D of a slab's S_out rows) over all slabs: GLIDE_ERR_UNSUPPORTED.
  */
 glide_status glide_kv8_read(const glide_attn_desc* desc, int32_t n_layers, const glide_kv8_cache* cache,
                             const int32_t* kv_len, int32_t S_out, void* K_out, void* V_out,
@@ -423,19 +425,23 @@ size_t glide_kv8_workspace_bytes(const glide_attn_desc* desc, int32_t n_queries)
 /*
  * glide_cross_attn over an 8-bit cache.  desc->dtype is that of q_draft [B,1,H,D] and
  * of out [B,1,H,D]: bf16 queries give a bf16 result (one rounding of an fp32
- * accumulation), fp32 queries an fp32 one.  0 <= max_kv_len <= S_cap; a sequence
+ * accumulation; glide_cross_attn and tree_verify_attn write fp32), fp32 queries an fp32
+ * one.  0 <= max_kv_len <= S_cap; a sequence
  * with kv_len 0 gets zeros.  H / H_kv <= 256.  desc->flags is ignored.  desc->max_ctas
  * bounds the attention kernel's CTAs (more than 64 query rows of bf16 for a cached head are
  * ceil(rows / 64) CTAs at least), not those that merge its partial results.  bf16 queries
- * over a cache of 2^31 - 128 rows or more (B * H_kv * S_cap, 32-bit TMA coordinates), or
- * over 2^30 tiles of 128 keys: GLIDE_ERR_UNSUPPORTED.
+ * over a cache of 2^31 - 128 rows or more (B * H_kv * S_cap, 32-bit TMA coordinates):
+ * GLIDE_ERR_UNSUPPORTED, but for at most 16 query rows a cached head over few enough keys
+ * that the kernel without TMA takes the call.
  * What is not finite has the definition's result: a query row with an infinity or a NaN
  * is NaN if it sees anything, a key with a NaN or of score +inf makes the rows that see it
  * NaN, and one of score -inf has no weight (a row that sees no other key is NaN); a value
  * that is not finite decides its column in the rows that see it.
  * bf16 queries: elements below 2^-6 of the largest of their row are held to 2^-14 of that
- * one, and a block's value exponent counts as at least -90 and at least the largest before
- * it in its head less 110.
+ * one.  A weight is held to 2^-8.5 of itself, and one that is below 2^-22 of the row's
+ * largest, both times their value block's scale, may be left out of the sum of the values.
+ * A block's value exponent counts as at least -90 and at least the largest before it in its
+ * head less 110.
  */
 glide_status glide_kv8_cross_attn(const glide_attn_desc* desc, const void* q_draft, const glide_kv8_cache* cache,
                                   const int32_t* kv_len, int32_t max_kv_len, void* out, void* workspace,

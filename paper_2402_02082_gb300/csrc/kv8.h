@@ -56,7 +56,7 @@ struct Kv8AttnArgs {
 
 cudaError_t launch_kv8_append(const Kv8AppendArgs& a, cudaStream_t st);
 cudaError_t launch_kv8_read(const Kv8ReadArgs& a, cudaStream_t st);
-// On the tensor cores, bf16 queries; cudaErrorNotSupported where launch_kv8_attn_fma is the one to take.
+// On the tensor cores, bf16 queries; cudaErrorNotSupported for a cache beyond 32-bit coordinates.
 cudaError_t launch_kv8_attn_tc(const Kv8AttnArgs& a, cudaStream_t st);
 // Few query rows, bf16, straight from global memory to registers; cudaErrorNotSupported where launch_kv8_attn_tc is
 // the one to take.

@@ -9,11 +9,12 @@
 // memory, the same address in every lane), lane = slice of the head dimension for the values.
 // Running maximum, sum and output are kept per warp and joined at the end.
 //
-// What bounds it: fp32 queries are for checks and comparisons at small sizes, where a call is a chain of latencies:
-// a tile after the other in each warp.  Sixteen warps with two rows keep it short and still share a tile's keys and values
+// What bounds it: at small sizes a call is a chain of latencies, a tile after the other in each warp.  Sixteen
+// warps with two rows keep it short and still share a tile's keys and values
 // (8 warps x 4 rows / 16 x 2 / 16 x 1, us: 5 nodes on 4 heads of 64 dims, 128 keys 6.4 / 6.5 / 6.1; 16 nodes on 2 x 2
 // cached heads of 1024 42 / 22 / 23; 32 nodes on 2 x 32 heads of 2048 307 / 251 / 816).  Nothing splits a slab's keys over
-// CTAs, so few heads leave most of the GPU idle.
+// CTAs, so few heads leave most of the GPU idle; the fp32 calls on a cache in fp32 do split them, and take less: 8 nodes
+// of 2 query heads to each of 2 x 2 cached of 1024 keys 20 us for 8.9, 32 nodes on 2 x 32 heads of 2048 262 for 164.
 #include <math_constants.h>
 
 #include "attn_common.cuh"

@@ -10,7 +10,7 @@
 //
 // 8-bit operands without 8-bit results.  A bf16 query has 8 significant bits, two codes' worth: with a row's largest
 // element scaled to at most 448, and at least 28, q = hi + lo exactly down to the codes' least step (2^-9, or 2^-13 at 8
-// rows, where lo is held 16 times itself).  Weights, up to 16 rows: p <= 430 is hi + lo / 28 to 2^-9 of itself, or to 2^-22
+// rows, where lo is held 16 times itself).  Weights, up to 16 rows: p <= 430 is hi + lo / 28 to 2^-8.5 of itself, or to 2^-22
 // of the row's largest, which is at least 2^8.  More rows: values are widened to fp16 in shared memory, weights rounded
 // to fp16 (2^-12 of themselves).  The tree's own bf16 keys and values are a tile of their own, multiplied as bf16
 // with bf16 queries and weights; a node's values are scaled by a power of two of its own, which its weight's exponent takes
@@ -27,18 +27,18 @@
 // Roles: groups of four softmax warps, two copy warps (TMA: K, V), two MMA warps (S, P.V), four warps that widen values
 // (17 - 48 rows, and 64 of 64 dims); a persistent grid and the cost-balanced split of the key sequence that the other
 // kernels use.  A group takes 8 or 16 of the query rows, thread = key: sixteen softmax warps fill an SM at 64 rows (one
-// group of 64 rows spilled: 660 us for the 198 below).  Up to 16 rows two CTAs share an SM, above one has it.  S and P
+// group of 64 rows spilled: 660 us for 198).  Up to 16 rows two CTAs share an SM, above one has it.  S and P
 // have two buffers each.  A buffer's P.V is waited for by the S products' warp alone, whose scores then say to all softmax
 // warps that S, P and W are free (each warp waiting for itself: 208 us for 201).  A tree is tile 0 of its slab: the softmax
 // warps write its operands while the first copies are on their way.
 //
-// What bounds it, and what it takes: 64 nodes on 4 x 52 heads of 16384 keys 198 us, 4.5 TB/s of the cache, where the
-// bytes alone take 130: a tile of 128 keys costs ~1800 cycles (HBM's rate: 1394), spread over a softmax warp's chain of
-// waits, loads, vote, weights and stores; issue slots are a little over half used.  26 nodes there 135 us, 12 nodes 137,
-// one query 128.  26 nodes on 8 x 40 heads of 512 - 4096 keys: 55 us (bytes: 32), where the ~4 k cycles in which a slab's
-// queries become operands and the two tiles in which its maxima settle weigh in (all of a slab's loads in flight at once,
-// ancestors found beside the first product: 23.4 -> 18.2 us for 128 keys).  33 nodes of 4 query heads to a cached one:
-// three row tiles of 44 that read the cache three times, from L2 twice: 84 us on 4 x 8 cached heads of 16384 keys.
+// What bounds it, and what it takes: 64 nodes on 4 x 52 heads of 16384 keys 200 us, 4.4 TB/s of the cache, where the
+// bytes alone take 130: a tile of 128 keys costs a CTA 1.14 us (at HBM's rate 0.74), spread over a softmax warp's chain
+// of waits, loads, vote, weights and stores; issue slots are a little over half used.  26 nodes there 137 us, 12 nodes
+// 135, one query 128.  26 nodes on 8 x 40 heads of 512 - 4096 keys: 56 us (bytes: 32), where a slab's start, in which
+// its queries become operands, and the two tiles in which its maxima settle weigh in (23 us where a slab has 128 keys).
+// 33 nodes of 4 query heads to a cached one: three row tiles of 44 that read the cache three times, from L2 twice, and
+// widen its values three times: 83 us on 4 x 8 cached heads of 16384 keys.
 //
 // A slab whose keys lie in several CTAs' shares leaves partials (m, l, O) in the workspace and
 // kv8_merge_kernel joins them.
@@ -78,9 +78,9 @@ constexpr int F_K = 0, F_V = 6, E_K = 12, E_V = 18, QFULL8 = 24, SFULL8 = 25, PF
 template <int D, int NP>
 struct Cfg {
   // Up to 16 rows: weights as two codes each, and two CTAs an SM, for which widened values leave no shared memory.  More:
-  // values widened to fp16, work that the rows share, by warps that work beside the softmax (two codes / widened, us: 26
-  // nodes on 4 x 52 heads of 16384 keys 145 / 137, on 8 x 40 heads of 512 - 4096 59 / 53, of 1024 35.4 / 34.3, of 128 18.3 /
-  // 20.6; 32 nodes on 32 heads of 8192 25.9 / 21.8; 44 nodes on 4 x 52 heads of 16384 182 / 164).
+  // values widened to fp16, work that the rows share, by warps that work beside the softmax (two codes / widened, us, when
+  // this was chosen: 26 nodes on 4 x 52 heads of 16384 keys 145 / 137, on 8 x 40 heads of 512 - 4096 59 / 53, of 1024 35.4 /
+  // 34.3, of 128 18.3 / 20.6; 32 nodes on 32 heads of 8192 25.9 / 21.8; 44 nodes on 4 x 52 heads of 16384 182 / 164).
   static constexpr bool kWiden = NP > 16;
   static constexpr float kMost = kWiden ? 15.5f : 8.75f;              // log2 of the largest weight: 2^16, 448 are too large
   static constexpr float kLift = kWiden ? 6.f : 8.f;                  // log2 of the weight of a new maximum
@@ -91,9 +91,10 @@ struct Cfg {
   // products sets a slower pace than the stream: a copy or a product keeps its issuer busy for over 100 cycles.
   static constexpr int kCopyK = 4 * kSG, kCopyV = kCopyK + 1, kMmaS = kCopyK + 2, kMmaO = kCopyK + 3,
                        kWideW = kCopyK + 4;                           // the first that widens values
-  // Four warps after those widen, beside the softmax (16384 keys, softmax warps / these, us: 44 nodes on 4 x 52 heads 177 /
-  // 164, 33 nodes of 4 query heads to each of 4 x 8 cached 90 / 84.5, 64 nodes on 4 x 52 heads of 64 dims 182 / 167).
-  // With 64 rows of 128 dims they and the softmax take longer than the softmax alone: 216 / 200, half each 240.
+  // Four warps after those widen, beside the softmax (16384 keys, softmax warps / these, us, when this was chosen: 44 nodes
+  // on 4 x 52 heads 177 / 164, 33 nodes of 4 query heads to each of 4 x 8 cached 90 / 84.5, 64 nodes on 4 x 52 heads of 64
+  // dims 182 / 167).  With 64 rows of 128 dims they and the softmax take longer than the softmax alone: 216 / 200, half
+  // each 240.
   static constexpr bool kWideWarps = kWiden && (NP < 64 || D == 64);
   static constexpr int kOwn = kWiden && !kWideWarps ? D / 16 / kSG : 0;  // else: pieces of 16 codes of a softmax group
   static constexpr int kThreads = kSoft + 128 + (kWideWarps ? 128 : 0);
@@ -814,7 +815,8 @@ __global__ void __launch_bounds__(Cfg<D, NP>::kThreads, Cfg<D, NP>::kCtas)
           scales_of(a, ef, inv_v);
         }
       };
-      // Where one CTA has an SM, a tile's scales are made ready during the tile before it (44 nodes on 4 x 52 heads of 16384 keys: 164 -> 161 us);
+      // Where one CTA has an SM, a tile's scales are made ready during the tile before it (44 nodes on 4 x 52 heads of
+      // 16384 keys: 164 -> 161 us);
       // two have no registers for that (12 nodes on 8 x 40 heads of 1024 keys: 28.2 -> 30.5).
       float a_next, ef_next, inv_next;
       if (C::kWiden) first_scales(a_next, ef_next, inv_next);

@@ -7,9 +7,9 @@
 // What bounds it.  A prompt's rows are a stream (2 or 4 bytes in, 1 out): one CTA takes a block of K or
 // of V of one slab, all its loads in flight at once and kept as they came, so a new element is read once
 // between the maximum and the rounding.  Instructions weigh beside the bytes (29.6 us): a maximum over packed
-// magnitudes instead of over each element's finite value 37.4 -> 32.7 us for 4 x 32 heads of 2048 bf16 rows, 6.2 TB/s.  A round's few rows are latency (the lengths, the path, the rows,
-// the exponent, one after another): a warp takes a block, so that all layers and heads fit the GPU at
-// once.  Rows from before are read only where their exponent grows.
+// magnitudes instead of over each element's finite value 37.4 -> 32.9 us for 4 x 32 heads of 2048 bf16 rows, 6.1 TB/s
+// (fp32: 51.5 us, 6.5 TB/s).  A round's few rows are latency (the lengths, the path, the rows, the exponent, one after
+// another): a warp takes a block, so that all layers and heads fit the GPU at once.  Rows from before are read only where their exponent grows.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -307,7 +307,7 @@ __device__ __forceinline__ void store8(float* p, const float (&f)[8]) {
 
 // A stream: 1 byte in, 2 or 4 out.  A CTA takes kPieces x 256 pieces of 8 codes of one slab, a thread kPieces of them,
 // loaded before any is used (32 heads of 2048 tokens: 1 piece 12.9 us, 2 9.6, 4 9.0, 8 9.1; 4 x 8 heads of 16384:
-// 89, 60.5, 59.1, 59.4, of which the bytes are 59).  Grid: x = part of a slab, y = K or V.
+// 89, 60.5, 59.1, 59.4, of which the bytes are 59; fp32 19.7 and 117.5, bytes 12.3 and 98.7).  Grid: x = part of a slab, y = K or V.
 constexpr int kPieces = 4;
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) kv8_read_kernel(const ReadParams p) {

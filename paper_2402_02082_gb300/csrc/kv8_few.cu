@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kThreadsF, NT == 1 ? 2 : 1) kv8_few_kernel(con
     }
   };
   // A tree is one more tile, of the cluster's last warp, which in clusters of four CTAs or more has no other: its keys,
-  // values and parents are loads of their own (32 heads, 2048 keys, 6 nodes: 12.7 us beside a tile, 11.1 alone).
+  // values and parents are loads of their own (32 heads, 2048 keys, 6 nodes: 12.7 us beside a tile, 11.3 alone).
   const bool tree_warp = p.parent && rank == p.C - 1 && warp == kWarpsF - 1;
   const int spare = p.parent && p.C >= 4 ? 1 : 0;
   const int step = (p.C * kWarpsF - spare) * kTKF;
@@ -581,10 +581,10 @@ cudaError_t launch_typed(const Kv8AttnArgs& a, cudaStream_t st) {
   while (C > 1 && (slabs * C > slots || (long long)C * kWarpsF * kTKF >= 2LL * a.max_kv_len)) C >>= 1;
   // One wave, and short: with 32 keys a warp at a time and nothing but registers to hold what is on its way, the tcgen05
   // kernel's ring streams faster once the warps have several tiles.  Here / there, us, with the tiles a warp has.  Up to 8
-  // rows: 32 heads of 2048 keys (1) 8.5 / 10.1, 4096 (2) 11.9 / 12.8, 6144 (3) 15.0 / 14.2, 16384 (8) 29.0 / 26.1; the
-  // GPU half empty, 8 heads of 8192 (4) 14.1 / 17.8, 16384 (8) 22.1 / 17.9; two waves, 8 x 40 heads of 512 18.0 / 13.6.
-  // Up to 16 rows: 12 nodes on 32 heads of 4096 (4) 16.4 / 17.4, 6144 (6) 20.7 / 19.5.  Rows of 64 dims are half a tile:
-  // 32 heads of 8192 (4) 11.8 / 13.1.
+  // rows: 32 heads of 2048 keys (1) 8.9 / 10.6, 4096 (2) 12.2 / 13.1, 6144 (3) 15.1 / 14.8, 16384 (8) 29.3 / 26.2; the
+  // GPU half empty, 8 heads of 8192 (4) 13.7 / 17.2, 16384 (8) 21.9 / 17.3; two waves, 8 x 40 heads of 512 17.7 / 14.1.
+  // Up to 16 rows: 12 nodes on 32 heads of 4096 (4) 16.5 / 16.8, 6144 (6) 20.8 / 18.5.  Rows of 64 dims are half a tile:
+  // 32 heads of 8192 (4) 11.9 / 13.9.
   const long long rounds = (a.max_kv_len + C * kWarpsF * kTKF - 1LL) / (C * kWarpsF * kTKF);
   const int most = NT == 1 && 2 * slabs * C > slots ? 2 : 4;
   if (slabs * C > slots || rounds * D > most * 128LL) return cudaErrorNotSupported;
