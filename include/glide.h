@@ -27,6 +27,10 @@
  *                      accepted path's keys/values become contiguous rows.
  *   glide_kv8_*        the same round on a cache held in 8 bits: append (quantise on
  *                      write), read back, cross-attention and verification.
+ *   glide_page_plan, glide_paged_append, glide_paged_attn, glide_prompt_attn
+ *                      the target's own step over a cache held in pages: page tables and slots
+ *                      from request lengths, new keys/values into their slots, attention of chunks
+ *                      of new tokens over the pages, attention of whole packed prompts.
  *   spec_sample_accept speculative-sampling acceptance of a chain proposal
  *                      (Section 2's other acceptance strategy, used for GliDe
  *                      alone in Section 4.1), with caller-supplied uniforms.
@@ -459,6 +463,105 @@ glide_status glide_kv8_verify_attn(const glide_attn_desc* desc, const void* q_tr
                                    const int32_t* parent_idx, const void* k_tree, const void* v_tree,
                                    const glide_kv8_cache* cache, const int32_t* kv_len, int32_t max_kv_len,
                                    void* out, void* workspace, size_t workspace_bytes, glide_stream_t stream);
+
+/* ------------------------------------------------------------------ cache in pages
+ * A serving program fills the target's cache and runs the target's own steps on it: prompts,
+ * chunks of prompts, chain proposals and single tokens of many requests of different lengths in
+ * one call (the paper takes the cache as given; Section 4 measures on ragged batches).  Requests
+ * grow at different rates, so the cache lies in pages that any request may hold:
+ *     K, V          [n_pages, H_kv, page_size, D]; page_size 16, 32, 64, 128 or 256
+ *     block_table   [B, table_width] int32: token t of request b is row t % page_size of page
+ *                   block_table[b, t / page_size]
+ *     slot          page * page_size + row, a token's place in every layer's pool
+ * New tokens of a step are packed, request behind request, without padding between them:
+ *     cu_q          [B + 1] int32: request b's new tokens are rows cu_q[b] .. cu_q[b+1]-1 of the
+ *                   step's T rows; rows at and past cu_q[B] are padding
+ *     q, k, v       [T, heads, D] with `stride` elements from token to token (a multiple of 16
+ *                   bytes, at least heads * D): parts of a fused projection's rows, as they are
+ * Entries of tables, offsets and lengths that lie outside their ranges are taken as the nearest
+ * inside, as everywhere in this header.
+ */
+typedef struct {
+  void* K;            /* [n_pages, H_kv, page_size, D], 16-byte aligned */
+  void* V;
+  int32_t n_pages;    /* n_pages * page_size <= 2^31 - 1 */
+  int32_t page_size;  /* 16, 32, 64, 128 or 256 (others: GLIDE_ERR_UNSUPPORTED) */
+} glide_page_pool;
+
+/*
+ * The tables of a step, from the requests' lengths, without the host:
+ *   q_len[b]   new tokens of request b in this step (0: none; below 0: the request has finished)
+ *   kv_len[b]  its tokens in the cache, held[b] its pages (the first held[b] entries of its row)
+ *   free_pages [free_cap]: a stack of unused pages, n_free[0] of them, the last on top
+ * Pages of finished requests go on top of the stack, in the requests' order and in a row's order
+ * (what free_cap has no room for is dropped).  Then every live request, in order, gets the pages
+ * that it needs, need = max(0, ceil((kv_len + m) / page_size) - held) where m > 0, from the top of
+ * the stack down, m its tokens among the step's T rows.  A request whose table row is too short for
+ * kv_len + m tokens gets none and is left out; so is one that needs pages when the stack has not enough for all
+ * that it and the requests before it ask for.
+ * Outputs: block_table and free_pages are updated in place.  cu_q [B + 1]: min(T, the new tokens
+ * of the requests before b), whether admitted or not.  slots [T]: where each new token's key and
+ * value go, -1 for the tokens of a request that is left out and for padding.  positions [T] (or
+ * NULL): the token's index in its request, 0 for padding.  new_kv_len, new_held [B]: with the
+ * admitted tokens and the pages got; 0 for a finished request.  new_n_free [1].
+ * Nothing written may overlap anything else (new_kv_len is not kv_len): GLIDE_ERR_INVALID.
+ * 1 <= B <= 1024, 0 <= T, 1 <= table_width, 1 <= free_cap; all int32 on the device.  No workspace.
+ */
+glide_status glide_page_plan(int32_t B, int32_t T, int32_t page_size, int32_t table_width, const int32_t* q_len,
+                             const int32_t* kv_len, const int32_t* held, int32_t* block_table, int32_t* free_pages,
+                             int32_t free_cap, const int32_t* n_free, int32_t* cu_q, int32_t* slots,
+                             int32_t* positions, int32_t* new_kv_len, int32_t* new_held, int32_t* new_n_free,
+                             glide_stream_t stream);
+
+/*
+ * New keys and values into one layer's pool: for every i < T with 0 <= slots[i] < n_pages * page_size,
+ *   K[slots[i] / page_size, h, slots[i] % page_size, :] = k_new[i, h, :]   (V the same)
+ * Tokens with other slots go nowhere; other rows keep their contents.  Slots of a call differ
+ * (of rows with the same slot, any may be kept, in parts).
+ * desc: H, H_kv, D, dtype (the other fields are ignored).  k_new [T, H_kv, D], k_stride elements from
+ * token to token, v_new likewise; they do not overlap the pool.  0 <= T.  No workspace.
+ */
+glide_status glide_paged_append(const glide_attn_desc* desc, const glide_page_pool* pool, const void* k_new,
+                                const void* v_new, int64_t k_stride, int64_t v_stride, int32_t T,
+                                const int32_t* slots, glide_stream_t stream);
+
+/* Bytes of workspace that glide_paged_attn (and glide_prompt_attn, with max_q = max_len) need
+ * for steps of up to T rows and max_q new tokens of a request; 0 if the descriptor is invalid.  A
+ * buffer sized for the largest T and max_q serves every smaller step. */
+size_t glide_paged_workspace_bytes(const glide_attn_desc* desc, int32_t T, int32_t max_q);
+
+/*
+ * Attention of new tokens over the pages, the new tokens' own keys and values (written before) among
+ * them: row i of a request's m = cu_q[b+1] - cu_q[b] new tokens sees its keys t <= kv_len[b] - m + i,
+ *   out[cu_q[b] + i, h, :] = SoftMax(q . K[t, h / (H / H_kv)] * scale) V[t, h / (H / H_kv)]
+ * kv_len counts the new tokens.  m = 1 is a decoding step, m > 1 a chunk of a prompt or a chain
+ * proposal; a call may mix them.  A row that sees nothing (kv_len < m) gets zeros.
+ * q [T, H, D] with q_stride; out [T, H, D] of desc->dtype, dense (one rounding of fp32 results).
+ * Rows of out behind cu_q[B], and rows of a request past its first max_q, are left as they were.
+ * max_q, max_kv_len: bounds of m and kv_len on the host; 1 <= max_q, 0 <= max_kv_len <=
+ * table_width * page_size.  desc: B, H, H_kv, D, dtype, scale, flags (GLIDE_FLAG_FORCE_FMA takes the CUDA-core
+ * kernel); S_cap and max_ctas are ignored.
+ * What is not finite has the definition's result: what a row does not see never reaches it, whatever it
+ * holds; a score that is NaN or +inf makes its row NaN, one of -inf has no weight, and a value that is not finite
+ * decides its column in the rows that see it.  bf16: weights are rounded to bf16 for the product with the values.
+ */
+glide_status glide_paged_attn(const glide_attn_desc* desc, const void* q, int64_t q_stride, int32_t T,
+                              const int32_t* cu_q, int32_t max_q, const glide_page_pool* pool,
+                              const int32_t* block_table, int32_t table_width, const int32_t* kv_len,
+                              int32_t max_kv_len, void* out, void* workspace, size_t workspace_bytes,
+                              glide_stream_t stream);
+
+/*
+ * Causal attention of whole prompts over themselves, packed one behind the other: row i of sequence b
+ * (rows cu[b] .. cu[b+1]-1) sees the sequence's rows 0 .. i.
+ * q [T, H, D], k and v [T, H_kv, D] with their strides; out [T, H, D] of desc->dtype, dense.
+ * max_len: bound of the lengths on the host, 1 <= max_len.  Rows past a sequence's first max_len, and rows at and past cu[B],
+ * are left as they were.  Everything else as in glide_paged_attn.
+ */
+glide_status glide_prompt_attn(const glide_attn_desc* desc, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, int32_t T, const int32_t* cu,
+                               int32_t max_len, void* out, void* workspace, size_t workspace_bytes,
+                               glide_stream_t stream);
 
 /*
  * Host-side check of a parent array (HOST memory, [B,n]): every entry is -1 or

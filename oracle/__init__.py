@@ -29,9 +29,13 @@ It is a plain, slow, fp64 restatement of what the path computes:
 * ``kv8.kv8_append``, ``kv8.kv8_read``, ``kv8.kv8_attn`` -- the cache in 8 bits with
   a power-of-two scale per block of 64 tokens and head (not in the paper): rows
   quantised as they join it, read back, and both attentions over it.
+* ``paged.page_plan``, ``paged.append``, ``paged.attend`` -- the cache in pages (not in
+  the paper): a step's page tables and slots, rows into their slots, attention of
+  packed rows of new tokens.
 
 Every function here is pinned by tests in ``tests/test_oracle.py`` (the 8-bit
-cache's in ``tests/test_kv8_oracle.py``) against
+cache's in ``tests/test_kv8_oracle.py``, the paged cache's in
+``tests/test_paged_oracle.py``) against
 closed forms, library routines, brute force and invariants; none is marked
 "parity unpinned".
 """
@@ -39,10 +43,11 @@ from .attention import (ancestors_or_self, block_cross_attn, block_mask, cape_ma
                         tree_allowed_mask, tree_verify_attn, widen)
 from .accept import row_argmax, tree_accept
 from .cape import cape_expand, expansion_size
+from . import paged
 from .kv8 import kv8_append, kv8_attn, kv8_read
 from .kvcache import kv_compact
 from .sampling import spec_sample_accept
 
 __all__ = ["ancestors_or_self", "block_cross_attn", "block_mask", "cape_mask", "cross_attn", "tree_allowed_mask",
            "tree_verify_attn", "widen", "row_argmax", "tree_accept", "cape_expand", "expansion_size", "kv_compact",
-           "kv8_append", "kv8_attn", "kv8_read", "spec_sample_accept"]
+           "paged", "kv8_append", "kv8_attn", "kv8_read", "spec_sample_accept"]

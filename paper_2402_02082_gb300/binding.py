@@ -56,6 +56,10 @@ class Kv8Cache(ctypes.Structure):
     _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("K_exp", ctypes.c_void_p), ("V_exp", ctypes.c_void_p)]
 
 
+class PagePool(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
 _P = ctypes.c_void_p
 _SIG = {
     "glide_abi_version": (ctypes.c_int32, []),
@@ -93,6 +97,16 @@ _SIG = {
     "glide_kv8_verify_attn": (ctypes.c_int, [ctypes.POINTER(AttnDesc), _P, ctypes.c_int32, _P, _P, _P,
                                              ctypes.POINTER(Kv8Cache), _P, ctypes.c_int32, _P, _P, ctypes.c_size_t,
                                              _P]),
+    "glide_page_plan": (ctypes.c_int, [ctypes.c_int32] * 4 + [_P] * 5 + [ctypes.c_int32] + [_P] * 8),
+    "glide_paged_append": (ctypes.c_int, [ctypes.POINTER(AttnDesc), ctypes.POINTER(PagePool), _P, _P, ctypes.c_int64,
+                                          ctypes.c_int64, ctypes.c_int32, _P, _P]),
+    "glide_paged_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(AttnDesc), ctypes.c_int32, ctypes.c_int32]),
+    "glide_paged_attn": (ctypes.c_int, [ctypes.POINTER(AttnDesc), _P, ctypes.c_int64, ctypes.c_int32, _P,
+                                        ctypes.c_int32, ctypes.POINTER(PagePool), _P, ctypes.c_int32, _P,
+                                        ctypes.c_int32, _P, _P, ctypes.c_size_t, _P]),
+    "glide_prompt_attn": (ctypes.c_int, [ctypes.POINTER(AttnDesc), _P, ctypes.c_int64, _P, ctypes.c_int64, _P,
+                                         ctypes.c_int64, ctypes.c_int32, _P, ctypes.c_int32, _P, _P, ctypes.c_size_t,
+                                         _P]),
     "spec_sample_accept": (ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P,
                                           _P, ctypes.c_size_t, _P]),
 }
@@ -568,6 +582,169 @@ def glide_kv8_verify_attn(q_tree: torch.Tensor, parent_idx: torch.Tensor, k_tree
                                      int(max_kv_len), out.data_ptr(), workspace.data_ptr(),
                                      workspace.numel() * workspace.element_size(), _stream(stream))
     _check(st, "glide_kv8_verify_attn")
+    return out
+
+
+# ------------------------------------------------------------------ cache in pages
+def _on_current_gpu(*tensors):
+    """The calls launch on the current device: tensors of another one are refused."""
+    for t in tensors:
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError("tensors must be on the current GPU")
+
+
+def _paged_ints(t: torch.Tensor, shape, what: str):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise TypeError(f"{what} must be contiguous int32 {list(shape)}")
+
+
+def _token_rows(t: torch.Tensor, what: str) -> int:
+    """The elements from token to token of [T, heads, D], heads and elements dense."""
+    if t.dim() != 3:
+        raise ValueError(f"{what} must be [T, heads, D]")
+    T, heads, D = t.shape
+    if heads < 1 or D < 1 or (D > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != D):
+        raise ValueError(f"{what}'s heads must lie densely behind one another")
+    return t.stride(0) if T > 1 else heads * D
+
+
+def _page_pool(K: torch.Tensor, V: torch.Tensor):
+    if K.dim() != 4 or V.shape != K.shape or V.dtype != K.dtype:
+        raise ValueError("K and V must be [n_pages, H_kv, page_size, D] of one type")
+    if not (K.is_contiguous() and V.is_contiguous()):
+        raise ValueError("K and V must be contiguous")
+    _on_current_gpu(K, V)
+    return PagePool(K.data_ptr(), V.data_ptr(), K.shape[0], K.shape[2])
+
+
+def _rows_out(q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor):
+    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out must be contiguous and of q's shape and type")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+
+
+def glide_paged_workspace_bytes(desc: AttnDesc, T: int, max_q: int) -> int:
+    return int(lib().glide_paged_workspace_bytes(ctypes.byref(desc), int(T), int(max_q)))
+
+
+def glide_page_plan(q_len: torch.Tensor, kv_len: torch.Tensor, held: torch.Tensor, block_table: torch.Tensor,
+                    free_pages: torch.Tensor, n_free: torch.Tensor, page_size: int, cu_q: torch.Tensor,
+                    slots: torch.Tensor, new_kv_len: torch.Tensor, new_held: torch.Tensor, new_n_free: torch.Tensor,
+                    positions: Optional[torch.Tensor] = None, stream=None):
+    """(cu_q [B+1], slots [T], new_kv_len [B], new_held [B], new_n_free [1]) and, updated in place, block_table
+    [B, width] and free_pages [cap] <- the pages and slots of a step in which request b adds q_len[b] tokens (below
+    0: it has finished) to its kv_len[b] in held[b] pages.  All int32; positions [T] is written if given."""
+    st = (_CALL or _native()).page_plan(q_len, kv_len, held, block_table, free_pages, n_free, page_size, cu_q, slots,
+                                        new_kv_len, new_held, new_n_free, positions, stream)
+    if st != GLIDE_OK:
+        if st > 0:
+            raise GlideError(st, "glide_page_plan")
+        if block_table.dim() != 2 or free_pages.dim() != 1 or slots.dim() != 1:
+            raise ValueError("block_table must be [B, width], free_pages [cap], slots [T]")
+        (B, width), T = block_table.shape, slots.shape[0]
+        for t, shape, what in ((q_len, (B,), "q_len"), (kv_len, (B,), "kv_len"), (held, (B,), "held"),
+                               (block_table, (B, width), "block_table"), (free_pages, tuple(free_pages.shape), "free_pages"),
+                               (n_free, (1,), "n_free"), (cu_q, (B + 1,), "cu_q"), (slots, (T,), "slots"),
+                               (new_kv_len, (B,), "new_kv_len"), (new_held, (B,), "new_held"),
+                               (new_n_free, (1,), "new_n_free")) + \
+                (((positions, (T,), "positions"),) if positions is not None else ()):
+            _paged_ints(t, shape, what)
+            _on_current_gpu(t)
+        st = lib().glide_page_plan(B, T, int(page_size), width, q_len.data_ptr(), kv_len.data_ptr(), held.data_ptr(),
+                                   block_table.data_ptr(), free_pages.data_ptr(), free_pages.shape[0],
+                                   n_free.data_ptr(), cu_q.data_ptr(), slots.data_ptr(),
+                                   positions.data_ptr() if positions is not None else None, new_kv_len.data_ptr(),
+                                   new_held.data_ptr(), new_n_free.data_ptr(), _stream(stream))
+        _check(st, "glide_page_plan")
+    return cu_q, slots, new_kv_len, new_held, new_n_free
+
+
+def glide_paged_append(k_new: torch.Tensor, v_new: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
+                       slots: torch.Tensor, stream=None):
+    """K, V [n_pages, H_kv, page_size, D], in place <- rows k_new, v_new [T, H_kv, D] (any stride between tokens)
+    at slots [T] int32 (page * page_size + row; outside the pool: nowhere)."""
+    st = (_CALL or _native()).paged_append(k_new, v_new, K, V, slots, stream)
+    if st != GLIDE_OK:
+        if st > 0:
+            raise GlideError(st, "glide_paged_append")
+        pool = _page_pool(K, V)
+        ks, vs = _token_rows(k_new, "k_new"), _token_rows(v_new, "v_new")
+        T = k_new.shape[0]
+        for t in (k_new, v_new):
+            if tuple(t.shape) != (T, K.shape[1], K.shape[3]) or t.dtype != K.dtype:
+                raise ValueError("k_new and v_new must be [T, H_kv, D] of the pool's sizes and type")
+        _paged_ints(slots, (T,), "slots")
+        _on_current_gpu(k_new, v_new, slots)
+        desc = make_desc(1, K.shape[1], K.shape[3], 1, _dtype_code(K))
+        st = lib().glide_paged_append(ctypes.byref(desc), ctypes.byref(pool), k_new.data_ptr(), v_new.data_ptr(), ks, vs,
+                                      T, slots.data_ptr(), _stream(stream))
+        _check(st, "glide_paged_append")
+    return K, V
+
+
+def glide_paged_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, block_table: torch.Tensor, cu_q: torch.Tensor,
+                     max_q: int, kv_len: torch.Tensor, max_kv_len: int, out: torch.Tensor, workspace: torch.Tensor,
+                     scale: float = 0.0, flags: int = 0, stream=None) -> torch.Tensor:
+    """out [T, H, D] (q's type) <- attention of the packed new tokens q [T, H, D] (any stride between tokens), rows
+    cu_q[b] .. cu_q[b+1]-1 of request b, over its kv_len[b] tokens (the new ones among them) in the pages that
+    block_table [B, width] names of K, V [n_pages, H_kv, page_size, D]: a token sees those up to itself."""
+    st = (_CALL or _native()).paged_attn(q, K, V, block_table, cu_q, max_q, kv_len, max_kv_len, out, workspace, scale,
+                                         flags, stream)
+    if st == GLIDE_OK:
+        return out
+    if st > 0:
+        raise GlideError(st, "glide_paged_attn")
+    pool = _page_pool(K, V)
+    stride = _token_rows(q, "q")
+    if q.shape[2] != K.shape[3] or q.dtype != K.dtype:
+        raise ValueError("q must be [T, H, D] of the pool's D and type")
+    _rows_out(q, out, workspace)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, width]")
+    B, width = block_table.shape
+    _paged_ints(block_table, (B, width), "block_table")
+    _paged_ints(cu_q, (B + 1,), "cu_q")
+    _paged_ints(kv_len, (B,), "kv_len")
+    _on_current_gpu(q, block_table, cu_q, kv_len, out, workspace)
+    T, H, D = q.shape
+    H_kv = K.shape[1]
+    desc = make_desc(B, H, D, 1, _dtype_code(K), scale, flags, H_kv=H_kv if H_kv != H else 0)
+    st = lib().glide_paged_attn(ctypes.byref(desc), q.data_ptr(), stride, T, cu_q.data_ptr(), int(max_q),
+                                ctypes.byref(pool), block_table.data_ptr(), width, kv_len.data_ptr(), int(max_kv_len),
+                                out.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                _stream(stream))
+    _check(st, "glide_paged_attn")
+    return out
+
+
+def glide_prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, max_len: int,
+                      out: torch.Tensor, workspace: torch.Tensor, scale: float = 0.0, flags: int = 0,
+                      stream=None) -> torch.Tensor:
+    """out [T, H, D] (q's type) <- causal attention of packed prompts: rows cu[b] .. cu[b+1]-1 of q [T, H, D] and of
+    k, v [T, H_kv, D] (any stride between tokens) are sequence b, whose row i sees its rows 0 .. i."""
+    st = (_CALL or _native()).prompt_attn(q, k, v, cu, max_len, out, workspace, scale, flags, stream)
+    if st == GLIDE_OK:
+        return out
+    if st > 0:
+        raise GlideError(st, "glide_prompt_attn")
+    qs, ks, vs = _token_rows(q, "q"), _token_rows(k, "k"), _token_rows(v, "v")
+    T, H, D = q.shape
+    H_kv = k.shape[1]
+    for t in (k, v):
+        if tuple(t.shape) != (T, H_kv, D) or t.dtype != q.dtype:
+            raise ValueError("k and v must be [T, H_kv, D] of q's T, D and type")
+    _rows_out(q, out, workspace)
+    if cu.dim() != 1 or cu.shape[0] < 2:
+        raise ValueError("cu must be [B + 1]")
+    B = cu.shape[0] - 1
+    _paged_ints(cu, (B + 1,), "cu")
+    _on_current_gpu(q, k, v, cu, out, workspace)
+    desc = make_desc(B, H, D, 1, _dtype_code(q), scale, flags, H_kv=H_kv if H_kv != H else 0)
+    st = lib().glide_prompt_attn(ctypes.byref(desc), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, T,
+                                 cu.data_ptr(), int(max_len), out.data_ptr(), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "glide_prompt_attn")
     return out
 
 

@@ -9,6 +9,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "kv8.h"
+#include "paged.h"
 
 namespace {
 
@@ -366,6 +367,164 @@ glide_status glide_kv8_verify_attn(const glide_attn_desc* desc, const void* q_tr
   if (n < 1 || n > glide::kMaxTree || !parent_idx || !k_tree || !v_tree) return GLIDE_ERR_INVALID;
   return kv8_attention(desc, q_tree, n, parent_idx, k_tree, v_tree, cache, kv_len, max_kv_len, out, workspace,
                        workspace_bytes, stream);
+}
+
+// ---------------------------------------------------------------- cache in pages
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static bool page_size_ok(int P) { return P == 16 || P == 32 || P == 64 || P == 128 || P == 256; }
+static int log2_of(int x) {
+  int s = 0;
+  while ((1 << s) < x) ++s;
+  return s;
+}
+static size_t elt_size(const glide_attn_desc* d) { return d->dtype == GLIDE_BF16 ? 2 : 4; }
+
+// A descriptor of which S_cap (and B, where a call has none) says nothing.
+static bool rows_desc(const glide_attn_desc* in, bool has_batch, glide_attn_desc* out) {
+  if (!in) return false;
+  *out = *in;
+  out->S_cap = 1;
+  out->max_ctas = 0;
+  if (!has_batch) {
+    out->B = 1;
+    out->scale = 0.f;
+  }
+  return desc_ok(out);
+}
+// Elements from token to token of rows with `heads` heads.
+static bool stride_ok(const glide_attn_desc* d, int64_t stride, int heads, int32_t T) {
+  if (stride < (int64_t)heads * d->D || (stride * elt_size(d)) % 16 != 0) return false;
+  return (double)T * (double)stride <= 1.0e18;
+}
+
+struct Range {
+  const void* at;
+  size_t bytes;
+  bool meets(const Range& o) const {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(at), b = reinterpret_cast<uintptr_t>(o.at);
+    return bytes > 0 && o.bytes > 0 && a < b + o.bytes && b < a + bytes;
+  }
+};
+
+glide_status glide_page_plan(int32_t B, int32_t T, int32_t page_size, int32_t table_width, const int32_t* q_len,
+                             const int32_t* kv_len, const int32_t* held, int32_t* block_table, int32_t* free_pages,
+                             int32_t free_cap, const int32_t* n_free, int32_t* cu_q, int32_t* slots,
+                             int32_t* positions, int32_t* new_kv_len, int32_t* new_held, int32_t* new_n_free,
+                             glide_stream_t stream) {
+  if (B < 1 || B > glide::kMaxBatch || T < 0 || table_width < 1 || free_cap < 1) return GLIDE_ERR_INVALID;
+  if (!page_size_ok(page_size) || (long long)B * table_width > 0x7fffffffLL) return GLIDE_ERR_UNSUPPORTED;
+  if (!q_len || !kv_len || !held || !block_table || !free_pages || !n_free || !cu_q || (!slots && T > 0) ||
+      !new_kv_len || !new_held || !new_n_free)
+    return GLIDE_ERR_INVALID;
+  const size_t n = (size_t)B * 4;
+  const Range r[] = {{q_len, n}, {kv_len, n}, {held, n}, {n_free, 4},  // read only
+                     {block_table, n * (size_t)table_width}, {free_pages, (size_t)free_cap * 4}, {cu_q, n + 4},
+                     {slots, (size_t)T * 4}, {positions, positions ? (size_t)T * 4 : 0}, {new_kv_len, n}, {new_held, n},
+                     {new_n_free, 4}};
+  const int count = sizeof(r) / sizeof(r[0]);
+  for (int i = 0; i < count; ++i) {
+    if (!aligned4(r[i].at)) return GLIDE_ERR_INVALID;
+    for (int j = i + 1; j < count; ++j)
+      if (j >= 4 && r[i].meets(r[j])) return GLIDE_ERR_INVALID;
+  }
+  glide::PlanArgs a;
+  a.q_len = q_len; a.kv_len = kv_len; a.held = held; a.n_free = n_free; a.table = block_table; a.free_pages = free_pages;
+  a.cu_q = cu_q; a.slots = slots; a.positions = positions; a.new_kv_len = new_kv_len; a.new_held = new_held;
+  a.new_n_free = new_n_free; a.B = B; a.T = T; a.P = page_size; a.W = table_width; a.free_cap = free_cap;
+  return from_cuda(glide::launch_page_plan(a, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+static glide_status pool_status(const glide_page_pool* pool, const glide_attn_desc* d) {
+  if (!pool || !pool->K || !pool->V || !aligned16(pool->K) || !aligned16(pool->V)) return GLIDE_ERR_INVALID;
+  if (pool->n_pages < 1) return GLIDE_ERR_INVALID;
+  if (!page_size_ok(pool->page_size)) return GLIDE_ERR_UNSUPPORTED;
+  if ((long long)pool->n_pages * pool->page_size > 0x7fffffffLL) return GLIDE_ERR_INVALID;
+  if ((double)pool->n_pages * pool->page_size * hkv(d) * d->D > 1.0e18) return GLIDE_ERR_INVALID;
+  return GLIDE_OK;
+}
+
+glide_status glide_paged_append(const glide_attn_desc* desc, const glide_page_pool* pool, const void* k_new,
+                                const void* v_new, int64_t k_stride, int64_t v_stride, int32_t T,
+                                const int32_t* slots, glide_stream_t stream) {
+  glide_attn_desc d;
+  if (!rows_desc(desc, false, &d) || T < 0) return GLIDE_ERR_INVALID;
+  const glide_status ps = pool_status(pool, &d);
+  if (ps != GLIDE_OK) return ps;
+  if (!stride_ok(&d, k_stride, hkv(&d), T) || !stride_ok(&d, v_stride, hkv(&d), T)) return GLIDE_ERR_INVALID;
+  if (T == 0) return GLIDE_OK;
+  if (!k_new || !v_new || !slots || !aligned16(k_new) || !aligned16(v_new) || !aligned4(slots)) return GLIDE_ERR_INVALID;
+  const size_t row = (size_t)hkv(&d) * d.D * elt_size(&d);
+  const size_t pool_bytes = (size_t)pool->n_pages * pool->page_size * row;
+  const Range to[] = {{pool->K, pool_bytes}, {pool->V, pool_bytes}};
+  const Range from[] = {{k_new, (size_t)(T - 1) * k_stride * elt_size(&d) + row},
+                        {v_new, (size_t)(T - 1) * v_stride * elt_size(&d) + row}, {slots, (size_t)T * 4}};
+  if (to[0].meets(to[1])) return GLIDE_ERR_INVALID;
+  for (const Range& t : to)
+    for (const Range& f : from)
+      if (t.meets(f)) return GLIDE_ERR_INVALID;
+  glide::PagedAppendArgs a;
+  a.K = pool->K; a.V = pool->V; a.k_new = k_new; a.v_new = v_new; a.slots = slots;
+  a.k_stride = (long long)(k_stride * (int64_t)elt_size(&d));
+  a.v_stride = (long long)(v_stride * (int64_t)elt_size(&d));
+  a.n_slots = (long long)pool->n_pages * pool->page_size;
+  a.T = T; a.H = hkv(&d); a.page_shift = log2_of(pool->page_size); a.row_bytes = (int)(d.D * elt_size(&d));
+  return from_cuda(glide::launch_paged_append(a, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t glide_paged_workspace_bytes(const glide_attn_desc* desc, int32_t T, int32_t max_q) {
+  glide_attn_desc d;
+  if (!rows_desc(desc, true, &d) || T < 0 || max_q < 1) return 0;
+  return glide::rows_workspace_bytes(d.B, d.H, hkv(&d), d.D, T, max_q, d.dtype == GLIDE_BF16 ? 0 : 1);
+}
+
+// Everything that the two calls share; K, V, lengths and tables are filled in by them.
+static glide_status rows_attention(const glide_attn_desc* d, glide::RowsArgs& a, const void* q, int64_t q_stride, int32_t T,
+                                   const int32_t* cu, int32_t max_q, void* out, void* ws, size_t ws_bytes,
+                                   glide_stream_t stream) {
+  if (T < 0 || max_q < 1 || !stride_ok(d, q_stride, d->H, T)) return GLIDE_ERR_INVALID;
+  if (!cu || !aligned4(cu) || !ws || !aligned16(ws)) return GLIDE_ERR_INVALID;
+  if (max_q > T) max_q = T > 0 ? T : 1;
+  if (ws_bytes < glide_paged_workspace_bytes(d, T, max_q)) return GLIDE_ERR_INVALID;
+  if (T == 0) return GLIDE_OK;
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return GLIDE_ERR_INVALID;
+  if ((double)T * d->H * d->D > 1.0e18) return GLIDE_ERR_INVALID;
+  a.q = q; a.out = out; a.ws = ws; a.cu = cu; a.q_stride = q_stride;
+  a.B = d->B; a.T = T; a.H = d->H; a.Hkv = hkv(d); a.D = d->D; a.max_q = max_q;
+  a.dtype = d->dtype == GLIDE_BF16 ? 0 : 1;
+  a.scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->D);
+  a.flags = d->flags;
+  return from_cuda(glide::launch_rows_fma(a, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+glide_status glide_paged_attn(const glide_attn_desc* desc, const void* q, int64_t q_stride, int32_t T,
+                              const int32_t* cu_q, int32_t max_q, const glide_page_pool* pool,
+                              const int32_t* block_table, int32_t table_width, const int32_t* kv_len,
+                              int32_t max_kv_len, void* out, void* workspace, size_t workspace_bytes,
+                              glide_stream_t stream) {
+  glide_attn_desc d;
+  if (!rows_desc(desc, true, &d)) return GLIDE_ERR_INVALID;
+  const glide_status ps = pool_status(pool, &d);
+  if (ps != GLIDE_OK) return ps;
+  if (table_width < 1 || max_kv_len < 0 || max_kv_len > (long long)table_width * pool->page_size) return GLIDE_ERR_INVALID;
+  if (!block_table || !kv_len || !aligned4(block_table) || !aligned4(kv_len)) return GLIDE_ERR_INVALID;
+  glide::RowsArgs a;
+  a.K = pool->K; a.V = pool->V; a.kv_len = kv_len; a.table = block_table; a.k_stride = 0; a.v_stride = 0;
+  a.W = table_width; a.n_pages = pool->n_pages; a.page_shift = log2_of(pool->page_size); a.max_kv = max_kv_len;
+  return rows_attention(&d, a, q, q_stride, T, cu_q, max_q, out, workspace, workspace_bytes, stream);
+}
+
+glide_status glide_prompt_attn(const glide_attn_desc* desc, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, int32_t T, const int32_t* cu,
+                               int32_t max_len, void* out, void* workspace, size_t workspace_bytes,
+                               glide_stream_t stream) {
+  glide_attn_desc d;
+  if (!rows_desc(desc, true, &d) || T < 0) return GLIDE_ERR_INVALID;
+  if (!stride_ok(&d, k_stride, hkv(&d), T) || !stride_ok(&d, v_stride, hkv(&d), T)) return GLIDE_ERR_INVALID;
+  if (T > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return GLIDE_ERR_INVALID;
+  glide::RowsArgs a;
+  a.K = k; a.V = v; a.kv_len = nullptr; a.table = nullptr; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.W = 0; a.n_pages = 0; a.page_shift = 0; a.max_kv = 0;
+  return rows_attention(&d, a, q, q_stride, T, cu, max_len, out, workspace, workspace_bytes, stream);
 }
 
 glide_status glide_validate_tree(const int32_t* parent_idx_host, int32_t B, int32_t n, int32_t require_root0) {

@@ -489,6 +489,165 @@ PyObject* kv8_attn(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------------------------ cache in pages
+// The calls launch on the current device.
+void on_current(std::initializer_list<const at::Tensor*> ts) { on(c10::cuda::current_device(), ts); }
+
+// Rows of new tokens [T, heads, D], heads and elements dense; the elements from token to token.
+struct TokenRows {
+  const at::Tensor* t;
+  int64_t stride;
+};
+TokenRows token_rows(Args& a) {
+  const at::Tensor& t = a.any_tensor();
+  if ((t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kFloat) || t.dim() != 3) throw NotTaken{};
+  for (int64_t s : t.sizes())
+    if (s < 1 || s > INT_MAX) throw NotTaken{};
+  if (t.stride(2) != 1 || (t.size(1) > 1 && t.stride(1) != t.size(2))) throw NotTaken{};
+  return {&t, t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2)};
+}
+struct Pool {
+  glide_page_pool c;
+  const at::Tensor* K;
+};
+Pool page_pool(Args& a) {
+  const at::Tensor &K = a.data(), &V = a.data();
+  if (K.dim() != 4 || V.sizes() != K.sizes() || V.scalar_type() != K.scalar_type()) throw NotTaken{};
+  on_current({&K, &V});
+  return {{K.data_ptr(), V.data_ptr(), dim(K, 0), dim(K, 2)}, &K};
+}
+glide_attn_desc describe_rows(int32_t B, const at::Tensor& q, int32_t H_kv) {
+  glide_attn_desc d{};
+  d.B = B;
+  d.H = dim(q, 1);
+  d.D = dim(q, 2);
+  d.S_cap = 1;
+  d.dtype = q.scalar_type() == at::kBFloat16 ? GLIDE_BF16 : GLIDE_F32;
+  d.H_kv = H_kv == d.H ? 0 : H_kv;
+  return d;
+}
+
+// q_len, kv_len, held, block_table, free_pages, n_free, page_size, cu_q, slots, new_kv_len, new_held, new_n_free,
+// positions, stream
+PyObject* page_plan(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return call([&] {
+    Args a(v, n, 14);
+    const at::Tensor &q = a.tensor(at::kInt), &kv = a.tensor(at::kInt), &held = a.tensor(at::kInt),
+                     &table = a.tensor(at::kInt), &free = a.tensor(at::kInt), &n_free = a.tensor(at::kInt, {1});
+    const int32_t P = a.i32();
+    if (table.dim() != 2 || !table.is_contiguous() || free.dim() != 1 || !free.is_contiguous()) throw NotTaken{};
+    const int64_t B = table.size(0);
+    if (B > INT_MAX - 1 || table.size(1) > INT_MAX || free.size(0) > INT_MAX) throw NotTaken{};
+    for (const at::Tensor* t : {&q, &kv, &held})
+      if (t->sizes() != at::IntArrayRef({B}) || !t->is_contiguous()) throw NotTaken{};
+    const at::Tensor &cu = a.tensor(at::kInt, {B + 1}), &slots = a.tensor(at::kInt);
+    if (slots.dim() != 1 || slots.size(0) > INT_MAX || !slots.is_contiguous()) throw NotTaken{};
+    const at::Tensor &nkv = a.tensor(at::kInt, {B}), &nheld = a.tensor(at::kInt, {B}), &nn = a.tensor(at::kInt, {1});
+    on_current({&q, &kv, &held, &table, &free, &n_free, &cu, &slots, &nkv, &nheld, &nn});
+    int32_t* pos = nullptr;
+    if (!a.none()) {
+      const at::Tensor& t = a.tensor(at::kInt, {slots.size(0)});
+      on_current({&t});
+      pos = ints(t);
+    }
+    const glide_stream_t stream = a.stream();
+    const int32_t b = static_cast<int32_t>(B), T = dim(slots, 0), W = dim(table, 1), cap = dim(free, 0);
+    const int32_t *pq = ints(q), *pk = ints(kv), *ph = ints(held), *pf = ints(n_free);
+    int32_t *pt = ints(table), *pfree = ints(free), *pc = ints(cu), *ps = ints(slots), *a1 = ints(nkv), *a2 = ints(nheld),
+            *a3 = ints(nn);
+    return without_gil(
+        [&] { return long(glide_page_plan(b, T, P, W, pq, pk, ph, pt, pfree, cap, pf, pc, ps, pos, a1, a2, a3, stream)); });
+  });
+}
+
+// k_new, v_new, K, V, slots, stream
+PyObject* paged_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return call([&] {
+    Args a(v, n, 6);
+    const TokenRows k = token_rows(a), w = token_rows(a);
+    const Pool pool = page_pool(a);
+    const at::Tensor& K = *pool.K;
+    const at::Tensor& slots = a.tensor(at::kInt, {k.t->size(0)});
+    for (const at::Tensor* t : {k.t, w.t})
+      if (t->scalar_type() != K.scalar_type() || t->sizes() != at::IntArrayRef({slots.size(0), K.size(1), K.size(3)}))
+        throw NotTaken{};
+    on_current({k.t, w.t, &slots});
+    const glide_stream_t stream = a.stream();
+    const glide_attn_desc d = describe_rows(1, *k.t, dim(K, 1));
+    const int32_t T = dim(slots, 0);
+    const void *pk = k.t->data_ptr(), *pv = w.t->data_ptr();
+    const int32_t* ps = ints(slots);
+    return without_gil([&] { return long(glide_paged_append(&d, &pool.c, pk, pv, k.stride, w.stride, T, ps, stream)); });
+  });
+}
+
+// What both attention calls end with: out, workspace, scale, flags, stream.
+struct RowsTail {
+  void *out, *ws;
+  size_t bytes;
+  glide_stream_t stream;
+};
+RowsTail rows_tail(Args& a, const at::Tensor& q, glide_attn_desc& d) {
+  const at::Tensor &out = a.data(), &w = a.any_tensor();
+  if (out.sizes() != q.sizes() || out.scalar_type() != q.scalar_type() || !w.is_contiguous()) throw NotTaken{};
+  on_current({&q, &out, &w});
+  d.scale = a.f32();
+  d.flags = a.u32();
+  return {out.data_ptr(), w.data_ptr(), w.nbytes(), a.stream()};
+}
+
+// q, K, V, block_table, cu_q, max_q, kv_len, max_kv_len, out, workspace, scale, flags, stream
+PyObject* paged_attn(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return call([&] {
+    Args a(v, n, 13);
+    const TokenRows q = token_rows(a);
+    const Pool pool = page_pool(a);
+    const at::Tensor& K = *pool.K;
+    const at::Tensor& table = a.tensor(at::kInt);
+    if (q.t->scalar_type() != K.scalar_type() || q.t->size(2) != K.size(3) || table.dim() != 2 || !table.is_contiguous() ||
+        table.size(0) > INT_MAX - 1 || table.size(1) > INT_MAX)
+      throw NotTaken{};
+    const int64_t B = table.size(0);
+    const at::Tensor& cu = a.tensor(at::kInt, {B + 1});
+    const int32_t max_q = a.i32();
+    const at::Tensor& len = a.tensor(at::kInt, {B});
+    const int32_t most = a.i32();
+    glide_attn_desc d = describe_rows(static_cast<int32_t>(B), *q.t, dim(K, 1));
+    on_current({&table, &cu, &len});
+    const RowsTail e = rows_tail(a, *q.t, d);
+    const int32_t T = dim(*q.t, 0), W = dim(table, 1);
+    const void* pq = q.t->data_ptr();
+    const int32_t *pc = ints(cu), *pt = ints(table), *pl = ints(len);
+    return without_gil([&] {
+      return long(glide_paged_attn(&d, pq, q.stride, T, pc, max_q, &pool.c, pt, W, pl, most, e.out, e.ws, e.bytes, e.stream));
+    });
+  });
+}
+
+// q, k, v, cu, max_len, out, workspace, scale, flags, stream
+PyObject* prompt_attn(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return call([&] {
+    Args a(v, n, 10);
+    const TokenRows q = token_rows(a), k = token_rows(a), w = token_rows(a);
+    for (const at::Tensor* t : {k.t, w.t})
+      if (t->scalar_type() != q.t->scalar_type() || t->sizes() != at::IntArrayRef({q.t->size(0), k.t->size(1), q.t->size(2)}))
+        throw NotTaken{};
+    const at::Tensor& cu = a.tensor(at::kInt);
+    if (cu.dim() != 1 || cu.size(0) < 2 || cu.size(0) > INT_MAX || !cu.is_contiguous()) throw NotTaken{};
+    const int32_t max_len = a.i32();
+    glide_attn_desc d = describe_rows(dim(cu, 0) - 1, *q.t, dim(*k.t, 1));
+    on_current({k.t, w.t, &cu});
+    const RowsTail e = rows_tail(a, *q.t, d);
+    const int32_t T = dim(*q.t, 0);
+    const void *pq = q.t->data_ptr(), *pk = k.t->data_ptr(), *pv = w.t->data_ptr();
+    const int32_t* pc = ints(cu);
+    return without_gil([&] {
+      return long(glide_prompt_attn(&d, pq, q.stride, pk, k.stride, pv, w.stride, T, pc, max_len, e.out, e.ws, e.bytes,
+                                    e.stream));
+    });
+  });
+}
+
 #define FN(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FN("cross_attn", cross_attn<false>),
                           FN("cross_attn_noalloc", cross_attn<true>),
@@ -502,6 +661,10 @@ PyMethodDef kMethods[] = {FN("cross_attn", cross_attn<false>),
                           FN("kv8_read", kv8_read),
                           FN("kv8_cross", kv8_attn<false>),
                           FN("kv8_verify", kv8_attn<true>),
+                          FN("page_plan", page_plan),
+                          FN("paged_append", paged_append),
+                          FN("paged_attn", paged_attn),
+                          FN("prompt_attn", prompt_attn),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_glidecall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,140 @@
+// One row of attention over a paged cache or packed keys and values, by a warp on the CUDA cores:
+// the whole of the simple kernel, and what the tensor-core kernels turn to for a row whose result is
+// not finite.
+//
+// The mathematics: u_t = (q . k_t) scale log2(e), m the running maximum of u, p_t = 2^(u_t - m),
+// out = sum p_t v_t / sum p_t, in fp32.  Lane t of a pass takes key t: its dot product needs no exchange;
+// for the values lane d takes D / 32 columns.  A weight is mathematically above 0 unless the score is
+// -inf, so one that underflows counts as the smallest normal number: an infinite value decides its
+// column at any weight, and 2^-126 moves no finite sum.
+#pragma once
+
+#include <cfloat>
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "attn_common.cuh"
+#include "common.cuh"
+#include "paged.h"
+
+namespace glide {
+namespace {
+
+struct RowsParams {
+  const unsigned char *q, *K, *V;
+  unsigned char* out;
+  const int *cu, *kv_len, *table;
+  long long q_stride, k_stride, v_stride;  // bytes from token to token
+  int B, T, H, Hkv, group, W, n_pages, page_shift;
+  int max_q, max_kv;
+  float scale_log2;
+};
+
+__host__ inline RowsParams rows_params(const RowsArgs& a) {
+  const int size = a.dtype == 0 ? 2 : 4;
+  RowsParams p;
+  p.q = static_cast<const unsigned char*>(a.q);
+  p.K = static_cast<const unsigned char*>(a.K);
+  p.V = static_cast<const unsigned char*>(a.V);
+  p.out = static_cast<unsigned char*>(a.out);
+  p.cu = a.cu; p.kv_len = a.kv_len; p.table = a.table;
+  p.q_stride = a.q_stride * size; p.k_stride = a.k_stride * size; p.v_stride = a.v_stride * size;
+  p.B = a.B; p.T = a.T; p.H = a.H; p.Hkv = a.Hkv; p.group = a.H / a.Hkv;
+  p.W = a.W; p.n_pages = a.n_pages; p.page_shift = a.page_shift;
+  p.max_q = a.max_q; p.max_kv = a.max_kv;
+  p.scale_log2 = a.scale * kLog2e;
+  return p;
+}
+
+__device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
+
+// Sequence b's rows and keys: its first row, how many of its rows are served, its rows in all and its keys.
+struct Seq {
+  int row0, rows, m, kv;
+};
+__device__ __forceinline__ Seq seq_of(const RowsParams& p, int b) {
+  Seq s;
+  s.row0 = clamp_to(p.cu[b], 0, p.T);
+  s.m = clamp_to(p.cu[b + 1], s.row0, p.T) - s.row0;
+  s.rows = s.m < p.max_q ? s.m : p.max_q;
+  s.kv = p.table ? clamp_to(p.kv_len[b], 0, p.max_kv) : s.m;
+  return s;
+}
+// Keys that row i of the sequence sees.
+__device__ __forceinline__ int seen(const Seq& s, int i) {
+  const int n = s.kv - s.m + i + 1;
+  return n < 0 ? 0 : n;
+}
+// The page that holds a request's tokens from page index j on.
+__device__ __forceinline__ int page_at(const RowsParams& p, int b, int j) {
+  return clamp_to(p.table[(size_t)b * p.W + j], 0, p.n_pages - 1);
+}
+
+// Byte offset of key row t of cached head h of sequence b (row0 its first packed row), and of its value row.
+template <int kRow>
+__device__ __forceinline__ size_t key_at(const RowsParams& p, int b, int row0, int h, int t, long long stride) {
+  if (!p.table) return (size_t)((long long)(row0 + t) * stride) + (size_t)h * kRow;
+  const int page = page_at(p, b, t >> p.page_shift), r = t & ((1 << p.page_shift) - 1);
+  return ((((size_t)page * p.Hkv + h) << p.page_shift) + r) * kRow;
+}
+
+// o[e], column lane * (D / 32) + e of the result of query head h in row `row` (row i of sequence b) over its first n > 0
+// keys.  All lanes of a warp.
+template <typename T, int D>
+__device__ __noinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, int n, float (&o)[D / 32]) {
+  constexpr int kE = D / 32, kRow = D * (int)sizeof(T), kC = 16 / (int)sizeof(T);
+  const int lane = threadIdx.x & 31, hk = h / p.group;
+  const unsigned char* q = p.q + (long long)(s.row0 + i) * p.q_stride + (size_t)h * kRow;
+  float m = -CUDART_INF_F, l = 0.f;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) o[e] = 0.f;
+  for (int t0 = 0; t0 < n; t0 += 32) {
+    const int t = t0 + lane;
+    float u = -CUDART_INF_F;
+    if (t < n) {
+      const unsigned char* k = p.K + key_at<kRow>(p, b, s.row0, hk, t, p.k_stride);
+      float acc[2] = {0.f, 0.f};
+#pragma unroll 4
+      for (int c = 0; c < D / kC; ++c)
+        dot_chunk<T>(*reinterpret_cast<const uint4*>(q + 16 * c), *reinterpret_cast<const uint4*>(k + 16 * c), acc);
+      u = (acc[0] + acc[1]) * p.scale_log2;
+    }
+    const float m_new = fmaxf(m, warp_max(u));
+    const float m_eff = m_new == -CUDART_INF_F ? 0.f : m_new;
+    float f = fast_exp2(m - m_eff);
+    if (m != -CUDART_INF_F) f = f < FLT_MIN ? FLT_MIN : f;  // (a NaN stays one)
+    float w = fast_exp2(u - m_eff);
+    if (u != -CUDART_INF_F) w = w < FLT_MIN ? FLT_MIN : w;
+    l = l * f + warp_sum(w);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) o[e] *= f;
+    m = m_new;
+    const int most = n - t0 < 32 ? n - t0 : 32;
+#pragma unroll 4
+    for (int j = 0; j < most; ++j) {
+      const float pj = __shfl_sync(0xffffffffu, w, j);
+      if (pj == 0.f) continue;  // a score of -inf: no weight, whatever the value
+      float v[kE];
+      load_row_chunk<T, kE>(reinterpret_cast<const T*>(p.V + key_at<kRow>(p, b, s.row0, hk, t0 + j, p.v_stride)) + lane * kE, v);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) o[e] = fmaf(pj, v[e], o[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kE; ++e) o[e] /= l;
+}
+
+template <int kE>
+__device__ __forceinline__ void store_row(float* at, const float (&o)[kE]) {
+#pragma unroll
+  for (int e = 0; e < kE; e += 2) *reinterpret_cast<float2*>(at + e) = make_float2(o[e], o[e + 1]);
+}
+template <int kE>
+__device__ __forceinline__ void store_row(__nv_bfloat16* at, const float (&o)[kE]) {
+#pragma unroll
+  for (int e = 0; e < kE; e += 2)
+    *reinterpret_cast<__nv_bfloat162*>(at + e) = __floats2bfloat162_rn(o[e], o[e + 1]);
+}
+
+}  // namespace
+}  // namespace glide
