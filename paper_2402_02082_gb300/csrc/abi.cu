@@ -493,7 +493,12 @@ static glide_status rows_attention(const glide_attn_desc* d, glide::RowsArgs& a,
   a.dtype = d->dtype == GLIDE_BF16 ? 0 : 1;
   a.scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->D);
   a.flags = d->flags;
-  return from_cuda(glide::launch_rows_fma(a, reinterpret_cast<cudaStream_t>(stream)));
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (!(a.flags & GLIDE_FLAG_FORCE_FMA)) {
+    const cudaError_t e = glide::launch_paged_few(a, st);
+    if (e != cudaErrorNotSupported) return from_cuda(e);
+  }
+  return from_cuda(glide::launch_rows_fma(a, st));
 }
 
 glide_status glide_paged_attn(const glide_attn_desc* desc, const void* q, int64_t q_stride, int32_t T,

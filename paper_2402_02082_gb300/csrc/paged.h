@@ -42,6 +42,8 @@ cudaError_t launch_page_plan(const PlanArgs& a, cudaStream_t st);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t st);
 // On the CUDA cores, a warp a row: every type and size.
 cudaError_t launch_rows_fma(const RowsArgs& a, cudaStream_t st);
+// bf16, pages, at most 16 query rows for a cached head; cudaErrorNotSupported for others.
+cudaError_t launch_paged_few(const RowsArgs& a, cudaStream_t st);
 
 size_t rows_workspace_bytes(int B, int H, int Hkv, int D, int T, int max_q, int dtype);
 
