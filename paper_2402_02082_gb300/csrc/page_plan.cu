@@ -71,9 +71,9 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   const int tid = threadIdx.x;
   pdl_wait();
   const bool real = tid < a.B;
-  const int q = real ? a.q_len[tid] : 0, kv0 = real ? a.kv_len[tid] : 0, held0 = real ? a.held[tid] : 0;
+  const int q = real ? __ldcg(a.q_len + tid) : 0, kv0 = real ? __ldcg(a.kv_len + tid) : 0, held0 = real ? __ldcg(a.held + tid) : 0;
   if (tid == 0) {
-    const int n = a.n_free[0];
+    const int n = __ldcg(a.n_free);
     s_n_free = n < 0 ? 0 : (n > a.free_cap ? a.free_cap : n);
     s_taken = 0;
     tok[0] = back[0] = ask[0] = 0;
@@ -108,9 +108,9 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
   const int taken = s_taken;
 
   const auto stack = [&](int x) {
-    if (x < n_free) return a.free_pages[x];
+    if (x < n_free) return __ldcg(a.free_pages + x);
     const int f = last_at_most(back, a.B, x - n_free);
-    return a.table[(size_t)f * a.W + (x - n_free - back[f])];
+    return __ldcg(a.table + (size_t)f * a.W + (x - n_free - back[f]));
   };
   const auto handed_out = [&](int y) { return stack(avail - 1 - y); };
 
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
       pos = at < 0x7fffffffLL ? (int)at : 0x7fffffff;
       if (oks[b]) {
         const int j = pos >> shift;
-        const int page = j < helds[b] ? a.table[(size_t)b * a.W + j] : handed_out(ask[b] + j - helds[b]);
+        const int page = j < helds[b] ? __ldcg(a.table + (size_t)b * a.W + j) : handed_out(ask[b] + j - helds[b]);
         const long long s = ((long long)page << shift) + (pos & (a.P - 1));
         slot = page >= 0 && s <= 0x7fffffffLL ? (int)s : -1;
       }

@@ -44,6 +44,9 @@ cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t st);
 cudaError_t launch_rows_fma(const RowsArgs& a, cudaStream_t st);
 // bf16, pages, at most 16 query rows for a cached head; cudaErrorNotSupported for others.
 cudaError_t launch_paged_few(const RowsArgs& a, cudaStream_t st);
+// bf16, at most 128 query heads for a cached head, on the tensor cores; cudaErrorNotSupported for others and beyond 32-bit
+// coordinates.
+cudaError_t launch_rows_tc(const RowsArgs& a, cudaStream_t st);
 
 size_t rows_workspace_bytes(int B, int H, int Hkv, int D, int T, int max_q, int dtype);
 

@@ -18,7 +18,7 @@ __global__ void __launch_bounds__(kAppThreads) paged_append_kernel(const PagedAp
   const long long total = (long long)a.T * pieces, step = (long long)gridDim.x * kAppThreads;
   for (long long x = (long long)blockIdx.x * kAppThreads + threadIdx.x; x < total; x += step) {
     const int i = (int)(x / pieces), c = (int)(x - (long long)i * pieces);
-    const int slot = a.slots[i];
+    const int slot = __ldcg(a.slots + i);
     if (slot < 0 || slot >= a.n_slots) continue;
     const int h = c >> row_shift, piece = c & ((1 << row_shift) - 1);
     const long long page = slot >> a.page_shift, r = slot & ((1 << a.page_shift) - 1);

@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
   pdl_wait();
   if (sorted) {  // the request of this rank by length, the longest first; B <= the block's threads
     int* len = reinterpret_cast<int*>(sm.red);
-    const int mine = threadIdx.x < p.B ? clamp_to(p.kv_len[threadIdx.x], 0, p.max_kv) : 0;
+    const int mine = threadIdx.x < p.B ? clamp_to(__ldcg(p.kv_len + threadIdx.x), 0, p.max_kv) : 0;
     if (threadIdx.x < p.B) len[threadIdx.x] = mine;
     __syncthreads();
     if (threadIdx.x < p.B) {

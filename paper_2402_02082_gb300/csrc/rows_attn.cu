@@ -17,7 +17,7 @@ __device__ __forceinline__ int seq_at(const RowsParams& p, int i) {
   int lo = 0, hi = p.B - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (p.cu[mid] <= i) lo = mid; else hi = mid - 1;
+    if (__ldcg(p.cu + mid) <= i) lo = mid; else hi = mid - 1;
   }
   return lo;
 }
@@ -60,7 +60,5 @@ cudaError_t launch_rows_fma(const RowsArgs& a, cudaStream_t st) {
   if (a.dtype == 0) return a.D == 128 ? launch_typed<__nv_bfloat16, 128>(p, st) : launch_typed<__nv_bfloat16, 64>(p, st);
   return a.D == 128 ? launch_typed<float, 128>(p, st) : launch_typed<float, 64>(p, st);
 }
-
-size_t rows_workspace_bytes(int, int, int, int, int, int, int) { return WsLayout::kHeader; }
 
 }  // namespace glide

@@ -54,10 +54,10 @@ struct Seq {
 };
 __device__ __forceinline__ Seq seq_of(const RowsParams& p, int b) {
   Seq s;
-  s.row0 = clamp_to(p.cu[b], 0, p.T);
-  s.m = clamp_to(p.cu[b + 1], s.row0, p.T) - s.row0;
+  s.row0 = clamp_to(__ldcg(p.cu + b), 0, p.T);
+  s.m = clamp_to(__ldcg(p.cu + b + 1), s.row0, p.T) - s.row0;
   s.rows = s.m < p.max_q ? s.m : p.max_q;
-  s.kv = p.table ? clamp_to(p.kv_len[b], 0, p.max_kv) : s.m;
+  s.kv = p.table ? clamp_to(__ldcg(p.kv_len + b), 0, p.max_kv) : s.m;
   return s;
 }
 // Keys that row i of the sequence sees.
@@ -67,7 +67,7 @@ __device__ __forceinline__ int seen(const Seq& s, int i) {
 }
 // The page that holds a request's tokens from page index j on.
 __device__ __forceinline__ int page_at(const RowsParams& p, int b, int j) {
-  return clamp_to(p.table[(size_t)b * p.W + j], 0, p.n_pages - 1);
+  return clamp_to(__ldcg(p.table + (size_t)b * p.W + j), 0, p.n_pages - 1);
 }
 
 // Byte offset of key row t of cached head h of sequence b (row0 its first packed row), and of its value row.
@@ -79,9 +79,9 @@ __device__ __forceinline__ size_t key_at(const RowsParams& p, int b, int row0, i
 }
 
 // o[e], column lane * (D / 32) + e of the result of query head h in row `row` (row i of sequence b) over its first n > 0
-// keys.  All lanes of a warp.
+// keys.  All lanes of a warp.  (Inlined: a kernel that splits its registers among its warps holds no call.)
 template <typename T, int D>
-__device__ __noinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, int n, float (&o)[D / 32]) {
+__device__ __forceinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, int n, float (&o)[D / 32]) {
   constexpr int kE = D / 32, kRow = D * (int)sizeof(T), kC = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 31, hk = h / p.group;
   const unsigned char* q = p.q + (long long)(s.row0 + i) * p.q_stride + (size_t)h * kRow;
