@@ -184,6 +184,14 @@ __device__ __forceinline__ void tma_prefetch_l2_2d(const CUtensorMap* map, int x
                : "memory");
 }
 
+// Box of a 3-D tensor map at element coordinates (x, y, z) into L2 only.
+__device__ __forceinline__ void tma_prefetch_l2_3d(const CUtensorMap* map, int x, int y, int z) {
+  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+
 // Box of a 3-D tensor map at element coordinates (x, y, z) from shared memory
 // to global memory, in this thread's current bulk async-group; elements
 // outside the tensor are not written.
