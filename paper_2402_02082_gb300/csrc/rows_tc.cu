@@ -26,10 +26,9 @@
 // Roles (512 threads, one CTA per SM):
 //   warps 0-7    softmax, two groups of four: warp w reads TMEM lane quarter w % 4, one thread a row, of the tiles of
 //                parity w / 4; they rescale O where the reference is raised (by more than 8, so seldom).
-//   warp 8       loads Q (two items' worth), K and V (a page's rows at a time, or 128 packed rows).
+//   warp 8       claims items and makes them, up to two ahead; loads Q (two items' worth) and K (a page's rows at a time,
+//                or 128 packed rows); warp 11 loads V and clears its rows past an item's last visible key.
 //   warp 9       S issue, warp 10 P V issue (lane 0).
-//   warp 11      claims items and makes them, up to three ahead of the loads; clears the V rows past an item's last
-//                visible key.
 //   warps 12-15  results: a TMEM lane quarter each, O / l through 4 KB of shared memory in whole rows.
 //
 // A result that is not finite (an infinity or NaN that the row sees, or one that it does not see, in a tile
@@ -50,9 +49,9 @@ namespace {
 
 constexpr int kBM = 128;          // rows of a row tile (MMA rows, TMEM lanes)
 constexpr int kBN = 128;          // keys of a tile
-constexpr int kLoadWarp = 8;
+constexpr int kKWarp = 8;
 constexpr int kSWarp = 9;
-constexpr int kItemWarp = 11;
+constexpr int kVWarp = 11;
 constexpr int kOutWarp0 = 12;
 constexpr int kTcThreads = 512;
 constexpr int kTmemCols = 512;
@@ -61,7 +60,6 @@ constexpr float kRescaleLog2 = 8.0f;
 constexpr int kSBufs = 3;
 constexpr int kItemSlots = 4;
 constexpr int kItemReaders = 15;       // warps that read an item beside the one that makes it
-constexpr int kItemsAhead = 3;
 constexpr int kMaxGrid = 160;
 constexpr int kMaxChunks = 3 * kMaxGrid;  // partial slots: below 2 grids of items and one grid more of chunks
 constexpr int kMinChunkTiles = 4;
@@ -80,7 +78,6 @@ struct Bars {
   uint64_t olast, ofree, lready, lfree;
   uint64_t turn[4][2];    // [quarter][tile parity]: a tile's reference is there
   uint64_t itemfull[kItemSlots], itemempty[kItemSlots];
-  uint64_t lastv[4];      // the load of an item's last V tile is on its way
   uint64_t drained[2];
 };
 
@@ -181,10 +178,10 @@ struct Boxes {
     return (uint32_t)(rows * kHalves * 128);
   }
   // coordinates of the lane's box, for key tile t of the item
-  __device__ __forceinline__ int2 where(const RowsParams& r, const TcItem& it, int t) const {
+  __device__ __forceinline__ int2 where(const RowsParams& r, int b, int h, int row0, int t) const {
     const int key = t * kBN + at;
-    if (!r.table) return make_int2(it.h, it.row0 + key);
-    return make_int2(key & ((1 << r.page_shift) - 1), page_at(r, it.b, key >> r.page_shift) * r.Hkv + it.h);
+    if (!r.table) return make_int2(h, row0 + key);
+    return make_int2(key & ((1 << r.page_shift) - 1), page_at(r, b, key >> r.page_shift) * r.Hkv + h);
   }
 };
 
@@ -226,7 +223,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     init(&bars->turn[0][0], 8, 1);
     init(bars->itemfull, kItemSlots, 1);
     init(bars->itemempty, kItemSlots, kItemReaders);
-    init(bars->lastv, 4 + 2, 1);  // and drained
+    init(bars->drained, 2, 1);
     misc->abort = 0;
     misc->levels = 0;
     misc->sum[0] = misc->sum[1] = misc->sum[2] = 0;
@@ -234,7 +231,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
   __syncthreads();
   pdl_wait();  // every global access and the TMEM allocation come after it
-  if (warp == kItemWarp) {
+  if (warp == kKWarp) {
     tc::tmem_alloc(&misc->tmem, kTmemCols);
     tc::tmem_relinquish();
   }
@@ -316,77 +313,24 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   tc::fence_after_sync();
   const uint32_t tmem = misc->tmem;
 
-  if (warp >= kLoadWarp && warp < kOutWarp0) {
+  if (warp >= kKWarp && warp < kOutWarp0) {
     tc_regs_down<88>();
-    if (warp == kLoadWarp) {
-      // ------------------------------------------------------------ loads
-      const uint64_t pol_q = policy_evict_first(), pol_kv = policy_evict_last();
-      if (lane < 3) tc::prefetch_tmap(lane == 0 ? &tmQ : lane == 1 ? &tmK : &tmV);
-      unsigned st = 0, phase = 1, k_issued = 0, v_issued = 0, q_issued = 0;
-      bool ok = true;
-      ItemReader reader;
+    if (warp == kKWarp) {
+      // ------------------------------------------------------------ items, Q and K
+      const uint64_t pol_q = policy_evict_first(), pol_k = policy_evict_last();
+      if (lane < 2) tc::prefetch_tmap(lane == 0 ? &tmQ : &tmK);
       const Boxes<C::kHalves> box(p, lane);
-      while (ok) {
-        const TcItem* at = reader.next(bars, items, abort_flag);
-        if (!at) break;
-        const TcItem it = *at;
-        reader.release(bars, lane);
-        if (it.te == it.t0) continue;
-        {
-          const unsigned qb = q_issued & 1;
-          ok = warp_wait_small(&bars->qempty[qb], ((q_issued >> 1) & 1) ^ 1, abort_flag);
-          if (!ok) break;
-          if (lane == 0) mbar_arrive_expect_tx(&bars->qfull[qb], (uint32_t)(C::kHalves * p.tokens * rp.group * 128));
-          __syncwarp();
-          if (lane < C::kHalves)
-            tc::tma_load_3d(base + C::off_Q + qb * C::kTile + lane * kAtom, &tmQ, lane * 64, it.h * rp.group, it.row0 + it.pos0,
-                            &bars->qfull[qb], pol_q);
-          ++q_issued;
-        }
-#pragma unroll 1
-        for (int t = it.t0; ok && t < it.te; ++t) {
-          const int left = it.klen - t * kBN;
-          const bool mine = box.any(left);
-          const int2 x = mine ? box.where(rp, it, t) : make_int2(0, 0);
-#pragma unroll 1
-          for (int v = 0; v < opaque(2); ++v) {
-            uint64_t* full = (v ? bars->vfull : bars->kfull) + st;
-            ok = ok && warp_wait_small((v ? bars->vempty : bars->kempty) + st, phase, abort_flag);
-            if (!ok) break;
-            if (lane == 0) mbar_arrive_expect_tx(full, box.bytes(left, !rp.table));
-            __syncwarp();
-            if (mine)
-              tc::tma_load_3d(base + (v ? C::off_V : C::off_K) + st * C::kTile + box.hd * kAtom + box.at * 128,
-                              v ? &tmV : &tmK, box.hd * 64, x.x, x.y, full, pol_kv);
-            __syncwarp();
-            if (v) ++v_issued; else ++k_issued;
-          }
-          if (++st == C::kNS) {
-            st = 0;
-            phase ^= 1;
-          }
-        }
-        if (lane == 0) mbar_arrive(&bars->lastv[(q_issued - 1) & 3]);
-      }
-      if (!ok) {  // aborted: let issued loads land before the CTA exits
-#pragma unroll 1
-        for (int v = 0; v < 2; ++v) {
-          const unsigned n = v ? v_issued : k_issued;
-          for (unsigned j = n > C::kNS ? n - C::kNS : 0; j < n; ++j)
-            mbar_drain((v ? bars->vfull : bars->kfull) + j % C::kNS, (j / C::kNS) & 1);
-        }
-        for (unsigned j = q_issued > 2 ? q_issued - 2 : 0; j < q_issued; ++j) mbar_drain(&bars->qfull[j & 1], (j >> 1) & 1);
-      }
-    } else if (warp == kItemWarp) {
-      // ------------------------------------------------------------ items, and the ends of V
       const int entries = misc->entries, head_group = misc->head_group, chunk_tiles = misc->chunk_tiles;
       const unsigned claims = (unsigned)entries * rp.Hkv, per_group = (unsigned)entries * head_group;  // below 2^31
       int level = misc->levels - 1, block = 0, acc = 0, group_at = 0;
-      unsigned next = blockIdx.x, made = 0, settled = 0, with_tiles = 0, v_pos = 0;
-      int ends[kItemsAhead], lefts[kItemsAhead];  // tiles of the items made and not settled; keys of the last one
-      bool ok = true, more = true;
-      while (ok && (more || settled < made)) {
-        if (more && made - settled < kItemsAhead) {
+      unsigned next = blockIdx.x, made = 0, cur = 0;  // items made, and the one whose keys are loaded
+      unsigned st = 0, phase = 1, k_issued = 0, q_issued = 0;
+      bool ok = true, more = true, started = false;
+      int b = 0, h = 0, row0 = 0, klen = 0, t = 0, te = 0;  // of that item
+#pragma unroll 1
+      while (ok) {
+        // the next item when there is none, and up to two ahead once the first keys of one are on their way
+        if (more && made < cur + (started ? 3u : 1u)) {
           const unsigned c = next;
           if (lane == 0) next = gridDim.x + atomicAdd(claim, 1u);
           next = __shfl_sync(0xffffffffu, next, 0);
@@ -460,45 +404,101 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             more = false;
             continue;
           }
-          // what the loads will find in L2
-          if (lane < C::kHalves && it.te > it.t0)
-            tc::tma_prefetch_l2_3d(&tmQ, lane * 64, it.h * rp.group, it.row0 + it.pos0);
-          const int n = it.te - it.t0, left = it.klen - (it.te - 1) * kBN;
-#pragma unroll
-          for (int i = 0; i < kItemsAhead; ++i)
-            if (made % kItemsAhead == (unsigned)i) {
-              ends[i] = n;
-              lefts[i] = left;
-            }
           ++made;
+          if (lane < C::kHalves && it.te > it.t0)  // what the loads will find in L2
+            tc::tma_prefetch_l2_3d(&tmQ, lane * 64, it.h * rp.group, it.row0 + it.pos0);
           continue;
         }
-        int n = 0, left = 0;
-#pragma unroll
-        for (int i = 0; i < kItemsAhead; ++i)
-          if (settled % kItemsAhead == (unsigned)i) {
-            n = ends[i];
-            left = lefts[i];
+        if (!started) {
+          if (cur == made) break;  // no more
+          const TcItem& it = items[cur % kItemSlots];
+          b = it.b; h = it.h; row0 = it.row0; klen = it.klen; t = it.t0; te = it.te;
+          if (t == te) {
+            ++cur;
+            continue;
           }
-        ++settled;
-        if (n == 0) continue;
-        v_pos += n;
-        ok = warp_wait_small(&bars->lastv[with_tiles & 3], (with_tiles >> 2) & 1, abort_flag);
-        ++with_tiles;
-        if (ok && left < kBN) {  // the item's last V tile: clear its rows past the last visible key
-          const unsigned j = v_pos - 1, st = j % C::kNS;
-          ok = warp_wait_small(&bars->vfull[st], (j / C::kNS) & 1, abort_flag);
+          const unsigned qb = q_issued & 1;
+          ok = warp_wait_small(&bars->qempty[qb], ((q_issued >> 1) & 1) ^ 1, abort_flag);
           if (!ok) break;
-          unsigned char* dst = base + C::off_V + st * C::kTile;
-#pragma unroll 1
-          for (int idx = left * C::kHalves * 8 + lane; idx < kBN * C::kHalves * 8; idx += 32)
-            *reinterpret_cast<uint4*>(dst + ((idx >> 3) % C::kHalves) * kAtom + idx / (C::kHalves * 8) * 128 +
-                                      (idx & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          tc::fence_async_smem();
+          if (lane == 0) mbar_arrive_expect_tx(&bars->qfull[qb], (uint32_t)(C::kHalves * p.tokens * rp.group * 128));
           __syncwarp();
-          if (lane == 0) mbar_arrive(&bars->vclr[st]);
+          if (lane < C::kHalves)
+            tc::tma_load_3d(base + C::off_Q + qb * C::kTile + lane * kAtom, &tmQ, lane * 64, h * rp.group, row0 + it.pos0,
+                            &bars->qfull[qb], pol_q);
+          ++q_issued;
+          started = true;
+        }
+        const int left = klen - t * kBN;
+        const int2 x = box.any(left) ? box.where(rp, b, h, row0, t) : make_int2(0, 0);
+        ok = warp_wait_small(&bars->kempty[st], phase, abort_flag);
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(&bars->kfull[st], box.bytes(left, !rp.table));
+        __syncwarp();
+        if (box.any(left))
+          tc::tma_load_3d(base + C::off_K + st * C::kTile + box.hd * kAtom + box.at * 128, &tmK, box.hd * 64, x.x, x.y,
+                          &bars->kfull[st], pol_k);
+        __syncwarp();
+        ++k_issued;
+        if (++st == C::kNS) {
+          st = 0;
+          phase ^= 1;
+        }
+        if (++t == te) {
+          started = false;
+          ++cur;
         }
       }
+      if (!ok) {  // aborted: let issued loads land before the CTA exits
+        for (unsigned j = k_issued > C::kNS ? k_issued - C::kNS : 0; j < k_issued; ++j)
+          mbar_drain(bars->kfull + j % C::kNS, (j / C::kNS) & 1);
+        for (unsigned j = q_issued > 2 ? q_issued - 2 : 0; j < q_issued; ++j) mbar_drain(&bars->qfull[j & 1], (j >> 1) & 1);
+      }
+    } else if (warp == kVWarp) {
+      // ------------------------------------------------------------ V
+      const uint64_t pol_v = policy_evict_last();
+      if (lane == 0) tc::prefetch_tmap(&tmV);
+      const Boxes<C::kHalves> box(p, lane);
+      unsigned st = 0, phase = 1, v_issued = 0;
+      bool ok = true;
+      ItemReader reader;
+      while (ok) {
+        const TcItem* at = reader.next(bars, items, abort_flag);
+        if (!at) break;
+        const int b = at->b, h = at->h, row0 = at->row0, klen = at->klen, t0 = at->t0, te = at->te;
+        reader.release(bars, lane);
+#pragma unroll 1
+        for (int t = t0; t < te; ++t) {
+          const int left = klen - t * kBN;
+          const int2 x = box.any(left) ? box.where(rp, b, h, row0, t) : make_int2(0, 0);
+          ok = warp_wait_small(&bars->vempty[st], phase, abort_flag);
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(&bars->vfull[st], box.bytes(left, !rp.table));
+          __syncwarp();
+          unsigned char* dst = base + C::off_V + st * C::kTile;
+          if (box.any(left))
+            tc::tma_load_3d(dst + box.hd * kAtom + box.at * 128, &tmV, box.hd * 64, x.x, x.y, &bars->vfull[st], pol_v);
+          __syncwarp();
+          ++v_issued;
+          if (left < kBN) {  // the item's last V tile: clear its rows past the last visible key
+            ok = warp_wait_small(&bars->vfull[st], phase ^ 1, abort_flag);
+            if (!ok) break;
+#pragma unroll 1
+            for (int idx = left * C::kHalves * 8 + lane; idx < kBN * C::kHalves * 8; idx += 32)
+              *reinterpret_cast<uint4*>(dst + ((idx >> 3) % C::kHalves) * kAtom + idx / (C::kHalves * 8) * 128 +
+                                        (idx & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            tc::fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->vclr[st]);
+          }
+          if (++st == C::kNS) {
+            st = 0;
+            phase ^= 1;
+          }
+        }
+      }
+      if (!ok)
+        for (unsigned j = v_issued > C::kNS ? v_issued - C::kNS : 0; j < v_issued; ++j)
+          mbar_drain(bars->vfull + j % C::kNS, (j / C::kNS) & 1);
     } else {
       // ------------------------------------------------------------ products
       const bool scores = warp == kSWarp;
@@ -941,7 +941,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       *finished = 0u;
     }
   }
-  if (warp == kItemWarp) {
+  if (warp == kKWarp) {
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem, kTmemCols);
   }
