@@ -64,7 +64,9 @@ constexpr int kMaxGrid = 160;
 constexpr int kMaxChunks = 3 * kMaxGrid;  // partial slots: below 2 grids of items and one grid more of chunks
 constexpr int kMinChunkTiles = 4;
 constexpr int kSortMost = 128;         // sequences that are taken in the order of their keys
-constexpr int kTableMost = 512;        // sequences whose lengths are kept in shared memory
+constexpr int kListMost = 3072;        // entries (sequence, row tile, chunk) that are listed in shared memory
+constexpr int kLevelMost = 4096;       // row tiles of a sequence, and chunks of one, that a list entry holds
+constexpr int kChunkMost = 512;
 constexpr long long kL2Bytes = 48ll << 20;
 
 // Workspace: status word, the claim counter and the count of finished CTAs in the header, arrival counters [chunk slot]
@@ -73,8 +75,11 @@ constexpr size_t kCountOff = WsLayout::kHeader;
 constexpr size_t kPartOff = (kCountOff + kMaxChunks * 4 * sizeof(unsigned) + 255) / 256 * 256;
 
 struct Bars {
-  uint64_t kfull[4], kempty[4], vfull[4], vempty[4], vclr[4];
-  uint64_t qfull[2], qempty[2], sfull[kSBufs], pfull[kSBufs], bfree[kSBufs];  // bfree: P V has read the buffer, and added to O
+  uint64_t kfull[4], vfull;  // vfull: of a V tile whose end is cleared before P meets it
+  uint64_t qfull[2], qempty[2];
+  uint64_t sfull[kSBufs];  // S is there, and its K stage free
+  uint64_t pvfull[kSBufs]; // P and the V tile that it meets are there
+  uint64_t bfree[kSBufs];  // P V has read both, and added to O
   uint64_t olast, ofree, lready, lfree;
   uint64_t turn[4][2];    // [quarter][tile parity]: a tile's reference is there
   uint64_t itemfull[kItemSlots], itemempty[kItemSlots];
@@ -93,7 +98,9 @@ template <int D>
 struct TcCfg {
   static constexpr int kHalves = D / 64;
   static constexpr uint32_t kTile = kHalves * kAtom;  // 128 rows x D
-  static constexpr unsigned kNS = D == 128 ? 2 : 4;   // stages of the K ring and of the V ring
+  // stages of the K ring and of the V ring; no more than S buffers, whose barriers say when a stage is free
+  static constexpr unsigned kNS = D == 128 ? 2 : 3;
+  static_assert(kNS <= kSBufs, "stage release");
   static constexpr uint32_t off_Q = 0;                // two items' queries
   static constexpr uint32_t off_K = 2 * kTile;
   static constexpr uint32_t off_V = off_K + kNS * kTile;
@@ -101,10 +108,11 @@ struct TcCfg {
   static constexpr uint32_t off_bar = off_stage + 4 * 4096;
   static constexpr uint32_t off_item = off_bar + sizeof(Bars);
   static constexpr uint32_t off_misc = (off_item + kItemSlots * sizeof(TcItem) + 15) / 16 * 16;
-  static constexpr uint32_t off_rows = off_misc + 64;               // [row] references, then sums [group][row], then final
+  static constexpr uint32_t off_rows = off_misc + 96;               // [row] references, then sums [group][row], then final
   static constexpr uint32_t off_table = off_rows + 4 * kBM * 4;     // lengths, in the order in which they are taken
-  static constexpr uint32_t off_order = off_table + kTableMost * 16;
-  static constexpr size_t kSmem = 1024 + off_order + kSortMost * 4;
+  static constexpr uint32_t off_order = off_table + kSortMost * 16;
+  static constexpr uint32_t off_list = off_order + kSortMost * 4;
+  static constexpr size_t kSmem = 1024 + off_list + kListMost * 4;
   static_assert(kSmem <= 227 * 1024, "shared memory");
   static constexpr uint32_t kColO = kSBufs * kBN;                   // TMEM columns: three S buffers, O
   static_assert(kColO + D <= kTmemCols, "TMEM columns");
@@ -124,6 +132,8 @@ struct Misc {
   int chunk_tiles;     // key tiles of a chunk
   int entries;         // (sequence, row tiles, chunk) triples
   int levels;          // the most row tiles of a sequence
+  int max_chunks;      // the most chunks of a row tile
+  int listed;          // the entries are in the list
   long long sum[3];
 };
 
@@ -137,6 +147,18 @@ __device__ __forceinline__ int chunks_of(const Seq& s, int tokens, int x, int ch
   if (x * tokens >= s.rows) return 0;
   const int nt = (keys_of(s, tokens, x) + kBN - 1) / kBN;
   return nt <= chunk_tiles ? 1 : (nt + chunk_tiles - 1) / chunk_tiles;
+}
+
+// n / d and the remainder by a multiplication, for n < 2^31 and r = reciprocal(d): the estimate is the quotient or one less.
+__device__ __forceinline__ unsigned reciprocal(unsigned d) { return d ? 0xffffffffu / d : 0u; }
+__device__ __forceinline__ unsigned divide(unsigned n, unsigned d, unsigned r, unsigned& rest) {
+  unsigned q = __umulhi(n, r);
+  rest = n - q * d;
+  if (rest >= d) {
+    rest -= d;
+    ++q;
+  }
+  return q;
 }
 
 template <int N>
@@ -200,6 +222,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   float* m_row = m_ref + 3 * kBM;                               // the item's last reference
   Seq* table = reinterpret_cast<Seq*>(base + C::off_table);
   int* order = reinterpret_cast<int*>(base + C::off_order);
+  uint32_t* list = reinterpret_cast<uint32_t*>(base + C::off_list);
   volatile int* abort_flag = &misc->abort;
   unsigned* status = reinterpret_cast<unsigned*>(p.ws);
   unsigned* claim = reinterpret_cast<unsigned*>(p.ws + WsLayout::kClaimOff);
@@ -212,9 +235,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll 1
       for (int i = 0; i < n; ++i) mbar_init(b + i, count);
     };
-    init(bars->kfull, 20, 1);  // kfull .. vclr
+    init(bars->kfull, 4, 1);
+    init(&bars->vfull, 1, 1);
     init(bars->qfull, 4 + kSBufs, 1);  // qfull, qempty, sfull
-    init(bars->pfull, kSBufs, 4);
+    init(bars->pvfull, kSBufs, 5);  // four softmax warps and the load
     init(bars->bfree, kSBufs, 1);
     init(&bars->olast, 1, 1);
     init(&bars->ofree, 1, 4);
@@ -226,6 +250,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     init(bars->drained, 2, 1);
     misc->abort = 0;
     misc->levels = 0;
+    misc->max_chunks = 1;
+    misc->listed = 0;
     misc->sum[0] = misc->sum[1] = misc->sum[2] = 0;
     fence_barrier_init();
   }
@@ -255,7 +281,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[2]), (unsigned long long)keys);
       atomicMax(&misc->levels, levels);
     }
-    if (rp.B <= kTableMost && threadIdx.x < rp.B) table[threadIdx.x] = seq_of(rp, threadIdx.x);
+    if (rp.B <= kSortMost && threadIdx.x < rp.B) table[threadIdx.x] = seq_of(rp, threadIdx.x);
     __syncthreads();
     if (rp.B <= kSortMost) {  // the most keys first
       Seq mine = {0, 0, 0, 0};
@@ -295,6 +321,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         } else {
 #pragma unroll 1
           for (int x = 0; x < n; ++x) entries += chunks_of(s, p.tokens, x, chunk);
+          if (n > 0) atomicMax(&misc->max_chunks, chunks_of(s, p.tokens, n - 1, chunk));  // (the last row tile sees the most)
         }
       }
       if (threadIdx.x == 0) misc->entries = 0;
@@ -307,6 +334,59 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       chunk = chunk > 0x3fffffff ? 0x7ffffffe : 2 * chunk;
     }
     if (threadIdx.x == 0) misc->chunk_tiles = chunk;
+    // The list of entries: level by level from the last rows on, in a level by sequence, in a row tile by chunk.  A warp a
+    // level; the levels' counts pass through the K stages, which hold nothing yet.
+    const int n_levels = misc->levels;
+    if (misc->entries <= kListMost && n_levels <= kLevelMost && misc->max_chunks <= kChunkMost) {
+      int* first = reinterpret_cast<int*>(base + C::off_K);
+      const auto entries_at = [&](int at, int level, bool& there) {
+        there = at < rp.B;
+        if (!there) return 0;
+        return chunks_of(rp.B <= kSortMost ? table[at] : seq_of(rp, at), p.tokens, level, chunk);
+      };
+#pragma unroll 1
+      for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+        for (int level = warp; level < n_levels; level += kTcThreads / 32) {
+          int to = pass ? first[level] : 0;
+#pragma unroll 1
+          for (int b0 = 0; b0 < rp.B; b0 += 32) {
+            bool there;
+            const int n = entries_at(b0 + lane, level, there);
+            int upto = n;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+              const int u = __shfl_up_sync(0xffffffffu, upto, off);
+              if (lane >= off) upto += u;
+            }
+            if (pass)
+              for (int c = 0; c < n; ++c) list[to + upto - n + c] = (uint32_t)(b0 + lane) | (uint32_t)level << 10 | (uint32_t)c << 22;
+            to += __shfl_sync(0xffffffffu, upto, 31);
+          }
+          if (!pass && lane == 0) first[level] = to;
+        }
+        __syncthreads();
+        if (pass) break;
+        if (warp == 0) {  // counts to places, the last level first
+          int before = 0;
+#pragma unroll 1
+          for (int l0 = n_levels - 1; l0 >= 0; l0 -= 32) {
+            const int level = l0 - lane, n = level >= 0 ? first[level] : 0;
+            int upto = n;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+              const int u = __shfl_up_sync(0xffffffffu, upto, off);
+              if (lane >= off) upto += u;
+            }
+            if (level >= 0) first[level] = before + upto - n;
+            before += __shfl_sync(0xffffffffu, upto, 31);
+          }
+        }
+        __syncthreads();
+      }
+      if (threadIdx.x == 0) misc->listed = 1;
+      tc::fence_async_smem();  // the loads write where the counts were
+    }
   }
   tc::fence_before_sync();
   __syncthreads();
@@ -322,37 +402,52 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const Boxes<C::kHalves> box(p, lane);
       const int entries = misc->entries, head_group = misc->head_group, chunk_tiles = misc->chunk_tiles;
       const unsigned claims = (unsigned)entries * rp.Hkv, per_group = (unsigned)entries * head_group;  // below 2^31
+      const unsigned by_group = reciprocal(per_group), by_heads = reciprocal(head_group),
+                     by_last = reciprocal(rp.Hkv % head_group);
       int level = misc->levels - 1, block = 0, acc = 0, group_at = 0;
       unsigned next = blockIdx.x, made = 0, cur = 0;  // items made, and the one whose keys are loaded
-      unsigned st = 0, phase = 1, k_issued = 0, q_issued = 0;
+      unsigned st = 0, k_issued = 0, q_issued = 0;
       bool ok = true, more = true, started = false;
       int b = 0, h = 0, row0 = 0, klen = 0, t = 0, te = 0;  // of that item
 #pragma unroll 1
       while (ok) {
         // the next item when there is none, and up to two ahead once the first keys of one are on their way
         if (more && made < cur + (started ? 3u : 1u)) {
-          const unsigned c = next;
-          if (lane == 0) next = gridDim.x + atomicAdd(claim, 1u);
-          next = __shfl_sync(0xffffffffu, next, 0);
+          const unsigned c = __shfl_sync(0xffffffffu, next, 0);
+          if (lane == 0) next = gridDim.x + atomicAdd(claim, 1u);  // needed for the item after this one
           TcItem it;
           it.b = -1;
           if (c < claims) {
-            const int hg = (int)(c / per_group), in_group = (int)(c - hg * per_group);
+            unsigned in_group, in_entry;
+            const int hg = (int)divide(c, per_group, by_group, in_group);
             const int left = rp.Hkv - hg * head_group, heads = left < head_group ? left : head_group;
-            const int e = in_group / heads;
+            const int e = (int)divide(in_group, heads, left < head_group ? by_last : by_heads, in_entry);
+            if (misc->listed) {
+              const uint32_t x = list[e];
+              const int at = x & 1023;
+              level = (x >> 10) & 4095;
+              it.chunk = x >> 22;
+              const Seq s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
+              it.b = rp.B <= kSortMost ? order[at] : at;
+              it.row0 = s.row0;
+              it.m = s.m;
+              it.kv = s.kv;
+              it.rows = s.rows;
+              it.chunks = chunks_of(s, p.tokens, level, chunk_tiles);
+            } else {
             if (hg != group_at) {
               group_at = hg;
               level = misc->levels - 1;
               block = acc = 0;
             }
-            // entry e: level by level from the last rows on, in a level by sequence
+            // entry e, found by the counts (many sequences or very long ones)
 #pragma unroll 1
             while (level >= 0) {
               const int at = block * 32 + lane;
               int n = 0;
               Seq s = {0, 0, 0, 0};
               if (at < rp.B) {
-                s = rp.B <= kTableMost ? table[at] : seq_of(rp, at);
+                s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
                 n = chunks_of(s, p.tokens, level, chunk_tiles);
               }
               int upto = n;
@@ -380,8 +475,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 --level;
               }
             }
+            }
             if (it.b >= 0) {
-              it.h = hg * head_group + (in_group - e * heads);
+              it.h = hg * head_group + (int)in_entry;
               it.pos0 = level * p.tokens;
               const Seq s = {it.row0, it.rows, it.m, it.kv};
               it.klen = keys_of(s, p.tokens, level);
@@ -430,8 +526,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
         const int left = klen - t * kBN;
         const int2 x = box.any(left) ? box.where(rp, b, h, row0, t) : make_int2(0, 0);
-        ok = warp_wait_small(&bars->kempty[st], phase, abort_flag);
-        if (!ok) break;
+        if (k_issued >= C::kNS) {  // S of the tile that had the stage
+          const unsigned j = k_issued - C::kNS;
+          ok = warp_wait_small(&bars->sfull[j % kSBufs], (j / kSBufs) & 1, abort_flag);
+          if (!ok) break;
+        }
         if (lane == 0) mbar_arrive_expect_tx(&bars->kfull[st], box.bytes(left, !rp.table));
         __syncwarp();
         if (box.any(left))
@@ -439,10 +538,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                           &bars->kfull[st], pol_k);
         __syncwarp();
         ++k_issued;
-        if (++st == C::kNS) {
-          st = 0;
-          phase ^= 1;
-        }
+        if (++st == C::kNS) st = 0;
         if (++t == te) {
           started = false;
           ++cur;
@@ -458,7 +554,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const uint64_t pol_v = policy_evict_last();
       if (lane == 0) tc::prefetch_tmap(&tmV);
       const Boxes<C::kHalves> box(p, lane);
-      unsigned st = 0, phase = 1, v_issued = 0;
+      unsigned st = 0, v_issued = 0, n_clear = 0;
       bool ok = true;
       ItemReader reader;
       while (ok) {
@@ -470,35 +566,39 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         for (int t = t0; t < te; ++t) {
           const int left = klen - t * kBN;
           const int2 x = box.any(left) ? box.where(rp, b, h, row0, t) : make_int2(0, 0);
-          ok = warp_wait_small(&bars->vempty[st], phase, abort_flag);
-          if (!ok) break;
-          if (lane == 0) mbar_arrive_expect_tx(&bars->vfull[st], box.bytes(left, !rp.table));
+          if (v_issued >= C::kNS) {  // P V of the tile that had the stage
+            const unsigned j = v_issued - C::kNS;
+            ok = warp_wait_small(&bars->bfree[j % kSBufs], (j / kSBufs) & 1, abort_flag);
+            if (!ok) break;
+          }
+          const unsigned bi = v_issued % kSBufs;
+          uint64_t* full = left < kBN ? &bars->vfull : &bars->pvfull[bi];
+          if (lane == 0) mbar_arrive_expect_tx(full, box.bytes(left, !rp.table));
           __syncwarp();
           unsigned char* dst = base + C::off_V + st * C::kTile;
           if (box.any(left))
-            tc::tma_load_3d(dst + box.hd * kAtom + box.at * 128, &tmV, box.hd * 64, x.x, x.y, &bars->vfull[st], pol_v);
+            tc::tma_load_3d(dst + box.hd * kAtom + box.at * 128, &tmV, box.hd * 64, x.x, x.y, full, pol_v);
           __syncwarp();
           ++v_issued;
           if (left < kBN) {  // the item's last V tile: clear its rows past the last visible key
-            ok = warp_wait_small(&bars->vfull[st], phase ^ 1, abort_flag);
+            ok = warp_wait_small(&bars->vfull, n_clear & 1, abort_flag);
             if (!ok) break;
+            ++n_clear;
 #pragma unroll 1
             for (int idx = left * C::kHalves * 8 + lane; idx < kBN * C::kHalves * 8; idx += 32)
               *reinterpret_cast<uint4*>(dst + ((idx >> 3) % C::kHalves) * kAtom + idx / (C::kHalves * 8) * 128 +
                                         (idx & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
             tc::fence_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->vclr[st]);
+            if (lane == 0) mbar_arrive(&bars->pvfull[bi]);
           }
-          if (++st == C::kNS) {
-            st = 0;
-            phase ^= 1;
-          }
+          if (++st == C::kNS) st = 0;
         }
       }
-      if (!ok)
+      if (!ok) {  // aborted: let issued loads land (a barrier that P never completes is waited for until its limit)
         for (unsigned j = v_issued > C::kNS ? v_issued - C::kNS : 0; j < v_issued; ++j)
-          mbar_drain(bars->vfull + j % C::kNS, (j / C::kNS) & 1);
+          mbar_drain(&bars->pvfull[j % kSBufs], (j / kSBufs) & 1);
+      }
     } else {
       // ------------------------------------------------------------ products
       const bool scores = warp == kSWarp;
@@ -507,14 +607,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const uint64_t dQ0 = tc::sw128_desc(smem_u32(base + C::off_Q), 16, 1024);
       const uint64_t dK0 = tc::sw128_desc(smem_u32(base + C::off_K), 16, 1024);
       const uint64_t dV0 = tc::sw128_desc(smem_u32(base + C::off_V), kAtom, 1024);
-      unsigned st = 0, phase = 0, bi = 0, b_phase = 0, n_items = 0, cleared = 0;
+      unsigned st = 0, phase = 0, bi = 0, b_phase = 0, n_items = 0;
       uint32_t col = tmem;
       bool ok = true;
       ItemReader reader;
       while (ok) {
         const TcItem* at = reader.next(bars, items, abort_flag);
         if (!at) break;
-        const int nt = at->te - at->t0, left = at->klen - (at->te - 1) * kBN;
+        const int nt = at->te - at->t0;
         reader.release(bars, lane);
         if (nt == 0) continue;
         if (lane == 0) {
@@ -535,7 +635,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 tc::mma_bf16(col, dQ + step, dK + step, idS, ks > 0 ? 1u : 0u);
               }
               tc::mma_commit(&bars->sfull[bi]);
-              tc::mma_commit(&bars->kempty[st]);
               if (t == 1) tc::mma_commit(&bars->qempty[n_items & 1]);
               if (++st == C::kNS) {
                 st = 0;
@@ -554,12 +653,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             uint32_t acc = 0;
 #pragma unroll 1
             for (int t = nt; ok && t > 0; --t) {
-              ok = mbar_wait_small(&bars->vfull[st], phase, abort_flag);
-              if (ok && t == 1 && left < kBN) {
-                ok = mbar_wait_small(&bars->vclr[st], (cleared >> st) & 1, abort_flag);
-                cleared ^= 1u << st;
-              }
-              ok = ok && mbar_wait_small(&bars->pfull[bi], b_phase, abort_flag);
+              ok = mbar_wait_small(&bars->pvfull[bi], b_phase, abort_flag);
               if (!ok) break;
               tc::fence_after_sync();
               const uint64_t dV = dV0 + st * desc_step(C::kTile);
@@ -568,7 +662,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 tc::mma_bf16_ts(tmem + C::kColO, col + ks * 8, dV + desc_step(ks * 16 * 128), idO, ks > 0 ? 1u : acc);
               acc = 1;
               tc::mma_commit(&bars->bfree[bi]);
-              tc::mma_commit(&bars->vempty[st]);
               if (t == 1) tc::mma_commit(&bars->olast);
               if (++st == C::kNS) {
                 st = 0;
@@ -905,7 +998,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         tc::tmem_wait_st();
         tc::fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->pfull[bi]);
+        if (lane == 0) mbar_arrive(&bars->pvfull[bi]);
         float a0, a1, b0, b1;
         unf2(fadd2(acc[0], acc[1]), a0, a1);
         unf2(fadd2(acc[2], acc[3]), b0, b1);
