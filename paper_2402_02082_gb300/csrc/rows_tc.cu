@@ -76,7 +76,7 @@ constexpr size_t kPartOff = (kCountOff + kMaxChunks * 4 * sizeof(unsigned) + 255
 
 struct Bars {
   uint64_t kfull[4], vfull;  // vfull: of a V tile whose end is cleared before P meets it
-  uint64_t qfull[2], qempty[2];
+  uint64_t qfull[2], qempty[2];  // qempty: the result warps are done with what was the queries' place
   uint64_t sfull[kSBufs];  // S is there, and its K stage free
   uint64_t pvfull[kSBufs]; // P and the V tile that it meets are there
   uint64_t bfree[kSBufs];  // P V has read both, and added to O
@@ -104,13 +104,13 @@ struct TcCfg {
   static constexpr uint32_t off_Q = 0;                // two items' queries
   static constexpr uint32_t off_K = 2 * kTile;
   static constexpr uint32_t off_V = off_K + kNS * kTile;
-  static constexpr uint32_t off_stage = off_V + kNS * kTile;  // 4 KB for each of the result warps
-  static constexpr uint32_t off_bar = off_stage + 4 * 4096;
+  static constexpr uint32_t off_bar = off_V + kNS * kTile;
   static constexpr uint32_t off_item = off_bar + sizeof(Bars);
   static constexpr uint32_t off_misc = (off_item + kItemSlots * sizeof(TcItem) + 15) / 16 * 16;
   static constexpr uint32_t off_rows = off_misc + 96;               // [row] references, then sums [group][row], then final
   static constexpr uint32_t off_table = off_rows + 4 * kBM * 4;     // lengths, in the order in which they are taken
-  static constexpr uint32_t off_order = off_table + kSortMost * 16;
+  static constexpr uint32_t off_rowat = off_table + kSortMost * 16;  // elements from a row tile's first row to its rows
+  static constexpr uint32_t off_order = off_rowat + kBM * 4;
   static constexpr uint32_t off_list = off_order + kSortMost * 4;
   static constexpr size_t kSmem = 1024 + off_list + kListMost * 4;
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -223,6 +223,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   Seq* table = reinterpret_cast<Seq*>(base + C::off_table);
   int* order = reinterpret_cast<int*>(base + C::off_order);
   uint32_t* list = reinterpret_cast<uint32_t*>(base + C::off_list);
+  int* row_at = reinterpret_cast<int*>(base + C::off_rowat);
   volatile int* abort_flag = &misc->abort;
   unsigned* status = reinterpret_cast<unsigned*>(p.ws);
   unsigned* claim = reinterpret_cast<unsigned*>(p.ws + WsLayout::kClaimOff);
@@ -237,7 +238,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     };
     init(bars->kfull, 4, 1);
     init(&bars->vfull, 1, 1);
-    init(bars->qfull, 4 + kSBufs, 1);  // qfull, qempty, sfull
+    init(bars->qfull, 2, 1);
+    init(bars->qempty, 2, 4);
+    init(bars->sfull, kSBufs, 1);
     init(bars->pvfull, kSBufs, 5);  // four softmax warps and the load
     init(bars->bfree, kSBufs, 1);
     init(&bars->olast, 1, 1);
@@ -261,6 +264,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     tc::tmem_alloc(&misc->tmem, kTmemCols);
     tc::tmem_relinquish();
   }
+  if (threadIdx.x < kBM) row_at[threadIdx.x] = (threadIdx.x / rp.group * rp.H + threadIdx.x % rp.group) * D;
   // ---- the plan of the call: what all CTAs find alike from the lengths
   {
     long long pairs = 0, units = 0, keys = 0;
@@ -394,7 +398,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const uint32_t tmem = misc->tmem;
 
   if (warp >= kKWarp && warp < kOutWarp0) {
-    tc_regs_down<88>();
+    tc_regs_down<104>();
     if (warp == kKWarp) {
       // ------------------------------------------------------------ items, Q and K
       const uint64_t pol_q = policy_evict_first(), pol_k = policy_evict_last();
@@ -635,7 +639,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 tc::mma_bf16(col, dQ + step, dK + step, idS, ks > 0 ? 1u : 0u);
               }
               tc::mma_commit(&bars->sfull[bi]);
-              if (t == 1) tc::mma_commit(&bars->qempty[n_items & 1]);
               if (++st == C::kNS) {
                 st = 0;
                 phase ^= 1;
@@ -686,22 +689,15 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       }
     }
   } else if (warp >= kOutWarp0) {
-    tc_regs_up<152>();
+    tc_regs_up<136>();
     // -------------------------------------------------------------- results
     const int quarter = warp - kOutWarp0;
-    unsigned char* stage = base + C::off_stage + quarter * 4096;
     const int r = quarter * 32 + lane;
     const int token = r / rp.group;
     const uint32_t o_col = tmem + ((uint32_t)(quarter * 32) << 16) + C::kColO;
     __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(rp.out);
     float* parts = reinterpret_cast<float*>(p.ws + kPartOff);
     constexpr size_t slot_floats = (size_t)kBM * (D + 2);
-    int row_at[8];  // elements from a row tile's first row to rows lane / 8 + 4 k of this quarter
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int x = quarter * 32 + (lane >> 3) + 4 * k, xt = x / rp.group;
-      row_at[k] = (xt * rp.H + (x - xt * rp.group)) * D;
-    }
     unsigned n_items = 0;  // with tiles
     ItemReader reader;
     bool ok = true;
@@ -738,85 +734,62 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (!ok) break;
       ++n_items;
       tc::fence_after_sync();
-      const auto free_o = [&] {
-        tc::fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->ofree);
-      };
-      if (!split) {
-        // 64 columns at a time: 128 bytes a row in the stage, 16-byte piece e of row x at e ^ (x & 7); then whole rows out
-        const float inv = sees > 0 ? 1.f / l : 0.f;
-        const uint64_t inv2 = f2(inv, inv);
-        uint64_t odd2 = 0ull;  // NaN once a result is not finite
-        __nv_bfloat16* const to = out + ((size_t)(it.row0 + it.pos0) * rp.H + it.h * rp.group) * D + 8 * (lane & 7);
+      // O, 32 columns at a time, through what was the place of the item's queries (S is done with them), then out in whole
+      // rows.  bf16: 16-byte piece e of row x at e ^ (x & 7) of its 256 (D = 64: 128) bytes; rolled loops (code size).
+      unsigned char* stage = base + C::off_Q + ((n_items - 1) & 1) * C::kTile + quarter * 32 * (2 * D);
+      const float inv = split ? 1.f : sees > 0 ? 1.f / l : 0.f;
+      const uint64_t inv2 = f2(inv, inv);
+      uint64_t odd2 = 0ull;  // NaN once a result is not finite
+      float* part = parts + it.slot * slot_floats + (size_t)(quarter * 32) * (D + 2);
 #pragma unroll 1
-        for (int c = 0; c < opaque(D / 64); ++c) {
-          uint32_t o[64];
-          tc::tmem_ld32(o_col + c * 64, *reinterpret_cast<uint32_t(*)[32]>(o));
-          tc::tmem_ld32(o_col + c * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(o + 32));
-          tc::tmem_wait_ld();
-          if (c == D / 64 - 1) free_o();
-          if (sees == 0) {
+      for (int c = 0; c < opaque(D / 32); ++c) {
+        uint32_t o[32];
+        tc::tmem_ld32(o_col + c * 32, o);
+        tc::tmem_wait_ld();
+        if (split) {  // a partial result: fp32, a row a lane
+          float* at = part + (size_t)lane * (D + 2) + 2 + 32 * c;  // (rows are 8-byte aligned)
+          if (valid) {
 #pragma unroll
-            for (int e = 0; e < 64; ++e) o[e] = 0u;
+            for (int e = 0; e < 32; e += 2) *reinterpret_cast<uint2*>(at + e) = make_uint2(sees ? o[e] : 0u, sees ? o[e + 1] : 0u);
           }
+          continue;
+        }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            uint32_t w[4];
+        for (int e = 0; e < 4; ++e) {
+          uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t* a = o + 8 * e + 2 * k;
-              const uint64_t v = ffma2(f2(__uint_as_float(a[0]), __uint_as_float(a[1])), inv2, 0ull);
-              odd2 = ffma2(v, 0ull, odd2);
-              float lo, hi;
-              unf2(v, lo, hi);
-              w[k] = pack_bf16x2(lo, hi);
-            }
-            *reinterpret_cast<uint4*>(stage + lane * 128 + ((e ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t* a = o + 8 * e + 2 * k;
+            const uint64_t v = ffma2(f2(__uint_as_float(a[0]), __uint_as_float(a[1])), inv2, 0ull);
+            odd2 = ffma2(v, 0ull, odd2);
+            float lo, hi;
+            unf2(v, lo, hi);
+            w[k] = sees ? pack_bf16x2(lo, hi) : 0u;
           }
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int x = (lane >> 3) + 4 * k;
-            const uint4 v = *reinterpret_cast<const uint4*>(stage + x * 128 + (((lane & 7) ^ (x & 7)) << 4));
-            if ((any >> x) & 1u) *reinterpret_cast<uint4*>(to + row_at[k] + 64 * c) = v;
-          }
-          __syncwarp();
+          *reinterpret_cast<uint4*>(stage + lane * (2 * D) + (((4 * c + e) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->ofree);
+      if (split) {
+        if (valid) *reinterpret_cast<float2*>(part + (size_t)lane * (D + 2)) = make_float2(mx, l);
+      } else {
+        constexpr int kPieces = D / 8, kRowsAt = 32 / kPieces;  // of a row; rows that the warp writes at once
+        const int e = lane % kPieces;
+        __nv_bfloat16* const to = out + ((size_t)(it.row0 + it.pos0) * rp.H + it.h * rp.group) * D + 8 * e;
+#pragma unroll 4
+        for (int x = lane / kPieces; x < 32; x += kRowsAt) {
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + x * (2 * D) + ((e ^ (x & 7)) << 4));
+          if ((any >> x) & 1u) *reinterpret_cast<uint4*>(to + row_at[quarter * 32 + x]) = v;
         }
         float lo, hi;
         unf2(odd2, lo, hi);
         again = __ballot_sync(0xffffffffu, sees > 0 && !(lo == 0.f && hi == 0.f));
-      } else {
-        // a partial result: 32 fp32 columns at a time, as above
-        float* part = parts + it.slot * slot_floats + (size_t)(quarter * 32) * (D + 2);
-#pragma unroll 1
-        for (int c = 0; c < opaque(D / 32); ++c) {
-          uint32_t o[32];
-          tc::tmem_ld32(o_col + c * 32, o);
-          tc::tmem_wait_ld();
-          if (c == D / 32 - 1) free_o();
-          if (sees == 0) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0u;
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint32_t* a = o + 4 * e;
-            *reinterpret_cast<uint4*>(stage + lane * 128 + ((e ^ (lane & 7)) << 4)) = make_uint4(a[0], a[1], a[2], a[3]);
-          }
-          __syncwarp();
-#pragma unroll 1
-          for (int x = lane >> 3; x < opaque(32); x += 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(stage + x * 128 + (((lane & 7) ^ (x & 7)) << 4));
-            if (!((any >> x) & 1u)) continue;
-            float* at = part + (size_t)x * (D + 2) + 2 + 32 * c + 4 * (lane & 7);  // (rows are 8-byte aligned)
-            *reinterpret_cast<uint2*>(at) = make_uint2(v.x, v.y);
-            *reinterpret_cast<uint2*>(at + 2) = make_uint2(v.z, v.w);
-          }
-          __syncwarp();
-        }
-        if (valid) *reinterpret_cast<float2*>(part + (size_t)lane * (D + 2)) = make_float2(mx, l);
+        tc::fence_async_smem();  // the next queries come by the asynchronous proxy
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->qempty[(n_items - 1) & 1]);
       // ---- this chunk's rows are there; the warp that completes the item's count merges its quarter's rows
       bool merge = split;
       if (split) {
@@ -915,12 +888,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         // keys that this row does not see: -inf (a suffix of the tile), written back in the 32-key chunks that have one
         const int key0 = (t0 + t) * kBN;
         if (key0 + kBN > all_see) {
-          const int nv = limit - key0, nv_min = __reduce_min_sync(0xffffffffu, nv);
+          const int nv = limit - key0, nv_min = __reduce_min_sync(0xffffffffu, nv), nv_max = __reduce_max_sync(0xffffffffu, nv);
 #pragma unroll 1
           for (int c = nv_min < 0 ? 0 : nv_min >> 5; c < opaque(kBN / 32); ++c) {
             uint32_t o[32];
-            tc::tmem_ld32(s_col + c * 32, o);
-            tc::tmem_wait_ld();
+            if (32 * c < nv_max) {
+              tc::tmem_ld32(s_col + c * 32, o);
+              tc::tmem_wait_ld();
+            }
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = 32 * c + e < nv ? o[e] : 0xff800000u;
             tc::tmem_st32(s_col + c * 32, o);
