@@ -78,52 +78,85 @@ __device__ __forceinline__ size_t key_at(const RowsParams& p, int b, int row0, i
   return ((((size_t)page * p.Hkv + h) << p.page_shift) + r) * kRow;
 }
 
-// o[e], column lane * (D / 32) + e of the result of query head h in row `row` (row i of sequence b) over its first n > 0
-// keys.  All lanes of a warp.  (Inlined: a kernel that splits its registers among its warps holds no call.)
-template <typename T, int D>
-__device__ __forceinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, int n, float (&o)[D / 32]) {
+// The softmax of some of a row's keys: (max, sum, columns lane * (D / 32) .. of the weighted values).
+template <int D>
+struct RowPart {
+  float m, l, o[D / 32];
+};
+
+template <int D>
+__device__ __forceinline__ RowPart<D> no_keys() {
+  RowPart<D> r;
+  r.m = -CUDART_INF_F;
+  r.l = 0.f;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) r.o[e] = 0.f;
+  return r;
+}
+
+// Query head h in row `row0 + i` (row i of sequence b) over its keys first .. first + 31, first + step .., below n > 0.  All
+// lanes of a warp.  kAtOnce: loads in flight.  (Inlined: a kernel that splits its registers among its warps holds no call.)
+template <typename T, int D, int kAtOnce>
+__device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Seq& s, int i, int h, int n, int first, int step,
+                                            RowPart<D>& r) {
   constexpr int kE = D / 32, kRow = D * (int)sizeof(T), kC = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 31, hk = h / p.group;
   const unsigned char* q = p.q + (long long)(s.row0 + i) * p.q_stride + (size_t)h * kRow;
-  float m = -CUDART_INF_F, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < kE; ++e) o[e] = 0.f;
-  for (int t0 = 0; t0 < n; t0 += 32) {
+#pragma unroll 1
+  for (int t0 = first; t0 < n; t0 += step) {
     const int t = t0 + lane;
     float u = -CUDART_INF_F;
+    size_t v_at = 0;  // of key t
     if (t < n) {
       const unsigned char* k = p.K + key_at<kRow>(p, b, s.row0, hk, t, p.k_stride);
+      v_at = key_at<kRow>(p, b, s.row0, hk, t, p.v_stride);
       float acc[2] = {0.f, 0.f};
-#pragma unroll 4
+#pragma unroll kAtOnce
       for (int c = 0; c < D / kC; ++c)
         dot_chunk<T>(*reinterpret_cast<const uint4*>(q + 16 * c), *reinterpret_cast<const uint4*>(k + 16 * c), acc);
       u = (acc[0] + acc[1]) * p.scale_log2;
     }
-    const float m_new = fmaxf(m, warp_max(u));
+    const float m_new = fmaxf(r.m, warp_max(u));
     const float m_eff = m_new == -CUDART_INF_F ? 0.f : m_new;
-    float f = fast_exp2(m - m_eff);
-    if (m != -CUDART_INF_F) f = f < FLT_MIN ? FLT_MIN : f;  // (a NaN stays one)
+    float f = fast_exp2(r.m - m_eff);
+    if (r.m != -CUDART_INF_F) f = f < FLT_MIN ? FLT_MIN : f;  // (a NaN stays one)
     float w = fast_exp2(u - m_eff);
     if (u != -CUDART_INF_F) w = w < FLT_MIN ? FLT_MIN : w;
-    l = l * f + warp_sum(w);
+    r.l = r.l * f + warp_sum(w);
 #pragma unroll
-    for (int e = 0; e < kE; ++e) o[e] *= f;
-    m = m_new;
+    for (int e = 0; e < kE; ++e) r.o[e] *= f;
+    r.m = m_new;
     const int most = n - t0 < 32 ? n - t0 : 32;
-#pragma unroll 4
-    for (int j = 0; j < most; ++j) {
-      const float pj = __shfl_sync(0xffffffffu, w, j);
-      if (pj == 0.f) continue;  // a score of -inf: no weight, whatever the value
-      float v[kE];
-      load_row_chunk<T, kE>(reinterpret_cast<const T*>(p.V + key_at<kRow>(p, b, s.row0, hk, t0 + j, p.v_stride)) + lane * kE, v);
+#pragma unroll 1
+    for (int j0 = 0; j0 < most; j0 += kAtOnce) {
+      float v[kAtOnce][kE];
 #pragma unroll
-      for (int e = 0; e < kE; ++e) o[e] = fmaf(pj, v[e], o[e]);
+      for (int j = 0; j < kAtOnce; ++j) {
+        const size_t at = __shfl_sync(0xffffffffu, v_at, (j0 + j) & 31);
+        if (j0 + j < most) load_row_chunk<T, kE>(reinterpret_cast<const T*>(p.V + at) + lane * kE, v[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const float pj = __shfl_sync(0xffffffffu, w, (j0 + j) & 31);
+        if (j0 + j >= most || pj == 0.f) continue;  // a score of -inf: no weight, whatever the value
+#pragma unroll
+        for (int e = 0; e < kE; ++e) r.o[e] = fmaf(pj, v[j][e], r.o[e]);
+      }
     }
   }
-#pragma unroll
-  for (int e = 0; e < kE; ++e) o[e] /= l;
 }
 
+// The whole row by one warp: o[e], column lane * (D / 32) + e of the result over the first n > 0 keys.
+template <typename T, int D>
+__device__ __forceinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, int n, float (&o)[D / 32]) {
+  RowPart<D> r = no_keys<D>();
+  attend_keys<T, D, 4>(p, b, s, i, h, n, 0, 32, r);
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) o[e] = r.o[e] / r.l;
+}
+
+__device__ __forceinline__ void store_one(float* at, float v) { *at = v; }
+__device__ __forceinline__ void store_one(__nv_bfloat16* at, float v) { *at = __float2bfloat16_rn(v); }
 template <int kE>
 __device__ __forceinline__ void store_row(float* at, const float (&o)[kE]) {
 #pragma unroll
