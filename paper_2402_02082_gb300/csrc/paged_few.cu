@@ -93,6 +93,11 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
     __syncthreads();
     b = sm.slab_b;
   }
+  const int step = C * kFewWarps * kFewKeys;
+  int key0 = (rank * kFewWarps + warp) * kFewKeys;
+  // (by the bound of the lengths, so that the first numbers are on their way beside the length)
+  const auto page_of = [&](int key0) { return key0 < p.max_kv ? page_at(p, b, key0 >> p.page_shift) : 0; };
+  int page = page_of(key0), page_next = page_of(key0 + step);
   const Seq s = seq_of(p, b);
   const int rows = s.rows * p.group < kR ? s.rows * p.group : kR;
   const int n = rows > 0 ? seen(s, s.rows - 1) : 0;  // keys that some row sees
@@ -100,7 +105,6 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
 
   // this lane's pieces of a tile; keys that no row sees are zeros (the pool may hold anything there)
   uint4 kr[2][kPK], vr[4][kPV];
-  const auto page_of = [&](int key0) { return key0 < n ? page_at(p, b, key0 >> p.page_shift) : 0; };
   const auto row_of = [&](const unsigned char* base, int page, int key) {
     return base + ((((size_t)page * p.Hkv + h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * (2 * D);
   };
@@ -128,9 +132,6 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
       }
     }
   };
-  const int step = C * kFewWarps * kFewKeys;
-  int key0 = (rank * kFewWarps + warp) * kFewKeys;
-  int page = page_of(key0), page_next = page_of(key0 + step);
   load_k(page, key0);
 
   if (warp < NT) {  // the queries' fragments, by a warp for 8 of them
@@ -339,6 +340,36 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
   }
 }
 
+// CTAs of a slab's cluster, for up to `keys` keys: the C of least estimated time.  A CTA alone streams ~40 GB/s and all of
+// them ~7 TB/s, each wave costs its start of ~2.5 us, and the last wave has what is left.  Only the bound of the lengths is
+// known here, so a call of several requests is judged by the sum of two: all at the bound, and half of that in the mean
+// with one at the bound, which the longest CTA then may decide.  us by C = 1 / 2 / 4 / 8: 208 slabs of 16384 keys 277 / 293 /
+// 264 / 268, 256 of 1024 to 16384 keys 201 / 153 / 160 / 180, 512 of up to 1024 keys 39 / 46 / 59 / 92, 32 of 8192
+// keys 85 / 47 / 30 / 26, 128 of up to 4096 keys (64 dims) 31 / 22 / 25 / 33.
+int pick(long long slabs, long long slots, int keys, int row_bytes, bool several) {
+  const float mb = 2e-6f * (float)keys * (float)row_bytes;
+  constexpr float kOne = 25.f, kAll = 1.f / 7.f, kStart = 2.5f;  // us per MB: a CTA alone, all together; us
+  int best = 1;
+  float least = 0.f;
+  for (int C = 1; C <= kMaxC; C *= 2) {
+    if (C > 1 && C * kFewWarps * kFewKeys >= 2LL * keys) break;  // no tiles for half of the warps
+    const long long n = slabs * C, full = n / slots, rest = n - full * slots;
+    const float part = mb / (float)C;
+    const auto wave = [&](float ctas) { return part * (ctas * kAll > kOne ? ctas * kAll : kOne); };
+    const float start = kStart * (float)(full + (rest ? 1 : 0));
+    float cost = (float)full * wave((float)slots) + (rest ? wave((float)rest) : 0.f) + start;
+    if (several) {
+      const float mean = 0.5f * mb * (float)slabs * kAll, longest = part * kOne;
+      cost += (mean > longest ? mean : longest) + start;
+    }
+    if (C == 1 || cost < least) {
+      least = cost;
+      best = C;
+    }
+  }
+  return best;
+}
+
 template <int D, int NT>
 cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   constexpr size_t kSmem = sizeof(FewSmem<D, NT>);
@@ -346,9 +377,7 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   cudaError_t e = allow_smem(allowed, paged_few_kernel<D, NT>, (int)kSmem);
   if (e != cudaSuccess) return e;
   const long long slabs = (long long)a.B * a.Hkv, slots = (NT == 1 ? 2LL : 1LL) * sm_count();
-  const long long tiles = ((long long)a.max_kv + kFewKeys - 1) / kFewKeys;
-  int C = kMaxC;
-  while (C > 1 && (slabs * C > slots && tiles < 4LL * C * kFewWarps || C * kFewWarps >= 2 * tiles)) C >>= 1;
+  const int C = pick(slabs, slots, a.max_kv, 2 * D, a.B > 1);
   if (slabs * C > 0x7fffffffLL) return cudaErrorNotSupported;
   const RowsParams p = rows_params(a);
   cudaLaunchConfig_t cfg = {};
