@@ -16,8 +16,8 @@
 //
 // Work items are (cached head, 128 / group tokens, keys), claimed from a counter: cached heads in groups whose keys and
 // values together stay in L2, in them the row tiles with the most keys first, so that the SMs end together.  Where there are
-// fewer than two items for an SM, an item's keys are cut into chunks; partial results (max, sum, o) go through the
-// workspace, and the warp that finishes an item's last chunk merges its rows in the chunks' order.
+// fewer than two items for an SM, an item's keys may be cut into chunks; their partial results (max, sum, o) go through the
+// workspace, rows side by side, and a second kernel merges them in the chunks' order.
 //
 // Code size counts: what does not stay in the instruction cache is fetched again by every role at every item.  A form of
 // this kernel with two row tiles a CTA, a softmax group each and rows of 128 scores in registers, unrolled, took 6000
@@ -62,17 +62,24 @@ constexpr int kItemSlots = 4;
 constexpr int kItemReaders = 15;       // warps that read an item beside the one that makes it
 constexpr int kMaxGrid = 160;
 constexpr int kMaxChunks = 3 * kMaxGrid;  // partial slots: below 2 grids of items and one grid more of chunks
-constexpr int kMinChunkTiles = 4;
+constexpr int kFewTiles = 12;          // key tiles of an item that are not worth a second kernel
 constexpr int kSortMost = 128;         // sequences that are taken in the order of their keys
 constexpr int kListMost = 3072;        // entries (sequence, row tile, chunk) that are listed in shared memory
-constexpr int kLevelMost = 4096;       // row tiles of a sequence, and chunks of one, that a list entry holds
-constexpr int kChunkMost = 512;
+constexpr int kLevelMost = 4096;       // row tiles of a sequence that a list entry holds
 constexpr long long kL2Bytes = 48ll << 20;
 
-// Workspace: status word, the claim counter and the count of finished CTAs in the header, arrival counters [chunk slot]
-// [quarter], then partial slots.
-constexpr size_t kCountOff = WsLayout::kHeader;
-constexpr size_t kPartOff = (kCountOff + kMaxChunks * 4 * sizeof(unsigned) + 255) / 256 * 256;
+// Workspace: in the header the status word, the claim counter, the count of finished CTAs, and for the merge the count of
+// items in chunks and that of its finished CTAs; then those items, then partial slots of [D + 2][128 rows] floats: a row's
+// maximum, its sum, its columns.
+struct PartItem {
+  int b, h, row0, m, kv, rows, pos0, chunks, slot, slot_step;
+};
+constexpr size_t kPartsOff = 64, kMergedOff = 96;
+constexpr size_t kPartItemsOff = WsLayout::kHeader;
+constexpr size_t kPartOff = (kPartItemsOff + 2 * kMaxGrid * sizeof(PartItem) + 255) / 256 * 256;
+// Chunks of the longest item that are tried: 2 .. 6, 8, 10, 12, 16, 20, 24.
+constexpr int kSplitCount = 11;
+__host__ __device__ constexpr int split_of(int i) { return i < 5 ? i + 2 : (i < 8 ? 2 * i - 2 : 4 * (i - 4)); }
 
 struct Bars {
   uint64_t kfull[4], vfull;  // vfull: of a V tile whose end is cleared before P meets it
@@ -107,7 +114,7 @@ struct TcCfg {
   static constexpr uint32_t off_bar = off_V + kNS * kTile;
   static constexpr uint32_t off_item = off_bar + sizeof(Bars);
   static constexpr uint32_t off_misc = (off_item + kItemSlots * sizeof(TcItem) + 15) / 16 * 16;
-  static constexpr uint32_t off_rows = off_misc + 96;               // [row] references, then sums [group][row], then final
+  static constexpr uint32_t off_rows = off_misc + 128;               // [row] references, then sums [group][row], then final
   static constexpr uint32_t off_table = off_rows + 4 * kBM * 4;     // lengths, in the order in which they are taken
   static constexpr uint32_t off_rowat = off_table + kSortMost * 16;  // elements from a row tile's first row to its rows
   static constexpr uint32_t off_order = off_rowat + kBM * 4;
@@ -121,6 +128,7 @@ struct TcCfg {
 struct TcParams {
   RowsParams r;
   unsigned char* ws;
+  int may_split;   // a merge kernel follows
   int tokens;      // of a row tile: 128 / group
   int box_rows;    // key rows of one TMA box: a page's, at most 128
 };
@@ -132,9 +140,10 @@ struct Misc {
   int chunk_tiles;     // key tiles of a chunk
   int entries;         // (sequence, row tiles, chunk) triples
   int levels;          // the most row tiles of a sequence
-  int max_chunks;      // the most chunks of a row tile
   int listed;          // the entries are in the list
-  long long sum[3];
+  long long sum[2];
+  int longest;         // key tiles of the item with the most
+  int splits[kSplitCount];  // entries by chunks of the longest item
 };
 
 // Row tiles of a sequence, and the keys that the last row of tile x sees.
@@ -231,10 +240,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const RowsParams& rp = p.r;
-  if (threadIdx.x == 0) {
-    const auto init = [](uint64_t* b, int n, int count) {
-#pragma unroll 1
-      for (int i = 0; i < n; ++i) mbar_init(b + i, count);
+  {  // a warp a kind, a lane a barrier
+    int w = 0;
+    const auto init = [&](uint64_t* b, int n, int count) {
+      if (warp == w++ && lane < n) mbar_init(b + lane, count);
     };
     init(bars->kfull, 4, 1);
     init(&bars->vfull, 1, 1);
@@ -251,11 +260,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     init(bars->itemfull, kItemSlots, 1);
     init(bars->itemempty, kItemSlots, kItemReaders);
     init(bars->drained, 2, 1);
-    misc->abort = 0;
-    misc->levels = 0;
-    misc->max_chunks = 1;
-    misc->listed = 0;
-    misc->sum[0] = misc->sum[1] = misc->sum[2] = 0;
+    if (warp == 15) {
+      if (lane < kSplitCount) misc->splits[lane] = 0;
+      if (lane == 0) {
+        misc->abort = 0;
+        misc->levels = 0;
+        misc->listed = 0;
+        misc->longest = 0;
+        misc->sum[0] = misc->sum[1] = 0;
+      }
+    }
     fence_barrier_init();
   }
   __syncthreads();
@@ -267,25 +281,26 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (threadIdx.x < kBM) row_at[threadIdx.x] = (threadIdx.x / rp.group * rp.H + threadIdx.x % rp.group) * D;
   // ---- the plan of the call: what all CTAs find alike from the lengths
   {
-    long long pairs = 0, units = 0, keys = 0;
-    int levels = 0;
+    long long tiles = 0, keys = 0;
+    int levels = 0, longest = 0;
+    if (rp.B <= kSortMost && threadIdx.x < rp.B) table[threadIdx.x] = seq_of(rp, threadIdx.x);
 #pragma unroll 1
     for (int b = threadIdx.x; b < rp.B; b += kTcThreads) {
       const Seq s = seq_of(rp, b);
       const int n = tiles_of(s, p.tokens);
-      const int mean = s.kv - s.m + (s.rows + 1) / 2;
-      pairs += n;
-      units += (long long)n * (((mean > 0 ? mean : 0) + kBN) / kBN);
+      if (n == 0) continue;
+      tiles += n;
       keys += s.kv;
       levels = n > levels ? n : levels;
+      const int nt = (keys_of(s, p.tokens, n - 1) + kBN - 1) / kBN;
+      longest = nt > longest ? nt : longest;
     }
-    if (pairs) {
-      atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[0]), (unsigned long long)pairs);
-      atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[1]), (unsigned long long)units);
-      atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[2]), (unsigned long long)keys);
+    if (tiles) {
+      atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[0]), (unsigned long long)tiles);
+      atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[1]), (unsigned long long)keys);
       atomicMax(&misc->levels, levels);
+      atomicMax(&misc->longest, longest);
     }
-    if (rp.B <= kSortMost && threadIdx.x < rp.B) table[threadIdx.x] = seq_of(rp, threadIdx.x);
     __syncthreads();
     if (rp.B <= kSortMost) {  // the most keys first
       Seq mine = {0, 0, 0, 0};
@@ -301,47 +316,47 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         order[before] = threadIdx.x;
       }
     }
-    const long long n_items = misc->sum[0] * rp.Hkv, n_units = misc->sum[1] * rp.Hkv;
     int chunk = 0x7fffffff;
-    if (n_items < 2ll * gridDim.x) {  // an SM's share of the key tiles
-      const long long c = (n_units + gridDim.x - 1) / gridDim.x;
-      chunk = c < kMinChunkTiles ? kMinChunkTiles : (int)c;
-    }
-    if (threadIdx.x == 0) {
-      const long long bytes = misc->sum[2] * D * 4;  // keys and values of a cached head
-      const long long g = bytes > 0 ? kL2Bytes / bytes : rp.Hkv;
-      misc->head_group = (int)(g < 1 ? 1 : (g > rp.Hkv ? rp.Hkv : g));
-    }
-    // whole items need no slots; chunks grow until there is one for each (no more than the items, then)
-#pragma unroll 1
-    while (true) {
-      int entries = 0;
+    long long entries = misc->sum[0];
+    const int G = gridDim.x;
+    longest = misc->longest;
+    if (p.may_split && entries * rp.Hkv < 2ll * G && longest > kFewTiles) {
+      // Chunks of the longest item: the number whose rounds over the SMs cost least, a chunk 3 key tiles beside its
+      // own and the merge 6.
 #pragma unroll 1
       for (int b = threadIdx.x; b < rp.B; b += kTcThreads) {
         const Seq s = seq_of(rp, b);
-        const int n = tiles_of(s, p.tokens);
-        if (chunk == 0x7fffffff) {
-          entries += n;
-        } else {
 #pragma unroll 1
-          for (int x = 0; x < n; ++x) entries += chunks_of(s, p.tokens, x, chunk);
-          if (n > 0) atomicMax(&misc->max_chunks, chunks_of(s, p.tokens, n - 1, chunk));  // (the last row tile sees the most)
-        }
+        for (int x = 0; x < tiles_of(s, p.tokens); ++x)
+#pragma unroll 1
+          for (int i = 0; i < kSplitCount; ++i)
+            atomicAdd(&misc->splits[i], chunks_of(s, p.tokens, x, (longest + split_of(i) - 1) / split_of(i)));
       }
-      if (threadIdx.x == 0) misc->entries = 0;
       __syncthreads();
-      if (entries) atomicAdd(&misc->entries, entries);
-      __syncthreads();
-      const int total = misc->entries;
-      __syncthreads();
-      if (chunk == 0x7fffffff || (long long)total * rp.Hkv <= kMaxChunks) break;
-      chunk = chunk > 0x3fffffff ? 0x7ffffffe : 2 * chunk;
+      long long least = (entries * rp.Hkv + G - 1) / G * (longest + 3);
+#pragma unroll 1
+      for (int i = 0; i < kSplitCount; ++i) {
+        const int c = (longest + split_of(i) - 1) / split_of(i);
+        const long long n = (long long)misc->splits[i] * rp.Hkv, cost = (n + G - 1) / G * (c + 3) + 6;
+        if (n > kMaxChunks || cost >= least) continue;
+        least = cost;
+        chunk = c;
+        entries = misc->splits[i];
+      }
     }
-    if (threadIdx.x == 0) misc->chunk_tiles = chunk;
-    // The list of entries: level by level from the last rows on, in a level by sequence, in a row tile by chunk.  A warp a
+    if (threadIdx.x == 0) {
+      const long long bytes = misc->sum[1] * D * 4;  // keys and values of a cached head
+      const long long g = bytes > 0 ? kL2Bytes / bytes : rp.Hkv;
+      misc->head_group = (int)(g < 1 ? 1 : (g > rp.Hkv ? rp.Hkv : g));
+      misc->chunk_tiles = chunk;
+      misc->entries = (int)entries;
+    }
+    __syncthreads();
+    // The list of entries, where a CTA makes several items: level by level from the last rows on, in a level by sequence, in a row tile by chunk.  A warp a
     // level; the levels' counts pass through the K stages, which hold nothing yet.
     const int n_levels = misc->levels;
-    if (misc->entries <= kListMost && n_levels <= kLevelMost && misc->max_chunks <= kChunkMost) {
+    if (misc->entries <= kListMost && n_levels <= kLevelMost &&
+        (entries * rp.Hkv > 2 * G || n_levels > 8)) {
       int* first = reinterpret_cast<int*>(base + C::off_K);
       const auto entries_at = [&](int at, int level, bool& there) {
         there = at < rp.B;
@@ -740,18 +755,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const float inv = split ? 1.f : sees > 0 ? 1.f / l : 0.f;
       const uint64_t inv2 = f2(inv, inv);
       uint64_t odd2 = 0ull;  // NaN once a result is not finite
-      float* part = parts + it.slot * slot_floats + (size_t)(quarter * 32) * (D + 2);
+      float* part = parts + it.slot * slot_floats + r;
 #pragma unroll 1
       for (int c = 0; c < opaque(D / 32); ++c) {
         uint32_t o[32];
         tc::tmem_ld32(o_col + c * 32, o);
         tc::tmem_wait_ld();
-        if (split) {  // a partial result: fp32, a row a lane
-          float* at = part + (size_t)lane * (D + 2) + 2 + 32 * c;  // (rows are 8-byte aligned)
-          if (valid) {
+        if (split) {  // a partial result: fp32, rows side by side
+          float* at = part + (2 + 32 * c) * kBM;
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) *reinterpret_cast<uint2*>(at + e) = make_uint2(sees ? o[e] : 0u, sees ? o[e + 1] : 0u);
-          }
+          for (int e = 0; e < 32; ++e) at[e * kBM] = __uint_as_float(o[e]);
           continue;
         }
 #pragma unroll
@@ -773,7 +786,12 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->ofree);
       if (split) {
-        if (valid) *reinterpret_cast<float2*>(part + (size_t)lane * (D + 2)) = make_float2(mx, l);
+        part[0] = mx;
+        part[kBM] = l;
+        if (it.chunk == 0 && quarter == 0 && lane == 0) {
+          const unsigned n = atomicAdd(reinterpret_cast<unsigned*>(p.ws + kPartsOff), 1u);
+          reinterpret_cast<PartItem*>(p.ws + kPartItemsOff)[n] = {it.b, it.h, it.row0, it.m, it.kv, it.rows, it.pos0, it.chunks, it.slot, it.slot_step};
+        }
       } else {
         constexpr int kPieces = D / 8, kRowsAt = 32 / kPieces;  // of a row; rows that the warp writes at once
         const int e = lane % kPieces;
@@ -790,58 +808,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->qempty[(n_items - 1) & 1]);
-      // ---- this chunk's rows are there; the warp that completes the item's count merges its quarter's rows
-      bool merge = split;
-      if (split) {
-        __threadfence();
-        __syncwarp();
-        unsigned* count = reinterpret_cast<unsigned*>(p.ws + kCountOff) + (size_t)(it.slot - it.chunk * it.slot_step) * 4 + quarter;
-        unsigned before = 0;
-        if (lane == 0) before = atomicAdd(count, 1u);
-        before = __shfl_sync(0xffffffffu, before, 0);
-        merge = before == (unsigned)it.chunks - 1u;
-        if (merge && lane == 0) *count = 0u;
-        __threadfence();
-      }
-#pragma unroll 1
-      for (int y = 0; merge && y < 32; ++y) {
-        const int xr = quarter * 32 + y, xt = xr / rp.group, xp = it.pos0 + xt;
-        if (xt >= p.tokens || xp >= it.rows) continue;
-        const int head = it.h * rp.group + (xr - xt * rp.group);
-        __nv_bfloat16* at = out + ((size_t)(it.row0 + xp) * rp.H + head) * D + lane * (D / 32);
-        float v[D / 32];
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) v[e] = 0.f;
-        const int sees = seen(s, xp);
-        if (sees > 0) {
-          const float* row = parts + (size_t)(it.slot - it.chunk * it.slot_step) * slot_floats + (size_t)xr * (D + 2);
-          const size_t step = (size_t)it.slot_step * slot_floats;
-          float m_all = -CUDART_INF_F, l_all = 0.f;
-#pragma unroll 1
-          for (int c = lane; c < it.chunks; c += 32) m_all = fmaxf(m_all, __ldcg(row + c * step));
-          m_all = warp_max(m_all);
-#pragma unroll 4
-          for (int c = 0; c < it.chunks; ++c) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(row + c * step));
-            const float f = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - m_all);
-            l_all += ml.x == -CUDART_INF_F ? ml.y : f * ml.y;  // (a NaN stays one)
-#pragma unroll
-            for (int e = 0; e < D / 32; e += 2) {
-              const float2 o = __ldcg(reinterpret_cast<const float2*>(row + c * step + 2 + lane * (D / 32) + e));
-              v[e] += f * o.x;
-              v[e + 1] += f * o.y;
-            }
-          }
-          bool odd = false;
-#pragma unroll
-          for (int e = 0; e < D / 32; ++e) {
-            v[e] /= l_all;
-            odd |= !isfinite(v[e]);
-          }
-          if (__any_sync(0xffffffffu, odd)) again |= 1u << y;
-        }
-        store_row<D / 32>(at, v);
-      }
 #pragma unroll 1
       while (again) {
         const int x = __ffs(again) - 1;
@@ -1015,6 +981,75 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
 }
 
+// The items in chunks: a warp for 32 rows and 8 columns of one, a lane a row.  out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c,
+// M = max_c m_c, in the order of the chunks.
+constexpr int kMergeThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParams p) {
+  constexpr int kTasks = kBM / 32 * (D / 8);
+  pdl_wait();
+  const RowsParams& rp = p.r;
+  const int lane = threadIdx.x & 31;
+  const int n = (int)__ldcg(reinterpret_cast<const unsigned*>(p.ws + kPartsOff));
+  const float* parts = reinterpret_cast<const float*>(p.ws + kPartOff);
+  __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(rp.out);
+  const int warps = gridDim.x * (kMergeThreads / 32);
+  for (int task = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5); task < n * kTasks; task += warps) {
+    const PartItem it = reinterpret_cast<const PartItem*>(p.ws + kPartItemsOff)[task / kTasks];
+    const int rest = task % kTasks, r = rest / (D / 8) * 32 + lane, col = rest % (D / 8) * 8;
+    const int token = r / rp.group, pos = it.pos0 + token, head = it.h * rp.group + (r - token * rp.group);
+    const bool valid = token < p.tokens && pos < it.rows;
+    if (!__any_sync(0xffffffffu, valid)) continue;
+    const Seq s = {it.row0, it.rows, it.m, it.kv};
+    const float* at = parts + (size_t)it.slot * kBM * (D + 2) + r;
+    const size_t step = (size_t)it.slot_step * kBM * (D + 2);
+    float m = -CUDART_INF_F, l = 0.f, v[8];
+#pragma unroll 8
+    for (int c = 0; c < it.chunks; ++c) m = fmaxf(m, __ldcg(at + c * step));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < it.chunks; ++c) {
+      const float mc = __ldcg(at + c * step), lc = __ldcg(at + c * step + kBM);
+      const float f = mc == -CUDART_INF_F ? 0.f : fast_exp2(mc - m);
+      l += mc == -CUDART_INF_F ? lc : f * lc;  // (a NaN stays one)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += f * __ldcg(at + c * step + (2 + col + e) * kBM);
+    }
+    const int sees = valid ? seen(s, pos) : 0;
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = sees > 0 ? v[e] / l : 0.f;
+      odd |= !isfinite(v[e]);
+    }
+    __nv_bfloat16* to = out + ((size_t)(it.row0 + pos) * rp.H + head) * D;
+    if (valid)
+      *reinterpret_cast<uint4*>(to + col) =
+          make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    unsigned again = __ballot_sync(0xffffffffu, odd);  // by the definition, this warp's columns
+#pragma unroll 1
+    while (again) {
+      const int x = __ffs(again) - 1, xr = rest / (D / 8) * 32 + x, xt = xr / rp.group, xp = it.pos0 + xt;
+      const int xh = it.h * rp.group + (xr - xt * rp.group);
+      again &= again - 1;
+      __syncwarp();  // the row's first result is written
+      float y[D / 32];
+      attend_row<__nv_bfloat16, D>(rp, it.b, s, xp, xh, seen(s, xp), y);
+      const int first = lane * (D / 32);
+      if (first >= col && first < col + 8) store_row<D / 32>(out + ((size_t)(it.row0 + xp) * rp.H + xh) * D + first, y);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    unsigned* merged = reinterpret_cast<unsigned*>(p.ws + kMergedOff);
+    if (atomicAdd(merged, 1u) == gridDim.x - 1) {  // the counts back to zero for the next call
+      *merged = 0u;
+      *reinterpret_cast<unsigned*>(p.ws + kPartsOff) = 0u;
+    }
+  }
+}
+
 // [d2, d1, d0] bf16 rows with strides of their own, in boxes of 64 x box1 x box2 with the 128-byte swizzle.
 bool rows_map(CUtensorMap* m, const void* base, long long d0, long long d1, long long d2, long long stride1, long long stride2,
               int box1, int box2) {
@@ -1060,7 +1095,12 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   if (most > 0x7fffffffLL - 2 * kMaxGrid || (long long)a.T + 4 * kBM > 0x7fffffffLL || (long long)a.max_kv + kBN > 0x7fffffffLL)
     return cudaErrorNotSupported;
   int G = sm_count() < kMaxGrid ? sm_count() : kMaxGrid;
-  return launch_pdl(rows_tc_kernel<D>, dim3((unsigned)G), dim3(kTcThreads), C::kSmem, st, mq, mk, mv, p);
+  // Few enough items that some may be cut, by what the host knows of them
+  const long long longest = ((long long)(a.table ? a.max_kv : a.max_q) + kBN - 1) / kBN;
+  p.may_split = 2 * most < 5ll * G && longest > kFewTiles;
+  e = launch_pdl(rows_tc_kernel<D>, dim3((unsigned)G), dim3(kTcThreads), C::kSmem, st, mq, mk, mv, p);
+  if (e != cudaSuccess || !p.may_split) return e;
+  return launch_pdl(rows_merge_kernel<D>, dim3((unsigned)(2 * G)), dim3(kMergeThreads), 0, st, p);
 }
 
 }  // namespace

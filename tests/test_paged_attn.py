@@ -31,6 +31,11 @@ CASES = [
     ([129, 300, 1], [129, 555, 800], 2, 2, 128, 256, "bf16", 0, True),
     ([200, 0, 77, 1], [700, 0, 100, 1], 8, 2, 128, 32, "bf16", 9, True),
     ([130], [1500], 4, 1, 64, 16, "bf16", 0, False),
+    ([40], [2600], 4, 1, 128, 16, "bf16", 0, True),          # few rows, long contexts: the keys are cut into chunks
+    ([33, 1, 20], [1700, 2500, 300], 2, 2, 64, 32, "bf16", 2, False),
+    ([260, 70], [2100, 1900], 3, 1, 128, 64, "bf16", 1, False),
+    ([300], [290], 1, 1, 128, 16, "bf16", 0, False),
+    ([150, 40], [1650, 20], 2, 1, 64, 128, "bf16", 0, True),
     ([3, 9], [1, 4], 4, 2, 128, 16, "bf16", 0, False),       # rows before any key: zeros
     ([150, 20], [90, 19], 4, 2, 128, 16, "bf16", 0, False),
     ([1, 5, 20], [77, 5, 300], 4, 2, 64, 16, "f32", 2, True),
@@ -81,7 +86,7 @@ def test_bounds_below_the_lengths(m):
 
 
 @pytest.mark.parametrize("flags", [0, gb.GLIDE_FLAG_FORCE_FMA])
-@pytest.mark.parametrize("m, kv", [([1, 1], [200, 300]), ([4, 5], [140, 300]), ([150, 140], [300, 140])])
+@pytest.mark.parametrize("m, kv", [([1, 1], [200, 300]), ([4, 5], [140, 300]), ([150, 140], [300, 140]), ([40, 70], [2400, 1800])])
 def test_what_is_not_finite(m, kv, flags):
     """In rows that some tokens see and others do not, and in the queries."""
     H, H_kv, D, P = 4, 2, 128, 16

@@ -26,6 +26,8 @@ CASES = [
     ([512, 3, 600], 3, 1, 128, "bf16", 0, True),
     ([300, 700], 8, 1, 64, "bf16", 1, True),
     ([1300], 4, 4, 128, "bf16", 0, True),
+    ([2300], 2, 1, 64, "bf16", 0, False),
+    ([1800, 5, 1601], 1, 1, 128, "bf16", 4, True),
     ([1, 1, 1, 1, 1, 1, 1, 200], 5, 5, 128, "bf16", 0, False),
     ([90], 34, 2, 64, "bf16", 0, True),
     ([60, 128], 4, 4, 64, "f32", 3, False),
