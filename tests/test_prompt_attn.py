@@ -5,7 +5,7 @@ import torch
 
 from paper_2402_02082_gb300 import binding as gb
 from paper_2402_02082_gb300 import build
-from paged_util import SENTINEL, Prompt, check, host
+from paged_util import SENTINEL, Prompt, check, host, tolerance, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -30,6 +30,9 @@ CASES = [
     ([1800, 5, 1601], 1, 1, 128, "bf16", 4, True),
     ([1, 1, 1, 1, 1, 1, 1, 200], 5, 5, 128, "bf16", 0, False),
     ([90], 34, 2, 64, "bf16", 0, True),
+    ([9, 1, 30], 64, 1, 128, "bf16", 0, False),
+    ([5, 2], 130, 1, 64, "bf16", 0, True),
+    ([70], 40, 1, 64, "bf16", 1, True),
     ([60, 128], 4, 4, 64, "f32", 3, False),
     ([33, 1, 100], 6, 2, 128, "f32", 0, True),
 ]
@@ -54,6 +57,24 @@ def test_many_sequences():
     s.upload()
     want, tol = s.want()
     check(host(s.run()), want, tol)
+
+
+def test_more_row_tiles_than_are_listed():
+    """4096 row tiles of four tokens: 1024 sequences of 13 tokens, 32 query heads over one cached head."""
+    B, n, H, D = 1024, 13, 32, 64
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn((B * n, H + 2, D), generator=gen, device="cuda").bfloat16()
+    q, k, v = x.split([H, 1, 1], 1)
+    cu = torch.arange(B + 1, device="cuda", dtype=torch.int32) * n
+    out = torch.full((B * n, H, D), SENTINEL, dtype=torch.bfloat16, device="cuda")
+    gb.glide_prompt_attn(q, k, v, cu, n, out, workspace(B, H, 1, D, "bf16", B * n, n))
+    Q, K, V = (t.double().view(B, n, -1, D).transpose(1, 2) for t in (q, k, v))
+    hidden = torch.ones((n, n), dtype=torch.bool, device="cuda").triu(1)
+    p = torch.softmax((Q @ K.transpose(-1, -2) * D ** -0.5).masked_fill(hidden, -float("inf")), -1)
+    want, mean = p @ V, p @ V.abs()
+    top = (Q.abs() @ K.abs().transpose(-1, -2)).amax(-1).reshape(-1) * D ** -0.5
+    want, mean = (t.reshape(-1, D).cpu().numpy() for t in (want, mean))
+    check(host(out.view(B, n, H, D).transpose(1, 2)).reshape(-1, D), want, tolerance(want, mean, top.cpu().numpy(), n, D, "bf16"))
 
 
 def test_rows_past_max_len():
