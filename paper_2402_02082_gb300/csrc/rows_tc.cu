@@ -15,7 +15,8 @@
 // memory; a group keeps its own sum and takes it to the item's last reference at the end.
 //
 // Work items are (cached head, 128 / group tokens, keys), claimed from a counter: cached heads in groups whose keys and
-// values together stay in L2, in them the row tiles with the most keys first, so that the SMs end together.  Where there are
+// values together stay in L2, in them the row tiles with the most keys first; the short ones of all heads come last, so
+// that the SMs end together.  Where there are
 // fewer than two items for an SM, an item's keys may be cut into chunks; their partial results (max, sum, o) go through the
 // workspace, rows side by side, and a second kernel merges them in the chunks' order.
 //
@@ -67,6 +68,7 @@ constexpr int kSortMost = 128;         // sequences that are taken in the order 
 constexpr int kListMost = 3072;        // entries (sequence, row tile, chunk) that are listed in shared memory
 constexpr int kLevelMost = 4096;       // row tiles of a sequence that a list entry holds
 constexpr long long kL2Bytes = 48ll << 20;
+constexpr int kLateTenths = 4;         // items with at most this part of the longest one's key tiles are left to the end
 
 // Workspace: in the header the status word, the claim counter, the count of finished CTAs, and for the merge the count of
 // items in chunks and that of its finished CTAs; then those items, then partial slots of [D + 2][128 rows] floats: a row's
@@ -141,6 +143,7 @@ struct Misc {
   int entries;         // (sequence, row tiles, chunk) triples
   int levels;          // the most row tiles of a sequence
   int listed;          // the entries are in the list
+  int grouped;         // entries that are taken head group by head group; the rest follow for all heads
   long long sum[2];
   int longest;         // key tiles of the item with the most
   int splits[kSplitCount];  // entries by chunks of the longest item
@@ -156,6 +159,14 @@ __device__ __forceinline__ int chunks_of(const Seq& s, int tokens, int x, int ch
   if (x * tokens >= s.rows) return 0;
   const int nt = (keys_of(s, tokens, x) + kBN - 1) / kBN;
   return nt <= chunk_tiles ? 1 : (nt + chunk_tiles - 1) / chunk_tiles;
+}
+
+// The first row tile with at least `count` key tiles (the number of row tiles: none).
+__device__ __forceinline__ int first_tile(const Seq& s, int tokens, int count) {
+  const int most = tiles_of(s, tokens);
+  if (count > 0 && (most == 0 || keys_of(s, tokens, most - 1) <= (count - 1) * kBN)) return most;
+  const int need = (count - 1) * kBN - (s.kv - s.m);  // of its tokens, counted from the sequence's first: more than these
+  return count <= 0 || need < 0 ? 0 : need / tokens;
 }
 
 // n / d and the remainder by a multiplication, for n < 2^31 and r = reciprocal(d): the estimate is the quotient or one less.
@@ -350,28 +361,31 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       misc->head_group = (int)(g < 1 ? 1 : (g > rp.Hkv ? rp.Hkv : g));
       misc->chunk_tiles = chunk;
       misc->entries = (int)entries;
+      misc->grouped = (int)entries;
     }
     __syncthreads();
-    // The list of entries, where a CTA makes several items: level by level from the last rows on, in a level by sequence, in a row tile by chunk.  A warp a
-    // level; the levels' counts pass through the K stages, which hold nothing yet.
-    const int n_levels = misc->levels;
-    if (misc->entries <= kListMost && n_levels <= kLevelMost &&
-        (entries * rp.Hkv > 2 * G || n_levels > 8)) {
+    // The list of entries, where a CTA makes several items: those with the most key tiles first (so that the SMs end
+    // together), among them by sequence, row tile and chunk.  A warp a count of key tiles; how many entries have it passes
+    // through the K stages, which hold nothing yet.
+    const int n_counts = longest + 1;
+    if (misc->entries <= kListMost && misc->levels <= kLevelMost && n_counts <= kLevelMost &&
+        (entries * rp.Hkv > 2 * G || misc->levels > 8)) {
       int* first = reinterpret_cast<int*>(base + C::off_K);
-      const auto entries_at = [&](int at, int level, bool& there) {
-        there = at < rp.B;
-        if (!there) return 0;
-        return chunks_of(rp.B <= kSortMost ? table[at] : seq_of(rp, at), p.tokens, level, chunk);
-      };
 #pragma unroll 1
       for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
-        for (int level = warp; level < n_levels; level += kTcThreads / 32) {
-          int to = pass ? first[level] : 0;
+        for (int count = warp; count < n_counts; count += kTcThreads / 32) {
+          int to = pass ? first[count] : 0;
+          const int pieces = count <= chunk ? 1 : (count + chunk - 1) / chunk;
 #pragma unroll 1
           for (int b0 = 0; b0 < rp.B; b0 += 32) {
-            bool there;
-            const int n = entries_at(b0 + lane, level, there);
+            const int at = b0 + lane;
+            int x = 0, n = 0;  // row tiles x .. of this sequence have `count` key tiles
+            if (at < rp.B) {
+              const Seq s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
+              x = first_tile(s, p.tokens, count);
+              n = (first_tile(s, p.tokens, count + 1) - x) * pieces;
+            }
             int upto = n;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
@@ -379,31 +393,35 @@ __global__ void __launch_bounds__(kTcThreads, 1)
               if (lane >= off) upto += u;
             }
             if (pass)
-              for (int c = 0; c < n; ++c) list[to + upto - n + c] = (uint32_t)(b0 + lane) | (uint32_t)level << 10 | (uint32_t)c << 22;
+              for (int c = 0; c < n; ++c)
+                list[to + upto - n + c] = (uint32_t)at | (uint32_t)(x + c / pieces) << 10 | (uint32_t)(c % pieces) << 22;
             to += __shfl_sync(0xffffffffu, upto, 31);
           }
-          if (!pass && lane == 0) first[level] = to;
+          if (!pass && lane == 0) first[count] = to;
         }
         __syncthreads();
         if (pass) break;
-        if (warp == 0) {  // counts to places, the last level first
+        if (warp == 0) {  // counts to places, the most key tiles first
           int before = 0;
 #pragma unroll 1
-          for (int l0 = n_levels - 1; l0 >= 0; l0 -= 32) {
-            const int level = l0 - lane, n = level >= 0 ? first[level] : 0;
+          for (int l0 = n_counts - 1; l0 >= 0; l0 -= 32) {
+            const int count = l0 - lane, n = count >= 0 ? first[count] : 0;
             int upto = n;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
               const int u = __shfl_up_sync(0xffffffffu, upto, off);
               if (lane >= off) upto += u;
             }
-            if (level >= 0) first[level] = before + upto - n;
+            if (count >= 0) first[count] = before + upto - n;
             before += __shfl_sync(0xffffffffu, upto, 31);
           }
         }
         __syncthreads();
       }
-      if (threadIdx.x == 0) misc->listed = 1;
+      if (threadIdx.x == 0) {
+        misc->listed = 1;
+        misc->grouped = first[longest * kLateTenths / 10];
+      }
       tc::fence_async_smem();  // the loads write where the counts were
     }
   }
@@ -420,7 +438,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (lane < 2) tc::prefetch_tmap(lane == 0 ? &tmQ : &tmK);
       const Boxes<C::kHalves> box(p, lane);
       const int entries = misc->entries, head_group = misc->head_group, chunk_tiles = misc->chunk_tiles;
-      const unsigned claims = (unsigned)entries * rp.Hkv, per_group = (unsigned)entries * head_group;  // below 2^31
+      const unsigned claims = (unsigned)entries * rp.Hkv, per_group = (unsigned)misc->grouped * head_group;  // below 2^31
+      const unsigned in_groups = (unsigned)misc->grouped * rp.Hkv, by_all = reciprocal(rp.Hkv);
       const unsigned by_group = reciprocal(per_group), by_heads = reciprocal(head_group),
                      by_last = reciprocal(rp.Hkv % head_group);
       int level = misc->levels - 1, block = 0, acc = 0, group_at = 0;
@@ -437,10 +456,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           TcItem it;
           it.b = -1;
           if (c < claims) {
-            unsigned in_group, in_entry;
-            const int hg = (int)divide(c, per_group, by_group, in_group);
-            const int left = rp.Hkv - hg * head_group, heads = left < head_group ? left : head_group;
-            const int e = (int)divide(in_group, heads, left < head_group ? by_last : by_heads, in_entry);
+            unsigned in_group = 0, in_entry;
+            int hg = 0, heads = rp.Hkv, e;
+            if (c < in_groups) {
+              hg = (int)divide(c, per_group, by_group, in_group);
+              const int left = rp.Hkv - hg * head_group;
+              heads = left < head_group ? left : head_group;
+              e = (int)divide(in_group, heads, left < head_group ? by_last : by_heads, in_entry);
+            } else {
+              e = misc->grouped + (int)divide(c - in_groups, rp.Hkv, by_all, in_entry);
+            }
             if (misc->listed) {
               const uint32_t x = list[e];
               const int at = x & 1023;
