@@ -205,25 +205,37 @@ struct ItemReader {
   }
 };
 
-// The box of a key tile that this lane loads: pages that hold keys of the tile, or packed rows, by halves of D.
-template <int kHalves>
+// A key tile in shared memory is made of 8-row x 128-byte swizzle atoms: row r, half hd of D (64 columns) at
+//   packed   hd * 16 KB + r * 128       (a 4-D box of 64 columns x 128 rows x halves)
+//   pages    (r / 8) * (halves KB) + hd KB + (r % 8) * 128   (a page's rows are one box of 64 columns x 8 rows x halves x
+//            groups of 8 rows)
+// so a box brings all of D, and the products' descriptors differ in two strides alone.
+template <int D>
+struct KeyTile {
+  static constexpr uint32_t kHalves = D / 64;
+  uint32_t group, half;  // bytes from 8 rows to the next, and from half to half
+  __device__ __forceinline__ explicit KeyTile(bool packed) : group(packed ? 1024 : kHalves * 1024), half(packed ? kAtom : 1024) {}
+  __device__ __forceinline__ uint32_t at(int row, int hd) const { return (row >> 3) * group + hd * half + (row & 7) * 128; }
+};
+
+// The box of a key tile that this lane loads: a page's keys of the tile, or 128 packed rows.
 struct Boxes {
-  int hd, at, shift;  // this lane's half and first row in a tile; log2 of a box's rows
+  int at, shift;  // this lane's first row in a tile; log2 of a box's rows
   __device__ __forceinline__ Boxes(const TcParams& p, int lane) {
     shift = 31 - __clz(p.box_rows);
-    hd = lane % kHalves;
-    at = (lane / kHalves) << shift;
+    at = lane << shift;
   }
   __device__ __forceinline__ bool any(int left) const { return at < kBN && at < left; }  // left: keys from the tile on
-  __device__ __forceinline__ uint32_t bytes(int left, bool packed) const {
+  __device__ __forceinline__ uint32_t bytes(int left, bool packed, int row_bytes) const {
     const int rows = left < kBN && !packed ? (left + (1 << shift) - 1) >> shift << shift : kBN;
-    return (uint32_t)(rows * kHalves * 128);
+    return (uint32_t)(rows * row_bytes);
   }
-  // coordinates of the lane's box, for key tile t of the item
+  // coordinates (y, w) of the lane's box, for key tile t of the item: packed rows and the head, or 0 and the group of 8 rows
   __device__ __forceinline__ int2 where(const RowsParams& r, int b, int h, int row0, int t) const {
     const int key = t * kBN + at;
-    if (!r.table) return make_int2(h, row0 + key);
-    return make_int2(key & ((1 << r.page_shift) - 1), page_at(r, b, key >> r.page_shift) * r.Hkv + h);
+    if (!r.table) return make_int2(row0 + key, h);
+    const int row = key & ((1 << r.page_shift) - 1);
+    return make_int2(0, (((page_at(r, b, key >> r.page_shift) * r.Hkv + h) << r.page_shift) + row) >> 3);
   }
 };
 
@@ -436,7 +448,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       // ------------------------------------------------------------ items, Q and K
       const uint64_t pol_q = policy_evict_first(), pol_k = policy_evict_last();
       if (lane < 2) tc::prefetch_tmap(lane == 0 ? &tmQ : &tmK);
-      const Boxes<C::kHalves> box(p, lane);
+      const Boxes box(p, lane);
+      const KeyTile<D> lay(!rp.table);
       const int entries = misc->entries, head_group = misc->head_group, chunk_tiles = misc->chunk_tiles;
       const unsigned claims = (unsigned)entries * rp.Hkv, per_group = (unsigned)misc->grouped * head_group;  // below 2^31
       const unsigned in_groups = (unsigned)misc->grouped * rp.Hkv, by_all = reciprocal(rp.Hkv);
@@ -575,11 +588,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           ok = warp_wait_small(&bars->sfull[j % kSBufs], (j / kSBufs) & 1, abort_flag);
           if (!ok) break;
         }
-        if (lane == 0) mbar_arrive_expect_tx(&bars->kfull[st], box.bytes(left, !rp.table));
+        if (lane == 0) mbar_arrive_expect_tx(&bars->kfull[st], box.bytes(left, !rp.table, 2 * D));
         __syncwarp();
         if (box.any(left))
-          tc::tma_load_3d(base + C::off_K + st * C::kTile + box.hd * kAtom + box.at * 128, &tmK, box.hd * 64, x.x, x.y,
-                          &bars->kfull[st], pol_k);
+          tc::tma_load_4d(base + C::off_K + st * C::kTile + lay.at(box.at, 0), &tmK, 0, x.x, 0, x.y, &bars->kfull[st], pol_k);
         __syncwarp();
         ++k_issued;
         if (++st == C::kNS) st = 0;
@@ -597,7 +609,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       // ------------------------------------------------------------ V
       const uint64_t pol_v = policy_evict_last();
       if (lane == 0) tc::prefetch_tmap(&tmV);
-      const Boxes<C::kHalves> box(p, lane);
+      const Boxes box(p, lane);
+      const KeyTile<D> lay(!rp.table);
       unsigned st = 0, v_issued = 0, n_clear = 0;
       bool ok = true;
       ItemReader reader;
@@ -617,11 +630,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           }
           const unsigned bi = v_issued % kSBufs;
           uint64_t* full = left < kBN ? &bars->vfull : &bars->pvfull[bi];
-          if (lane == 0) mbar_arrive_expect_tx(full, box.bytes(left, !rp.table));
+          if (lane == 0) mbar_arrive_expect_tx(full, box.bytes(left, !rp.table, 2 * D));
           __syncwarp();
           unsigned char* dst = base + C::off_V + st * C::kTile;
           if (box.any(left))
-            tc::tma_load_3d(dst + box.hd * kAtom + box.at * 128, &tmV, box.hd * 64, x.x, x.y, full, pol_v);
+            tc::tma_load_4d(dst + lay.at(box.at, 0), &tmV, 0, x.x, 0, x.y, full, pol_v);
           __syncwarp();
           ++v_issued;
           if (left < kBN) {  // the item's last V tile: clear its rows past the last visible key
@@ -630,8 +643,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             ++n_clear;
 #pragma unroll 1
             for (int idx = left * C::kHalves * 8 + lane; idx < kBN * C::kHalves * 8; idx += 32)
-              *reinterpret_cast<uint4*>(dst + ((idx >> 3) % C::kHalves) * kAtom + idx / (C::kHalves * 8) * 128 +
-                                        (idx & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              *reinterpret_cast<uint4*>(dst + lay.at(idx / (C::kHalves * 8), (idx >> 3) % C::kHalves) + (idx & 7) * 16) =
+                  make_uint4(0u, 0u, 0u, 0u);
             tc::fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->pvfull[bi]);
@@ -649,8 +662,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       constexpr uint32_t idS = tc::idesc_bf16_f32(kBM, kBN, false, false);
       constexpr uint32_t idO = tc::idesc_bf16_f32(kBM, D, false, true);
       const uint64_t dQ0 = tc::sw128_desc(smem_u32(base + C::off_Q), 16, 1024);
-      const uint64_t dK0 = tc::sw128_desc(smem_u32(base + C::off_K), 16, 1024);
-      const uint64_t dV0 = tc::sw128_desc(smem_u32(base + C::off_V), kAtom, 1024);
+      const KeyTile<D> lay(!rp.table);
+      const uint64_t dK0 = tc::sw128_desc(smem_u32(base + C::off_K), 16, lay.group);
+      const uint64_t dV0 = tc::sw128_desc(smem_u32(base + C::off_V), lay.half, lay.group);
+      const uint64_t k_half = desc_step(lay.half), v_step = desc_step(2 * lay.group);  // 64 columns on; 16 keys on
       unsigned st = 0, phase = 0, bi = 0, b_phase = 0, n_items = 0;
       uint32_t col = tmem;
       bool ok = true;
@@ -675,8 +690,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
               const uint64_t dK = dK0 + st * desc_step(C::kTile);
 #pragma unroll
               for (int ks = 0; ks < D / 16; ++ks) {
-                const uint64_t step = desc_step((ks >> 2) * kAtom + (ks & 3) * 32);
-                tc::mma_bf16(col, dQ + step, dK + step, idS, ks > 0 ? 1u : 0u);
+                const uint64_t step = desc_step((ks & 3) * 32);
+                tc::mma_bf16(col, dQ + desc_step((ks >> 2) * kAtom) + step, dK + (ks >> 2) * k_half + step, idS, ks > 0 ? 1u : 0u);
               }
               tc::mma_commit(&bars->sfull[bi]);
               if (++st == C::kNS) {
@@ -702,7 +717,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
               const uint64_t dV = dV0 + st * desc_step(C::kTile);
 #pragma unroll
               for (int ks = 0; ks < kBN / 16; ++ks)
-                tc::mma_bf16_ts(tmem + C::kColO, col + ks * 8, dV + desc_step(ks * 16 * 128), idO, ks > 0 ? 1u : acc);
+                tc::mma_bf16_ts(tmem + C::kColO, col + ks * 8, dV + ks * v_step, idO, ks > 0 ? 1u : acc);
               acc = 1;
               tc::mma_commit(&bars->bfree[bi]);
               if (t == 1) tc::mma_commit(&bars->olast);
@@ -1075,6 +1090,20 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParam
   }
 }
 
+// bf16 keys or values in boxes of 64 columns x box1 x halves of D x box3 with the 128-byte swizzle; strides in elements.
+bool keys_map(CUtensorMap* m, const void* base, int halves, long long d1, long long stride1, int box1, long long d3,
+              long long stride3, int box3) {
+  PFN_cuTensorMapEncodeTiled_v12000 fn = tensor_map_encoder();
+  if (!fn) return false;
+  const cuuint64_t dims[4] = {64, (cuuint64_t)d1, (cuuint64_t)halves, (cuuint64_t)d3};
+  const cuuint64_t strides[3] = {(cuuint64_t)stride1 * 2, 128, (cuuint64_t)stride3 * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box1, (cuuint32_t)halves, (cuuint32_t)box3};
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // [d2, d1, d0] bf16 rows with strides of their own, in boxes of 64 x box1 x box2 with the 128-byte swizzle.
 bool rows_map(CUtensorMap* m, const void* base, long long d0, long long d1, long long d2, long long stride1, long long stride2,
               int box1, int box2) {
@@ -1105,14 +1134,15 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   if (a.table) {
     const int P = 1 << a.page_shift;
     p.box_rows = P < kBN ? P : kBN;
-    const long long slabs = (long long)a.n_pages * a.Hkv;
-    if (slabs > 0x7fffffffLL) return cudaErrorNotSupported;  // 32-bit TMA coordinates
-    if (!rows_map(&mk, a.K, D, P, slabs, D, (long long)P * D, p.box_rows, 1) ||
-        !rows_map(&mv, a.V, D, P, slabs, D, (long long)P * D, p.box_rows, 1))
+    const long long groups = (long long)a.n_pages * a.Hkv * (P / 8);  // of 8 rows
+    if (groups > 0x7fffffffLL / 8) return cudaErrorNotSupported;  // 32-bit TMA coordinates
+    if (!keys_map(&mk, a.K, C::kHalves, 8, D, 8, groups, 8 * D, p.box_rows / 8) ||
+        !keys_map(&mv, a.V, C::kHalves, 8, D, 8, groups, 8 * D, p.box_rows / 8))
       return cudaErrorNotSupported;
   } else {
     p.box_rows = kBN;
-    if (!rows_map(&mk, a.K, D, a.Hkv, a.T, D, a.k_stride, 1, kBN) || !rows_map(&mv, a.V, D, a.Hkv, a.T, D, a.v_stride, 1, kBN))
+    if (!keys_map(&mk, a.K, C::kHalves, a.T, a.k_stride, kBN, a.Hkv, D, 1) ||
+        !keys_map(&mv, a.V, C::kHalves, a.T, a.v_stride, kBN, a.Hkv, D, 1))
       return cudaErrorNotSupported;
   }
   // claims, their counter's reach past the last one, and token coordinates past the last row stay in 32 bits
