@@ -1021,12 +1021,12 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
 }
 
-// The items in chunks: a warp for 32 rows and 8 columns of one, a lane a row.  out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c,
+// The items in chunks: a warp for 32 rows and 4 columns of one, a lane a row, 8 chunks' loads in flight.  out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c,
 // M = max_c m_c, in the order of the chunks.
 constexpr int kMergeThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParams p) {
-  constexpr int kTasks = kBM / 32 * (D / 8);
+  constexpr int kCols = 4, kTasks = kBM / 32 * (D / kCols);
   pdl_wait();
   const RowsParams& rp = p.r;
   const int lane = threadIdx.x & 31;
@@ -1036,48 +1036,64 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParam
   const int warps = gridDim.x * (kMergeThreads / 32);
   for (int task = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5); task < n * kTasks; task += warps) {
     const PartItem it = reinterpret_cast<const PartItem*>(p.ws + kPartItemsOff)[task / kTasks];
-    const int rest = task % kTasks, r = rest / (D / 8) * 32 + lane, col = rest % (D / 8) * 8;
+    const int rest = task % kTasks, r = rest / (D / kCols) * 32 + lane, col = rest % (D / kCols) * kCols;
     const int token = r / rp.group, pos = it.pos0 + token, head = it.h * rp.group + (r - token * rp.group);
     const bool valid = token < p.tokens && pos < it.rows;
     if (!__any_sync(0xffffffffu, valid)) continue;
     const Seq s = {it.row0, it.rows, it.m, it.kv};
     const float* at = parts + (size_t)it.slot * kBM * (D + 2) + r;
     const size_t step = (size_t)it.slot_step * kBM * (D + 2);
-    float m = -CUDART_INF_F, l = 0.f, v[8];
-#pragma unroll 8
-    for (int c = 0; c < it.chunks; ++c) m = fmaxf(m, __ldcg(at + c * step));
+    float m = -CUDART_INF_F, l = 0.f, v[kCols];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-#pragma unroll 4
-    for (int c = 0; c < it.chunks; ++c) {
-      const float mc = __ldcg(at + c * step), lc = __ldcg(at + c * step + kBM);
-      const float f = mc == -CUDART_INF_F ? 0.f : fast_exp2(mc - m);
-      l += mc == -CUDART_INF_F ? lc : f * lc;  // (a NaN stays one)
+    for (int e = 0; e < kCols; ++e) v[e] = 0.f;
+#pragma unroll 1
+    for (int c0 = 0; c0 < it.chunks; c0 += 8) {
+      float mc[8], lc[8], o[8][kCols];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += f * __ldcg(at + c * step + (2 + col + e) * kBM);
+      for (int c = 0; c < 8; ++c) {
+        const float* from = at + (c0 + c) * step;
+        const bool there = c0 + c < it.chunks;
+        mc[c] = there ? __ldcg(from) : -CUDART_INF_F;
+        lc[c] = there ? __ldcg(from + kBM) : 0.f;
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) o[c][e] = there ? __ldcg(from + (2 + col + e) * kBM) : 0.f;
+      }
+      float top = m;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) top = fmaxf(top, mc[c]);
+      const float old = m == -CUDART_INF_F ? 1.f : fast_exp2(m - top);  // (sums without a maximum: zeros, or NaN to stay)
+      l *= old;
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) v[e] *= old;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float f = mc[c] == -CUDART_INF_F ? 0.f : fast_exp2(mc[c] - top);
+        l += mc[c] == -CUDART_INF_F ? lc[c] : f * lc[c];
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) v[e] += f * o[c][e];
+      }
+      m = top;
     }
     const int sees = valid ? seen(s, pos) : 0;
     bool odd = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < kCols; ++e) {
       v[e] = sees > 0 ? v[e] / l : 0.f;
       odd |= !isfinite(v[e]);
     }
     __nv_bfloat16* to = out + ((size_t)(it.row0 + pos) * rp.H + head) * D;
-    if (valid)
-      *reinterpret_cast<uint4*>(to + col) =
-          make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    if (valid) *reinterpret_cast<uint2*>(to + col) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     unsigned again = __ballot_sync(0xffffffffu, odd);  // by the definition, this warp's columns
 #pragma unroll 1
     while (again) {
-      const int x = __ffs(again) - 1, xr = rest / (D / 8) * 32 + x, xt = xr / rp.group, xp = it.pos0 + xt;
+      const int x = __ffs(again) - 1, xr = rest / (D / kCols) * 32 + x, xt = xr / rp.group, xp = it.pos0 + xt;
       const int xh = it.h * rp.group + (xr - xt * rp.group);
       again &= again - 1;
       __syncwarp();  // the row's first result is written
       float y[D / 32];
       attend_row<__nv_bfloat16, D>(rp, it.b, s, xp, xh, seen(s, xp), y);
       const int first = lane * (D / 32);
-      if (first >= col && first < col + 8) store_row<D / 32>(out + ((size_t)(it.row0 + xp) * rp.H + xh) * D + first, y);
+      if (first >= col && first < col + kCols) store_row<D / 32>(out + ((size_t)(it.row0 + xp) * rp.H + xh) * D + first, y);
     }
   }
   __syncthreads();
