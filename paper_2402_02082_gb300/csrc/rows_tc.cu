@@ -836,7 +836,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         constexpr int kPieces = D / 8, kRowsAt = 32 / kPieces;  // of a row; rows that the warp writes at once
         const int e = lane % kPieces;
         __nv_bfloat16* const to = out + ((size_t)(it.row0 + it.pos0) * rp.H + it.h * rp.group) * D + 8 * e;
-#pragma unroll 4
+#pragma unroll 8
         for (int x = lane / kPieces; x < 32; x += kRowsAt) {
           const uint4 v = *reinterpret_cast<const uint4*>(stage + x * (2 * D) + ((e ^ (x & 7)) << 4));
           if ((any >> x) & 1u) *reinterpret_cast<uint4*>(to + row_at[quarter * 32 + x]) = v;
