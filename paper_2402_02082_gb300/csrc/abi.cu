@@ -496,7 +496,7 @@ static glide_status rows_attention(const glide_attn_desc* d, glide::RowsArgs& a,
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (!(a.flags & GLIDE_FLAG_FORCE_FMA)) {
     cudaError_t e = glide::launch_paged_few(a, st);
-    if (e == cudaErrorNotSupported) e = glide::launch_rows_tc(a, st);
+    if (e == cudaErrorNotSupported && !glide::rows_fma_leads(a)) e = glide::launch_rows_tc(a, st);
     if (e != cudaErrorNotSupported) return from_cuda(e);
   }
   return from_cuda(glide::launch_rows_fma(a, st));

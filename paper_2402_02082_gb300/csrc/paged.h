@@ -40,8 +40,10 @@ struct RowsArgs {
 
 cudaError_t launch_page_plan(const PlanArgs& a, cudaStream_t st);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t st);
-// On the CUDA cores, a warp a row: every type and size.
+// On the CUDA cores, every type and size.
 cudaError_t launch_rows_fma(const RowsArgs& a, cudaStream_t st);
+// Whether that kernel is the faster one for bf16 rows that launch_paged_few does not take.
+bool rows_fma_leads(const RowsArgs& a);
 // bf16, pages, at most 16 query rows for a cached head; cudaErrorNotSupported for others.
 cudaError_t launch_paged_few(const RowsArgs& a, cudaStream_t st);
 // bf16, at most 128 query heads for a cached head, on the tensor cores; cudaErrorNotSupported for others and beyond 32-bit

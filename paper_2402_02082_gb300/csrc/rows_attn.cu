@@ -1,10 +1,11 @@
 // Attention of packed rows of new tokens over a paged cache or over the pack itself, a block for each row and query
 // head on the CUDA cores: fp32, and everything that the tensor-core kernels do not take.
 //
-// What bounds it.  Every row reads all the keys that it sees, so the calls that it is meant for are the small
-// ones in fp32; there the chain of a row counts.  Four warps take its keys in turn, 32 at a time, with 16 loads in flight
-// each: 32 dot products at once (a lane a key), one maximum and one sum over the warp, then the values column by column;
-// the warps' results meet in shared memory.  Two prompts of 60 to 128 tokens, 4 heads of 64: a warp a row 40 us.
+// What bounds it.  Every row reads all the keys that it sees, so the calls that it is meant for are the small ones; there
+// the chain of a row counts.  A block's four warps take a row's keys in turn, 32 at a time, with 16 loads in flight each:
+// 32 dot products at once (a lane a key), one maximum and one sum over the warp, then the values column by column; the
+// warps' results meet in shared memory.  Where no row can see more than 32 keys, each warp has a row of its own.
+// Two fp32 prompts of 60 to 128 tokens, 4 heads of 64: 9.8 us (a warp a row and 4 loads in flight: 40).
 #include "kernels.h"
 #include "rows_attn.cuh"
 
@@ -23,14 +24,16 @@ __device__ __forceinline__ int seq_at(const RowsParams& p, int i) {
   return lo;
 }
 
-template <typename T, int D>
+// kPerRow: warps of a row, 1 or all of the block.
+template <typename T, int D, int kPerRow>
 __global__ void __launch_bounds__(kRowWarps * 32) rows_kernel(const RowsParams p) {
   constexpr int kE = D / 32;
   __shared__ float part_o[kRowWarps][D], part_m[kRowWarps], part_l[kRowWarps];
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long total = (long long)p.T * p.H;
-  for (long long x = blockIdx.x; x < total; x += gridDim.x) {
+  constexpr int kRowsAt = kRowWarps / kPerRow;
+  for (long long x = (long long)blockIdx.x * kRowsAt + (kPerRow == 1 ? warp : 0); x < total; x += (long long)gridDim.x * kRowsAt) {
     const int row = (int)(x / p.H), h = (int)(x - (long long)row * p.H);
     const int b = seq_at(p, row);
     const Seq s = seq_of(p, b);
@@ -38,7 +41,13 @@ __global__ void __launch_bounds__(kRowWarps * 32) rows_kernel(const RowsParams p
     if (i < 0 || i >= s.rows) continue;
     const int n = seen(s, i);
     RowPart<D> r = no_keys<D>();
-    if (n > 0) attend_keys<T, D, 16>(p, b, s, i, h, n, warp * 32, kRowWarps * 32, r);
+    if (n > 0) attend_keys<T, D, 16>(p, b, s, i, h, n, (kPerRow == 1 ? 0 : warp) * 32, kPerRow * 32, r);
+    if constexpr (kPerRow == 1) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) r.o[e] = n > 0 ? r.o[e] / r.l : 0.f;
+      store_row<kE>(reinterpret_cast<T*>(p.out) + x * D + lane * kE, r.o);
+      continue;
+    }
     __syncthreads();  // the row before has been read
 #pragma unroll
     for (int e = 0; e < kE; ++e) part_o[warp][lane * kE + e] = r.o[e];
@@ -65,18 +74,34 @@ __global__ void __launch_bounds__(kRowWarps * 32) rows_kernel(const RowsParams p
 }
 
 template <typename T, int D>
-cudaError_t launch_typed(const RowsParams& p, cudaStream_t st) {
-  const long long blocks = (long long)p.T * p.H;
+cudaError_t launch_typed(const RowsParams& p, int keys, cudaStream_t st) {
+  const long long rows = (long long)p.T * p.H, blocks = keys <= 32 ? (rows + kRowWarps - 1) / kRowWarps : rows;
   const unsigned grid = (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30));
-  return launch_pdl(rows_kernel<T, D>, dim3(grid), dim3(kRowWarps * 32), 0, st, p);
+  if (keys <= 32) return launch_pdl(rows_kernel<T, D, 1>, dim3(grid), dim3(kRowWarps * 32), 0, st, p);
+  return launch_pdl(rows_kernel<T, D, kRowWarps>, dim3(grid), dim3(kRowWarps * 32), 0, st, p);
 }
+
+constexpr int most_keys(const RowsArgs& a) { return a.table ? a.max_kv : a.max_q; }
 
 }  // namespace
 
+// A row of at most 32 keys is one pass of a warp here, and the tensor-core kernel starts for about 9 us and then has a
+// chain of 4.7 us for each of an SM's items (a request's rows of one cached head), however few they are.  Measured, here
+// and there, 8 or 32 query heads of 128 over 8 cached: about 3.3 us + 2.7 ns a row against 9 + 0.031 an item.  Prompts of
+// 4 tokens, 8 heads: 1024 rows 5.1 and 16.6 us, 16384 rows 39 and 137; of 32 tokens: 2048 rows 9.8 and 10.5, 8192 rows
+// 27 and 16; four heads to a cached one, prompts of 16: 2048 rows 6.7 and 10.2, 8192 rows 20 and 12.  Above 32 keys the
+// tensor cores lead almost from the first row on (48 keys: 768 rows 8.6 and 9.7 us, 1920 rows 17 and 10).
+bool rows_fma_leads(const RowsArgs& a) {
+  const long long items = (long long)a.B * a.Hkv * (((long long)a.max_q * (a.H / a.Hkv) + 127) / 128);
+  return most_keys(a) <= 32 && (long long)a.T * a.H <= 2048 + 12 * items;
+}
+
 cudaError_t launch_rows_fma(const RowsArgs& a, cudaStream_t st) {
   const RowsParams p = rows_params(a);
-  if (a.dtype == 0) return a.D == 128 ? launch_typed<__nv_bfloat16, 128>(p, st) : launch_typed<__nv_bfloat16, 64>(p, st);
-  return a.D == 128 ? launch_typed<float, 128>(p, st) : launch_typed<float, 64>(p, st);
+  const int keys = most_keys(a);
+  if (a.dtype == 0)
+    return a.D == 128 ? launch_typed<__nv_bfloat16, 128>(p, keys, st) : launch_typed<__nv_bfloat16, 64>(p, keys, st);
+  return a.D == 128 ? launch_typed<float, 128>(p, keys, st) : launch_typed<float, 64>(p, keys, st);
 }
 
 }  // namespace glide

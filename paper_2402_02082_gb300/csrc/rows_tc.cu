@@ -65,7 +65,7 @@ constexpr int kMaxGrid = 160;
 constexpr int kMaxChunks = 3 * kMaxGrid;  // partial slots: below 2 grids of items and one grid more of chunks
 constexpr int kFewTiles = 12;          // key tiles of an item that are not worth a second kernel
 constexpr int kSortMost = 128;         // sequences that are taken in the order of their keys
-constexpr int kListMost = 3072;        // entries (sequence, row tile, chunk) that are listed in shared memory
+constexpr int kListMost = 3000;        // entries (sequence, row tile, chunk) that are listed in shared memory
 constexpr int kLevelMost = 4096;       // row tiles of a sequence that a list entry holds
 constexpr long long kL2Bytes = 48ll << 20;
 constexpr int kLateTenths = 4;         // items with at most this part of the longest one's key tiles are left to the end

@@ -51,12 +51,25 @@ def test_rows(case, flags):
     assert gb.glide_read_device_status(s.ws) == gb.GLIDE_OK
 
 
-def test_many_sequences():
+@pytest.mark.parametrize("max_len", [12, 33])
+def test_many_sequences(max_len):
     rng = np.random.default_rng(0)
     s = Prompt(1, rng.integers(0, 12, 1024).tolist(), 2, 1, 64, "bf16", pad=2)
     s.upload()
     want, tol = s.want()
-    check(host(s.run()), want, tol)
+    check(host(s.run(max_len=max_len)), want, tol)
+
+
+@pytest.mark.parametrize("n", [1, 31, 32, 33])
+@pytest.mark.parametrize("B", [1, 9, 40])
+def test_short_sequences(B, n):
+    """On both sides of the lengths and of the numbers of rows that decide the kernel."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, n + 1, B)
+    lens[B // 2] = n
+    s = Prompt(10 + n, lens.tolist(), 8, 2, 64, "bf16", pad=1, fused=True)
+    s.upload()
+    check(host(s.run()), *s.want())
 
 
 def test_more_row_tiles_than_are_listed():
