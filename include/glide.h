@@ -538,6 +538,8 @@ size_t glide_paged_workspace_bytes(const glide_attn_desc* desc, int32_t T, int32
  * proposal; a call may mix them.  A row that sees nothing (kv_len < m) gets zeros.
  * q [T, H, D] with q_stride; out [T, H, D] of desc->dtype, dense (one rounding of fp32 results).
  * Rows of out behind cu_q[B], and rows of a request past its first max_q, are left as they were.
+ * Nothing written (out, the workspace) overlaps anything else, the rows between a tensor's first and last
+ * element included: GLIDE_ERR_INVALID.
  * max_q, max_kv_len: bounds of m and kv_len on the host; 1 <= max_q, 0 <= max_kv_len <=
  * table_width * page_size.  desc: B, H, H_kv, D, dtype, scale, flags (GLIDE_FLAG_FORCE_FMA takes the CUDA-core
  * kernel); S_cap and max_ctas are ignored.

@@ -488,6 +488,17 @@ static glide_status rows_attention(const glide_attn_desc* d, glide::RowsArgs& a,
   if (T == 0) return GLIDE_OK;
   if (!q || !out || !aligned16(q) || !aligned16(out)) return GLIDE_ERR_INVALID;
   if ((double)T * d->H * d->D > 1.0e18) return GLIDE_ERR_INVALID;
+  const size_t e = elt_size(d), row = (size_t)d->H * d->D * e, kv_row = (size_t)hkv(d) * d->D * e;
+  const auto span = [&](long long stride, size_t last) { return (size_t)(T - 1) * stride * e + last; };
+  const size_t pool = ((size_t)a.n_pages << a.page_shift) * kv_row;
+  const Range to[] = {{out, span((long long)d->H * d->D, row)}, {ws, glide_paged_workspace_bytes(d, T, max_q)}};
+  const Range from[] = {{q, span(q_stride, row)}, {a.K, a.table ? pool : span(a.k_stride, kv_row)},
+                        {a.V, a.table ? pool : span(a.v_stride, kv_row)}, {cu, ((size_t)d->B + 1) * 4},
+                        {a.kv_len, a.table ? (size_t)d->B * 4 : 0}, {a.table, a.table ? (size_t)d->B * a.W * 4 : 0}};
+  if (to[0].meets(to[1])) return GLIDE_ERR_INVALID;
+  for (const Range& t : to)
+    for (const Range& f : from)
+      if (t.meets(f)) return GLIDE_ERR_INVALID;
   a.q = q; a.out = out; a.ws = ws; a.cu = cu; a.q_stride = q_stride;
   a.B = d->B; a.T = T; a.H = d->H; a.Hkv = hkv(d); a.D = d->D; a.max_q = max_q;
   a.dtype = d->dtype == GLIDE_BF16 ? 0 : 1;
@@ -495,9 +506,9 @@ static glide_status rows_attention(const glide_attn_desc* d, glide::RowsArgs& a,
   a.flags = d->flags;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (!(a.flags & GLIDE_FLAG_FORCE_FMA)) {
-    cudaError_t e = glide::launch_paged_few(a, st);
-    if (e == cudaErrorNotSupported && !glide::rows_fma_leads(a)) e = glide::launch_rows_tc(a, st);
-    if (e != cudaErrorNotSupported) return from_cuda(e);
+    cudaError_t err = glide::launch_paged_few(a, st);
+    if (err == cudaErrorNotSupported && !glide::rows_fma_leads(a)) err = glide::launch_rows_tc(a, st);
+    if (err != cudaErrorNotSupported) return from_cuda(err);
   }
   return from_cuda(glide::launch_rows_fma(a, st));
 }

@@ -71,14 +71,15 @@ constexpr long long kL2Bytes = 48ll << 20;
 constexpr int kLateTenths = 4;         // items with at most this part of the longest one's key tiles are left to the end
 
 // Workspace: in the header the status word, the claim counter, the count of finished CTAs, and for the merge the count of
-// items in chunks and that of its finished CTAs; then those items, then partial slots of [D + 2][128 rows] floats: a row's
-// maximum, its sum, its columns.
+// items in chunks and that of its finished CTAs.  Then, behind what the other calls' counters may take (they start at zero,
+// so nothing is left there), those items and partial slots of [D + 2][128 rows] floats: a row's maximum, its sum, its columns.
 struct PartItem {
   int b, h, row0, m, kv, rows, pos0, chunks, slot, slot_step;
 };
 constexpr size_t kPartsOff = 64, kMergedOff = 96;
-constexpr size_t kPartItemsOff = WsLayout::kHeader;
-constexpr size_t kPartOff = (kPartItemsOff + 2 * kMaxGrid * sizeof(PartItem) + 255) / 256 * 256;
+constexpr size_t kPartItemsBytes = (2 * kMaxGrid * sizeof(PartItem) + 255) / 256 * 256;
+// of a counter for each head (up to 1024) of the most sequences of a call
+size_t scratch_off(int H) { return WsLayout::align(WsLayout::kHeader + 4 * (size_t)kMaxBatch * (H < 1024 ? H : 1024)); }
 // Chunks of the longest item that are tried: 2 .. 6, 8, 10, 12, 16, 20, 24.
 constexpr int kSplitCount = 11;
 __host__ __device__ constexpr int split_of(int i) { return i < 5 ? i + 2 : (i < 8 ? 2 * i - 2 : 4 * (i - 4)); }
@@ -129,7 +130,7 @@ struct TcCfg {
 
 struct TcParams {
   RowsParams r;
-  unsigned char* ws;
+  unsigned char *ws, *scratch;
   int may_split;   // a merge kernel follows
   int tokens;      // of a row tile: 128 / group
   int box_rows;    // key rows of one TMA box: a page's, at most 128
@@ -751,7 +752,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int token = r / rp.group;
     const uint32_t o_col = tmem + ((uint32_t)(quarter * 32) << 16) + C::kColO;
     __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(rp.out);
-    float* parts = reinterpret_cast<float*>(p.ws + kPartOff);
+    float* parts = reinterpret_cast<float*>(p.scratch + kPartItemsBytes);
     constexpr size_t slot_floats = (size_t)kBM * (D + 2);
     unsigned n_items = 0;  // with tiles
     ItemReader reader;
@@ -830,7 +831,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         part[kBM] = l;
         if (it.chunk == 0 && quarter == 0 && lane == 0) {
           const unsigned n = atomicAdd(reinterpret_cast<unsigned*>(p.ws + kPartsOff), 1u);
-          reinterpret_cast<PartItem*>(p.ws + kPartItemsOff)[n] = {it.b, it.h, it.row0, it.m, it.kv, it.rows, it.pos0, it.chunks, it.slot, it.slot_step};
+          reinterpret_cast<PartItem*>(p.scratch)[n] = {it.b, it.h, it.row0, it.m, it.kv, it.rows, it.pos0, it.chunks, it.slot, it.slot_step};
         }
       } else {
         constexpr int kPieces = D / 8, kRowsAt = 32 / kPieces;  // of a row; rows that the warp writes at once
@@ -1031,11 +1032,14 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParam
   const RowsParams& rp = p.r;
   const int lane = threadIdx.x & 31;
   const int n = (int)__ldcg(reinterpret_cast<const unsigned*>(p.ws + kPartsOff));
-  const float* parts = reinterpret_cast<const float*>(p.ws + kPartOff);
+  const float* parts = reinterpret_cast<const float*>(p.scratch + kPartItemsBytes);
   __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(rp.out);
   const int warps = gridDim.x * (kMergeThreads / 32);
   for (int task = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5); task < n * kTasks; task += warps) {
-    const PartItem it = reinterpret_cast<const PartItem*>(p.ws + kPartItemsOff)[task / kTasks];
+    PartItem it;
+    constexpr int kWords = sizeof(PartItem) / 4;
+#pragma unroll
+    for (int e = 0; e < kWords; ++e) reinterpret_cast<int*>(&it)[e] = __ldcg(reinterpret_cast<const int*>(p.scratch) + task / kTasks * kWords + e);
     const int rest = task % kTasks, r = rest / (D / kCols) * 32 + lane, col = rest % (D / kCols) * kCols;
     const int token = r / rp.group, pos = it.pos0 + token, head = it.h * rp.group + (r - token * rp.group);
     const bool valid = token < p.tokens && pos < it.rows;
@@ -1143,6 +1147,7 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   TcParams p;
   p.r = rows_params(a);
   p.ws = static_cast<unsigned char*>(a.ws);
+  p.scratch = p.ws + scratch_off(a.H);
   const int group = p.r.group;
   p.tokens = kBM / group;
   CUtensorMap mq, mk, mv;
@@ -1181,7 +1186,7 @@ size_t rows_workspace_bytes(int B, int H, int Hkv, int D, int T, int max_q, int 
   (void)T;
   (void)max_q;
   if (dtype != 0 || H / Hkv > kBM) return WsLayout::kHeader;
-  return kPartOff + (size_t)kMaxChunks * kBM * (D + 2) * sizeof(float);
+  return scratch_off(H) + kPartItemsBytes + (size_t)kMaxChunks * kBM * (D + 2) * sizeof(float);
 }
 
 cudaError_t launch_rows_tc(const RowsArgs& a, cudaStream_t st) {

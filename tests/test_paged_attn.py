@@ -164,3 +164,22 @@ def test_a_pool_beyond_32_bits():
         s.Kd, s.Vd = K, V
         s.tabled = torch.where((s.tabled >= 0) & (s.tabled < far), s.tabled + (n - far), s.tabled)
         check(host(s.run()), want, tol)
+
+
+def test_a_workspace_shared_with_tree_verification():
+    """A step whose keys are cut into chunks leaves at zero what other calls on its workspace take their counters from."""
+    s = Paged(70, [40], [2600], 4, 1, 128, 16, "bf16")
+    s.upload()
+    out = s.run()
+    assert not s.ws[: 256 + 4 * 1024 * s.H].any()
+    n, B, H, D, S = 5, 3, 4, 128, 700
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    q, K, V = (torch.randn(shape, generator=gen, device="cuda").bfloat16() for shape in ((B, n, H, D), (B, H, S, D), (B, H, S, D)))
+    kv, parent = i32([600, 1, 333]), i32([[-1, 0, 1, 1, 0]] * B)
+    results = []
+    for ws in (s.ws, torch.zeros(256 << 20, dtype=torch.uint8, device="cuda")):
+        for flags in (0, gb.GLIDE_FLAG_FORCE_FMA):
+            results.append(gb.tree_verify_attn(q, parent, K, V, kv, 600, torch.empty((B, n, H, D), device="cuda"), ws, flags=flags))
+        results.append(s.run(ws=ws))
+    assert all(torch.equal(a, b) for a, b in zip(results[:3], results[3:]))
+    assert torch.equal(results[2], out)

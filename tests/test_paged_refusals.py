@@ -110,6 +110,27 @@ def test_attention(L):
     assert paged(T=0, q=None, out=None) == gb.GLIDE_OK and prompt(T=0, q=None, k=None, v=None, out=None) == gb.GLIDE_OK
 
 
+def test_attention_refuses_overlaps(L):
+    """out [9, 4, 64] bf16 (4608 bytes) and the workspace beside every input; one past its end they may not be refused for it."""
+    at = {n: FAKE + (x << 33) for x, n in enumerate(("q", "K", "V", "cu", "table", "kv", "out", "ws"))}
+    out_bytes = 9 * 4 * 64 * 2
+
+    def paged(**kw):
+        a = {**at, **kw}
+        return L.glide_paged_attn(desc(), a["q"], 512, 9, a["cu"], 4, pool(K=a["K"], V=a["V"]), a["table"], 7, a["kv"], 100,
+                                  a["out"], a["ws"], 1 << 28, None)
+
+    def prompt(**kw):
+        a = {**at, **kw}
+        return L.glide_prompt_attn(desc(), a["q"], 512, a["K"], 512, a["V"], 512, 9, a["cu"], 4, a["out"], a["ws"], 1 << 28, None)
+    for call, names in ((paged, ("q", "K", "V", "cu", "table", "kv")), (prompt, ("q", "K", "V", "cu"))):
+        for n in names:
+            assert call(out=at[n]) == INVALID and call(ws=at[n]) == INVALID, n
+            assert call(out=at[n] - out_bytes + 16) == INVALID, n
+        assert call(out=at["ws"]) == INVALID
+        assert call(q=at["out"] + out_bytes - 16) == INVALID
+
+
 @pytest.mark.parametrize("device", ["cpu", pytest.param("cuda", marks=pytest.mark.gpu)])
 def test_binding_refuses(L, device):
     """Host tensors, which are refused themselves, and every unusual argument beside good ones on the GPU."""
