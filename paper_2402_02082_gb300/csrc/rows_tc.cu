@@ -80,8 +80,16 @@ constexpr size_t kPartsOff = 64, kMergedOff = 96;
 constexpr size_t kPartItemsBytes = (2 * kMaxGrid * sizeof(PartItem) + 255) / 256 * 256;
 // of a counter for each head (up to 1024) of the most sequences of a call
 size_t scratch_off(int H) { return WsLayout::align(WsLayout::kHeader + 4 * (size_t)kMaxBatch * (H < 1024 ? H : 1024)); }
-// Chunks of the longest item that are tried: 2 .. 6, 8, 10, 12, 16, 20, 24.
-constexpr int kSplitCount = 11;
+constexpr int kSplitCount = 11;  // chunks of the longest item that are tried: 2 .. 6, 8, 10, 12, 16, 20, 24
+constexpr int kMergeTiles = 7;
+constexpr int kAlone = 4;  // row tiles of a sequence that one lane counts
+// The cost of n items of at most `tiles` key tiles on G SMs, in key tiles: an item takes 3 beside its own, a chunk 5, and
+// the merge and its launch 7.  us without chunks and with: 256 new tokens over 6000 keys, 32 heads over 8 cached 51 and
+// 39; 16 over 16384 121 and 28; two requests of 64 over 16384, 32 heads 128 and 94; 512 over 4000, 52 heads 65 and 75.
+__host__ __device__ constexpr int rounds_cost(int n, int G, int tiles) { return (n + G - 1) / G * (tiles + 3); }
+__host__ __device__ constexpr int split_cost(int n, int G, int tiles) {
+  return n > kMaxChunks ? 0x7fffffff : rounds_cost(n, G, tiles + 2) + kMergeTiles;
+}
 __host__ __device__ constexpr int split_of(int i) { return i < 5 ? i + 2 : (i < 8 ? 2 * i - 2 : 4 * (i - 4)); }
 
 struct Bars {
@@ -104,6 +112,20 @@ struct TcItem {
   int chunks, chunk, slot, slot_step;  // chunks of the item, this one, its partial slot, slots from chunk to chunk
 };
 
+struct Misc {
+  uint32_t tmem;
+  int abort;
+  int head_group;      // cached heads that are worked on together
+  int chunk_tiles;     // key tiles of a chunk
+  int entries;         // (sequence, row tiles, chunk) triples
+  int levels;          // the most row tiles of a sequence
+  int listed;          // the entries are in the list
+  int grouped;         // entries that are taken head group by head group; the rest follow for all heads
+  long long sum[2];
+  int longest;         // key tiles of the item with the most
+  int4 splits[kSplitCount];  // by chunks of the longest item: entries, key tiles of a chunk, cost
+};
+
 template <int D>
 struct TcCfg {
   static constexpr int kHalves = D / 64;
@@ -117,7 +139,7 @@ struct TcCfg {
   static constexpr uint32_t off_bar = off_V + kNS * kTile;
   static constexpr uint32_t off_item = off_bar + sizeof(Bars);
   static constexpr uint32_t off_misc = (off_item + kItemSlots * sizeof(TcItem) + 15) / 16 * 16;
-  static constexpr uint32_t off_rows = off_misc + 128;               // [row] references, then sums [group][row], then final
+  static constexpr uint32_t off_rows = off_misc + sizeof(Misc);      // [row] references, then sums [group][row], then final
   static constexpr uint32_t off_table = off_rows + 4 * kBM * 4;     // lengths, in the order in which they are taken
   static constexpr uint32_t off_rowat = off_table + kSortMost * 16;  // elements from a row tile's first row to its rows
   static constexpr uint32_t off_order = off_rowat + kBM * 4;
@@ -134,20 +156,6 @@ struct TcParams {
   int may_split;   // a merge kernel follows
   int tokens;      // of a row tile: 128 / group
   int box_rows;    // key rows of one TMA box: a page's, at most 128
-};
-
-struct Misc {
-  uint32_t tmem;
-  int abort;
-  int head_group;      // cached heads that are worked on together
-  int chunk_tiles;     // key tiles of a chunk
-  int entries;         // (sequence, row tiles, chunk) triples
-  int levels;          // the most row tiles of a sequence
-  int listed;          // the entries are in the list
-  int grouped;         // entries that are taken head group by head group; the rest follow for all heads
-  long long sum[2];
-  int longest;         // key tiles of the item with the most
-  int splits[kSplitCount];  // entries by chunks of the longest item
 };
 
 // Row tiles of a sequence, and the keys that the last row of tile x sees.
@@ -285,7 +293,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     init(bars->itemempty, kItemSlots, kItemReaders);
     init(bars->drained, 2, 1);
     if (warp == 15) {
-      if (lane < kSplitCount) misc->splits[lane] = 0;
       if (lane == 0) {
         misc->abort = 0;
         misc->levels = 0;
@@ -345,27 +352,44 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int G = gridDim.x;
     longest = misc->longest;
     if (p.may_split && entries * rp.Hkv < 2ll * G && longest > kFewTiles) {
-      // Chunks of the longest item: the number whose rounds over the SMs cost least, a chunk 3 key tiles beside its
-      // own and the merge 6.
+      // The number of chunks of the longest item whose rounds over the SMs cost least.
+      // A warp a number of chunks; a lane a sequence, or where it has many row tiles, all lanes that sequence.
+      if (warp < kSplitCount) {
+        const int c = (longest + split_of(warp) - 1) / split_of(warp);
+        int n = 0;
 #pragma unroll 1
-      for (int b = threadIdx.x; b < rp.B; b += kTcThreads) {
-        const Seq s = seq_of(rp, b);
+        for (int b0 = 0; b0 < rp.B; b0 += 32) {
+          const int at = b0 + lane;
+          Seq s = {0, 0, 0, 0};
+          if (at < rp.B) s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
+          const int most = tiles_of(s, p.tokens);
+          if (most <= kAlone) {
 #pragma unroll 1
-        for (int x = 0; x < tiles_of(s, p.tokens); ++x)
+            for (int x = 0; x < most; ++x) n += chunks_of(s, p.tokens, x, c);
+          }
+          unsigned rest = __ballot_sync(0xffffffffu, most > kAlone);
 #pragma unroll 1
-          for (int i = 0; i < kSplitCount; ++i)
-            atomicAdd(&misc->splits[i], chunks_of(s, p.tokens, x, (longest + split_of(i) - 1) / split_of(i)));
+          while (rest) {
+            const int who = __ffs(rest) - 1;
+            rest &= rest - 1;
+            const Seq o = {0, __shfl_sync(0xffffffffu, s.rows, who), __shfl_sync(0xffffffffu, s.m, who), __shfl_sync(0xffffffffu, s.kv, who)};
+#pragma unroll 1
+            for (int x = lane; x * p.tokens < o.rows; x += 32) n += chunks_of(o, p.tokens, x, c);
+          }
+        }
+        n = __reduce_add_sync(0xffffffffu, n);
+        const int items = n * rp.Hkv;
+        if (lane == 0) misc->splits[warp] = make_int4(n, c, split_cost(items, G, c), 0);
       }
       __syncthreads();
-      long long least = (entries * rp.Hkv + G - 1) / G * (longest + 3);
+      int least = rounds_cost((int)entries * rp.Hkv, G, longest);
 #pragma unroll 1
       for (int i = 0; i < kSplitCount; ++i) {
-        const int c = (longest + split_of(i) - 1) / split_of(i);
-        const long long n = (long long)misc->splits[i] * rp.Hkv, cost = (n + G - 1) / G * (c + 3) + 6;
-        if (n > kMaxChunks || cost >= least) continue;
-        least = cost;
-        chunk = c;
-        entries = misc->splits[i];
+        const int4 x = misc->splits[i];
+        if (x.z >= least) continue;
+        least = x.z;
+        chunk = x.y;
+        entries = x.x;
       }
     }
     if (threadIdx.x == 0) {
@@ -1022,19 +1046,21 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
 }
 
-// The items in chunks: a warp for 32 rows and 4 columns of one, a lane a row, 8 chunks' loads in flight.  out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c,
-// M = max_c m_c, in the order of the chunks.
+// The items in chunks: a warp for 32 rows and kCols columns of one, a lane a row, four chunks' loads in flight.
+//   out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c,  M = max_c m_c, in the order of the chunks
+// Sixteen columns write whole 32-byte sectors of a row; eight make twice the tasks, for few items in many chunks.  Two
+// requests of up to 512 new tokens, 40 heads (a call, us): 4 columns and eight chunks 91, eight 82, sixteen 78; one of 16
+// tokens over 16384 keys, 32 heads over 8 cached: 32.8, 32.4 and 33.8.
 constexpr int kMergeThreads = 256;
-template <int D>
-__global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParams p) {
-  constexpr int kCols = 4, kTasks = kBM / 32 * (D / kCols);
-  pdl_wait();
+template <int D, int kCols>
+__device__ __forceinline__ void merge_parts(const TcParams& p, int n) {
+  constexpr int kTasks = kBM / 32 * (D / kCols), kAtOnce = 4;
   const RowsParams& rp = p.r;
   const int lane = threadIdx.x & 31;
-  const int n = (int)__ldcg(reinterpret_cast<const unsigned*>(p.ws + kPartsOff));
   const float* parts = reinterpret_cast<const float*>(p.scratch + kPartItemsBytes);
   __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(rp.out);
   const int warps = gridDim.x * (kMergeThreads / 32);
+#pragma unroll 1
   for (int task = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5); task < n * kTasks; task += warps) {
     PartItem it;
     constexpr int kWords = sizeof(PartItem) / 4;
@@ -1051,10 +1077,10 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParam
 #pragma unroll
     for (int e = 0; e < kCols; ++e) v[e] = 0.f;
 #pragma unroll 1
-    for (int c0 = 0; c0 < it.chunks; c0 += 8) {
-      float mc[8], lc[8], o[8][kCols];
+    for (int c0 = 0; c0 < it.chunks; c0 += kAtOnce) {
+      float mc[kAtOnce], lc[kAtOnce], o[kAtOnce][kCols];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
+      for (int c = 0; c < kAtOnce; ++c) {
         const float* from = at + (c0 + c) * step;
         const bool there = c0 + c < it.chunks;
         mc[c] = there ? __ldcg(from) : -CUDART_INF_F;
@@ -1064,13 +1090,13 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParam
       }
       float top = m;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) top = fmaxf(top, mc[c]);
+      for (int c = 0; c < kAtOnce; ++c) top = fmaxf(top, mc[c]);
       const float old = m == -CUDART_INF_F ? 1.f : fast_exp2(m - top);  // (sums without a maximum: zeros, or NaN to stay)
       l *= old;
 #pragma unroll
       for (int e = 0; e < kCols; ++e) v[e] *= old;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
+      for (int c = 0; c < kAtOnce; ++c) {
         const float f = mc[c] == -CUDART_INF_F ? 0.f : fast_exp2(mc[c] - top);
         l += mc[c] == -CUDART_INF_F ? lc[c] : f * lc[c];
 #pragma unroll
@@ -1085,8 +1111,12 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParam
       v[e] = sees > 0 ? v[e] / l : 0.f;
       odd |= !isfinite(v[e]);
     }
-    __nv_bfloat16* to = out + ((size_t)(it.row0 + pos) * rp.H + head) * D;
-    if (valid) *reinterpret_cast<uint2*>(to + col) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    __nv_bfloat16* to = out + ((size_t)(it.row0 + pos) * rp.H + head) * D + col;
+    if (valid)
+#pragma unroll
+      for (int e = 0; e < kCols; e += 8)
+        *reinterpret_cast<uint4*>(to + e) = make_uint4(pack_bf16x2(v[e], v[e + 1]), pack_bf16x2(v[e + 2], v[e + 3]),
+                                                       pack_bf16x2(v[e + 4], v[e + 5]), pack_bf16x2(v[e + 6], v[e + 7]));
     unsigned again = __ballot_sync(0xffffffffu, odd);  // by the definition, this warp's columns
 #pragma unroll 1
     while (again) {
@@ -1100,6 +1130,16 @@ __global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParam
       if (first >= col && first < col + kCols) store_row<D / 32>(out + ((size_t)(it.row0 + xp) * rp.H + xh) * D + first, y);
     }
   }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads) rows_merge_kernel(const TcParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the next call's start overlaps the merge
+  pdl_wait();
+  const int n = (int)__ldcg(reinterpret_cast<const unsigned*>(p.ws + kPartsOff));
+  constexpr int kWide = kBM / 32 * (D / 16);  // tasks of an item
+  if (n * kWide >= (int)gridDim.x * (kMergeThreads / 32) / 2) merge_parts<D, 16>(p, n);
+  else merge_parts<D, 8>(p, n);
   __syncthreads();
   if (threadIdx.x == 0) {
     unsigned* merged = reinterpret_cast<unsigned*>(p.ws + kMergedOff);
@@ -1174,6 +1214,14 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   // Few enough items that some may be cut, by what the host knows of them
   const long long longest = ((long long)(a.table ? a.max_kv : a.max_q) + kBN - 1) / kBN;
   p.may_split = 2 * most < 5ll * G && longest > kFewTiles;
+  if (p.may_split && a.B == 1) {  // one sequence's items are known here, and so is a merge that would have nothing to do
+    const int items = (a.max_q + p.tokens - 1) / p.tokens * a.Hkv, least = rounds_cost(items, G, (int)longest);
+    p.may_split = 0;
+    for (int i = 0; i < kSplitCount && items < 2 * G; ++i) {
+      const int c = (int)((longest + split_of(i) - 1) / split_of(i)), n = (int)((longest + c - 1) / c);
+      p.may_split |= split_cost(items * n, G, c) < least;
+    }
+  }
   e = launch_pdl(rows_tc_kernel<D>, dim3((unsigned)G), dim3(kTcThreads), C::kSmem, st, mq, mk, mv, p);
   if (e != cudaSuccess || !p.may_split) return e;
   return launch_pdl(rows_merge_kernel<D>, dim3((unsigned)(2 * G)), dim3(kMergeThreads), 0, st, p);
