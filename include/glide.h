@@ -97,8 +97,9 @@ typedef enum {
 typedef enum { GLIDE_BF16 = 0, GLIDE_F32 = 1 } glide_dtype;
 
 /* flags */
-#define GLIDE_FLAG_FORCE_FMA 1u   /* tree_verify_attn: use the CUDA-core kernel even where the
-                                     tensor-core kernel applies (testing and comparison)     */
+#define GLIDE_FLAG_FORCE_FMA 1u   /* tree_verify_attn, glide_paged_attn, glide_prompt_attn: use the
+                                     CUDA-core kernel even where a tensor-core kernel applies
+                                     (testing and comparison)                                */
 #define GLIDE_FLAG_TILE64 2u      /* grouped-query slabs and slabs of more than 64 query rows:
                                      use the 64-row tensor-core kernel rather than the 128-row
                                      one (testing and comparison)                            */

@@ -68,7 +68,7 @@ __device__ __forceinline__ float bf16hi(uint32_t w) { return __uint_as_float(w &
 // tail.  pdl_wait() blocks until the previous grid has completed and its
 // writes are visible; a kernel calls it before its first global-memory access
 // and before it allocates tensor memory, so it never reads an input early nor
-// holds resources the previous grid could wait for.  Only the two split-merge
+// holds resources the previous grid could wait for.  Only the split-merge
 // kernels signal their dependents early (griddepcontrol.launch_dependents, at
 // their start): the next attention kernel's CTAs are then placed on the SMs
 // the small merge grid leaves free and wait there, so its launch overlaps the

@@ -10,7 +10,7 @@
 // itself and writes its share of the outputs.
 //
 // What bounds it: latency.  The lengths are a few kB; a step of 32 requests is one CTA with five dependent
-// loads.
+// loads: 4.4 us, a launch without work ~3.  1024 requests with 80 thousand new tokens: 6.5 us (0.85 MB).
 #include "common.cuh"
 #include "device.h"
 #include "kernels.h"
