@@ -74,6 +74,7 @@ constexpr int kSortMost = 128;         // sequences that are taken in the order 
 constexpr int kListMost = 3000;        // entries (sequence, row tile, chunk) that are listed in shared memory
 constexpr int kLevelMost = 4096;       // row tiles of a sequence that a list entry holds
 constexpr long long kL2Bytes = 48ll << 20;
+constexpr int kManyKeys = 1 << 24;     // that no part of L2 holds; sums of two for each lane of a warp stay in 32 bits
 constexpr int kLateTenths = 4;         // items with at most this part of the longest one's key tiles are left to the end
 
 // Workspace: in the header the status word, the claim counter, the count of finished CTAs, and for the merge the count of
@@ -161,11 +162,27 @@ struct TcParams {
   unsigned char *ws, *scratch;
   int may_split;   // a merge kernel follows
   int tokens;      // of a row tile: 128 / group
+  unsigned by_tokens, by_heads;  // reciprocals, of H_kv the second
   int box_rows;    // key rows of one TMA box: a page's, at most 128
 };
 
+// n / d and the remainder by a multiplication, for n < 2^31 and r = reciprocal(d): the estimate is the quotient or one less.
+__host__ __device__ __forceinline__ unsigned reciprocal(unsigned d) { return d ? 0xffffffffu / d : 0u; }
+__device__ __forceinline__ unsigned divide(unsigned n, unsigned d, unsigned r, unsigned& rest) {
+  unsigned q = __umulhi(n, r);
+  rest = n - q * d;
+  if (rest >= d) {
+    rest -= d;
+    ++q;
+  }
+  return q;
+}
+
 // Row tiles of a sequence, and the keys that the last row of tile x sees.
-__device__ __forceinline__ int tiles_of(const Seq& s, int tokens) { return (s.rows + tokens - 1) / tokens; }
+__device__ __forceinline__ int tiles_of(const Seq& s, int tokens, unsigned by_tokens) {
+  unsigned rest;
+  return s.rows > 0 ? (int)divide((unsigned)(s.rows - 1), tokens, by_tokens, rest) + 1 : 0;
+}
 __device__ __forceinline__ int keys_of(const Seq& s, int tokens, int x) {
   const int last = (x + 1) * tokens;
   return seen(s, (last < s.rows ? last : s.rows) - 1);
@@ -176,24 +193,12 @@ __device__ __forceinline__ int chunks_of(const Seq& s, int tokens, int x, int ch
   return nt <= chunk_tiles ? 1 : (nt + chunk_tiles - 1) / chunk_tiles;
 }
 
-// The first row tile with at least `count` key tiles (the number of row tiles: none).
-__device__ __forceinline__ int first_tile(const Seq& s, int tokens, int count) {
-  const int most = tiles_of(s, tokens);
+// The first row tile of `most` with at least `count` key tiles (`most`: none).
+__device__ __forceinline__ int first_tile(const Seq& s, int most, int tokens, unsigned by_tokens, int count) {
   if (count > 0 && (most == 0 || keys_of(s, tokens, most - 1) <= (count - 1) * kBN)) return most;
   const int need = (count - 1) * kBN - (s.kv - s.m);  // of its tokens, counted from the sequence's first: more than these
-  return count <= 0 || need < 0 ? 0 : need / tokens;
-}
-
-// n / d and the remainder by a multiplication, for n < 2^31 and r = reciprocal(d): the estimate is the quotient or one less.
-__device__ __forceinline__ unsigned reciprocal(unsigned d) { return d ? 0xffffffffu / d : 0u; }
-__device__ __forceinline__ unsigned divide(unsigned n, unsigned d, unsigned r, unsigned& rest) {
-  unsigned q = __umulhi(n, r);
-  rest = n - q * d;
-  if (rest >= d) {
-    rest -= d;
-    ++q;
-  }
-  return q;
+  unsigned rest;
+  return count <= 0 || need < 0 ? 0 : (int)divide((unsigned)need, tokens, by_tokens, rest);
 }
 
 template <int N>
@@ -318,39 +323,49 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (threadIdx.x < kBM) row_at[threadIdx.x] = (threadIdx.x / rp.group * rp.H + threadIdx.x % rp.group) * D;
   // ---- the plan of the call: what all CTAs find alike from the lengths
   {
-    long long tiles = 0, keys = 0;
+    unsigned tiles = 0, keys = 0;
     int levels = 0, longest = 0;
     if (rp.B <= kSortMost && threadIdx.x < rp.B) table[threadIdx.x] = seq_of(rp, threadIdx.x);
 #pragma unroll 1
     for (int b = threadIdx.x; b < rp.B; b += kTcThreads) {
       const Seq s = seq_of(rp, b);
-      const int n = tiles_of(s, p.tokens);
+      const int n = tiles_of(s, p.tokens, p.by_tokens);
       if (n == 0) continue;
       tiles += n;
-      keys += s.kv;
+      keys += s.kv < kManyKeys ? s.kv : kManyKeys;
       levels = n > levels ? n : levels;
       const int nt = (keys_of(s, p.tokens, n - 1) + kBN - 1) / kBN;
       longest = nt > longest ? nt : longest;
     }
-    if (tiles) {
-      atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[0]), (unsigned long long)tiles);
-      atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[1]), (unsigned long long)keys);
-      atomicMax(&misc->levels, levels);
-      atomicMax(&misc->longest, longest);
+    if (warp * 32 < rp.B) {  // (atomics of a warp's lanes on one word would go one by one)
+      tiles = __reduce_add_sync(0xffffffffu, tiles);
+      keys = __reduce_add_sync(0xffffffffu, keys);
+      levels = __reduce_max_sync(0xffffffffu, levels);
+      longest = __reduce_max_sync(0xffffffffu, longest);
+      if (lane == 0) {
+        atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[0]), (unsigned long long)tiles);
+        atomicAdd(reinterpret_cast<unsigned long long*>(&misc->sum[1]), (unsigned long long)keys);
+        atomicMax(&misc->levels, levels);
+        atomicMax(&misc->longest, longest);
+      }
     }
     __syncthreads();
-    if (rp.B <= kSortMost) {  // the most keys first
+    if (rp.B <= kSortMost) {  // the most keys first, four threads a sequence
+      static_assert(4 * kSortMost <= kTcThreads, "threads of the sort");
+      const int at = threadIdx.x >> 2;
       Seq mine = {0, 0, 0, 0};
       int before = 0;
-      if (threadIdx.x < rp.B) {
-        mine = table[threadIdx.x];
-#pragma unroll 1
-        for (int x = 0; x < rp.B; ++x) before += table[x].kv > mine.kv || (table[x].kv == mine.kv && x < threadIdx.x);
+      if (at < rp.B) {
+        mine = table[at];
+#pragma unroll 4
+        for (int x = threadIdx.x & 3; x < rp.B; x += 4) before += table[x].kv > mine.kv || (table[x].kv == mine.kv && x < at);
       }
+      before += __shfl_xor_sync(0xffffffffu, before, 1);
+      before += __shfl_xor_sync(0xffffffffu, before, 2);
       __syncthreads();
-      if (threadIdx.x < rp.B) {
+      if (at < rp.B && (threadIdx.x & 3) == 0) {
         table[before] = mine;
-        order[before] = threadIdx.x;
+        order[before] = at;
       }
     }
     int chunk = 0x7fffffff;
@@ -368,7 +383,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           const int at = b0 + lane;
           Seq s = {0, 0, 0, 0};
           if (at < rp.B) s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
-          const int most = tiles_of(s, p.tokens);
+          const int most = tiles_of(s, p.tokens, p.by_tokens);
           if (most <= kAlone) {
 #pragma unroll 1
             for (int x = 0; x < most; ++x) n += chunks_of(s, p.tokens, x, c);
@@ -408,39 +423,52 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     }
     __syncthreads();
     // The list of entries, where a CTA makes several items: those with the most key tiles first (so that the SMs end
-    // together), among them by sequence, row tile and chunk.  A warp a count of key tiles; how many entries have it passes
-    // through the K stages, which hold nothing yet.
+    // together), among them by sequence, row tile and chunk.  A group of lanes a count of key tiles, a lane of it a
+    // sequence; how many entries have that count passes through the K stages, which hold nothing yet.
     const int n_counts = longest + 1;
     if (misc->entries <= kListMost && misc->levels <= kLevelMost && n_counts <= kLevelMost &&
         (entries * rp.Hkv > 2 * G || misc->levels > 8)) {
       int* first = reinterpret_cast<int*>(base + C::off_K);
+      const int wide = rp.B >= 32 ? 5 : 32 - __clz(rp.B - 1), width = 1 << wide, sub = lane & (width - 1);  // B = 1: one lane
 #pragma unroll 1
       for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
-        for (int count = warp; count < n_counts; count += kTcThreads / 32) {
-          int to = pass ? first[count] : 0;
+        for (int count0 = 0; count0 < n_counts; count0 += kTcThreads >> wide) {
+          const int count = count0 + (threadIdx.x >> wide);
+          const bool some = count < n_counts;
+          int to = pass && some ? first[count] : 0;
           const int pieces = count <= chunk ? 1 : (count + chunk - 1) / chunk;
 #pragma unroll 1
-          for (int b0 = 0; b0 < rp.B; b0 += 32) {
-            const int at = b0 + lane;
+          for (int b0 = 0; b0 < rp.B; b0 += width) {
+            const int at = b0 + sub;
             int x = 0, n = 0;  // row tiles x .. of this sequence have `count` key tiles
-            if (at < rp.B) {
+            if (some && at < rp.B) {
               const Seq s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
-              x = first_tile(s, p.tokens, count);
-              n = (first_tile(s, p.tokens, count + 1) - x) * pieces;
+              const int most = tiles_of(s, p.tokens, p.by_tokens);
+              x = first_tile(s, most, p.tokens, p.by_tokens, count);
+              n = (first_tile(s, most, p.tokens, p.by_tokens, count + 1) - x) * pieces;
             }
             int upto = n;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-              const int u = __shfl_up_sync(0xffffffffu, upto, off);
-              if (lane >= off) upto += u;
+#pragma unroll 1
+            for (int off = 1; off < width; off <<= 1) {
+              const int u = __shfl_up_sync(0xffffffffu, upto, off, width);
+              if (sub >= off) upto += u;
             }
-            if (pass)
-              for (int c = 0; c < n; ++c)
-                list[to + upto - n + c] = (uint32_t)at | (uint32_t)(x + c / pieces) << 10 | (uint32_t)(c % pieces) << 22;
-            to += __shfl_sync(0xffffffffu, upto, 31);
+            if (pass) {
+              uint32_t* put = list + to + upto - n;
+              int piece = 0;
+#pragma unroll 1
+              for (int c = 0; c < n; ++c) {
+                put[c] = (uint32_t)at | (uint32_t)x << 10 | (uint32_t)piece << 22;
+                if (++piece == pieces) {
+                  piece = 0;
+                  ++x;
+                }
+              }
+            }
+            to += __shfl_sync(0xffffffffu, upto, width - 1, width);
           }
-          if (!pass && lane == 0) first[count] = to;
+          if (!pass && some && sub == 0) first[count] = to;
         }
         __syncthreads();
         if (pass) break;
@@ -483,9 +511,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const KeyTile<D> lay(!rp.table);
       const int entries = misc->entries, head_group = misc->head_group, chunk_tiles = misc->chunk_tiles;
       const unsigned claims = (unsigned)entries * rp.Hkv, per_group = (unsigned)misc->grouped * head_group;  // below 2^31
-      const unsigned in_groups = (unsigned)misc->grouped * rp.Hkv, by_all = reciprocal(rp.Hkv);
-      const unsigned by_group = reciprocal(per_group), by_heads = reciprocal(head_group),
-                     by_last = reciprocal(rp.Hkv % head_group);
+      const unsigned in_groups = (unsigned)misc->grouped * rp.Hkv;
+      const bool one_group = head_group == rp.Hkv;
+      const unsigned by_group = one_group ? 0u : reciprocal(per_group), by_heads = one_group ? p.by_heads : reciprocal(head_group),
+                     by_last = one_group ? 0u : reciprocal(rp.Hkv % head_group);
       int level = misc->levels - 1, block = 0, acc = 0, group_at = 0;
       unsigned next = blockIdx.x, made = 0, cur = 0;  // items made, and the one whose keys are loaded
       unsigned st = 0, k_issued = 0, q_issued = 0;
@@ -503,12 +532,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             unsigned in_group = 0, in_entry;
             int hg = 0, heads = rp.Hkv, e;
             if (c < in_groups) {
-              hg = (int)divide(c, per_group, by_group, in_group);
+              if (one_group) in_group = c;
+              else hg = (int)divide(c, per_group, by_group, in_group);
               const int left = rp.Hkv - hg * head_group;
               heads = left < head_group ? left : head_group;
               e = (int)divide(in_group, heads, left < head_group ? by_last : by_heads, in_entry);
             } else {
-              e = misc->grouped + (int)divide(c - in_groups, rp.Hkv, by_all, in_entry);
+              e = misc->grouped + (int)divide(c - in_groups, rp.Hkv, p.by_heads, in_entry);
             }
             if (misc->listed) {
               const uint32_t x = list[e];
@@ -1196,6 +1226,8 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   p.scratch = p.ws + scratch_off(a.H);
   const int group = p.r.group;
   p.tokens = kBM / group;
+  p.by_tokens = reciprocal(p.tokens);
+  p.by_heads = reciprocal(a.Hkv);
   CUtensorMap mq, mk, mv;
   if (!rows_map(&mq, a.q, D, a.H, a.T, D, a.q_stride, group, p.tokens)) return cudaErrorNotSupported;
   if (a.table) {
