@@ -316,7 +316,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
   __syncthreads();
   pdl_wait();  // every global access and the TMEM allocation come after it
+  unsigned next = 0;  // the claim of the second item, under way beside the plan
   if (warp == kKWarp) {
+    if (lane == 0) next = atomicAdd(claim, 1u);
     tc::tmem_alloc(&misc->tmem, kTmemCols);
     tc::tmem_relinquish();
   }
@@ -424,29 +426,36 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     __syncthreads();
     // The list of entries, where a CTA makes several items: those with the most key tiles first (so that the SMs end
     // together), among them by sequence, row tile and chunk.  A group of lanes a count of key tiles, a lane of it a
-    // sequence; how many entries have that count passes through the K stages, which hold nothing yet.
-    const int n_counts = longest + 1;
-    if (misc->entries <= kListMost && misc->levels <= kLevelMost && n_counts <= kLevelMost &&
+    // sequence; the entries before are one for each row tile of more key tiles than the count and each chunk before its last.
+    if (misc->entries <= kListMost && misc->levels <= kLevelMost && longest < kLevelMost &&
         (entries * rp.Hkv > 2 * G || misc->levels > 8)) {
-      int* first = reinterpret_cast<int*>(base + C::off_K);
       const int wide = rp.B >= 32 ? 5 : 32 - __clz(rp.B - 1), width = 1 << wide, sub = lane & (width - 1);  // B = 1: one lane
+      const int at_once = kTcThreads >> wide;
 #pragma unroll 1
-      for (int pass = 0; pass < 2; ++pass) {
+      for (int count0 = 0; count0 <= longest; count0 += at_once) {
+        const int count = count0 + (threadIdx.x >> wide);
+        const bool some = count <= longest;
+        const int pieces = count <= chunk ? 1 : (count + chunk - 1) / chunk;
+        int to = 0;
 #pragma unroll 1
-        for (int count0 = 0; count0 < n_counts; count0 += kTcThreads >> wide) {
-          const int count = count0 + (threadIdx.x >> wide);
-          const bool some = count < n_counts;
-          int to = pass && some ? first[count] : 0;
-          const int pieces = count <= chunk ? 1 : (count + chunk - 1) / chunk;
+        for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
           for (int b0 = 0; b0 < rp.B; b0 += width) {
             const int at = b0 + sub;
-            int x = 0, n = 0;  // row tiles x .. of this sequence have `count` key tiles
+            int x = 0, n = 0;
             if (some && at < rp.B) {
               const Seq s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
               const int most = tiles_of(s, p.tokens, p.by_tokens);
-              x = first_tile(s, most, p.tokens, p.by_tokens, count);
-              n = (first_tile(s, most, p.tokens, p.by_tokens, count + 1) - x) * pieces;
+              const int more = first_tile(s, most, p.tokens, p.by_tokens, count + 1);
+              if (pass) {  // row tiles x .. more - 1 have `count` key tiles
+                x = first_tile(s, most, p.tokens, p.by_tokens, count);
+                n = (more - x) * pieces;
+              } else {
+                n = most - more;
+#pragma unroll 1
+                for (int j = chunk; j < longest; j += chunk)  // (a chunk is longer than that, or far from overflow)
+                  n += most - first_tile(s, most, p.tokens, p.by_tokens, (j > count ? j : count) + 1);
+              }
             }
             int upto = n;
 #pragma unroll 1
@@ -468,32 +477,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             }
             to += __shfl_sync(0xffffffffu, upto, width - 1, width);
           }
-          if (!pass && some && sub == 0) first[count] = to;
+          if (!pass && sub == 0 && count == longest * kLateTenths / 10) misc->grouped = to;
         }
-        __syncthreads();
-        if (pass) break;
-        if (warp == 0) {  // counts to places, the most key tiles first
-          int before = 0;
-#pragma unroll 1
-          for (int l0 = n_counts - 1; l0 >= 0; l0 -= 32) {
-            const int count = l0 - lane, n = count >= 0 ? first[count] : 0;
-            int upto = n;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-              const int u = __shfl_up_sync(0xffffffffu, upto, off);
-              if (lane >= off) upto += u;
-            }
-            if (count >= 0) first[count] = before + upto - n;
-            before += __shfl_sync(0xffffffffu, upto, 31);
-          }
-        }
-        __syncthreads();
       }
-      if (threadIdx.x == 0) {
-        misc->listed = 1;
-        misc->grouped = first[longest * kLateTenths / 10];
-      }
-      tc::fence_async_smem();  // the loads write where the counts were
+      if (threadIdx.x == 0) misc->listed = 1;
     }
   }
   tc::fence_before_sync();
@@ -516,7 +503,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const unsigned by_group = one_group ? 0u : reciprocal(per_group), by_heads = one_group ? p.by_heads : reciprocal(head_group),
                      by_last = one_group ? 0u : reciprocal(rp.Hkv % head_group);
       int level = misc->levels - 1, block = 0, acc = 0, group_at = 0;
-      unsigned next = blockIdx.x, made = 0, cur = 0;  // items made, and the one whose keys are loaded
+      bool first = true;
+      unsigned made = 0, cur = 0;  // items made, and the one whose keys are loaded
       unsigned st = 0, k_issued = 0, q_issued = 0;
       bool ok = true, more = true, started = false;
       int b = 0, h = 0, row0 = 0, klen = 0, t = 0, te = 0;  // of that item
@@ -524,8 +512,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       while (ok) {
         // the next item when there is none, and up to two ahead once the first keys of one are on their way
         if (more && made < cur + (started ? 3u : 1u)) {
-          const unsigned c = __shfl_sync(0xffffffffu, next, 0);
-          if (lane == 0) next = gridDim.x + atomicAdd(claim, 1u);  // needed for the item after this one
+          const unsigned c = first ? blockIdx.x : gridDim.x + __shfl_sync(0xffffffffu, next, 0);
+          if (lane == 0 && !first) next = atomicAdd(claim, 1u);  // needed for the item after this one
+          first = false;
           TcItem it;
           it.b = -1;
           if (c < claims) {
