@@ -40,6 +40,11 @@ CASES = [
     ([150, 20], [90, 19], 4, 2, 128, 16, "bf16", 0, False),
     ([1, 5, 20], [77, 5, 300], 4, 2, 64, 16, "f32", 2, True),
     ([2, 30], [1, 30], 3, 1, 128, 32, "f32", 0, False),
+    # many row tiles, few of them, with long contexts: chunks of entries that are listed
+    ([40, 33, 1, 0, 20, 7], [2600, 1700, 2000, 30, 900, 2400], 32, 1, 64, 16, "bf16", 0, True),
+    # more requests than a warp's lanes, and than are sorted, one of them long
+    ([3, 0, 1, 9] * 10, [40, 7, 300, 20] * 8 + [2500, 0, 130, 9, 3, 3, 1, 1990], 32, 1, 64, 16, "bf16", 3, False),
+    ([1, 1, 0, 1] * 50, [70, 129, 5, 300] * 49 + [0, 2300, 8, 1], 32, 1, 64, 16, "bf16", 0, False),
 ]
 
 

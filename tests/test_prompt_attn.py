@@ -144,3 +144,21 @@ def test_two_graphs_of_one_workspace():
     torch.cuda.synchronize()
     for s, o in zip((a, b), outs):
         check(host(o), *s.want())
+
+
+def test_two_streams_at_once():
+    """Calls that run beside one another, on workspaces of their own, give what they give alone."""
+    cases = [Prompt(7, [200, 90, 400], 4, 2, 128, "bf16"), Prompt(8, [2300], 2, 1, 64, "bf16"), Prompt(9, [5, 1, 3], 4, 4, 64, "bf16")]
+    alone, streams = [], [torch.cuda.Stream() for _ in cases]
+    for s in cases:
+        s.upload()
+        alone.append(s.run())
+    torch.cuda.synchronize()
+    outs = [[] for _ in cases]
+    for _ in range(10):
+        for i, (s, stream) in enumerate(zip(cases, streams)):
+            with torch.cuda.stream(stream):
+                outs[i].append(s.run(ws=s.ws))
+    torch.cuda.synchronize()
+    for want, got in zip(alone, outs):
+        assert all(torch.equal(want, g) for g in got)
