@@ -505,9 +505,9 @@ static glide_status rows_attention(const glide_attn_desc* d, glide::RowsArgs& a,
   a.scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->D);
   a.flags = d->flags;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (!(a.flags & GLIDE_FLAG_FORCE_FMA)) {
+  if (!(a.flags & GLIDE_FLAG_FORCE_FMA) && !glide::rows_fma_leads(a)) {
     cudaError_t err = glide::launch_paged_few(a, st);
-    if (err == cudaErrorNotSupported && !glide::rows_fma_leads(a)) err = glide::launch_rows_tc(a, st);
+    if (err == cudaErrorNotSupported) err = glide::launch_rows_tc(a, st);
     if (err != cudaErrorNotSupported) return from_cuda(err);
   }
   return from_cuda(glide::launch_rows_fma(a, st));

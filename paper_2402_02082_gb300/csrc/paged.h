@@ -42,7 +42,7 @@ cudaError_t launch_page_plan(const PlanArgs& a, cudaStream_t st);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t st);
 // On the CUDA cores, every type and size.
 cudaError_t launch_rows_fma(const RowsArgs& a, cudaStream_t st);
-// Whether that kernel is the faster one for bf16 rows that launch_paged_few does not take.
+// Whether that kernel is the fastest one for bf16 rows.
 bool rows_fma_leads(const RowsArgs& a);
 // bf16, pages, at most 16 query rows for a cached head; cudaErrorNotSupported for others.
 cudaError_t launch_paged_few(const RowsArgs& a, cudaStream_t st);

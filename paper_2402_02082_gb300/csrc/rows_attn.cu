@@ -6,6 +6,7 @@
 // 32 dot products at once (a lane a key), one maximum and one sum over the warp, then the values column by column; the
 // warps' results meet in shared memory.  Where no row can see more than 32 keys, each warp has a row of its own.
 // Two fp32 prompts of 60 to 128 tokens, 4 heads of 64: 9.8 us (a warp a row and 4 loads in flight: 40).
+#include "device.h"
 #include "kernels.h"
 #include "rows_attn.cuh"
 
@@ -91,9 +92,15 @@ constexpr int most_keys(const RowsArgs& a) { return a.table ? a.max_kv : a.max_q
 // 4 tokens, 8 heads: 1024 rows 5.1 and 16.6 us, 16384 rows 39 and 137; of 32 tokens: 2048 rows 9.8 and 10.5, 8192 rows
 // 27 and 16; four heads to a cached one, prompts of 16: 2048 rows 6.7 and 10.2, 8192 rows 20 and 12.  Above 32 keys the
 // tensor cores lead almost from the first row on (48 keys: 768 rows 8.6 and 9.7 us, 1920 rows 17 and 10).
+// Where launch_paged_few would serve the rows (pages, at most 16 of a cached head), its CTA for each cached head leads until
+// they are more than two for an SM; from there, a call of 1200 cached heads, 128 dims: 1 row of 16 keys 6.3 us here and 25.8
+// there, 2 of 32 keys 12 and 27, 4 of 16 keys 17 and 27, but 8 of 32 keys 43 and 31.
 bool rows_fma_leads(const RowsArgs& a) {
-  const long long items = (long long)a.B * a.Hkv * (((long long)a.max_q * (a.H / a.Hkv) + 127) / 128);
-  return most_keys(a) <= 32 && (long long)a.T * a.H <= 2048 + 12 * items;
+  const long long slabs = (long long)a.B * a.Hkv, slab_rows = (long long)a.max_q * (a.H / a.Hkv);
+  if (most_keys(a) > 32) return false;
+  if (a.table && slab_rows <= 16) return slabs > 2LL * sm_count() && most_keys(a) * slab_rows <= 64;
+  const long long items = slabs * ((slab_rows + 127) / 128);
+  return (long long)a.T * a.H <= 2048 + 12 * items;
 }
 
 cudaError_t launch_rows_fma(const RowsArgs& a, cudaStream_t st) {

@@ -44,6 +44,8 @@ CASES = [
     ([40, 33, 1, 0, 20, 7], [2600, 1700, 2000, 30, 900, 2400], 32, 1, 64, 16, "bf16", 0, True),
     # more requests than a warp's lanes, and than are sorted, one of them long
     ([3, 0, 1, 9] * 10, [40, 7, 300, 20] * 8 + [2500, 0, 130, 9, 3, 3, 1, 1990], 32, 1, 64, 16, "bf16", 3, False),
+    # many short requests
+    ([1, 1, 2, 0] * 45, [1, 30, 2, 0] * 45, 2, 2, 64, 16, "bf16", 1, False),
     ([1, 1, 0, 1] * 50, [70, 129, 5, 300] * 49 + [0, 2300, 8, 1], 32, 1, 64, 16, "bf16", 0, False),
 ]
 
