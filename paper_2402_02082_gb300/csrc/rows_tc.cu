@@ -14,17 +14,18 @@
 // between) takes three times the products, so tensor memory holds three S buffers beside O: S of tile i + 3 waits for P V of
 // tile i.  Two softmax groups of four warps take the key tiles in turn; the reference maximum passes from tile to tile, so
 // from group to group, through shared memory; a group keeps its own sum and takes it to the item's last reference at the end.
-// An item costs 3000 to 4000 cycles beside its tiles, and a call ~10 us.
+// An item costs 3000 to 4000 cycles beside its tiles, and a call ~9 us: 7000 cycles from the plan to the first scores, most
+// of them latency (lengths, code that runs once, queries, keys).
 //
-// Measured (bf16, D = 128; us): a prompt of 16384 tokens, 32 heads over 8 cached, 1365, and 1500 call after call under the
-// power limit (1.61 and 1.47 PFLOP/s of visible pairs); four of 2048, 32 heads, 126 to 132 (1.04 to 1.09); 24 of up to 333,
-// 52 heads, 62; eight requests of up to 512 new tokens over 512 to 4096 keys, 40 heads, 110.
+// Measured (bf16, D = 128; us): a prompt of 16384 tokens, 32 heads over 8 cached, 1350, and 1490 call after call under the
+// power limit (1.63 and 1.48 PFLOP/s of visible pairs); four of 2048, 32 heads, 123 to 128 (1.07 to 1.12); 24 of up to 333,
+// 52 heads, 57; eight requests of up to 512 new tokens over 512 to 4096 keys, 40 heads, 105.
 //
 // Work items are (cached head, 128 / group tokens, keys), claimed from a counter: cached heads in groups whose keys and
 // values together stay in L2, in them the row tiles with the most keys first; the short ones of all heads come last, so
-// that the SMs end together.  Where there are
-// fewer than two items for an SM, an item's keys may be cut into chunks, as many as cost least (split_cost); their partial
-// results (max, sum, o) go through the workspace, rows side by side, and a second kernel merges them in the chunks' order.
+// that the SMs end together.  Where there are fewer than two items for an SM, an item's keys may be cut into chunks, as many
+// as cost least (split_cost); their partial results (max, sum, o) go through the workspace, rows side by side, and a second
+// kernel merges them in the chunks' order.
 //
 // Code size counts: what does not stay in the instruction cache is fetched again by every role at every item.  A form of
 // this kernel with two row tiles a CTA, a softmax group each and rows of 128 scores in registers, unrolled, took 6000
