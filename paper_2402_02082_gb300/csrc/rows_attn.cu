@@ -1,5 +1,6 @@
 // Attention of packed rows of new tokens over a paged cache or over the pack itself, a block for each row and query
-// head on the CUDA cores: fp32, and everything that the tensor-core kernels do not take.
+// head on the CUDA cores: fp32, everything that the tensor-core kernels do not take, and bf16 calls of at most 32 keys that
+// are small for them (rows_fma_leads).
 //
 // What bounds it.  Every row reads all the keys that it sees, so the calls that it is meant for are the small ones; there
 // the chain of a row counts.  A block's four warps take a row's keys in turn, 32 at a time, with 16 loads in flight each:

@@ -8,12 +8,15 @@
 // A row tile packs the H / H_kv query heads that share a cached head: row r is token r / group, head r % group, so
 // 128 / group tokens and every key once for the whole group.
 //
-// What bounds it: shared memory.  A row tile and 128 keys of 128 take two products of ~520 cycles, in which S reads 64 KB and
-// P V 32, while the loads write 64: ~1430 cycles a tile measured, 1250 at 128 bytes a cycle.  (Two CTAs that share their
-// operands would need less; not built.)  The chain of a tile (S, the softmax of a row by one thread, P V, and the hand-overs
-// between) takes three times the products, so tensor memory holds three S buffers beside O: S of tile i + 3 waits for P V of
-// tile i.  Two softmax groups of four warps take the key tiles in turn; the reference maximum passes from tile to tile, so
-// from group to group, through shared memory; a group keeps its own sum and takes it to the item's last reference at the end.
+// What bounds it: a row tile and 128 keys of 128 take two products of ~520 cycles, in which S reads 64 KB of shared memory
+// and P V 32, while the loads write 64 (1250 cycles at 128 bytes a cycle); ~1430 cycles a tile measured.  At D = 64, half
+// of all that, ~1300: so the chain of a tile (S, the softmax of a row by one thread, P V, and the hand-overs between), which
+// takes three times the products, counts as much.  Tensor memory holds three S buffers beside O: S of tile i + 3 waits for
+// P V of tile i.  Two softmax groups of four warps take the key tiles in turn; the reference maximum passes from tile to
+// tile, so from group to group, through shared memory; a group keeps its own sum and takes it to the item's last reference at
+// the end.  Of a long prompt's cycles the tensor pipe is busy in 66% (D = 64: 37%), issue in 47, the exponentials' pipe in
+// 33.  Slower: a third softmax group (+7%), one eighth of the exponentials as polynomials (+3%), four S buffers of 96 keys
+// (long prompts +1.5%, paged calls up to +20%, prompts of 1000 tokens -5%).
 // An item costs 3000 to 4000 cycles beside its tiles, and a call ~9 us: 7000 cycles from the plan to the first scores, most
 // of them latency (lengths, code that runs once, queries, keys).
 //
