@@ -111,9 +111,9 @@ def test_attention(L):
 
 
 def test_attention_refuses_overlaps(L):
-    """out [9, 4, 64] bf16 (4608 bytes) and the workspace beside every input; one past its end they may not be refused for it."""
+    """out and the workspace on every input, and out's last 16 bytes on an input's first."""
     at = {n: FAKE + (x << 33) for x, n in enumerate(("q", "K", "V", "cu", "table", "kv", "out", "ws"))}
-    out_bytes = 9 * 4 * 64 * 2
+    out_bytes = 9 * 4 * 128 * 2
 
     def paged(**kw):
         a = {**at, **kw}
