@@ -96,25 +96,26 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
     __syncthreads();
     b = sm.slab_b;
   }
-  const int step = C * kFewWarps * kFewKeys;
-  int key0 = (rank * kFewWarps + warp) * kFewKeys;
+  // (keys are counted without a sign: there may be 2^31 - 1 of them, and the count passes that by two steps)
+  const unsigned step = C * kFewWarps * kFewKeys;
+  unsigned key0 = (rank * kFewWarps + warp) * kFewKeys;
   // (by the bound of the lengths, so that the first numbers are on their way beside the length)
-  const auto page_of = [&](int key0) { return key0 < p.max_kv ? page_at(p, b, key0 >> p.page_shift) : 0; };
+  const auto page_of = [&](unsigned key0) { return key0 < (unsigned)p.max_kv ? page_at(p, b, (int)(key0 >> p.page_shift)) : 0; };
   int page = page_of(key0), page_next = page_of(key0 + step);
   const Seq s = seq_of(p, b);
   const int rows = s.rows * p.group < kR ? s.rows * p.group : kR;
-  const int n = rows > 0 ? seen(s, s.rows - 1) : 0;  // keys that some row sees
+  const unsigned n = rows > 0 ? seen(s, s.rows - 1) : 0;  // keys that some row sees
   const uint64_t pol = policy_evict_first();
 
   // this lane's pieces of a tile; keys that no row sees are zeros (the pool may hold anything there)
   uint4 kr[2][kPK], vr[4][kPV];
-  const auto row_of = [&](const unsigned char* base, int page, int key) {
+  const auto row_of = [&](const unsigned char* base, int page, unsigned key) {
     return base + ((((size_t)page * p.Hkv + h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * (2 * D);
   };
-  const auto load_k = [&](int page, int key0) {
+  const auto load_k = [&](int page, unsigned key0) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int key = key0 + g + 8 * i;
+      const unsigned key = key0 + g + 8 * i;
       const unsigned char* at = row_of(p.K, page, key) + 16 * t;
 #pragma unroll
       for (int c = 0; c < kPK; ++c) {
@@ -123,10 +124,10 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
       }
     }
   };
-  const auto load_v = [&](int page, int key0) {
+  const auto load_v = [&](int page, unsigned key0) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int key = key0 + 8 * (i >> 1) + 2 * t + (i & 1);
+      const unsigned key = key0 + 8 * (i >> 1) + 2 * t + (i & 1);
       const unsigned char* at = row_of(p.V, page, key) + 16 * g;
 #pragma unroll
       for (int c = 0; c < kPV; ++c) {
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
       sm.qf[(warp * kSteps + 2 * c + 1) * 32 + lane] = make_uint2(x.z, x.w);
     }
   }
-  int vis[NT][2];  // keys that rows 2t, 2t + 1 see
+  unsigned vis[NT][2];  // keys that rows 2t, 2t + 1 see
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -156,7 +157,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
       const int r = 8 * nt + 2 * t + x;
       vis[nt][x] = r < rows ? seen(s, r / p.group) : 0;
     }
-  const int all_see = rows > 0 ? seen(s, 0) : 0;
+  const unsigned all_see = rows > 0 ? seen(s, 0) : 0;
   __syncthreads();
 
   float m[NT][2], l[NT][2], o[kSteps][NT][4];

@@ -95,21 +95,22 @@ __device__ __forceinline__ RowPart<D> no_keys() {
 }
 
 // Query head h in row `row0 + i` (row i of sequence b) over its keys first .. first + 31, first + step .., below n > 0.  All
-// lanes of a warp.  kAtOnce: loads in flight.  (Inlined: a kernel that splits its registers among its warps holds no call.)
+// lanes of a warp.  kAtOnce: loads in flight.  Keys are counted without a sign: n may be 2^31 - 1, and the count passes it by a
+// step.  (Inlined: a kernel that splits its registers among its warps holds no call.)
 template <typename T, int D, int kAtOnce>
-__device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Seq& s, int i, int h, int n, int first, int step,
-                                            RowPart<D>& r) {
+__device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Seq& s, int i, int h, unsigned n, unsigned first,
+                                            unsigned step, RowPart<D>& r) {
   constexpr int kE = D / 32, kRow = D * (int)sizeof(T), kC = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & 31, hk = h / p.group;
   const unsigned char* q = p.q + (long long)(s.row0 + i) * p.q_stride + (size_t)h * kRow;
 #pragma unroll 1
-  for (int t0 = first; t0 < n; t0 += step) {
-    const int t = t0 + lane;
+  for (unsigned t0 = first; t0 < n; t0 += step) {
+    const unsigned t = t0 + lane;
     float u = -CUDART_INF_F;
     size_t v_at = 0;  // of key t
     if (t < n) {
-      const unsigned char* k = p.K + key_at<kRow>(p, b, s.row0, hk, t, p.k_stride);
-      v_at = key_at<kRow>(p, b, s.row0, hk, t, p.v_stride);
+      const unsigned char* k = p.K + key_at<kRow>(p, b, s.row0, hk, (int)t, p.k_stride);
+      v_at = key_at<kRow>(p, b, s.row0, hk, (int)t, p.v_stride);
       float acc[2] = {0.f, 0.f};
 #pragma unroll kAtOnce
       for (int c = 0; c < D / kC; ++c)
@@ -126,7 +127,7 @@ __device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Se
 #pragma unroll
     for (int e = 0; e < kE; ++e) r.o[e] *= f;
     r.m = m_new;
-    const int most = n - t0 < 32 ? n - t0 : 32;
+    const int most = n - t0 < 32 ? (int)(n - t0) : 32;
 #pragma unroll 1
     for (int j0 = 0; j0 < most; j0 += kAtOnce) {
       float v[kAtOnce][kE];
