@@ -547,6 +547,8 @@ size_t glide_paged_workspace_bytes(const glide_attn_desc* desc, int32_t T, int32
  * What is not finite has the definition's result: what a row does not see never reaches it, whatever it
  * holds; a score that is NaN or +inf makes its row NaN, one of -inf has no weight, and a value that is not finite
  * decides its column in the rows that see it.  bf16: weights may be rounded to bf16 for the product with the values.
+ * Scores are formed in fp32: one whose products pass fp32's range counts as infinite.  A weight below 2^-126 of the row's
+ * largest counts as 0 for finite values.
  */
 glide_status glide_paged_attn(const glide_attn_desc* desc, const void* q, int64_t q_stride, int32_t T,
                               const int32_t* cu_q, int32_t max_q, const glide_page_pool* pool,

@@ -3,10 +3,12 @@
 // are small for them (rows_fma_leads).
 //
 // What bounds it.  Every row reads all the keys that it sees, so the calls that it is meant for are the small ones; there
-// the chain of a row counts.  A block's four warps take a row's keys in turn, 32 at a time, with 16 loads in flight each:
+// the chain of a row counts.  A block's four warps take a row's keys in turn, 32 at a time, with up to 16 loads in flight each:
 // 32 dot products at once (a lane a key), one maximum and one sum over the warp, then the values column by column; the
 // warps' results meet in shared memory.  Where no row can see more than 32 keys, each warp has a row of its own.
-// Two fp32 prompts of 60 to 128 tokens, 4 heads of 64: 9.8 us (a warp a row and 4 loads in flight: 40).
+// Two fp32 prompts of 60 to 128 tokens, 4 heads of 64: 9.9 us (a warp a row and 4 loads in flight: 40).  Registers are bounded for
+// six blocks an SM (four with 128 dims), where the values of eight keys at once fit without spills; 12 or 16 keys do not (prompts of
+// 32 tokens, 4 heads of 64: 5.2, 5.4 and 5.5 us; of 115 and 120: 10.6, 12.0 and 11.9).
 #include "device.h"
 #include "kernels.h"
 #include "rows_attn.cuh"
@@ -26,15 +28,34 @@ __device__ __forceinline__ int seq_at(const RowsParams& p, int i) {
   return lo;
 }
 
+// Output rows x = row * H + head = x0, x0 + step, .. by the definition.  (Out of line, after a loop that is done: the kernel keeps its
+// registers.  With grids of up to 2^30 blocks there is mostly one row.)
+template <typename T, int D, int kRowsAt>
+__device__ __noinline__ void define_rows(const RowsParams& p) {
+  const long long total = (long long)p.T * p.H;
+#pragma unroll 1
+  for (long long x = (long long)blockIdx.x * kRowsAt + (kRowsAt > 1 ? threadIdx.x >> 5 : 0); x < total; x += (long long)gridDim.x * kRowsAt) {
+    const int row = (int)(x / p.H), h = (int)(x - (long long)row * p.H);
+    const int b = seq_at(p, row);
+    const Seq s = seq_of(p, b);
+    const int i = row - s.row0;
+    if (i < 0 || i >= s.rows || seen(s, i) == 0) continue;
+    float o[D / 32];
+    attend_row<T, D>(p, b, s, i, h, seen(s, i), o);
+    store_row<D / 32>(reinterpret_cast<T*>(p.out) + x * D + (threadIdx.x & 31) * (D / 32), o);
+  }
+}
+
 // kPerRow: warps of a row, 1 or all of the block.
 template <typename T, int D, int kPerRow>
-__global__ void __launch_bounds__(kRowWarps * 32) rows_kernel(const RowsParams p) {
+__global__ void __launch_bounds__(kRowWarps * 32, D == 64 ? 6 : 4) rows_kernel(const __grid_constant__ RowsParams p) {
   constexpr int kE = D / 32;
   __shared__ float part_o[kRowWarps][D], part_m[kRowWarps], part_l[kRowWarps];
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long total = (long long)p.T * p.H;
   constexpr int kRowsAt = kRowWarps / kPerRow;
+  bool again = false;
   for (long long x = (long long)blockIdx.x * kRowsAt + (kPerRow == 1 ? warp : 0); x < total; x += (long long)gridDim.x * kRowsAt) {
     const int row = (int)(x / p.H), h = (int)(x - (long long)row * p.H);
     const int b = seq_at(p, row);
@@ -43,36 +64,46 @@ __global__ void __launch_bounds__(kRowWarps * 32) rows_kernel(const RowsParams p
     if (i < 0 || i >= s.rows) continue;
     const int n = seen(s, i);
     RowPart<D> r = no_keys<D>();
-    if (n > 0) attend_keys<T, D, 16>(p, b, s, i, h, n, (kPerRow == 1 ? 0 : warp) * 32, kPerRow * 32, r);
+    if (n > 0) attend_keys<T, D>(p, b, s, i, h, n, (kPerRow == 1 ? 0 : warp) * 32, kPerRow * 32, r);
+    // A sum of weights that is 0 or NaN makes the row NaN by definition; a result that is not finite beside another sum of
+    // weights has to be computed again.
     if constexpr (kPerRow == 1) {
+      bool odd = false;
 #pragma unroll
-      for (int e = 0; e < kE; ++e) r.o[e] = n > 0 ? r.o[e] / r.l : 0.f;
-      store_row<kE>(reinterpret_cast<T*>(p.out) + x * D + lane * kE, r.o);
-      continue;
-    }
-    __syncthreads();  // the row before has been read
-#pragma unroll
-    for (int e = 0; e < kE; ++e) part_o[warp][lane * kE + e] = r.o[e];
-    if (lane == 0) {
-      part_m[warp] = r.m;
-      part_l[warp] = r.l;
-    }
-    __syncthreads();
-    if (threadIdx.x < D) {
-      float m = -CUDART_INF_F, l = 0.f, o = 0.f;
-#pragma unroll
-      for (int w = 0; w < kRowWarps; ++w) m = fmaxf(m, part_m[w]);
-      const float ref = m == -CUDART_INF_F ? 0.f : m;
-#pragma unroll
-      for (int w = 0; w < kRowWarps; ++w) {
-        float f = fast_exp2(part_m[w] - ref);
-        if (part_m[w] != -CUDART_INF_F) f = f < FLT_MIN ? FLT_MIN : f;  // an infinite value keeps its weight (a NaN stays one)
-        l += f * part_l[w];
-        o += f * part_o[w][threadIdx.x];
+      for (int e = 0; e < kE; ++e) {
+        r.o[e] = n > 0 ? r.o[e] / r.l : 0.f;
+        odd |= !isfinite(r.o[e]);
       }
-      store_one(reinterpret_cast<T*>(p.out) + x * D + threadIdx.x, n > 0 ? o / l : 0.f);
+      store_row<kE>(reinterpret_cast<T*>(p.out) + x * D + lane * kE, r.o);
+      again |= __any_sync(0xffffffffu, odd) && r.l > 0.f;
+    } else {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) part_o[warp][lane * kE + e] = r.o[e];
+      if (lane == 0) {
+        part_m[warp] = r.m;
+        part_l[warp] = r.l;
+      }
+      __syncthreads();
+      bool odd = false;
+      if (threadIdx.x < D) {
+        float m = -CUDART_INF_F, l = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRowWarps; ++w) m = fmaxf(m, part_m[w]);
+        const float ref = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+        for (int w = 0; w < kRowWarps; ++w) {
+          const float f = fast_exp2(part_m[w] - ref);
+          l += f * part_l[w];
+          o += f * part_o[w][threadIdx.x];
+        }
+        o = n > 0 ? o / l : 0.f;
+        odd = !isfinite(o) && l > 0.f;
+        store_one(reinterpret_cast<T*>(p.out) + x * D + threadIdx.x, o);
+      }
+      again |= __syncthreads_or(odd) != 0;  // (the row's parts have been read, and its first result is written)
     }
   }
+  if (again && (kPerRow == 1 || warp == 0)) define_rows<T, D, kRowsAt>(p);
 }
 
 template <typename T, int D>

@@ -4,9 +4,13 @@
 //
 // The mathematics: u_t = (q . k_t) scale log2(e), m the running maximum of u, p_t = 2^(u_t - m),
 // out = sum p_t v_t / sum p_t, in fp32.  Lane t of a pass takes key t: its dot product needs no exchange;
-// for the values lane d takes D / 32 columns.  A weight is mathematically above 0 unless the score is
-// -inf, so one that underflows counts as the smallest normal number: an infinite value decides its
-// column at any weight, and 2^-126 moves no finite sum.
+// for the values lane d takes D / 32 columns.
+//
+// Two forms.  The plain sums (attend_keys) hold for results that are finite.  They are not finite where a value is
+// infinite or NaN (a weight of 0 makes NaN of it), or where a sum passes the type's range although the mean does not.  Then the row
+// is computed again by the definition (attend_row): values that are not finite decide their column at any weight but that of
+// a score of -inf and are summed apart, the others have their true weight, which may be 0, and are held as the mean so far, which
+// never passes its largest term.  A weight below 2^-126 of the largest counts as 0 in both.
 #pragma once
 
 #include <cfloat>
@@ -94,13 +98,27 @@ __device__ __forceinline__ RowPart<D> no_keys() {
   return r;
 }
 
+// u of key t < n for the query at `q`, cached head hk of sequence b; v_at: where its value is.  kAtOnce: 16-byte pieces loaded at once.
+template <typename T, int D, int kAtOnce>
+__device__ __forceinline__ float key_score(const RowsParams& p, int b, const Seq& s, int hk, const unsigned char* q, unsigned t,
+                                           size_t& v_at) {
+  constexpr int kRow = D * (int)sizeof(T), kC = 16 / (int)sizeof(T);
+  const unsigned char* k = p.K + key_at<kRow>(p, b, s.row0, hk, (int)t, p.k_stride);
+  v_at = key_at<kRow>(p, b, s.row0, hk, (int)t, p.v_stride);
+  float acc[2] = {0.f, 0.f};
+#pragma unroll kAtOnce
+  for (int c = 0; c < D / kC; ++c)
+    dot_chunk<T>(*reinterpret_cast<const uint4*>(q + 16 * c), *reinterpret_cast<const uint4*>(k + 16 * c), acc);
+  return (acc[0] + acc[1]) * p.scale_log2;
+}
+
 // Query head h in row `row0 + i` (row i of sequence b) over its keys first .. first + 31, first + step .., below n > 0.  All
 // lanes of a warp.  kAtOnce: loads in flight.  Keys are counted without a sign: n may be 2^31 - 1, and the count passes it by a
-// step.  (Inlined: a kernel that splits its registers among its warps holds no call.)
-template <typename T, int D, int kAtOnce>
+// step.
+template <typename T, int D>
 __device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Seq& s, int i, int h, unsigned n, unsigned first,
                                             unsigned step, RowPart<D>& r) {
-  constexpr int kE = D / 32, kRow = D * (int)sizeof(T), kC = 16 / (int)sizeof(T);
+  constexpr int kE = D / 32, kRow = D * (int)sizeof(T), kAtOnce = 8;  // keys whose values are loaded at once
   const int lane = threadIdx.x & 31, hk = h / p.group;
   const unsigned char* q = p.q + (long long)(s.row0 + i) * p.q_stride + (size_t)h * kRow;
 #pragma unroll 1
@@ -108,21 +126,10 @@ __device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Se
     const unsigned t = t0 + lane;
     float u = -CUDART_INF_F;
     size_t v_at = 0;  // of key t
-    if (t < n) {
-      const unsigned char* k = p.K + key_at<kRow>(p, b, s.row0, hk, (int)t, p.k_stride);
-      v_at = key_at<kRow>(p, b, s.row0, hk, (int)t, p.v_stride);
-      float acc[2] = {0.f, 0.f};
-#pragma unroll kAtOnce
-      for (int c = 0; c < D / kC; ++c)
-        dot_chunk<T>(*reinterpret_cast<const uint4*>(q + 16 * c), *reinterpret_cast<const uint4*>(k + 16 * c), acc);
-      u = (acc[0] + acc[1]) * p.scale_log2;
-    }
+    if (t < n) u = key_score<T, D, 16>(p, b, s, hk, q, t, v_at);
     const float m_new = fmaxf(r.m, warp_max(u));
     const float m_eff = m_new == -CUDART_INF_F ? 0.f : m_new;
-    float f = fast_exp2(r.m - m_eff);
-    if (r.m != -CUDART_INF_F) f = f < FLT_MIN ? FLT_MIN : f;  // (a NaN stays one)
-    float w = fast_exp2(u - m_eff);
-    if (u != -CUDART_INF_F) w = w < FLT_MIN ? FLT_MIN : w;
+    const float f = fast_exp2(r.m - m_eff), w = fast_exp2(u - m_eff);
     r.l = r.l * f + warp_sum(w);
 #pragma unroll
     for (int e = 0; e < kE; ++e) r.o[e] *= f;
@@ -139,7 +146,7 @@ __device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Se
 #pragma unroll
       for (int j = 0; j < kAtOnce; ++j) {
         const float pj = __shfl_sync(0xffffffffu, w, (j0 + j) & 31);
-        if (j0 + j >= most || pj == 0.f) continue;  // a score of -inf: no weight, whatever the value
+        if (j0 + j >= most) continue;
 #pragma unroll
         for (int e = 0; e < kE; ++e) r.o[e] = fmaf(pj, v[j][e], r.o[e]);
       }
@@ -147,13 +154,59 @@ __device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Se
   }
 }
 
-// The whole row by one warp: o[e], column lane * (D / 32) + e of the result over the first n > 0 keys.
+// The whole row by one warp and the definition: o[e], column lane * (D / 32) + e of the result over the first n > 0 keys.  Called
+// where the plain sums are not finite.  (Inlined: a kernel that splits its registers among its warps holds no call.)
 template <typename T, int D>
-__device__ __forceinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, int n, float (&o)[D / 32]) {
-  RowPart<D> r = no_keys<D>();
-  attend_keys<T, D, 4>(p, b, s, i, h, n, 0, 32, r);
+__device__ __forceinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, unsigned n, float (&o)[D / 32]) {
+  constexpr int kE = D / 32, kRow = D * (int)sizeof(T), kAtOnce = 4;
+  const int lane = threadIdx.x & 31, hk = h / p.group;
+  const unsigned char* q = p.q + (long long)(s.row0 + i) * p.q_stride + (size_t)h * kRow;
+  float m = -CUDART_INF_F, l = 0.f, bad[kE];  // bad: the sum of values that are not finite
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e) o[e] = r.o[e] / r.l;
+  for (int e = 0; e < kE; ++e) o[e] = bad[e] = 0.f;  // o: half of the mean so far, so that its terms' rounding stays in range too
+#pragma unroll 1
+  for (unsigned t0 = 0; t0 < n; t0 += 32) {
+    float u = -CUDART_INF_F;
+    size_t v_at = 0;
+    if (t0 + lane < n) u = key_score<T, D, kAtOnce>(p, b, s, hk, q, t0 + lane, v_at);
+    const float m_new = fmaxf(m, warp_max(u));
+    const float m_eff = m_new == -CUDART_INF_F ? 0.f : m_new;
+    const float before = l * fast_exp2(m - m_eff);
+    float w = fast_exp2(u - m_eff);
+    l = before + warp_sum(w);  // NaN from the first score that is NaN or +inf on
+    const float inv = l > 0.f ? 1.f / l : 0.f, keep = before * inv;
+    w *= 0.5f * inv;
+    m = m_new;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) o[e] *= keep;
+    const unsigned weighs = __ballot_sync(0xffffffffu, u != -CUDART_INF_F);
+    const int most = n - t0 < 32 ? (int)(n - t0) : 32;
+#pragma unroll 1
+    for (int j0 = 0; j0 < most; j0 += kAtOnce) {
+      float v[kAtOnce][kE];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const size_t at = __shfl_sync(0xffffffffu, v_at, (j0 + j) & 31);
+        if (j0 + j < most) load_row_chunk<T, kE>(reinterpret_cast<const T*>(p.V + at) + lane * kE, v[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const float pj = __shfl_sync(0xffffffffu, w, (j0 + j) & 31);
+        if (j0 + j >= most || !((weighs >> (j0 + j)) & 1u)) continue;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const bool finite = fabsf(v[j][e]) <= FLT_MAX;
+          o[e] = fmaf(pj, finite ? v[j][e] : 0.f, o[e]);
+          bad[e] += finite ? 0.f : v[j][e];
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    const float mean = fmaxf(-FLT_MAX, fminf(2.f * o[e], FLT_MAX));
+    o[e] = l > 0.f ? (bad[e] == 0.f ? mean : bad[e]) : CUDART_NAN_F;
+  }
 }
 
 __device__ __forceinline__ void store_one(float* at, float v) { *at = v; }
