@@ -18,7 +18,9 @@
 //   S^T (16 keys x 8 queries): lane (g, t) reads pieces t, t + 4, .. of keys g, g + 8, and of query g
 //   O^T (16 dims x 8 queries): lane (g, t) reads pieces g, g + 8 of keys 2t, 2t + 1, 2t + 8, 2t + 9
 // The weights of S^T become the second product's operand by a transpose of 8 x 8 within the warp.
-// The reference maximum is raised only where a tile's exceeds it by more than 8, so O is seldom rescaled.
+// The reference maximum is raised only where a tile's exceeds it by more than 8, so O is seldom rescaled.  The tensor cores' sums lose
+// what lies 2^-25 below O with every product, so a warp's O takes in 2^17 keys and then joins fp32 sums in shared memory (the
+// mean of 2^24 keys of like weight, a CTA a slab, relative error: -5e-3 without, -1e-4 with it).
 //
 // A result that is not finite (an infinity or NaN that the row sees, or one that it does not see, in a tile
 // that it shares) is computed again by the definition, the row alone.
@@ -37,6 +39,7 @@ constexpr int kFewWarps = 8;
 constexpr int kFewThreads = kFewWarps * 32;
 constexpr int kFewKeys = 16;  // keys of a tile: no page is smaller
 constexpr int kMaxC = 8;
+constexpr unsigned kSpanTiles = 8192;  // tiles of a warp that one O takes in (2^17 keys)
 constexpr float kRaise = 8.f;  // log2 of how far a weight may exceed 1
 
 __device__ __forceinline__ void mma_bf16_16x8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -170,93 +173,130 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[j][nt][k] = 0.f;
   }
+  unsigned stop = step * kSpanTiles < n ? step * kSpanTiles : n;  // (at most 2^23 keys a span)
+  bool first = true;
 #pragma unroll 1
-  for (; key0 < n; key0 += step) {
-    load_v(page, key0);
-    float u[NT][4];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) u[nt][k] = 0.f;
-#pragma unroll
-    for (int c = 0; c < kPK; ++c) {
-      const uint32_t a0[4] = {kr[0][c].x, kr[1][c].x, kr[0][c].y, kr[1][c].y};
-      const uint32_t a1[4] = {kr[0][c].z, kr[1][c].z, kr[0][c].w, kr[1][c].w};
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const uint2 q0 = sm.qf[(nt * kSteps + 2 * c) * 32 + lane], q1 = sm.qf[(nt * kSteps + 2 * c + 1) * 32 + lane];
-        mma_bf16_16x8(u[nt], a0, q0.x, q0.y);
-        mma_bf16_16x8(u[nt], a1, q1.x, q1.y);
-      }
-    }
-    load_k(page_next, key0 + step);  // the next tile's keys, under this one's softmax and values
-    page = page_next;
-    page_next = page_of(key0 + 2 * step);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) u[nt][k] *= p.scale_log2;
-    if (key0 + kFewKeys > all_see) {
+  while (true) {
+#pragma unroll 1
+    for (; key0 < stop; key0 += step) {
+      load_v(page, key0);
+      float u[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) u[nt][k] = key0 + g + 4 * (k & 2) < vis[nt][k & 1] ? u[nt][k] : -CUDART_INF_F;
+        for (int k = 0; k < 4; ++k) u[nt][k] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kPK; ++c) {
+        const uint32_t a0[4] = {kr[0][c].x, kr[1][c].x, kr[0][c].y, kr[1][c].y};
+        const uint32_t a1[4] = {kr[0][c].z, kr[1][c].z, kr[0][c].w, kr[1][c].w};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint2 q0 = sm.qf[(nt * kSteps + 2 * c) * 32 + lane], q1 = sm.qf[(nt * kSteps + 2 * c + 1) * 32 + lane];
+          mma_bf16_16x8(u[nt], a0, q0.x, q0.y);
+          mma_bf16_16x8(u[nt], a1, q1.x, q1.y);
+        }
+      }
+      load_k(page_next, key0 + step);  // the next tile's keys, under this one's softmax and values
+      page = page_next;
+      page_next = page_of(key0 + 2 * step);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[nt][k] *= p.scale_log2;
+      if (key0 + kFewKeys > all_see) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) u[nt][k] = key0 + g + 4 * (k & 2) < vis[nt][k & 1] ? u[nt][k] : -CUDART_INF_F;
+      }
+      uint32_t pt[NT][2];
+      bool raise = false;
+      float top[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float v = fmaxf(u[nt][x], u[nt][x + 2]);
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+          top[nt][x] = v;
+          raise |= v > m[nt][x] + kRaise;
+        }
+      if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float f[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float m_new = top[nt][x] > m[nt][x] + kRaise ? top[nt][x] : m[nt][x];
+            f[x] = m[nt][x] == m_new ? 1.f : fast_exp2(m[nt][x] - m_new);
+            l[nt][x] *= f[x];
+            m[nt][x] = m_new;
+          }
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j) {
+            o[j][nt][0] *= f[0];
+            o[j][nt][1] *= f[1];
+            o[j][nt][2] *= f[0];
+            o[j][nt][3] *= f[1];
+          }
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const float ref = m[nt][x] == -CUDART_INF_F ? 0.f : m[nt][x];
+          u[nt][x] = fast_exp2(u[nt][x] - ref);
+          u[nt][x + 2] = fast_exp2(u[nt][x + 2] - ref);
+          l[nt][x] += u[nt][x] + u[nt][x + 2];
+        }
+        pt[nt][0] = transposed8(pack_bf16x2(u[nt][0], u[nt][1]));
+        pt[nt][1] = transposed8(pack_bf16x2(u[nt][2], u[nt][3]));
+      }
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        const int c = j >> 2;
+        const auto word = [&](int i) { return (j & 3) == 0 ? vr[i][c].x : (j & 3) == 1 ? vr[i][c].y : (j & 3) == 2 ? vr[i][c].z : vr[i][c].w; };
+        // dims 8 (g + 8 c) + 2 (j % 4) and the next are the product's rows g and g + 8
+        const uint32_t a[4] = {__byte_perm(word(0), word(1), 0x5410), __byte_perm(word(0), word(1), 0x7632),
+                               __byte_perm(word(2), word(3), 0x5410), __byte_perm(word(2), word(3), 0x7632)};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) mma_bf16_16x8(o[j][nt], a, pt[nt][0], pt[nt][1]);
+      }
     }
-    uint32_t pt[NT][2];
-    bool raise = false;
-    float top[NT][2];
+
+    // a span's results, and those of the spans before
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        float v = fmaxf(u[nt][x], u[nt][x + 2]);
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
-        top[nt][x] = v;
-        raise |= v > m[nt][x] + kRaise;
-      }
-    if (__any_sync(0xffffffffu, raise)) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float f[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float m_new = top[nt][x] > m[nt][x] + kRaise ? top[nt][x] : m[nt][x];
-          f[x] = m[nt][x] == m_new ? 1.f : fast_exp2(m[nt][x] - m_new);
-          l[nt][x] *= f[x];
-          m[nt][x] = m_new;
+        const int r = 8 * nt + 2 * t + x;
+        float f = 0.f;
+        if (!first) {
+          const float before = sm.stat[warp * kR + r].x;
+          f = before == m[nt][x] ? 1.f : fast_exp2(before - m[nt][x]);
         }
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-          o[j][nt][0] *= f[0];
-          o[j][nt][1] *= f[1];
-          o[j][nt][2] *= f[0];
-          o[j][nt][3] *= f[1];
+          float2* at = reinterpret_cast<float2*>(&sm.red[(warp * kR + r) * kStride + 64 * (j >> 2) + 8 * g + 2 * (j & 3)]);
+          float2 sum = make_float2(o[j][nt][x], o[j][nt][x + 2]);
+          if (!first) sum = make_float2(sum.x + f * at->x, sum.y + f * at->y);
+          *at = sum;
+          o[j][nt][x] = o[j][nt][x + 2] = 0.f;
         }
       }
+    __syncwarp();
+    if (g == 0) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) sm.stat[warp * kR + 8 * nt + 2 * t + x].x = m[nt][x];
     }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float ref = m[nt][x] == -CUDART_INF_F ? 0.f : m[nt][x];
-        u[nt][x] = fast_exp2(u[nt][x] - ref);
-        u[nt][x + 2] = fast_exp2(u[nt][x + 2] - ref);
-        l[nt][x] += u[nt][x] + u[nt][x + 2];
-      }
-      pt[nt][0] = transposed8(pack_bf16x2(u[nt][0], u[nt][1]));
-      pt[nt][1] = transposed8(pack_bf16x2(u[nt][2], u[nt][3]));
-    }
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j) {
-      const int c = j >> 2;
-      const auto word = [&](int i) { return (j & 3) == 0 ? vr[i][c].x : (j & 3) == 1 ? vr[i][c].y : (j & 3) == 2 ? vr[i][c].z : vr[i][c].w; };
-      // dims 8 (g + 8 c) + 2 (j % 4) and the next are the product's rows g and g + 8
-      const uint32_t a[4] = {__byte_perm(word(0), word(1), 0x5410), __byte_perm(word(0), word(1), 0x7632),
-                             __byte_perm(word(2), word(3), 0x5410), __byte_perm(word(2), word(3), 0x7632)};
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_bf16_16x8(o[j][nt], a, pt[nt][0], pt[nt][1]);
-    }
+    __syncwarp();
+    if (key0 >= n) break;
+    first = false;
+    stop = n - stop < step * kSpanTiles ? n : stop + step * kSpanTiles;
   }
 
   // ---- the warps' results, then the cluster's
@@ -265,14 +305,9 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int r = 8 * nt + 2 * t + x;
 #pragma unroll
       for (int off = 4; off < 32; off <<= 1) l[nt][x] += __shfl_xor_sync(0xffffffffu, l[nt][x], off);
-      if (g == 0) sm.stat[warp * kR + r] = make_float2(m[nt][x], l[nt][x]);
-#pragma unroll
-      for (int j = 0; j < kSteps; ++j)
-        *reinterpret_cast<float2*>(&sm.red[(warp * kR + r) * kStride + 64 * (j >> 2) + 8 * g + 2 * (j & 3)]) =
-            make_float2(o[j][nt][x], o[j][nt][x + 2]);
+      if (g == 0) sm.stat[warp * kR + 8 * nt + 2 * t + x].y = l[nt][x];
     }
   __syncthreads();
   // a warp or CTA without a tile has the maximum -inf, zeros, and weight 0

@@ -24,6 +24,10 @@
 // power limit (1.63 and 1.48 PFLOP/s of visible pairs); four of 2048, 32 heads, 123 to 128 (1.07 to 1.12); 24 of up to 333,
 // 52 heads, 57; eight requests of up to 512 new tokens over 512 to 4096 keys, 40 heads, 105.
 //
+// The tensor cores' sums lose what lies 2^-25 below O with every product (measured), which the sum of a row's weights does not.  So
+// one O takes in 2^17 keys at most: an item of more goes in segments, whose (max, sum, o) the result warps fold in fp32 in the
+// workspace.  The mean of 2^22 keys of like weight, relative error: -2.5e-2 in one O, -5e-5 in segments; of 2^24, -0.1 and -5e-5.
+//
 // Work items are (cached head, 128 / group tokens, keys), claimed from a counter: cached heads in groups whose keys and
 // values together stay in L2, in them the row tiles with the most keys first; the short ones of all heads come last, so
 // that the SMs end together.  Where there are fewer than two items for an SM, an item's keys may be cut into chunks, as many
@@ -79,6 +83,7 @@ constexpr int kListMost = 3000;        // entries (sequence, row tile, chunk) th
 constexpr int kLevelMost = 4096;       // row tiles of a sequence that a list entry holds
 constexpr long long kL2Bytes = 48ll << 20;
 constexpr int kManyKeys = 1 << 24;     // that no part of L2 holds; sums of two for each lane of a warp stay in 32 bits
+constexpr int kSegTiles = 1024;        // key tiles that one O takes in (2^17 keys)
 constexpr int kLateTenths = 4;         // items with at most this part of the longest one's key tiles are left to the end
 
 // Workspace: in the header the status word, the claim counter, the count of finished CTAs, and for the merge the count of
@@ -115,10 +120,12 @@ struct Bars {
   uint64_t drained[2];
 };
 
+constexpr int kMore = 1, kAfter = 2;
 struct TcItem {
   int b;                  // -1: no more
   int h, row0, m, kv, rows, pos0;
-  int t0, te;             // key tiles
+  int t0, te;             // key tiles (of this segment)
+  int segment;            // kMore: segments of the item follow, kAfter: some came before
   int klen;               // keys that some row of the item sees
   int chunks, chunk, slot, slot_step;  // chunks of the item, this one, its partial slot, slots from chunk to chunk
 };
@@ -263,7 +270,8 @@ struct Boxes {
   }
 };
 
-template <int D>
+// kLong: items may have more than kSegTiles key tiles.  (Short prompts take 57 us without the code for that, 58 with it.)
+template <int D, bool kLong>
 __global__ void __launch_bounds__(kTcThreads, 1)
     rows_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                    const __grid_constant__ CUtensorMap tmV, const TcParams p) {
@@ -510,93 +518,110 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       bool first = true;
       unsigned made = 0, cur = 0;  // items made, and the one whose keys are loaded
       unsigned st = 0, k_issued = 0, q_issued = 0;
-      bool ok = true, more = true, started = false;
+      bool ok = true, more = true, started = false, rest = false;
+      int end = 0;  // of the last item made; rest: it has more segments
       int b = 0, h = 0, row0 = 0, klen = 0, t = 0, te = 0;  // of that item
 #pragma unroll 1
       while (ok) {
         // the next item when there is none, and up to two ahead once the first keys of one are on their way
         if (more && made < cur + (started ? 3u : 1u)) {
-          const unsigned c = first ? blockIdx.x : gridDim.x + __shfl_sync(0xffffffffu, next, 0);
-          if (lane == 0 && !first) next = atomicAdd(claim, 1u);  // needed for the item after this one
-          first = false;
           TcItem it;
-          it.b = -1;
-          if (c < claims) {
-            unsigned in_group = 0, in_entry;
-            int hg = 0, heads = rp.Hkv, e;
-            if (c < in_groups) {
-              if (one_group) in_group = c;
-              else hg = (int)divide(c, per_group, by_group, in_group);
-              const int left = rp.Hkv - hg * head_group;
-              heads = left < head_group ? left : head_group;
-              e = (int)divide(in_group, heads, left < head_group ? by_last : by_heads, in_entry);
-            } else {
-              e = misc->grouped + (int)divide(c - in_groups, rp.Hkv, p.by_heads, in_entry);
-            }
-            if (misc->listed) {
-              const uint32_t x = list[e];
-              const int at = x & 1023;
-              level = (x >> 10) & 4095;
-              it.chunk = x >> 22;
-              const Seq s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
-              it.b = rp.B <= kSortMost ? order[at] : at;
-              it.row0 = s.row0;
-              it.m = s.m;
-              it.kv = s.kv;
-              it.rows = s.rows;
-              it.chunks = chunks_of(s, p.tokens, level, chunk_tiles);
-            } else {
-            if (hg != group_at) {
-              group_at = hg;
-              level = misc->levels - 1;
-              block = acc = 0;
-            }
-            // entry e, found by the counts (many sequences or very long ones)
+          if (kLong && rest) {
+            it = items[(made - 1) % kItemSlots];
+            it.t0 = it.te;
+            it.segment = kAfter;
+          } else {
+            const unsigned c = first ? blockIdx.x : gridDim.x + __shfl_sync(0xffffffffu, next, 0);
+            if (lane == 0 && !first) next = atomicAdd(claim, 1u);  // needed for the item after this one
+            first = false;
+            it.b = -1;
+            if (c < claims) {
+              unsigned in_group = 0, in_entry;
+              int hg = 0, heads = rp.Hkv, e;
+              if (c < in_groups) {
+                if (one_group) in_group = c;
+                else hg = (int)divide(c, per_group, by_group, in_group);
+                const int left = rp.Hkv - hg * head_group;
+                heads = left < head_group ? left : head_group;
+                e = (int)divide(in_group, heads, left < head_group ? by_last : by_heads, in_entry);
+              } else {
+                e = misc->grouped + (int)divide(c - in_groups, rp.Hkv, p.by_heads, in_entry);
+              }
+              if (misc->listed) {
+                const uint32_t x = list[e];
+                const int at = x & 1023;
+                level = (x >> 10) & 4095;
+                it.chunk = x >> 22;
+                const Seq s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
+                it.b = rp.B <= kSortMost ? order[at] : at;
+                it.row0 = s.row0;
+                it.m = s.m;
+                it.kv = s.kv;
+                it.rows = s.rows;
+                it.chunks = chunks_of(s, p.tokens, level, chunk_tiles);
+              } else {
+              if (hg != group_at) {
+                group_at = hg;
+                level = misc->levels - 1;
+                block = acc = 0;
+              }
+              // entry e, found by the counts (many sequences or very long ones)
 #pragma unroll 1
-            while (level >= 0) {
-              const int at = block * 32 + lane;
-              int n = 0;
-              Seq s = {0, 0, 0, 0};
-              if (at < rp.B) {
-                s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
-                n = chunks_of(s, p.tokens, level, chunk_tiles);
-              }
-              int upto = n;
+              while (level >= 0) {
+                const int at = block * 32 + lane;
+                int n = 0;
+                Seq s = {0, 0, 0, 0};
+                if (at < rp.B) {
+                  s = rp.B <= kSortMost ? table[at] : seq_of(rp, at);
+                  n = chunks_of(s, p.tokens, level, chunk_tiles);
+                }
+                int upto = n;
 #pragma unroll
-              for (int off = 1; off < 32; off <<= 1) {
-                const int u = __shfl_up_sync(0xffffffffu, upto, off);
-                if (lane >= off) upto += u;
+                for (int off = 1; off < 32; off <<= 1) {
+                  const int u = __shfl_up_sync(0xffffffffu, upto, off);
+                  if (lane >= off) upto += u;
+                }
+                const int total = __shfl_sync(0xffffffffu, upto, 31);
+                if (e < acc + total) {
+                  const int who = __ffs(__ballot_sync(0xffffffffu, e < acc + upto)) - 1;
+                  it.b = __shfl_sync(0xffffffffu, at, who);
+                  if (rp.B <= kSortMost) it.b = order[it.b];
+                  it.chunks = __shfl_sync(0xffffffffu, n, who);
+                  it.chunk = e - acc - (__shfl_sync(0xffffffffu, upto, who) - it.chunks);
+                  it.row0 = __shfl_sync(0xffffffffu, s.row0, who);
+                  it.m = __shfl_sync(0xffffffffu, s.m, who);
+                  it.kv = __shfl_sync(0xffffffffu, s.kv, who);
+                  it.rows = __shfl_sync(0xffffffffu, s.rows, who);
+                  break;
+                }
+                acc += total;
+                if (++block * 32 >= rp.B) {
+                  block = 0;
+                  --level;
+                }
               }
-              const int total = __shfl_sync(0xffffffffu, upto, 31);
-              if (e < acc + total) {
-                const int who = __ffs(__ballot_sync(0xffffffffu, e < acc + upto)) - 1;
-                it.b = __shfl_sync(0xffffffffu, at, who);
-                if (rp.B <= kSortMost) it.b = order[it.b];
-                it.chunks = __shfl_sync(0xffffffffu, n, who);
-                it.chunk = e - acc - (__shfl_sync(0xffffffffu, upto, who) - it.chunks);
-                it.row0 = __shfl_sync(0xffffffffu, s.row0, who);
-                it.m = __shfl_sync(0xffffffffu, s.m, who);
-                it.kv = __shfl_sync(0xffffffffu, s.kv, who);
-                it.rows = __shfl_sync(0xffffffffu, s.rows, who);
-                break;
               }
-              acc += total;
-              if (++block * 32 >= rp.B) {
-                block = 0;
-                --level;
+              if (it.b >= 0) {
+                it.h = hg * head_group + (int)in_entry;
+                it.pos0 = level * p.tokens;
+                const Seq s = {it.row0, it.rows, it.m, it.kv};
+                it.klen = keys_of(s, p.tokens, level);
+                // a slot for each item of a call that has chunks (kMaxChunks at most), one for each CTA of another
+                it.slot = chunk_tiles < 0x7fffffff ? (int)c : (int)blockIdx.x;
+                it.slot_step = heads;
+                it.t0 = it.chunks > 1 ? it.chunk * chunk_tiles : 0;
+                const int nt = (it.klen + kBN - 1) / kBN;
+                end = it.chunks > 1 && nt - it.t0 > chunk_tiles ? it.t0 + chunk_tiles : nt;
+                it.segment = 0;
               }
             }
-            }
-            if (it.b >= 0) {
-              it.h = hg * head_group + (int)in_entry;
-              it.pos0 = level * p.tokens;
-              const Seq s = {it.row0, it.rows, it.m, it.kv};
-              it.klen = keys_of(s, p.tokens, level);
-              it.slot = (int)c;
-              it.slot_step = heads;
-              it.t0 = it.chunks > 1 ? it.chunk * chunk_tiles : 0;
-              const int nt = (it.klen + kBN - 1) / kBN;
-              it.te = it.chunks > 1 && nt - it.t0 > chunk_tiles ? it.t0 + chunk_tiles : nt;
+          }
+          it.te = end;
+          if constexpr (kLong) {
+            rest = it.b >= 0 && end - it.t0 > kSegTiles;
+            if (rest) {
+              it.te = it.t0 + kSegTiles;
+              it.segment |= kMore;
             }
           }
           const unsigned slot = made % kItemSlots;
@@ -815,7 +840,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (!item) break;
       const TcItem& it = *item;  // let go at the item's end
       const Seq s = {it.row0, it.rows, it.m, it.kv};
-      const bool split = it.chunks > 1;
+      const bool split = it.chunks > 1, keep = split || (kLong && (it.segment & kMore));  // keep: the results stay in the slot
       unsigned again = 0;  // rows whose result is not finite
       const int pos = it.pos0 + token;
       const bool valid = token < p.tokens && pos < it.rows;
@@ -836,7 +861,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       }
       ok = warp_wait_small(&bars->lready, n_items & 1, abort_flag);
       if (!ok) break;
-      const float l = l_row[r] + l_row[kBM + r], mx = m_row[r];
+      float l = l_row[r] + l_row[kBM + r], mx = m_row[r];
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->lfree);
       ok = warp_wait_small(&bars->olast, n_items & 1, abort_flag);
@@ -846,16 +871,34 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       // O, 32 columns at a time, through what was the place of the item's queries (S is done with them), then out in whole
       // rows.  bf16: 16-byte piece e of row x at e ^ (x & 7) of its 256 (D = 64: 128) bytes; rolled loops (code size).
       unsigned char* stage = base + C::off_Q + ((n_items - 1) & 1) * C::kTile + quarter * 32 * (2 * D);
-      const float inv = split ? 1.f : sees > 0 ? 1.f / l : 0.f;
+      float* part = parts + it.slot * slot_floats + r;
+      if (kLong && (it.segment & kAfter)) {  // what this thread left there joins O
+        const float m_before = part[0], top = fmaxf(mx, m_before);
+        const float f = mx == top ? 1.f : fast_exp2(mx - top);  // (without a maximum: zeros, or NaN to stay)
+        const float f_before = m_before == top ? 1.f : fast_exp2(m_before - top);
+        l = f * l + f_before * part[kBM];
+        mx = top;
+#pragma unroll 1
+        for (int c = 0; c < opaque(D / 32); ++c) {
+          uint32_t o[32];
+          tc::tmem_ld32(o_col + c * 32, o);
+          tc::tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            o[e] = __float_as_uint(f * __uint_as_float(o[e]) + f_before * part[(2 + 32 * c + e) * kBM]);
+          tc::tmem_st32(o_col + c * 32, o);
+        }
+        tc::tmem_wait_st();
+      }
+      const float inv = keep ? 1.f : sees > 0 ? 1.f / l : 0.f;
       const uint64_t inv2 = f2(inv, inv);
       uint64_t odd2 = 0ull;  // NaN once a result is not finite
-      float* part = parts + it.slot * slot_floats + r;
 #pragma unroll 1
       for (int c = 0; c < opaque(D / 32); ++c) {
         uint32_t o[32];
         tc::tmem_ld32(o_col + c * 32, o);
         tc::tmem_wait_ld();
-        if (split) {  // a partial result: fp32, rows side by side
+        if (keep) {  // a partial result: fp32, rows side by side
           float* at = part + (2 + 32 * c) * kBM;
 #pragma unroll
           for (int e = 0; e < 32; ++e) at[e * kBM] = __uint_as_float(o[e]);
@@ -879,10 +922,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       tc::fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->ofree);
-      if (split) {
+      if (keep) {
         part[0] = mx;
         part[kBM] = l;
-        if (it.chunk == 0 && quarter == 0 && lane == 0) {
+        if (split && !(kLong && (it.segment & kMore)) && it.chunk == 0 && quarter == 0 && lane == 0) {
           const unsigned n = atomicAdd(reinterpret_cast<unsigned*>(p.ws + kPartsOff), 1u);
           reinterpret_cast<PartItem*>(p.scratch)[n] = {it.b, it.h, it.row0, it.m, it.kv, it.rows, it.pos0, it.chunks, it.slot, it.slot_step};
         }
@@ -1207,11 +1250,14 @@ bool rows_map(CUtensorMap* m, const void* base, long long d0, long long d1, long
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+// Key tiles of the longest item, by the bounds that the host has.
+long long most_tiles(const RowsArgs& a) { return ((long long)(a.table ? a.max_kv : a.max_q) + kBN - 1) / kBN; }
+
+template <int D, bool kLong>
 cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   using C = TcCfg<D>;
   static PerDevice<int> allowed;
-  cudaError_t e = allow_smem(allowed, rows_tc_kernel<D>, (int)C::kSmem);
+  cudaError_t e = allow_smem(allowed, rows_tc_kernel<D, kLong>, (int)C::kSmem);
   if (e != cudaSuccess) return e;
   TcParams p;
   p.r = rows_params(a);
@@ -1243,7 +1289,7 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
     return cudaErrorNotSupported;
   int G = sm_count() < kMaxGrid ? sm_count() : kMaxGrid;
   // Few enough items that some may be cut, by what the host knows of them
-  const long long longest = ((long long)(a.table ? a.max_kv : a.max_q) + kBN - 1) / kBN;
+  const long long longest = most_tiles(a);
   p.may_split = 2 * most < 5ll * G && longest > kFewTiles;
   if (p.may_split && a.B == 1) {  // one sequence's items are known here, and so is a merge that would have nothing to do
     const int items = (a.max_q + p.tokens - 1) / p.tokens * a.Hkv, least = rounds_cost(items, G, (int)longest);
@@ -1253,7 +1299,7 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
       p.may_split |= split_cost(items * n, G, c) < least;
     }
   }
-  e = launch_pdl(rows_tc_kernel<D>, dim3((unsigned)G), dim3(kTcThreads), C::kSmem, st, mq, mk, mv, p);
+  e = launch_pdl(rows_tc_kernel<D, kLong>, dim3((unsigned)G), dim3(kTcThreads), C::kSmem, st, mq, mk, mv, p);
   if (e != cudaSuccess || !p.may_split) return e;
   return launch_pdl(rows_merge_kernel<D>, dim3((unsigned)(2 * G)), dim3(kMergeThreads), 0, st, p);
 }
@@ -1270,7 +1316,8 @@ size_t rows_workspace_bytes(int B, int H, int Hkv, int D, int T, int max_q, int 
 
 cudaError_t launch_rows_tc(const RowsArgs& a, cudaStream_t st) {
   if (a.dtype != 0 || a.H / a.Hkv > kBM) return cudaErrorNotSupported;
-  return a.D == 128 ? launch_typed<128>(a, st) : launch_typed<64>(a, st);
+  if (most_tiles(a) > kSegTiles) return a.D == 128 ? launch_typed<128, true>(a, st) : launch_typed<64, true>(a, st);
+  return a.D == 128 ? launch_typed<128, false>(a, st) : launch_typed<64, false>(a, st);
 }
 
 }  // namespace glide

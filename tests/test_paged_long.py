@@ -4,7 +4,7 @@ import torch
 
 from paper_2402_02082_gb300 import binding as gb
 from paper_2402_02082_gb300 import build
-from paged_util import i32, workspace
+from paged_util import check, host, i32, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,75 @@ def test_a_token_over_the_longest_context():
     gb.glide_paged_attn(q.cuda(), K.cuda(), V.cuda(), table, i32([0, 1]), 1, i32([kv]), kv, out, ws)
     assert ((out.cpu().double() - V[1, 0, last].double()).abs() < 1e-15).all()
     assert gb.glide_read_device_status(ws) == gb.GLIDE_OK
+
+
+def expected(q, K, V, table, kv, i, m):
+    """(want, tolerance) [H, D] of row i of m new tokens: a softmax over the pool's rows, each as often as it is seen.
+
+    A score is off by no more than in paged_util.tolerance.  Sums: a tensor core may lose 2^-25 of the sum so far at every key (it
+    takes in at most 2^17 keys: 2^-8 of the mean of |v|) and 2^-23 at every 16 (2^-10); sums beyond that are in fp32, in few
+    steps.  Each weight is rounded to bf16, 2^-8 of it, and the result."""
+    H, D = q.shape[1:]
+    H_kv, P = K.shape[1:3]
+    n = kv - m + 1 + i
+    times = torch.bincount(table[: n // P], minlength=len(K)).double()[:, None].expand(len(K), P).clone()
+    if n % P:
+        times[table[n // P], : n % P] += 1
+    K, V, q = (x.double().cuda() for x in (K, V, q))
+    K, V = (x.transpose(0, 1).reshape(H_kv, -1, D).repeat_interleave(H // H_kv, 0) for x in (K, V))
+    s = torch.einsum("hkd,hd->hk", K, q[i]) * D ** -0.5
+    top = (torch.einsum("hkd,hd->hk", K.abs(), q[i].abs()).amax(1) * D ** -0.5)[:, None]
+    w = torch.exp(s - s.amax(1, keepdim=True)) * times.reshape(1, -1).cuda()
+    w /= w.sum(1, keepdim=True)
+    want, mean = torch.einsum("hk,hkd->hd", w, V), torch.einsum("hk,hkd->hd", w, V.abs())
+    score = (D / 2 + 8) * top * 2.0 ** -23 + (top + 1) * 2.0 ** -22
+    tol = (2 * score + 2.0 ** -8 + 2.0 ** -10 + 2.0 ** -8) * mean + 2.0 ** -8 * want.abs() * (1 + 2.0 ** -7)
+    return host(want), host(tol)
+
+
+SMS = 152
+CASES = [
+    # new tokens, keys, H, H_kv, D: few rows, a warp's keys in two spans and three; rows of a group
+    (1, 2 ** 20 + 300, 2 * SMS + 2, 2 * SMS + 2, 64),
+    (2, 2 ** 21 + 2 ** 19, 4 * SMS, 2 * SMS, 128),
+    (5, 2 ** 21 + 777, 2 * SMS, SMS, 128),
+    (3, 2 ** 24 + 2 ** 22 + 5, 2, 1, 64),
+    # row tiles: an item in three segments, in eight; a call with its keys in chunks of more than one segment
+    (17, 2 ** 18 + 5000, 2 * SMS, 2 * SMS, 64),
+    (20, 2 ** 20, 2 * SMS, 2 * SMS, 128),
+    (17, 2 ** 20 + 130, 8, 8, 128),
+    (33, 2 ** 22 + 70, 2, 1, 64),
+    (200, 2 ** 19 + 2 ** 18, 3 * SMS, SMS, 64),
+    (40, 2 ** 19 + 1, SMS - 2, SMS - 2, 64),
+]
+
+
+@pytest.mark.parametrize("like", [True, False])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_sums_of_very_many_keys(case, like):
+    """Weights that are all alike, of values that are not 0 in the mean; and stretches of keys whose scores and values differ."""
+    m, kv, H, H_kv, D = CASES[case]
+    P, gen = 256, torch.Generator().manual_seed(case)
+    stretches, each = 5, 3
+    K = torch.zeros((stretches * each, H_kv, P, D)) if like else torch.randn((stretches * each, H_kv, P, D), generator=gen)
+    V = 1 + torch.rand((stretches * each, H_kv, P, D), generator=gen)
+    q = torch.randn((m, H, D), generator=gen)
+    width = -(-kv // P)
+    table = torch.randint(each, (width,), generator=gen) + torch.arange(width) * stretches // width * each
+    if not like:  # a maximum that rises and falls from stretch to stretch
+        q[..., 0] = 4.0
+        for x, shift in enumerate((0.0, 2.0, -3.0, 2.5, 1.0)):
+            K[x * each: (x + 1) * each, ..., 0] = shift * D ** 0.5 / 4
+            V[x * each: (x + 1) * each] += x
+    q, K, V = (x.bfloat16() for x in (q, K, V))
+    out = torch.zeros((m, H, D), dtype=torch.bfloat16, device="cuda")
+    ws = workspace(1, H, H_kv, D, "bf16", m, m)
+    gb.glide_paged_attn(q.cuda(), K.cuda(), V.cuda(), i32(table.numpy())[None], i32([0, m]), m, i32([kv]), kv, out, ws)
+    assert gb.glide_read_device_status(ws) == gb.GLIDE_OK
+    got = host(out)
+    for i in sorted({0, m // 2, m - 1}):
+        want, tol = expected(q, K, V, table, kv, i, m)
+        check(got[i], want, tol, f"row {i}")
+    again = torch.zeros_like(out)
+    gb.glide_paged_attn(q.cuda(), K.cuda(), V.cuda(), i32(table.numpy())[None], i32([0, m]), m, i32([kv]), kv, again, ws)
+    assert torch.equal(out, again)
