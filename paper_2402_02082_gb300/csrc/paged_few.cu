@@ -22,8 +22,9 @@
 // what lies 2^-25 below O with every product, so a warp's O takes in 2^17 keys and then joins fp32 sums in shared memory (the
 // mean of 2^24 keys of like weight, a CTA a slab, relative error: -5e-3 without, -1e-4 with it).
 //
-// A result that is not finite (an infinity or NaN that the row sees, or one that it does not see, in a tile
-// that it shares) is computed again by the definition, the row alone.
+// A result that is not finite (an infinity or NaN among the values that the row sees, or one that it does not see, in a tile that it
+// shares; or an overflow) is computed again by the definition, the row alone, unless its sum of weights is 0 or NaN, which makes
+// it NaN.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -67,7 +68,7 @@ struct FewSmem {
   float2 peer_ml[kMaxC * kR];             // from the cluster's CTAs
   float2 peer_o[kR * D / 2 + kMaxC];      // this CTA's pairs of columns, from each
   uint2 qf[NT * (D / 16) * 32];           // the queries' fragments
-  int odd[kR];                            // the row has a result that is not finite
+  int odd[kR];                            // the row has to be computed again
   int slab_b;
 };
 
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) paged_few_kernel
       const float inv = 1.f / l_all;
       sum.x *= inv;
       sum.y *= inv;
-      if (!isfinite(sum.x) || !isfinite(sum.y)) sm.odd[r] = 1;
+      if (l_all > 0.f && !(isfinite(sum.x) && isfinite(sum.y))) sm.odd[r] = 1;
     }
     *reinterpret_cast<uint32_t*>(out_at(r) + d) = pack_bf16x2(sum.x, sum.y);
   }

@@ -155,9 +155,14 @@ __device__ __forceinline__ void attend_keys(const RowsParams& p, int b, const Se
 }
 
 // The whole row by one warp and the definition: o[e], column lane * (D / 32) + e of the result over the first n > 0 keys.  Called
-// where the plain sums are not finite.  (Inlined: a kernel that splits its registers among its warps holds no call.)
-template <typename T, int D>
-__device__ __forceinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, unsigned n, float (&o)[D / 32]) {
+// where the plain sums are not finite.  step(): once for every 32 keys.  (Inlined: a kernel that splits its registers among its
+// warps holds no call.)
+struct NoStep {
+  __device__ __forceinline__ void operator()() const {}
+};
+template <typename T, int D, class Step = NoStep>
+__device__ __forceinline__ void attend_row(const RowsParams& p, int b, const Seq& s, int i, int h, unsigned n, float (&o)[D / 32],
+                                           Step step = {}) {
   constexpr int kE = D / 32, kRow = D * (int)sizeof(T), kAtOnce = 4;
   const int lane = threadIdx.x & 31, hk = h / p.group;
   const unsigned char* q = p.q + (long long)(s.row0 + i) * p.q_stride + (size_t)h * kRow;
@@ -166,6 +171,7 @@ __device__ __forceinline__ void attend_row(const RowsParams& p, int b, const Seq
   for (int e = 0; e < kE; ++e) o[e] = bad[e] = 0.f;  // o: half of the mean so far, so that its terms' rounding stays in range too
 #pragma unroll 1
   for (unsigned t0 = 0; t0 < n; t0 += 32) {
+    step();
     float u = -CUDART_INF_F;
     size_t v_at = 0;
     if (t0 + lane < n) u = key_score<T, D, kAtOnce>(p, b, s, hk, q, t0 + lane, v_at);

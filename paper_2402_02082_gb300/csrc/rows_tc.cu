@@ -46,8 +46,9 @@
 //   warp 9       S issue, warp 10 P V issue (lane 0).
 //   warps 12-15  results: a TMEM lane quarter each, O / l through 4 KB of shared memory in whole rows.
 //
-// A result that is not finite (an infinity or NaN that the row sees, or one that it does not see, in a tile
-// that it shares) is computed again by the definition, the row alone.
+// A result that is not finite (an infinity or NaN among the values that the row sees, or one that it does not see, in a tile that it
+// shares; or an overflow) is computed again by the definition, the row alone, unless its sum of weights is 0 or NaN, which makes
+// it NaN.  The other warps' waits are put off meanwhile.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -55,6 +56,7 @@
 #include "device.h"
 #include "kernels.h"
 #include "rows_attn.cuh"
+#include "rows_wait.cuh"
 #include "tc_attn.cuh"
 #include "tc_ptx.cuh"
 #include "tensor_map.h"
@@ -131,8 +133,8 @@ struct TcItem {
 };
 
 struct Misc {
+  Watch watch;
   uint32_t tmem;
-  int abort;
   int head_group;      // cached heads that are worked on together
   int chunk_tiles;     // key tiles of a chunk
   int entries;         // (sequence, row tiles, chunk) triples
@@ -224,9 +226,9 @@ __device__ __forceinline__ void tc_regs_down() {
 // The items as every other warp reads them: a slot is the warp's until it lets go.
 struct ItemReader {
   unsigned n = 0;
-  __device__ __forceinline__ const TcItem* next(Bars* bars, const TcItem* items, volatile int* abort) {
+  __device__ __forceinline__ const TcItem* next(Bars* bars, const TcItem* items, Watch* watch) {
     const unsigned slot = n % kItemSlots;
-    if (!warp_wait_small(&bars->itemfull[slot], (n / kItemSlots) & 1, abort)) return nullptr;
+    if (!warp_wait_watched(&bars->itemfull[slot], (n / kItemSlots) & 1, watch)) return nullptr;
     return items[slot].b >= 0 ? items + slot : nullptr;
   }
   __device__ __forceinline__ void release(Bars* bars, int lane) {
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   int* order = reinterpret_cast<int*>(base + C::off_order);
   uint32_t* list = reinterpret_cast<uint32_t*>(base + C::off_list);
   int* row_at = reinterpret_cast<int*>(base + C::off_rowat);
-  volatile int* abort_flag = &misc->abort;
+  Watch* watch = &misc->watch;
   unsigned* status = reinterpret_cast<unsigned*>(p.ws);
   unsigned* claim = reinterpret_cast<unsigned*>(p.ws + WsLayout::kClaimOff);
   unsigned* finished = reinterpret_cast<unsigned*>(p.ws + WsLayout::kDoneOff);
@@ -317,7 +319,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     init(bars->drained, 2, 1);
     if (warp == 15) {
       if (lane == 0) {
-        misc->abort = 0;
+        misc->watch.abort = 0;
         misc->levels = 0;
         misc->listed = 0;
         misc->longest = 0;
@@ -495,6 +497,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (threadIdx.x == 0) misc->listed = 1;
     }
   }
+  if (threadIdx.x == 0) put_off(watch);  // (the kernel before, which pdl_wait waits for, may have taken any time)
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
@@ -625,9 +628,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             }
           }
           const unsigned slot = made % kItemSlots;
-          ok = warp_wait_small(&bars->itemempty[slot], ((made / kItemSlots) & 1) ^ 1, abort_flag);
+          ok = warp_wait_watched(&bars->itemempty[slot], ((made / kItemSlots) & 1) ^ 1, watch);
           if (!ok) break;
           if (lane == 0) {
+            put_off(watch);
             items[slot] = it;
             mbar_arrive(&bars->itemfull[slot]);
           }
@@ -650,7 +654,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             continue;
           }
           const unsigned qb = q_issued & 1;
-          ok = warp_wait_small(&bars->qempty[qb], ((q_issued >> 1) & 1) ^ 1, abort_flag);
+          ok = warp_wait_watched(&bars->qempty[qb], ((q_issued >> 1) & 1) ^ 1, watch);
           if (!ok) break;
           if (lane == 0) mbar_arrive_expect_tx(&bars->qfull[qb], (uint32_t)(C::kHalves * p.tokens * rp.group * 128));
           __syncwarp();
@@ -664,7 +668,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const int2 x = box.any(left) ? box.where(rp, b, h, row0, t) : make_int2(0, 0);
         if (k_issued >= C::kNS) {  // S of the tile that had the stage
           const unsigned j = k_issued - C::kNS;
-          ok = warp_wait_small(&bars->sfull[j % kSBufs], (j / kSBufs) & 1, abort_flag);
+          ok = warp_wait_watched(&bars->sfull[j % kSBufs], (j / kSBufs) & 1, watch);
           if (!ok) break;
         }
         if (lane == 0) mbar_arrive_expect_tx(&bars->kfull[st], box.bytes(left, !rp.table, 2 * D));
@@ -694,7 +698,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       bool ok = true;
       ItemReader reader;
       while (ok) {
-        const TcItem* at = reader.next(bars, items, abort_flag);
+        const TcItem* at = reader.next(bars, items, watch);
         if (!at) break;
         const int b = at->b, h = at->h, row0 = at->row0, klen = at->klen, t0 = at->t0, te = at->te;
         reader.release(bars, lane);
@@ -704,7 +708,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           const int2 x = box.any(left) ? box.where(rp, b, h, row0, t) : make_int2(0, 0);
           if (v_issued >= C::kNS) {  // P V of the tile that had the stage
             const unsigned j = v_issued - C::kNS;
-            ok = warp_wait_small(&bars->bfree[j % kSBufs], (j / kSBufs) & 1, abort_flag);
+            ok = warp_wait_watched(&bars->bfree[j % kSBufs], (j / kSBufs) & 1, watch);
             if (!ok) break;
           }
           const unsigned bi = v_issued % kSBufs;
@@ -717,7 +721,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           __syncwarp();
           ++v_issued;
           if (left < kBN) {  // the item's last V tile: clear its rows past the last visible key
-            ok = warp_wait_small(&bars->vfull, n_clear & 1, abort_flag);
+            ok = warp_wait_watched(&bars->vfull, n_clear & 1, watch);
             if (!ok) break;
             ++n_clear;
 #pragma unroll 1
@@ -750,7 +754,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       bool ok = true;
       ItemReader reader;
       while (ok) {
-        const TcItem* at = reader.next(bars, items, abort_flag);
+        const TcItem* at = reader.next(bars, items, watch);
         if (!at) break;
         const int nt = at->te - at->t0;
         reader.release(bars, lane);
@@ -759,11 +763,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           if (scores) {
             // S(i) = Q K(i)^T into buffer i % 3, once P V of tile i - 3 has read that buffer
             const uint64_t dQ = dQ0 + (n_items & 1) * desc_step(C::kTile);
-            ok = mbar_wait_small(&bars->qfull[n_items & 1], (n_items >> 1) & 1, abort_flag);
+            ok = wait_watched(&bars->qfull[n_items & 1], (n_items >> 1) & 1, watch);
 #pragma unroll 1
             for (int t = nt; ok && t > 0; --t) {
-              ok = mbar_wait_small(&bars->kfull[st], phase, abort_flag) &&
-                   mbar_wait_small(&bars->bfree[bi], b_phase ^ 1, abort_flag);
+              ok = wait_watched(&bars->kfull[st], phase, watch) &&
+                   wait_watched(&bars->bfree[bi], b_phase ^ 1, watch);
               if (!ok) break;
               tc::fence_after_sync();
               const uint64_t dK = dK0 + st * desc_step(C::kTile);
@@ -786,11 +790,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             }
           } else {
             // O (+)= P(i) V(i), P in the first 64 columns of buffer i % 3
-            if (n_items > 0) ok = mbar_wait_small(&bars->ofree, (n_items - 1) & 1, abort_flag);
+            if (n_items > 0) ok = wait_watched(&bars->ofree, (n_items - 1) & 1, watch);
             uint32_t acc = 0;
 #pragma unroll 1
             for (int t = nt; ok && t > 0; --t) {
-              ok = mbar_wait_small(&bars->pvfull[bi], b_phase, abort_flag);
+              ok = wait_watched(&bars->pvfull[bi], b_phase, watch);
               if (!ok) break;
               tc::fence_after_sync();
               const uint64_t dV = dV0 + st * desc_step(C::kTile);
@@ -836,7 +840,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     ItemReader reader;
     bool ok = true;
     while (ok) {
-      const TcItem* item = reader.next(bars, items, abort_flag);
+      const TcItem* item = reader.next(bars, items, watch);
       if (!item) break;
       const TcItem& it = *item;  // let go at the item's end
       const Seq s = {it.row0, it.rows, it.m, it.kv};
@@ -859,12 +863,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         reader.release(bars, lane);
         continue;
       }
-      ok = warp_wait_small(&bars->lready, n_items & 1, abort_flag);
+      ok = warp_wait_watched(&bars->lready, n_items & 1, watch);
       if (!ok) break;
+      if (lane == 0) put_off(watch);
       float l = l_row[r] + l_row[kBM + r], mx = m_row[r];
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->lfree);
-      ok = warp_wait_small(&bars->olast, n_items & 1, abort_flag);
+      ok = warp_wait_watched(&bars->olast, n_items & 1, watch);
       if (!ok) break;
       ++n_items;
       tc::fence_after_sync();
@@ -940,7 +945,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
         float lo, hi;
         unf2(odd2, lo, hi);
-        again = __ballot_sync(0xffffffffu, sees > 0 && !(lo == 0.f && hi == 0.f));
+        again = __ballot_sync(0xffffffffu, sees > 0 && l > 0.f && !(lo == 0.f && hi == 0.f));
         tc::fence_async_smem();  // the next queries come by the asynchronous proxy
       }
       __syncwarp();
@@ -953,7 +958,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const int xr = quarter * 32 + x, xt = xr / rp.group, xp = it.pos0 + xt;
         const int head = it.h * rp.group + (xr - xt * rp.group);
         float y[D / 32];
-        attend_row<__nv_bfloat16, D>(rp, it.b, s, xp, head, seen(s, xp), y);
+        attend_row<__nv_bfloat16, D>(rp, it.b, s, xp, head, seen(s, xp), y, [&] {
+          if (lane == 0) put_off(watch);
+        });
         store_row<D / 32>(out + ((size_t)(it.row0 + xp) * rp.H + head) * D + lane * (D / 32), y);
       }
       reader.release(bars, lane);
@@ -971,7 +978,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     ItemReader reader;
     bool ok = true;
     while (ok) {
-      const TcItem* at = reader.next(bars, items, abort_flag);
+      const TcItem* at = reader.next(bars, items, watch);
       if (!at) break;
       const Seq s = {at->row0, at->rows, at->m, at->kv};
       const int pos = at->pos0 + token;
@@ -985,7 +992,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       for (int t = (int)((i ^ grp) & 1u); t < nt; t += 2) {
         const unsigned ti = i + t, bi = ti % kSBufs;
         const uint32_t s_col = lane_base + bi * kBN;
-        ok = warp_wait_small(&bars->sfull[bi], (ti / kSBufs) & 1, abort_flag);
+        ok = warp_wait_watched(&bars->sfull[bi], (ti / kSBufs) & 1, watch);
         if (!ok) break;
         tc::fence_after_sync();
         // keys that this row does not see: -inf (a suffix of the tile), written back in the 32-key chunks that have one
@@ -1023,7 +1030,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         // the next).
         float m_prev = -CUDART_INF_F;
         if (t > 0) {
-          ok = warp_wait_small(&bars->turn[quarter][(ti - 1) & 1], ((ti - 1) >> 1) & 1, abort_flag);
+          ok = warp_wait_watched(&bars->turn[quarter][(ti - 1) & 1], ((ti - 1) >> 1) & 1, watch);
           if (!ok) break;
           m_prev = m_ref[r];
         }
@@ -1035,7 +1042,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (__any_sync(0xffffffffu, need) && t > 0) {
           // O holds P V of this item's earlier tiles, the other group's last one included: rescale it
           const unsigned before = ti - 1;
-          ok = warp_wait_small(&bars->bfree[before % kSBufs], (before / kSBufs) & 1, abort_flag);
+          ok = warp_wait_watched(&bars->bfree[before % kSBufs], (before / kSBufs) & 1, watch);
           if (!ok) break;
           const float f = need ? fast_exp2(m_prev - m_used) : 1.f;
           tc::fence_after_sync();
@@ -1085,14 +1092,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (!ok) break;
       i += nt;
       if (((i ^ grp) & 1u) == 0) {  // the other group had the last tile: take this sum to its reference
-        ok = warp_wait_small(&bars->turn[quarter][(i - 1) & 1], ((i - 1) >> 1) & 1, abort_flag);
+        ok = warp_wait_watched(&bars->turn[quarter][(i - 1) & 1], ((i - 1) >> 1) & 1, watch);
         if (!ok) break;
         const float m_last = m_ref[r];
         if (m != m_last) l *= fast_exp2(m - m_last);
         m = m_last;
       }
       // to the result warps, once they have read the item before
-      ok = warp_wait_small(&bars->lfree, (n_items & 1) ^ 1, abort_flag);
+      ok = warp_wait_watched(&bars->lfree, (n_items & 1) ^ 1, watch);
       if (!ok) break;
       l_row[grp * kBM + r] = l;
       if (((i ^ grp) & 1u) != 0) m_row[r] = m;
@@ -1106,7 +1113,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   tc::fence_before_sync();
   __syncthreads();
   if (threadIdx.x == 0) {
-    record_abort(abort_flag, status);
+    record_abort(&watch->abort, status);
     if (atomicAdd(finished, 1u) == gridDim.x - 1) {  // the counters back to zero for the next call
       *claim = 0u;
       *finished = 0u;
@@ -1181,7 +1188,7 @@ __device__ __forceinline__ void merge_parts(const TcParams& p, int n) {
 #pragma unroll
     for (int e = 0; e < kCols; ++e) {
       v[e] = sees > 0 ? v[e] / l : 0.f;
-      odd |= !isfinite(v[e]);
+      odd |= !isfinite(v[e]) && l > 0.f;
     }
     __nv_bfloat16* to = out + ((size_t)(it.row0 + pos) * rp.H + head) * D + col;
     if (valid)
