@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             it.segment = kAfter;
           } else {
             const unsigned c = first ? blockIdx.x : gridDim.x + __shfl_sync(0xffffffffu, next, 0);
-            if (lane == 0 && !first) next = atomicAdd(claim, 1u);  // needed for the item after this one
+            if (lane == 0 && !first && c < claims) next = atomicAdd(claim, 1u);  // needed for the item after this one
             first = false;
             it.b = -1;
             if (c < claims) {
@@ -681,6 +681,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (++t == te) {
           started = false;
           ++cur;
+        }
+      }
+      // The CTA has made its last claim, and the fence waits for it (of a CTA without an item nothing has looked at the result): the
+      // last CTA sets the counters back to zero for the next call.  Here, under the last item's work; at the end of the kernel
+      // the fences cost 0.9 us.
+      if (lane == 0) {
+        __threadfence();
+        if (atomicAdd(finished, 1u) == gridDim.x - 1) {
+          __threadfence();
+          *claim = 0u;
+          *finished = 0u;
         }
       }
       if (!ok) {  // aborted: let issued loads land before the CTA exits
@@ -1112,13 +1123,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   __syncwarp();
   tc::fence_before_sync();
   __syncthreads();
-  if (threadIdx.x == 0) {
-    record_abort(&watch->abort, status);
-    if (atomicAdd(finished, 1u) == gridDim.x - 1) {  // the counters back to zero for the next call
-      *claim = 0u;
-      *finished = 0u;
-    }
-  }
+  if (threadIdx.x == 0) record_abort(&watch->abort, status);
   if (warp == kKWarp) {
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem, kTmemCols);
