@@ -65,7 +65,9 @@
  *   use.  It holds a status word, arrival counters (and, for tree_accept,
  *   argmax slots) that must start at zero, and scratch for split partial
  *   results.  Every successful call returns the words that must start at zero
- *   to zero, so one buffer can be reused across calls on the same stream.
+ *   to zero, and no call leaves anything else where another call has such words,
+ *   so one buffer, of the largest of their sizes, serves calls of any kind and
+ *   shape on the same stream.
  *   Calls that run concurrently on different streams need separate
  *   workspaces.
  * - Kernel waits are bounded.  A kernel that gives up waiting records
@@ -314,11 +316,11 @@ glide_status glide_block_cross_attn(const glide_attn_desc* desc, const void* q, 
  * host engine owns and budgets all device memory, or a serving loop that has
  * given nearly all of HBM to its KV cache and bans allocator calls on its
  * per-token path.  Same arguments and result as glide_cross_attn, minus the
- * workspace: the scratch lives in one fixed 32 MiB array inside the library,
+ * workspace: the scratch lives in one fixed array of 32 MiB + 64 KiB inside the library,
  * held on every GPU that loads the library until the process exits.
  * - Shapes whose workspace (glide_attn_workspace_bytes(desc, 1)) exceeds
- *   32 MiB are rejected with GLIDE_ERR_UNSUPPORTED (B*H up to 7035 for D = 128,
- *   14835 for D = 64).
+ *   that are rejected with GLIDE_ERR_UNSUPPORTED (served: B*H up to 7028 for
+ *   D = 128, 14807 for D = 64).
  * - Every call looks up the array's device address in the current device's
  *   context (so a context created again after cudaDeviceReset is served
  *   correctly); the first call on a device also loads the library's device

@@ -440,6 +440,8 @@ cudaError_t launch_tree_accept(const AcceptArgs& a, cudaStream_t st) {
   p.status = reinterpret_cast<unsigned*>(ws);
   p.counters = reinterpret_cast<unsigned*>(ws + 256);
   p.slots = reinterpret_cast<unsigned long long*>(ws + 256 + counters_bytes(a.B));
+  const cudaError_t cleared = clear_beyond(ws, accept_workspace_bytes(a.B, a.n), st);
+  if (cleared != cudaSuccess) return cleared;
   p.B = a.B; p.n = a.n; p.V = a.V;
   p.splits = (a.V + kChunk - 1) / kChunk;
   const long long nchunks = (long long)a.B * a.n * p.splits;

@@ -320,17 +320,15 @@ __global__ void __launch_bounds__(kThreads) cape_expand_kernel(const CapeParams 
   if (threadIdx.x == 0) p.seq_counters[b] = 0u;
 }
 
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
-
 int cape_splits(int V) { return (V + kChunk - 1) / kChunk; }
 
 }  // namespace
 
-// Workspace: [0,256) status | sequence counters [B] | chunk slots
-// [B*gamma, splits, 8] u64.
+// Workspace: [0,256) status | sequence counters [B] | behind the bytes that are
+// zero between calls, chunk slots [B*gamma, splits, 8] u64.
 size_t cape_workspace_bytes(int B, int gamma, int V) {
   const size_t rows = (size_t)B * gamma;
-  return 256 + align256((size_t)B * sizeof(unsigned)) + rows * (size_t)cape_splits(V) * kTop * sizeof(u64);
+  return WsLayout::scratch_off(256 + (size_t)B * sizeof(unsigned)) + rows * (size_t)cape_splits(V) * kTop * sizeof(u64);
 }
 
 cudaError_t launch_cape_expand(const CapeArgs& a, cudaStream_t st) {
@@ -341,12 +339,13 @@ cudaError_t launch_cape_expand(const CapeArgs& a, cudaStream_t st) {
   p.splits = cape_splits(a.V);
   const size_t rows = (size_t)a.B * a.gamma;
   unsigned char* ws = static_cast<unsigned char*>(a.ws);
-  size_t off = 256;
-  p.seq_counters = reinterpret_cast<unsigned*>(ws + off);
-  off += align256((size_t)a.B * sizeof(unsigned));
-  p.slots = reinterpret_cast<u64*>(ws + off);
+  const size_t end = 256 + (size_t)a.B * sizeof(unsigned);
+  p.seq_counters = reinterpret_cast<unsigned*>(ws + 256);
+  p.slots = reinterpret_cast<u64*>(ws + WsLayout::scratch_off(end));
   const long long grid = (long long)rows * p.splits;
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+  const cudaError_t e = clear_beyond(ws, end, st);
+  if (e != cudaSuccess) return e;
   return launch_pdl(cape_expand_kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, p);
 }
 

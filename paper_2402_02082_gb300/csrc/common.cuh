@@ -16,24 +16,40 @@ constexpr uint64_t kWaitLimitNs = 1000000000ull; // 1 s: far beyond any legitima
 constexpr float kLog2e = 1.4426950408889634f;
 
 // ---------------------------------------------------------------- workspace
-// Attention workspace: [0,256) header (the status word at byte 0; the
-// cross-attention chunk-claim counter at byte 128 and its CTA-done counter at
-// byte 192); then per-(b,h) arrival counters (4 bytes each, tree kernels);
-// then per-(b,h) chunk ranges (8 bytes each, cross-attention scratch); then
+// Every workspace begins with the same kZeros bytes, in which all words lie that
+// have to be zero when a call begins, and nothing else: no call leaves scratch
+// there, so calls of any kind and shape may share a workspace.  [0,256) header:
+// the status word at byte 0; at bytes 64 and 96 the items in chunks and the
+// finished CTAs of the merge of packed rows; at bytes 128 and 192 the claim
+// counter and the CTA-done counter of cross-attention and of packed rows.  Then
+// the words that depend on the call: arrival counters (tree kernels on the CUDA
+// cores, 4 bytes a row tile of a (b,h)), the counters and argmax slots of the
+// acceptance, the counters of the expansion.  Where a call's words reach beyond
+// kZeros it clears that part itself (clear_beyond).
+// Scratch of the attention calls: per-(b,h) chunk ranges (8 bytes each), then
 // 256-aligned partial slots of nq*(D+2) floats.
 struct WsLayout {
   static constexpr size_t kHeader = 256;
   static constexpr size_t kClaimOff = 128;
   static constexpr size_t kDoneOff = 192;
+  static constexpr size_t kZeros = 64 << 10;
   static __host__ __device__ size_t align(size_t x) { return (x + 255) & ~size_t(255); }
   static __host__ __device__ size_t counters_off() { return kHeader; }
+  // behind words that end at `end`
+  static __host__ __device__ size_t scratch_off(size_t end) { return align(end > kZeros ? end : kZeros); }
   static __host__ __device__ size_t ranges_off(int B, int H) {
-    return align(kHeader + sizeof(unsigned) * (size_t)B * H);
+    return scratch_off(kHeader + sizeof(unsigned) * (size_t)B * H);
   }
   static __host__ __device__ size_t partials_off(int B, int H) {
     return align(ranges_off(B, H) + 2 * sizeof(int) * (size_t)B * H);
   }
 };
+
+// Zeroes what a call's words, which end at byte `end`, take beyond kZeros.
+inline cudaError_t clear_beyond(void* ws, size_t end, cudaStream_t st) {
+  if (end <= WsLayout::kZeros) return cudaSuccess;
+  return cudaMemsetAsync(static_cast<unsigned char*>(ws) + WsLayout::kZeros, 0, end - WsLayout::kZeros, st);
+}
 
 // -------------------------------------------------------------------- misc
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {

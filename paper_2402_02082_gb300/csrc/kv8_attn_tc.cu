@@ -1280,8 +1280,8 @@ cudaError_t launch_np(const Kv8AttnArgs& a, int R, int per_tile, cudaStream_t st
   p.out = static_cast<__nv_bfloat16*>(a.out);
   unsigned char* ws = static_cast<unsigned char*>(a.ws);
   p.status = reinterpret_cast<unsigned*>(ws);
-  p.ranges = reinterpret_cast<int2*>(ws + WsLayout::kHeader);
-  p.partials = reinterpret_cast<float*>(ws + WsLayout::align(WsLayout::kHeader + 8 * (size_t)a.B * a.Hkv));
+  p.ranges = reinterpret_cast<int2*>(ws + WsLayout::kZeros);
+  p.partials = reinterpret_cast<float*>(ws + WsLayout::align(WsLayout::kZeros + 8 * (size_t)a.B * a.Hkv));
   p.B = a.B; p.H = a.H; p.Hkv = a.Hkv; p.S_cap = a.S_cap; p.max_kv_len = a.max_kv_len; p.n = a.nq;
   p.group = a.H / a.Hkv; p.rows = a.nq * p.group; p.R = R; p.per_tile = per_tile; p.tree = tree; p.ns = ns;
   p.blocks = kv8_blocks(a.S_cap);
@@ -1308,7 +1308,7 @@ cudaError_t launch_d(const Kv8AttnArgs& a, cudaStream_t st) {
 }  // namespace
 
 size_t kv8_workspace_bytes(int B, int Hkv, int D, int rows) {
-  return WsLayout::align(WsLayout::kHeader + 8 * (size_t)B * Hkv) +
+  return WsLayout::align(WsLayout::kZeros + 8 * (size_t)B * Hkv) +
          ((size_t)kMaxShares + (size_t)B * Hkv) * rows * (D + 2) * sizeof(float);
 }
 

@@ -22,7 +22,7 @@
 
 namespace {
 
-constexpr size_t kScratchBytes = 32u << 20;  // 32 MiB per GPU
+constexpr size_t kScratchBytes = (32u << 20) + glide::WsLayout::kZeros;  // per GPU
 
 // The scratch itself.  In host code this name is only a host-side stand-in
 // for the symbol, never a device address: host code obtains the real address
@@ -56,14 +56,16 @@ extern "C" glide_status glide_cross_attn_noalloc(const glide_attn_desc* desc, co
   if (need > kScratchBytes) return GLIDE_ERR_UNSUPPORTED;
   void* scratch = nullptr;
   if (scratch_address(&scratch) != cudaSuccess) return GLIDE_ERR_CUDA;
-  // The array keeps whatever the previous call left.  The counters after the
-  // status word must start at zero; the status word itself (bytes 0..3) is
+  // The array keeps whatever the previous call left.  The words after the
+  // status word that must start at zero are cleared, as they are not after a
+  // wait that ran out; the status word itself (bytes 0..3) is
   // left alone, so a wait that ran out in an earlier call stays reported
   // until glide_noalloc_read_device_status reads and clears it.
   // (cudaMemsetAsync does not allocate.)
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const size_t first = glide::WsLayout::kClaimOff;
-  const size_t zeroed = glide::WsLayout::partials_off(desc->B, desc->H) - first;
+  const size_t counted = glide::WsLayout::counters_off() + 4 * (size_t)desc->B * desc->H;
+  const size_t zeroed = (counted < glide::WsLayout::kZeros ? counted : glide::WsLayout::kZeros) - first;
   if (cudaMemsetAsync(static_cast<unsigned char*>(scratch) + first, 0, zeroed, st) != cudaSuccess)
     return GLIDE_ERR_CUDA;
   return glide_cross_attn(desc, q_draft, K_cache, V_cache, kv_len, max_kv_len, out, scratch, kScratchBytes,

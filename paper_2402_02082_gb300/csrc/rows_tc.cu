@@ -89,15 +89,12 @@ constexpr int kSegTiles = 1024;        // key tiles that one O takes in (2^17 ke
 constexpr int kLateTenths = 4;         // items with at most this part of the longest one's key tiles are left to the end
 
 // Workspace: in the header the status word, the claim counter, the count of finished CTAs, and for the merge the count of
-// items in chunks and that of its finished CTAs.  Then, behind what the other calls' counters may take (they start at zero,
-// so nothing is left there), those items and partial slots of [D + 2][128 rows] floats: a row's maximum, its sum, its columns.
+// items in chunks and that of its finished CTAs.  Behind the bytes that are zero between calls, those items and partial slots of [D + 2][128 rows] floats: a row's maximum, its sum, its columns.
 struct PartItem {
   int b, h, row0, m, kv, rows, pos0, chunks, slot, slot_step;
 };
 constexpr size_t kPartsOff = 64, kMergedOff = 96;
 constexpr size_t kPartItemsBytes = (2 * kMaxGrid * sizeof(PartItem) + 255) / 256 * 256;
-// of a counter for each head (up to 1024) of the most sequences of a call
-size_t scratch_off(int H) { return WsLayout::align(WsLayout::kHeader + 4 * (size_t)kMaxBatch * (H < 1024 ? H : 1024)); }
 constexpr int kSplitCount = 11;  // chunks of the longest item that are tried: 2 .. 6, 8, 10, 12, 16, 20, 24
 constexpr int kMergeTiles = 7;
 constexpr int kAlone = 4;  // row tiles of a sequence that one lane counts
@@ -1274,7 +1271,7 @@ cudaError_t launch_typed(const RowsArgs& a, cudaStream_t st) {
   TcParams p;
   p.r = rows_params(a);
   p.ws = static_cast<unsigned char*>(a.ws);
-  p.scratch = p.ws + scratch_off(a.H);
+  p.scratch = p.ws + WsLayout::kZeros;
   const int group = p.r.group;
   p.tokens = kBM / group;
   p.by_tokens = reciprocal(p.tokens);
@@ -1323,7 +1320,7 @@ size_t rows_workspace_bytes(int B, int H, int Hkv, int D, int T, int max_q, int 
   (void)T;
   (void)max_q;
   if (dtype != 0 || H / Hkv > kBM) return WsLayout::kHeader;
-  return scratch_off(H) + kPartItemsBytes + (size_t)kMaxChunks * kBM * (D + 2) * sizeof(float);
+  return WsLayout::kZeros + kPartItemsBytes + (size_t)kMaxChunks * kBM * (D + 2) * sizeof(float);
 }
 
 cudaError_t launch_rows_tc(const RowsArgs& a, cudaStream_t st) {

@@ -282,6 +282,8 @@ cudaError_t launch_typed(const AttnArgs& a, cudaStream_t st) {
   p.B = a.B; p.H = a.H; p.S_cap = a.S_cap; p.max_kv_len = a.max_kv_len; p.n = a.nq;
   p.Hkv = a.Hkv; p.group = a.H / a.Hkv; p.rows = rows; p.R = R; p.tree = a.tree;
   p.scale_log2 = a.scale * kLog2e;
+  e = clear_beyond(ws, WsLayout::counters_off() + sizeof(unsigned) * (size_t)a.B * a.Hkv * R, st);
+  if (e != cudaSuccess) return e;
   return launch_pdl(tree_attn_fma_kernel<T, D>, dim3((unsigned)(G * R)), dim3(kThreads), C::smem_bytes(a.B), st, p);
 }
 
