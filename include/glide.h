@@ -482,7 +482,8 @@ glide_status glide_kv8_verify_attn(const glide_attn_desc* desc, const void* q_tr
  *     q, k, v       [T, heads, D] with `stride` elements from token to token (a multiple of 16
  *                   bytes, at least heads * D): parts of a fused projection's rows, as they are
  * Entries of tables, offsets and lengths that lie outside their ranges are taken as the nearest
- * inside, as everywhere in this header.
+ * inside, as everywhere in this header; a plan, which does not know the pool, gives the slot -1 where a
+ * page number is below 0 or its slot beyond 2^31 - 1.
  */
 typedef struct {
   void* K;            /* [n_pages, H_kv, page_size, D], 16-byte aligned */
@@ -545,10 +546,12 @@ size_t glide_paged_workspace_bytes(const glide_attn_desc* desc, int32_t T, int32
  * element included: GLIDE_ERR_INVALID.
  * max_q, max_kv_len: bounds of m and kv_len on the host; 1 <= max_q, 0 <= max_kv_len <=
  * table_width * page_size.  desc: B, H, H_kv, D, dtype, scale, flags (GLIDE_FLAG_FORCE_FMA takes the CUDA-core
- * kernel); S_cap and max_ctas are ignored.
+ * kernel); S_cap and max_ctas are ignored.  fp32, more than 128 query heads a cached one, a max_kv_len above
+ * 2^31 - 129, and strides that a TMA descriptor cannot hold run on the CUDA cores too, a block a row: right,
+ * but slow for many rows.
  * What is not finite has the definition's result: what a row does not see never reaches it, whatever it
  * holds; a score that is NaN or +inf makes its row NaN, one of -inf has no weight, and a value that is not finite
- * decides its column in the rows that see it.  bf16: weights may be rounded to bf16 for the product with the values.
+ * decides its column in the rows that see it.  A row with such values is computed by itself, so many are slow.  bf16: weights may be rounded to bf16 for the product with the values.
  * Scores are formed in fp32: one whose products pass fp32's range counts as infinite.  A weight below 2^-126 of the row's
  * largest counts as 0 for finite values.
  */

@@ -7,9 +7,11 @@
 // loads two tiles ahead; a tile's 8 KB go to registers, the next keys while the warp works on this tile's values.  No
 // ring, no barrier until the end; the warps' partial results meet in shared memory, the CTAs' in distributed shared memory, in
 // a fixed order.  Clusters start with the longest requests, so that the SMs end together.
-// Measured (D = 128, us): 32 requests of 1024 to 16384 keys, 32 heads over 8 cached, 152 (6.8 TB/s, as a copy); six new tokens
-// of four requests of 16384, 52 heads, 263; one request of 2048, 32 heads, 10.2 (33.6 MB, 5 at that rate: the launch, the
-// lengths and page numbers, the first loads and the merge, one after another).
+// Measured (D = 128, us): 32 requests of 1024 to 16384 keys, 32 heads over 8 cached, 148 to 151 (6.8 TB/s and more, as a copy); six
+// new tokens of four requests of 16384, 52 heads, 259 to 268; one request of 2048, 32 heads, 9.9 (33.6 MB, 5 at that rate: the
+// launch, the lengths and page numbers, the first loads and the merge, one after another).  9 to 16 rows (one CTA an SM): four new
+// tokens of eight requests of 8192, 32 heads over 8, 59.5 (268 MB, 40 at that rate); one token of them, pages of 256, 45.5.  A bound of
+// 131072 keys for any of these: no slower.
 //
 // The mathematics: u = (q . k) scale log2(e), p = 2^(u - m) with m a running maximum, out = sum p v / sum p.  The
 // products are warp-level bf16 ones with fp32 sums, keys (and value columns) their 16 rows and queries their 8 columns;

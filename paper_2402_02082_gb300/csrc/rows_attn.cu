@@ -6,7 +6,7 @@
 // the chain of a row counts.  A block's four warps take a row's keys in turn, 32 at a time, with up to 16 loads in flight each:
 // 32 dot products at once (a lane a key), one maximum and one sum over the warp, then the values column by column; the
 // warps' results meet in shared memory.  Where no row can see more than 32 keys, each warp has a row of its own.
-// Two fp32 prompts of 60 to 128 tokens, 4 heads of 64: 9.9 us (a warp a row and 4 loads in flight: 40).  Registers are bounded for
+// Two fp32 prompts of 60 to 128 tokens, 4 heads of 64: 9.8 to 10.1 us, 940 blocks where 912 are resident (a warp a row and 4 loads in flight: 40).  Registers are bounded for
 // six blocks an SM (four with 128 dims), where the values of eight keys at once fit without spills; 12 or 16 keys do not (prompts of
 // 32 tokens, 4 heads of 64: 5.2, 5.4 and 5.5 us; of 115 and 120: 10.6, 12.0 and 11.9).
 #include "device.h"
@@ -118,15 +118,15 @@ constexpr int most_keys(const RowsArgs& a) { return a.table ? a.max_kv : a.max_q
 
 }  // namespace
 
-// A row of at most 32 keys is one pass of a warp here, and the tensor-core kernel starts for about 9 us and then has a
-// chain of 4.7 us for each of an SM's items (a request's rows of one cached head), however few they are.  Measured, here
-// and there, 8 or 32 query heads of 128 over 8 cached: about 3.3 us + 2.7 ns a row against 9 + 0.031 an item.  Prompts of
-// 4 tokens, 8 heads: 1024 rows 5.1 and 16.6 us, 16384 rows 39 and 137; of 32 tokens: 2048 rows 9.8 and 10.5, 8192 rows
-// 27 and 16; four heads to a cached one, prompts of 16: 2048 rows 6.7 and 10.2, 8192 rows 20 and 12.  Above 32 keys the
-// tensor cores lead almost from the first row on (48 keys: 768 rows 8.6 and 9.7 us, 1920 rows 17 and 10).
+// A row of at most 32 keys is one pass of a warp here, and the tensor-core kernel starts for about 6 us and then has a
+// chain of 3.7 us for each of an SM's items (a request's rows of one cached head), however few they are.  Measured, here
+// and there, 8 or 32 query heads of 128 over 8 cached: about 2.5 us + 2 ns a row against 6 + 0.025 an item.  Prompts of
+// 4 tokens, 8 heads: 1024 rows 4.6 and 12.1 us, 16384 rows 36 and 106; of 32 tokens: 2048 rows 9.2 and 9.1, 8192 rows
+// 25 and 12; four heads to a cached one, prompts of 16: 2048 rows 6.6 and 8.9, 8192 rows 19 and 9.  Above 32 keys the
+// tensor cores lead almost from the first row on (48 keys: 768 rows 8.5 and 8.8 us, 1920 rows 17 and 9).
 // Where launch_paged_few would serve the rows (pages, at most 16 of a cached head), its CTA for each cached head leads until
-// they are more than two for an SM; from there, a call of 1200 cached heads, 128 dims: 1 row of 16 keys 6.3 us here and 25.8
-// there, 2 of 32 keys 12 and 27, 4 of 16 keys 17 and 27, but 8 of 32 keys 43 and 31.
+// they are more than two for an SM; from there, a call of 1200 cached heads, 128 dims: 1 row of 16 keys 6.2 us here and 16.3
+// there, 2 of 32 keys 11 and 17, 4 of 16 keys 14 and 18, but 8 of 32 keys 40 and 21.
 bool rows_fma_leads(const RowsArgs& a) {
   const long long slabs = (long long)a.B * a.Hkv, slab_rows = (long long)a.max_q * (a.H / a.Hkv);
   if (most_keys(a) > 32) return false;
