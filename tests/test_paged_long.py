@@ -109,3 +109,69 @@ def test_sums_of_very_many_keys(case, like):
     again = torch.zeros_like(out)
     gb.glide_paged_attn(q.cuda(), K.cuda(), V.cuda(), i32(table.numpy())[None], i32([0, m]), m, i32([kv]), kv, again, ws)
     assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("m, H, D", [(1, SMS, 64), (3, SMS, 128), (17, SMS, 64), (40, SMS, 128)])
+def test_requests_of_very_different_lengths(m, H, D):
+    """In one call: one of many sums, one of few tokens, one of none but the new ones."""
+    P, gen, lens = 256, torch.Generator().manual_seed(m), [m, 2 ** 20 + 300, 700, 2 ** 17 + 1280]
+    K = torch.randn((8, H, P, D), generator=gen).bfloat16()
+    V = (1 + torch.rand((8, H, P, D), generator=gen)).bfloat16()
+    q = torch.randn((m * len(lens), H, D), generator=gen).bfloat16()
+    table = torch.randint(8, (len(lens), -(-max(lens) // P)), generator=gen)
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda")
+    ws = workspace(len(lens), H, H, D, "bf16", len(q), m)
+    gb.glide_paged_attn(q.cuda(), K.cuda(), V.cuda(), i32(table.numpy()), i32([m * b for b in range(len(lens) + 1)]), m, i32(lens),
+                        max(lens), out, ws)
+    assert gb.glide_read_device_status(ws) == gb.GLIDE_OK
+    got = host(out)
+    for b, kv in enumerate(lens):
+        for i in {0, m - 1}:
+            want, tol = expected(q[b * m: (b + 1) * m], K, V, table[b], kv, i, m)
+            check(got[b * m + i], want, tol, f"request {b}, row {i}")
+
+
+@pytest.mark.parametrize("m, H, D, kv", [(1, 2 * SMS + 2, 64, 2 ** 20 + 300), (17, 2 * SMS, 64, 2 ** 17 + 5000), (40, 8, 128, 2 ** 20 + 1)])
+def test_infinite_values_in_long_contexts(m, H, D, kv):
+    """One in the first keys, that every row sees, one in the last key, that the last row alone sees, and NaN in a key and a value
+    behind it that no row sees.  (A warp's spans, an item's segments, segments of chunks.)"""
+    P, gen = 256, torch.Generator().manual_seed(m)
+    K = torch.randn((6, H, P, D), generator=gen).bfloat16()
+    V = (1 + torch.rand((6, H, P, D), generator=gen)).bfloat16()
+    q = torch.randn((m, H, D), generator=gen).bfloat16()
+    width, last = -(-kv // P), (kv - 1) % P
+    table = torch.randint(1, 4, (width,), generator=gen)
+    table[0], table[-1] = 4, 5
+    V[4, :, 2, 3] = float("inf")
+    V[5, :, last, 7] = -float("inf")
+    if last + 1 < P:
+        K[5, :, last + 1], V[5, :, last + 1] = float("nan"), float("nan")
+    out = torch.zeros((m, H, D), dtype=torch.bfloat16, device="cuda")
+    ws = workspace(1, H, H, D, "bf16", m, m)
+    gb.glide_paged_attn(q.cuda(), K.cuda(), V.cuda(), i32(table.numpy())[None], i32([0, m]), m, i32([kv]), kv, out, ws)
+    assert gb.glide_read_device_status(ws) == gb.GLIDE_OK
+    got = host(out)
+    finite_K, finite_V = (torch.where(X.isfinite(), X, 0) for X in (K, V))
+    for i in sorted({0, m - 1}):
+        want, tol = expected(q, finite_K, finite_V, table, kv, i, m)
+        assert (got[i, :, 3] == float("inf")).all()
+        assert (got[i, :, 7] == -float("inf")).all() if i == m - 1 else True
+        odd = [3, 7] if i == m - 1 else [3]
+        got[i][:, odd], want[:, odd] = 0, 0
+        check(got[i], want, tol, f"row {i}")
+
+
+def test_a_prompt_of_more_keys_than_one_sum_takes():
+    n, H, H_kv, D = 2 ** 17 + 2 ** 14 + 77, 2, 1, 64
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((n, H + 2 * H_kv, D), generator=gen, device="cuda")
+    x[:, H + H_kv:] = 1 + x[:, H + H_kv:].abs()
+    q, k, v = x.bfloat16().split([H, H_kv, H_kv], 1)
+    out = torch.zeros((n, H, D), dtype=torch.bfloat16, device="cuda")
+    ws = workspace(1, H, H_kv, D, "bf16", n, n)
+    gb.glide_prompt_attn(q, k, v, i32([0, n]), n, out, ws)
+    assert gb.glide_read_device_status(ws) == gb.GLIDE_OK
+    pool = [t.transpose(0, 1)[:, None].reshape(1, 1, n, D) for t in (k, v)]  # one page of all keys
+    for i in (5, 2 ** 17 - 1, 2 ** 17, 2 ** 17 + 129, n - 1):
+        want, tol = expected(q[i: i + 1], *(t[:, :, : i + 1] for t in pool), torch.tensor([0]), i + 1, 0, 1)
+        check(host(out[i]), want, tol, f"row {i}")
